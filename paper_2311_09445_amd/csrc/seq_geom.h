@@ -1,0 +1,63 @@
+// Arguments of the sequence operators' kernels and their launchers (host side of seq_attention.hip and seq_rotate.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/per_seq.h"
+
+namespace per {
+
+// Rows of a pass over heads: head h of the pass reads head h / share.
+struct SeqRows {
+  void* d;
+  int64_t batch, token, head;
+  uint32_t share;
+  uint32_t wide;   // address and strides are multiples of 16 bytes
+};
+
+struct SeqStates {
+  float* d;
+  int64_t batch, head;
+};
+
+// Sizes of a linear attention.
+struct AttentionSizes {
+  uint32_t dtype, B, L, H, G, dk, dv;
+  float scale;
+  const float* log_decay;
+  const int32_t* lengths;
+};
+
+size_t attention_work_bytes(const AttentionSizes& a, bool backward);
+hipError_t launch_attention(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
+                            const per_seq_states* state, const per_seq_rows& out, const per_seq_states* out_state, void* work,
+                            hipStream_t s);
+hipError_t launch_attention_backward(const AttentionSizes& a, const per_seq_rows& dout, const per_seq_rows& q,
+                                     const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state,
+                                     const per_seq_states* dstate, const per_seq_rows& dq, const per_seq_rows& dk,
+                                     const per_seq_rows& dv, const per_seq_states* dstate0, void* work, hipStream_t s);
+hipError_t launch_attention_step(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
+                                 const per_seq_states& state, const per_seq_rows& out, hipStream_t s);
+
+// One tensor of a rotation: its rows, where they go, the norm's weight.
+struct RotarySide {
+  SeqRows x, out, dout;   // dout: gradients only
+  const float* weight;
+  uint32_t heads;
+};
+struct RotaryArgs {
+  RotarySide side[2];     // queries, keys
+  uint32_t B, L, dim, rot, layout;
+  const int32_t* at;
+  int64_t at_batch, at_token;
+  const float* freqs;
+  float magnitude, sign;  // sign: -1 turns the other way
+  float eps;
+  float* partial;         // gradients only: [blocks][2][dim] sums for the weights
+};
+
+enum RotaryKind { ROTATE, NORM_ROTATE, NORM_ROTATE_BACK };
+size_t rotary_work_bytes(uint64_t tokens, uint32_t heads, uint32_t dim);
+hipError_t launch_rotary(RotaryKind kind, uint32_t dtype, RotaryArgs a, float* dqw, float* dkw, hipStream_t s);
+
+}  // namespace per
