@@ -17,56 +17,55 @@ struct AttentionPass {
   SeqRows x, y, z, out;
   uint32_t L, H, dx, dz;
   uint32_t back;                 // against time (and lag 1)
+  uint32_t out_f32;              // out is fp32 whatever the rows' type
   float c_in, c_state, c_out;
   const float* log_decay;
   const int32_t* lengths;
-  // states [b][h], element (i of dx, j of dz) at i * in_x + j * in_z
+  // states [b][h] (and [segment]), element (i of dx, j of dz) at i * in_x + j * in_z
   const float* in;
-  int64_t in_batch, in_head;
+  int64_t in_batch, in_head, in_segment;
   uint32_t in_x, in_z;
   float* to;
   int64_t to_batch, to_head;
+  float* part;                   // [b][h][segment][dx][dz]: what each segment brings
+};
+struct AttentionPasses {
+  AttentionPass pass[3];
+  uint32_t count, items, slices, segments, segment;   // items: workgroups of a pass; segment: tokens
 };
 
-template <typename T, typename O>
-__global__ __launch_bounds__(128) void k_attend_tokens(AttentionPass p) {
-  __shared__ float xs[128], ys[128];
-  const uint32_t h = blockIdx.x % p.H, b = blockIdx.x / p.H, j = threadIdx.x;
-  const uint32_t n = valid_tokens(p.lengths, b, p.L);
-  const float decay = expf(p.log_decay[h]);
-  float S[128];
+struct JoinPass {
+  float* part;
+  const float* in;
+  int64_t in_batch, in_head;
+  float* to;
+  int64_t to_batch, to_head;
+  uint32_t dx, dz;
+};
+struct JoinPasses {
+  JoinPass pass[2];
+  uint32_t BH, H, L, segments, segment;
+  const float* log_decay;
+  const int32_t* lengths;
+};
+
+// Four results side by side, `left` elements before the end of the row.
+template <typename O>
+__device__ __forceinline__ void store4(O* p, const float __attribute__((ext_vector_type(4))) & v, bool wide, uint32_t left) {
+  typedef O Four __attribute__((ext_vector_type(4)));
+  if (wide && left >= 4) {
+    Four o;
 #pragma unroll
-  for (uint32_t i = 0; i < 128; ++i) {
-    S[i] = 0.0f;
-    if (p.in && i < p.dx && j < p.dz) S[i] = p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + (int64_t)i * p.in_x + (int64_t)j * p.in_z];
+    for (int i = 0; i < 4; ++i) o[i] = (O)v[i];
+    *reinterpret_cast<Four*>(p) = o;
+    return;
   }
-  for (uint32_t i = 0; i < p.L; ++i) {
-    const uint32_t t = i < n && p.back ? n - 1 - i : i;
-    float sum = 0.0f;
-    if (i < n) {
-      __syncthreads();
-      xs[j] = j < p.dx ? as_float(row_of<T>(p.x, b, t, h)[j]) : 0.0f;
-      ys[j] = j < p.dx ? as_float(row_of<T>(p.y, b, t, h)[j]) : 0.0f;
-      __syncthreads();
-      const float z = j < p.dz ? as_float(row_of<T>(p.z, b, t, h)[j]) : 0.0f;
-      float dot = 0.0f;
 #pragma unroll
-      for (uint32_t m = 0; m < 128; ++m) {
-        if (!p.back) S[m] *= decay;
-        sum = fmaf(xs[m], S[m], sum);
-        dot = fmaf(xs[m], ys[m], dot);
-        S[m] = fmaf(ys[m], z * p.c_state, S[m]);
-        if (p.back) S[m] *= decay;
-      }
-      sum = p.c_out * sum + p.c_in * dot * z;
-    }
-    if (j < p.dz) row_to<O>(p.out, b, t, h)[j] = (O)sum;
-  }
-  if (p.to && j < p.dz)
-#pragma unroll
-    for (uint32_t i = 0; i < 128; ++i)
-      if (i < p.dx) p.to[(int64_t)b * p.to_batch + (int64_t)h * p.to_head + (int64_t)i * p.dz + j] = S[i];
+  for (uint32_t i = 0; i < 4; ++i)
+    if (i < left) p[i] = (O)v[i];
 }
+
+#include "k_attend.h"
 
 // Rows of heads that share one, added up: from [B][L][H][d] in fp32 to [B][L][G][d].
 template <typename T>
@@ -110,7 +109,7 @@ SeqRows rows(const per_seq_rows& r, uint32_t dtype, uint32_t share) {
 }
 // Packed rows [B][L][H][d] in fp32.
 SeqRows packed(float* d, const AttentionSizes& a, uint32_t width) {
-  return SeqRows{d, (int64_t)a.L * a.H * width, (int64_t)a.H * width, (int64_t)width, 1, 0};
+  return SeqRows{d, (int64_t)a.L * a.H * width, (int64_t)a.H * width, (int64_t)width, 1, width % 4 == 0};
 }
 
 AttentionPass make_pass(const AttentionSizes& a, bool back, uint32_t dx, uint32_t dz) {
@@ -144,58 +143,185 @@ void to_states(AttentionPass* p, const per_seq_states* s) {
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-template <typename T, typename O>
-hipError_t run_pass(const AttentionSizes& a, const AttentionPass& p, hipStream_t s) {
-  k_attend_tokens<T, O><<<a.B * a.H, 128, 0, s>>>(p);
+// How a sequence is cut.  A workgroup takes its tokens one chunk behind the other, so what cuts the time of few sequences is
+// workgroups: the sequence in segments, each from the state that those before it bring.  That costs another pass over keys and
+// values for those states, and a state in memory per segment.
+struct Cut {
+  uint32_t segments, segment;
+};
+Cut cut(const AttentionSizes& a) {
+  const uint64_t rows = (uint64_t)a.B * a.H;
+  uint64_t segments = 1;
+  if (rows && rows < 256) segments = (512 + rows - 1) / rows;
+  const uint64_t most = a.L / 256;
+  if (segments > most) segments = most;
+  if (segments < 2) return Cut{1, a.L ? a.L : 1};
+  const uint32_t segment = (uint32_t)((a.L + segments - 1) / segments + kChunk - 1) / kChunk * kChunk;
+  return Cut{(a.L + segment - 1) / segment, segment};
+}
+size_t part_bytes(const AttentionSizes& a, const Cut& c) {
+  return c.segments < 2 ? 0 : align256((size_t)a.B * a.H * c.segments * a.dk * a.dv * sizeof(float));
+}
+size_t fold_bytes(const AttentionSizes& a, uint32_t width) { return a.H == a.G ? 0 : align256((size_t)a.B * a.L * a.H * width * sizeof(float)); }
+
+template <typename T, int DX, int NT, int WAVES, int TERMS, bool OUT>
+hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
+  constexpr uint32_t lds = 2 * chunk_elements<T, DX, 16 * NT * WAVES, OUT>() * sizeof(T);
+  auto* kernel = k_attend<T, DX, NT, WAVES, TERMS, OUT>;
+  if (lds > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<(p.items + 7) / 8 * 8 * p.count, 64 * WAVES, lds, s>>>(p);
+  return hipGetLastError();
+}
+template <typename T, int DX, int TERMS, bool OUT>
+hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {
+  const uint32_t dz = p.pass[0].dz;
+  p.slices = 1;
+  p.items = rows * p.segments;
+  if (dz <= 32) return launch_as<T, DX, 1, 2, TERMS, OUT>(p, s);
+  if (dz <= 64) return launch_as<T, DX, 1, 4, TERMS, OUT>(p, s);
+  return launch_as<T, DX, 2, 4, TERMS, OUT>(p, s);
+}
+// Passes of the same widths, in one launch.
+template <typename T, int TERMS, bool OUT>
+hipError_t launch_passes(AttentionPasses p, uint32_t rows, hipStream_t s) {
+  const uint32_t dx = p.pass[0].dx;
+  if (dx <= 32) return launch_dz<T, 32, TERMS, OUT>(p, rows, s);
+  if (dx <= 64) return launch_dz<T, 64, TERMS, OUT>(p, rows, s);
+  return launch_dz<T, 128, TERMS, OUT>(p, rows, s);
+}
+
+void join_from(JoinPass* j, const per_seq_states* s) {
+  if (s) { j->in = s->d; j->in_batch = s->batch; j->in_head = s->head; }
+}
+void join_to(JoinPass* j, const per_seq_states* s) {
+  if (s) { j->to = s->d; j->to_batch = s->batch; j->to_head = s->head; }
+}
+// A pass whose segments start from the joined states.
+void from_parts(AttentionPass* p, float* part, const AttentionSizes& a, const Cut& c, bool transposed) {
+  const int64_t per = (int64_t)a.dk * a.dv;
+  p->in = part;
+  p->in_segment = per;
+  p->in_head = per * c.segments;
+  p->in_batch = p->in_head * a.H;
+  p->in_x = transposed ? 1 : a.dv;
+  p->in_z = transposed ? a.dv : 1;
+}
+hipError_t launch_join(JoinPasses j, const AttentionSizes& a, const Cut& c, uint32_t count, hipStream_t s) {
+  j.BH = a.B * a.H;
+  j.H = a.H;
+  j.L = a.L;
+  j.segments = c.segments;
+  j.segment = c.segment;
+  j.log_decay = a.log_decay;
+  j.lengths = a.lengths;
+  const uint64_t n = (uint64_t)j.BH * a.dk * a.dv;
+  k_join<<<dim3((uint32_t)((n + 255) / 256), count), 256, 0, s>>>(j);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
-                   const per_seq_states* state, const per_seq_rows& out, const per_seq_states* out_state, void*, hipStream_t s) {
-  const uint32_t share = a.H / a.G;
-  AttentionPass p = make_pass(a, false, a.dk, a.dv);
+                   const per_seq_states* state, const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
+  constexpr bool F = sizeof(T) == 4;
+  const uint32_t share = a.H / a.G, bh = a.B * a.H;
+  const Cut c = cut(a);
+  AttentionPasses all{};
+  all.count = 1;
+  all.segments = c.segments;
+  all.segment = c.segment;
+  AttentionPass& p = all.pass[0];
+  p = make_pass(a, false, a.dk, a.dv);
   p.x = rows(q, a.dtype, 1);
   p.y = rows(k, a.dtype, share);
   p.z = rows(v, a.dtype, share);
   p.out = rows(out, a.dtype, 1);
-  from_states(&p, state, a.dv, false);
-  to_states(&p, out_state);
-  return run_pass<T, T>(a, p, s);
+  if (c.segments == 1) {
+    from_states(&p, state, a.dv, false);
+    to_states(&p, out_state);
+    return out_state ? launch_passes<T, F ? 1 : 3, true>(all, bh, s) : launch_passes<T, F ? 1 : 2, true>(all, bh, s);
+  }
+  p.part = static_cast<float*>(work);
+  hipError_t e = launch_passes<T, F ? 1 : 3, false>(all, bh, s);
+  if (e != hipSuccess) return e;
+  JoinPasses j{};
+  j.pass[0] = JoinPass{p.part, nullptr, 0, 0, nullptr, 0, 0, a.dk, a.dv};
+  join_from(&j.pass[0], state);
+  join_to(&j.pass[0], out_state);
+  e = launch_join(j, a, c, 1, s);
+  if (e != hipSuccess) return e;
+  from_parts(&p, p.part, a, c, false);
+  return launch_passes<T, F ? 1 : 2, true>(all, bh, s);
 }
 
 template <typename T>
 hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per_seq_rows& q, const per_seq_rows& k,
                     const per_seq_rows& v, const per_seq_states* state, const per_seq_states* dstate, const per_seq_rows& dq,
                     const per_seq_rows& dk, const per_seq_rows& dv, const per_seq_states* dstate0, void* work, hipStream_t s) {
-  const uint32_t share = a.H / a.G;
+  constexpr bool F = sizeof(T) == 4;
+  const uint32_t share = a.H / a.G, bh = a.B * a.H;
+  const Cut c = cut(a);
   const SeqRows Q = rows(q, a.dtype, 1), K = rows(k, a.dtype, share), V = rows(v, a.dtype, share), D = rows(dout, a.dtype, 1);
-  float* fold = static_cast<float*>(work);
-  AttentionPass p = make_pass(a, false, a.dv, a.dk);
-  p.x = D; p.y = V; p.z = K;
-  p.out = rows(dq, a.dtype, 1);
-  from_states(&p, state, a.dv, true);
-  hipError_t e = run_pass<T, T>(a, p, s);
-  for (int which = 0; which < 2 && e == hipSuccess; ++which) {
-    const bool of_v = which == 1;   // (last: it may write over dstate)
-    const uint32_t width = of_v ? a.dv : a.dk;
-    p = make_pass(a, true, of_v ? a.dk : a.dv, width);
-    p.x = of_v ? K : V;
-    p.y = of_v ? Q : D;
-    p.z = of_v ? D : Q;
-    from_states(&p, dstate, a.dv, !of_v);
-    if (of_v) to_states(&p, dstate0);
-    const SeqRows to = rows(of_v ? dv : dk, a.dtype, 1);
-    if (share == 1) {
-      p.out = to;
-      e = run_pass<T, T>(a, p, s);
-      continue;
-    }
-    p.out = packed(fold, a, width);
-    e = run_pass<T, float>(a, p, s);
+  uint8_t* at = static_cast<uint8_t*>(work);
+  float* part[2];   // of the states, of their gradients
+  for (int i = 0; i < 2; ++i, at += part_bytes(a, c)) part[i] = reinterpret_cast<float*>(at);
+  float* const fold_k = reinterpret_cast<float*>(at);
+  float* const fold_v = reinterpret_cast<float*>(at + fold_bytes(a, a.dk));
+
+  AttentionPass of_q = make_pass(a, false, a.dv, a.dk), of_k = make_pass(a, true, a.dv, a.dk), of_v = make_pass(a, true, a.dk, a.dv);
+  of_q.x = D; of_q.y = V; of_q.z = K;
+  of_k.x = V; of_k.y = D; of_k.z = Q;
+  of_v.x = K; of_v.y = Q; of_v.z = D;
+  of_q.out = rows(dq, a.dtype, 1);
+  of_k.out = share == 1 ? rows(dk, a.dtype, 1) : packed(fold_k, a, a.dk);
+  of_v.out = share == 1 ? rows(dv, a.dtype, 1) : packed(fold_v, a, a.dv);
+  of_k.out_f32 = of_v.out_f32 = share > 1;
+  AttentionPasses all{};
+  all.segments = c.segments;
+  all.segment = c.segment;
+  hipError_t e;
+  if (c.segments == 1) {
+    from_states(&of_q, state, a.dv, true);
+    from_states(&of_k, dstate, a.dv, true);
+    from_states(&of_v, dstate, a.dv, false);
+    to_states(&of_v, dstate0);
+  } else {
+    all.count = 2;
+    all.pass[0] = make_pass(a, false, a.dk, a.dv);
+    all.pass[0].y = K;
+    all.pass[0].z = V;
+    all.pass[1] = of_v;
+    for (int i = 0; i < 2; ++i) all.pass[i].part = part[i];
+    e = launch_passes<T, F ? 1 : 3, false>(all, bh, s);
+    if (e != hipSuccess) return e;
+    JoinPasses j{};
+    for (int i = 0; i < 2; ++i) j.pass[i] = JoinPass{part[i], nullptr, 0, 0, nullptr, 0, 0, a.dk, a.dv};
+    join_from(&j.pass[0], state);
+    join_from(&j.pass[1], dstate);
+    join_to(&j.pass[1], dstate0);
+    e = launch_join(j, a, c, 2, s);
+    if (e != hipSuccess) return e;
+    from_parts(&of_q, part[0], a, c, true);
+    from_parts(&of_k, part[1], a, c, true);
+    from_parts(&of_v, part[1], a, c, false);
+  }
+  // (the gradient of k reads dstate, which that of v may write over: it comes first)
+  all.count = 2;
+  all.pass[0] = of_q;
+  all.pass[1] = of_k;
+  e = launch_passes<T, F ? 1 : 2, true>(all, bh, s);
+  if (e != hipSuccess) return e;
+  all.count = 1;
+  all.pass[0] = of_v;
+  e = of_v.to ? launch_passes<T, F ? 1 : 3, true>(all, bh, s) : launch_passes<T, F ? 1 : 2, true>(all, bh, s);
+  if (e != hipSuccess || share == 1) return e;
+  for (int i = 0; i < 2 && e == hipSuccess; ++i) {
+    const uint32_t width = i ? a.dv : a.dk;
     const uint64_t n = (uint64_t)a.B * a.L * a.G * width;
-    if (e != hipSuccess || !n) continue;
-    k_fold_heads<T><<<(uint32_t)((n + 255) / 256), 256, 0, s>>>(fold, to, a.L, a.G, share, width, n);
+    if (!n) continue;
+    k_fold_heads<T><<<(uint32_t)((n + 255) / 256), 256, 0, s>>>(i ? fold_v : fold_k, rows(i ? dv : dk, a.dtype, 1), a.L, a.G, share, width, n);
     e = hipGetLastError();
   }
   return e;
@@ -204,8 +330,8 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
 }  // namespace
 
 size_t attention_work_bytes(const AttentionSizes& a, bool backward) {
-  if (!backward || a.H == a.G) return 0;
-  return align256((size_t)a.B * a.L * a.H * (a.dk > a.dv ? a.dk : a.dv) * sizeof(float));
+  const Cut c = cut(a);
+  return backward ? 2 * part_bytes(a, c) + fold_bytes(a, a.dk) + fold_bytes(a, a.dv) : part_bytes(a, c);
 }
 
 hipError_t launch_attention(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
