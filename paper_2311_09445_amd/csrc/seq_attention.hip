@@ -80,27 +80,16 @@ __global__ __launch_bounds__(256) void k_fold_heads(const float* from, SeqRows t
   row_to<T>(to, b, t, g)[e] = (T)sum;
 }
 
-template <typename T>
-__global__ __launch_bounds__(128) void k_attend_step(SeqRows q, SeqRows k, SeqRows v, SeqStates st, SeqRows out, uint32_t H, uint32_t dk, uint32_t dv,
-                                                     float scale, const float* log_decay, const int32_t* lengths) {
-  const uint32_t h = blockIdx.x % H, b = blockIdx.x / H, j = threadIdx.x;
-  if (j >= dv) return;
-  T* o = row_to<T>(out, b, 0, h);
-  if (lengths && lengths[b] < 1) {
-    o[j] = (T)0.0f;
-    return;
-  }
-  const T *x = row_of<T>(q, b, 0, h), *y = row_of<T>(k, b, 0, h);
-  const float z = as_float(row_of<T>(v, b, 0, h)[j]), decay = expf(log_decay[h]);
-  float* S = st.d + (int64_t)b * st.batch + (int64_t)h * st.head + j;
-  float sum = 0.0f;
-  for (uint32_t i = 0; i < dk; ++i) {
-    const float s = fmaf(as_float(y[i]), z, S[(size_t)i * dv] * decay);
-    S[(size_t)i * dv] = s;
-    sum = fmaf(as_float(x[i]), s, sum);
-  }
-  o[j] = (T)(scale * sum);
-}
+struct AttentionStep {
+  SeqRows q, k, v, out;
+  SeqStates state;
+  uint32_t H, dk, dv, groups;
+  float scale;
+  const float* log_decay;
+  const int32_t* active;
+};
+
+#include "k_attend_step.h"
 
 SeqRows rows(const per_seq_rows& r, uint32_t dtype, uint32_t share) {
   const int64_t per16 = dtype == PER_SEQ_BF16 ? 8 : 4;
@@ -349,16 +338,24 @@ hipError_t launch_attention_backward(const AttentionSizes& a, const per_seq_rows
                                  : backward<float>(a, dout, q, k, v, state, dstate, dq, dk, dv, dstate0, work, s);
 }
 
+template <typename T>
+static hipError_t step(AttentionStep p, uint32_t rows, hipStream_t s) {
+  const bool wide = p.dv % 4 == 0 && (reinterpret_cast<uintptr_t>(p.state.d) & 15) == 0 && p.state.batch % 4 == 0 && p.state.head % 4 == 0;
+  const uint32_t columns = wide ? p.dv / 4 : p.dv;
+  p.groups = 256 / columns < p.dk ? 256 / columns : p.dk;
+  const bool few = (p.dk + p.groups - 1) / p.groups <= 4;   // rows of a thread
+  if (wide && few) k_attend_step<T, 4, 4><<<rows, 256, 0, s>>>(p);
+  else if (wide) k_attend_step<T, 4, 16><<<rows, 256, 0, s>>>(p);
+  else k_attend_step<T, 1, 16><<<rows, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
 hipError_t launch_attention_step(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
                                  const per_seq_states& state, const per_seq_rows& out, hipStream_t s) {
   const uint32_t share = a.H / a.G;
-  const SeqRows Q = rows(q, a.dtype, 1), K = rows(k, a.dtype, share), V = rows(v, a.dtype, share), O = rows(out, a.dtype, 1);
-  const SeqStates st{state.d, state.batch, state.head};
-  if (a.dtype == PER_SEQ_BF16)
-    k_attend_step<bf16><<<a.B * a.H, 128, 0, s>>>(Q, K, V, st, O, a.H, a.dk, a.dv, a.scale, a.log_decay, a.lengths);
-  else
-    k_attend_step<float><<<a.B * a.H, 128, 0, s>>>(Q, K, V, st, O, a.H, a.dk, a.dv, a.scale, a.log_decay, a.lengths);
-  return hipGetLastError();
+  const AttentionStep p{rows(q, a.dtype, 1), rows(k, a.dtype, share), rows(v, a.dtype, share), rows(out, a.dtype, 1),
+                        SeqStates{state.d, state.batch, state.head}, a.H, a.dk, a.dv, 0, a.scale, a.log_decay, a.lengths};
+  return a.dtype == PER_SEQ_BF16 ? step<bf16>(p, a.B * a.H, s) : step<float>(p, a.B * a.H, s);
 }
 
 }  // namespace per

@@ -54,6 +54,7 @@ struct RotaryArgs {
   float magnitude, sign;  // sign: -1 turns the other way
   float eps;
   float* partial;         // gradients only: [blocks][2][dim] sums for the weights
+  uint32_t tokens, tiles; // heads in vectors: tokens that a workgroup takes at a time, and how often there are so many
 };
 
 enum RotaryKind { ROTATE, NORM_ROTATE, NORM_ROTATE_BACK };

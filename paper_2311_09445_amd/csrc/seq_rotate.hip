@@ -9,7 +9,9 @@ namespace per {
 
 namespace {
 
-constexpr uint32_t kSums = 512;   // most workgroups that leave sums for the weights' gradients
+constexpr uint32_t kSums = 1024;   // most workgroups that leave sums for the weights' gradients
+
+#include "k_rotate.h"
 
 // Any width, alignment and layout: a wave per head, a lane holds elements lane, lane + 64, ... and the partner of each.
 template <typename T, RotaryKind KIND>
@@ -111,37 +113,97 @@ __global__ __launch_bounds__(256) void k_rotate_any(RotaryArgs a) {
   }
 }
 
-// The weights' gradients from the workgroups' sums, in their order.
-__global__ __launch_bounds__(256) void k_weight_sums(const float* partial, uint32_t blocks, uint32_t dim, float* dqw, float* dkw) {
-  const uint32_t i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;   // 32 lanes per element
-  if (i >= 2 * dim) return;
+// The weights' gradients from the workgroups' sums, in a fixed order: a workgroup takes 16 elements, 64 rows of sums at a time.
+__global__ __launch_bounds__(1024) void k_weight_sums(const float* partial, uint32_t blocks, uint32_t dim, float* dqw, float* dkw) {
+  __shared__ float all[64][16];
+  const uint32_t e = threadIdx.x & 15, row = threadIdx.x >> 4, i = blockIdx.x * 16 + e;
   float sum = 0.0f;
-  for (uint32_t b = lane; b < blocks; b += 32) sum += partial[(size_t)b * 2 * dim + i];
+  if (i < 2 * dim) {
+    float s[kSums / 64];
 #pragma unroll
-  for (int m = 16; m; m >>= 1) sum += __shfl_xor(sum, m);
+    for (uint32_t k = 0; k < kSums / 64; ++k) s[k] = row + 64 * k < blocks ? partial[(size_t)(row + 64 * k) * 2 * dim + i] : 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < kSums / 64; ++k) sum += s[k];
+  }
+  all[row][e] = sum;
+  __syncthreads();
+  for (uint32_t m = 32; m; m >>= 1) {
+    if (row < m) all[row][e] += all[row + m][e];
+    __syncthreads();
+  }
   float* out = i < dim ? dqw : dkw;
-  if (lane == 0 && out) out[i < dim ? i : i - dim] = sum;
+  if (row == 0 && i < 2 * dim && out) out[i < dim ? i : i - dim] = all[0][e];
 }
 
+// Workgroups of a gradient: as the workspace is sized, before it is known which kernel takes it.
 uint32_t sum_blocks(uint64_t tokens, uint32_t heads) {
   const uint64_t n = (tokens * heads + 3) / 4;
   return (uint32_t)(n < kSums ? (n ? n : 1) : kSums);
 }
 
-template <typename T>
-hipError_t launch(RotaryKind kind, const RotaryArgs& a, float* dqw, float* dkw, hipStream_t s) {
-  const uint32_t heads = a.side[0].heads + a.side[1].heads;
-  const uint64_t tokens = (uint64_t)a.B * a.L, waves = tokens * heads;
-  if (kind == NORM_ROTATE_BACK) {
-    const uint32_t blocks = sum_blocks(tokens, heads);
-    k_rotate_any<T, NORM_ROTATE_BACK><<<blocks, 256, 0, s>>>(a);
-    if (dqw || dkw) k_weight_sums<<<(2 * a.dim + 7) / 8, 256, 0, s>>>(a.partial, blocks, a.dim, dqw, dkw);
-  } else {
-    const uint64_t n = (waves + 3) / 4;
-    const uint32_t blocks = (uint32_t)(n < 16384 ? n : 16384);
-    if (kind == ROTATE) k_rotate_any<T, ROTATE><<<blocks, 256, 0, s>>>(a);
-    else k_rotate_any<T, NORM_ROTATE><<<blocks, 256, 0, s>>>(a);
+template <typename T, int W, RotaryKind KIND, bool INTERLEAVED>
+hipError_t launch_units(const RotaryArgs& a, uint32_t blocks, hipStream_t s) {
+  const uint32_t units = a.dim / (2 * W), lds = a.tokens * (a.rot / 2) * sizeof(float2);
+  if (units <= 4) k_rotate_units<T, W, 4, KIND, INTERLEAVED><<<blocks, 256, lds, s>>>(a);
+  else if (units <= 8) k_rotate_units<T, W, 8, KIND, INTERLEAVED><<<blocks, 256, lds, s>>>(a);
+  else if (units <= 16) k_rotate_units<T, W, 16, KIND, INTERLEAVED><<<blocks, 256, lds, s>>>(a);
+  else if (W <= 4 && units <= 32) k_rotate_units<T, W, W <= 4 ? 32 : 16, KIND, INTERLEAVED><<<blocks, 256, lds, s>>>(a);
+  else k_rotate_units<T, W, W <= 2 ? 64 : 16, KIND, INTERLEAVED><<<blocks, 256, lds, s>>>(a);   // (dim is at most 256)
+  return hipGetLastError();
+}
+template <typename T, int W>
+hipError_t launch_units(RotaryKind kind, const RotaryArgs& a, uint32_t blocks, hipStream_t s) {
+  const bool il = a.layout == PER_SEQ_INTERLEAVED;
+  switch (kind) {
+    case ROTATE: return il ? launch_units<T, W, ROTATE, true>(a, blocks, s) : launch_units<T, W, ROTATE, false>(a, blocks, s);
+    case NORM_ROTATE: return il ? launch_units<T, W, NORM_ROTATE, true>(a, blocks, s) : launch_units<T, W, NORM_ROTATE, false>(a, blocks, s);
+    default: return il ? launch_units<T, W, NORM_ROTATE_BACK, true>(a, blocks, s) : launch_units<T, W, NORM_ROTATE_BACK, false>(a, blocks, s);
   }
+}
+
+// Elements of the widest vectors (16 or 8 bytes) that all rows and the pairs' places allow; 0: none.
+uint32_t vector_width(const RotaryArgs& a, RotaryKind kind, uint32_t element) {
+  for (uint32_t w = 16 / element; w * element >= 8; w /= 2) {
+    bool fits = a.dim % (2 * w) == 0 && a.rot % (2 * w) == 0;
+    for (int i = 0; i < 2; ++i) {
+      const RotarySide& sd = a.side[i];
+      if (!sd.heads) continue;
+      for (const SeqRows* r : {&sd.x, &sd.out, kind == NORM_ROTATE_BACK ? &sd.dout : &sd.x})
+        fits = fits && reinterpret_cast<uintptr_t>(r->d) % (w * element) == 0 && r->batch % w == 0 && r->token % w == 0 && r->head % w == 0;
+    }
+    if (fits) return w;
+  }
+  return 0;
+}
+
+template <typename T>
+hipError_t launch(RotaryKind kind, RotaryArgs a, float* dqw, float* dkw, hipStream_t s) {
+  const uint32_t heads = a.side[0].heads + a.side[1].heads, most = sum_blocks((uint64_t)a.B * a.L, heads);
+  const uint64_t tokens = (uint64_t)a.B * a.L;
+  const uint32_t w = tokens && heads ? vector_width(a, kind, sizeof(T)) : 0;
+  uint32_t blocks;
+  hipError_t e;
+  if (w) {
+    // As many tokens to a workgroup as give its lanes eight units each, but fewer where that would leave the chip without workgroups;
+    // their cosines take at most 32 KiB.
+    const uint32_t lanes = a.dim / (2 * w) <= 4 ? 4 : a.dim / (2 * w) <= 8 ? 8 : a.dim / (2 * w) <= 16 ? 16 : a.dim / (2 * w) <= 32 ? 32 : 64;
+    uint64_t n = 8 * 256 / lanes / heads;
+    if (n > tokens / 1024) n = tokens / 1024;
+    if (n > 4096 / (a.rot / 2 + 1)) n = 4096 / (a.rot / 2 + 1);
+    a.tokens = n ? (uint32_t)n : 1;
+    a.tiles = (uint32_t)((tokens + a.tokens - 1) / a.tokens);
+    blocks = kind == NORM_ROTATE_BACK && a.tiles > most ? most : a.tiles;
+    e = w * sizeof(T) == 16 ? launch_units<T, 16 / sizeof(T)>(kind, a, blocks, s) : launch_units<T, 8 / sizeof(T)>(kind, a, blocks, s);
+  } else {
+    const uint64_t n = (tokens * heads + 3) / 4;
+    blocks = kind == NORM_ROTATE_BACK ? most : (uint32_t)(n < 16384 ? n : 16384);
+    if (kind == ROTATE) k_rotate_any<T, ROTATE><<<blocks, 256, 0, s>>>(a);
+    else if (kind == NORM_ROTATE) k_rotate_any<T, NORM_ROTATE><<<blocks, 256, 0, s>>>(a);
+    else k_rotate_any<T, NORM_ROTATE_BACK><<<blocks, 256, 0, s>>>(a);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || kind != NORM_ROTATE_BACK || (!dqw && !dkw)) return e;
+  k_weight_sums<<<(2 * a.dim + 15) / 16, 1024, 0, s>>>(a.partial, blocks, a.dim, dqw, dkw);
   return hipGetLastError();
 }
 
