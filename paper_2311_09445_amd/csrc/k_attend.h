@@ -5,12 +5,18 @@
 // w_j = c_state decay^(n-1-j+lag) for the n tokens of the chunk,
 //   out = diag(f) X S + (c_in X Y^T . decay^(i-j) for j <= i) Z,     S <- decay^n S + Y^T diag(w) Z.
 // Everything is computed transposed (out^T = S^T X^T + ...), because then what one product leaves in registers is what the next
-// one reads: the 16 x 16 result of a matrix instruction holds, in lane 16 g + m, column m and rows 4 g .. 4 g + 3, and its 32-deep
-// operand column (or row) m and any eight places of the inner dimension, as long as both operands take the same ones.  Taking the
-// places 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3, two results stacked are an operand: S^T, and the decayed products of pairs.
+// one reads.  The 16 x 16 result of a matrix instruction holds, in lane 16 g + m, column m and rows 4 g .. 4 g + 3; a 32-deep operand
+// holds column (or row) m and eight places of the inner dimension, whichever, if both operands take the same.  So two results
+// stacked are an operand: S^T, and the decayed products of pairs.  Which row of the state is which place of dx is free too: row
+// 4 g + r of tile 2 k + s is place 32 k + 8 g + 4 s + r, so that the operand it meets is eight elements in a row; the columns of a
+// wave's two tiles are mixed likewise, so that a lane ends up with eight outputs in a row.
 //
 // A wave holds 16 NT columns of the state for all of dx in registers; the waves of a workgroup share the chunk's rows in LDS, and
 // each works out the products of pairs for itself (3 tiles; sharing them would cost a barrier).
+//
+// Rows lie in LDS in pieces of 16 bytes, piece p of row r at place p ^ turn(r), so that reads along rows and across them meet the
+// banks evenly without padding; memory can then be loaded straight into LDS, 64 pieces an instruction, several chunks ahead
+// (DIRECT).  Rows that cannot (odd widths, alignments or strides) go through registers, one chunk ahead.
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -19,25 +25,45 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kChunk = 32;
 
+// Where row, piece of 32 rows of D elements lies in LDS, in elements.
+template <typename T, int D>
+struct Tile {
+  static constexpr uint32_t W = 16 / sizeof(T), PIECES = D / W;
+  // What is read at once: 16 rows of one piece (along), for which the turns of 16 rows (those that share 256 bytes aside) differ; or
+  // (across) rows 0 .. 7 of four pieces in a row, in 2 bytes an element, and rows i, 4 + i, 8 + i, 12 + i of every other piece, in 4.
+  __device__ __forceinline__ static uint32_t turn(uint32_t row) {
+    const uint32_t q = (row & 15) / (PIECES < 16 ? 16 / PIECES : 1);
+    if (sizeof(T) == 2) return PIECES >= 16 ? (q & 3) << 2 | q >> 2 : PIECES == 8 ? (q & 1) << 2 | q >> 1 : q;
+    return PIECES >= 16 ? (q & 3) << 1 | (q >> 2 & 1) | (q >> 3) << 3 : (q & 1) << 1 | (q >> 1 & 1) | (q >> 2) << 2;
+  }
+  __device__ __forceinline__ static uint32_t at(uint32_t row, uint32_t piece) { return row * D + (piece ^ turn(row)) * W; }
+};
+
+// The place of dx that row m of tile a of the state is; the column of the wave's that column m of tile c is.
+__device__ __forceinline__ uint32_t state_row(uint32_t a, uint32_t m) { return 32 * (a >> 1) + 8 * (m >> 2) + 4 * (a & 1) + (m & 3); }
+template <int NT>
+__device__ __forceinline__ uint32_t state_column(uint32_t c, uint32_t m) { return NT == 2 ? 8 * (m >> 2) + 4 * c + (m & 3) : 16 * c + m; }
+
 // Operand of 16 x 32 places: 8 of the inner dimension per lane.
 template <typename T>
 struct Operand;
 
 template <>
 struct Operand<bf16> {
-  static constexpr uint32_t kWide = 8;                    // elements of 16 bytes
-  static constexpr uint32_t kPadX = 8, kPadZ = 16;        // elements behind a row: rows read along their length, across it
   bf16x8 v;
-  // Rows m of a tile, the inner dimension along them.
-  __device__ __forceinline__ static Operand along(const bf16* row, uint32_t g) {
-    const bf16x4 a = *reinterpret_cast<const bf16x4*>(row + 4 * g), b = *reinterpret_cast<const bf16x4*>(row + 16 + 4 * g);
-    return {__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
+  // A row of the tile, the inner dimension along it: 32 k + 8 g ..
+  template <int D>
+  __device__ __forceinline__ static Operand along(const bf16* tile, uint32_t row, uint32_t k, uint32_t g) {
+    return {*reinterpret_cast<const bf16x8*>(tile + Tile<bf16, D>::at(row, 4 * k + g))};
   }
-  // Columns m of a tile, the inner dimension across the rows (a transposing read: 16 lanes read 4 rows of 16 elements).
-  __device__ __forceinline__ static Operand across(const bf16* tile, uint32_t stride, uint32_t m, uint32_t g) {
+  // Columns column(0) .. column(15), of which four in a row are neighbours, the inner dimension across the 32 rows: a transposing
+  // read, in which 16 lanes read 4 rows of 4 x 4 elements.
+  template <int D, typename F>
+  __device__ __forceinline__ static Operand across(const bf16* tile, F column, uint32_t m, uint32_t g) {
     typedef __attribute__((address_space(3))) s16x4 Lds;
-    const bf16* at = tile + (4 * g + (m >> 2)) * stride + 4 * (m & 3);
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + 16 * stride));
+    const uint32_t first = column(4 * (m & 3));
+    const bf16* at = tile + Tile<bf16, D>::at(4 * g + (m >> 2), first >> 3) + (first & 4);
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + 16 * D));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     const s16x8 v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     return {__builtin_bit_cast(bf16x8, v)};
@@ -48,7 +74,18 @@ struct Operand<bf16> {
     for (int i = 0; i < 4; ++i) { o.v[i] = (bf16)a[i]; o.v[i + 4] = (bf16)b[i]; }
     return o;
   }
-  __device__ __forceinline__ float at(int i) const { return (float)v[i]; }
+  // The elements in fp32, two by two from their 32 bits.
+  __device__ __forceinline__ void widen(f32x4* a, f32x4* b) const {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      (*a)[2 * i] = __builtin_bit_cast(float, u[i] << 16);
+      (*a)[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xFFFF0000u);
+      (*b)[2 * i] = __builtin_bit_cast(float, u[i + 2] << 16);
+      (*b)[2 * i + 1] = __builtin_bit_cast(float, u[i + 2] & 0xFFFF0000u);
+    }
+  }
   __device__ __forceinline__ static f32x4 mma(const Operand& a, const Operand& b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
   }
@@ -56,17 +93,22 @@ struct Operand<bf16> {
 
 template <>
 struct Operand<float> {
-  static constexpr uint32_t kWide = 4;
-  static constexpr uint32_t kPadX = 4, kPadZ = 4;
   float v[8];
-  __device__ __forceinline__ static Operand along(const float* row, uint32_t g) {
-    return of(*reinterpret_cast<const f32x4*>(row + 4 * g), *reinterpret_cast<const f32x4*>(row + 16 + 4 * g));
+  template <int D>
+  __device__ __forceinline__ static Operand along(const float* tile, uint32_t row, uint32_t k, uint32_t g) {
+    return of(*reinterpret_cast<const f32x4*>(tile + Tile<float, D>::at(row, 8 * k + 2 * g)),
+              *reinterpret_cast<const f32x4*>(tile + Tile<float, D>::at(row, 8 * k + 2 * g + 1)));
   }
-  __device__ __forceinline__ static Operand across(const float* tile, uint32_t stride, uint32_t m, uint32_t g) {
+  template <int D, typename F>
+  __device__ __forceinline__ static Operand across(const float* tile, F column, uint32_t m, uint32_t g) {
     Operand o;
-    const float* at = tile + 4 * g * stride + m;
+    const uint32_t c = column(m);
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) { o.v[i] = at[i * stride]; o.v[i + 4] = at[(16 + i) * stride]; }
+    for (uint32_t i = 0; i < 4; ++i) {
+      const float* at = tile + Tile<float, D>::at(4 * g + i, c >> 2) + (c & 3);
+      o.v[i] = at[0];
+      o.v[i + 4] = at[16 * D];
+    }
     return o;
   }
   __device__ __forceinline__ static Operand of(f32x4 a, f32x4 b) {
@@ -75,7 +117,10 @@ struct Operand<float> {
     for (int i = 0; i < 4; ++i) { o.v[i] = a[i]; o.v[i + 4] = b[i]; }
     return o;
   }
-  __device__ __forceinline__ float at(int i) const { return v[i]; }
+  __device__ __forceinline__ void widen(f32x4* a, f32x4* b) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { (*a)[i] = v[i]; (*b)[i] = v[i + 4]; }
+  }
   __device__ __forceinline__ static f32x4 mma(const Operand& a, const Operand& b, f32x4 c) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
@@ -83,31 +128,48 @@ struct Operand<float> {
   }
 };
 
-// What a wave's lane adds to the state: Z^T w in TERMS operands whose sum is the fp32 product to 8 TERMS bits.
-template <typename T, int TERMS>
-struct Scaled {
-  Operand<T> part[TERMS];
-  __device__ __forceinline__ Scaled(const Operand<T>& z, const f32x4& w0, const f32x4& w1) {
+// What a wave's lane adds to the state, Z^T w: in 32 bits, or in bfloat16 as operands whose sum holds 16 bits of it, 24 with the
+// third.  (The state is fp32 whatever the rows are; where only rows in bfloat16 come of it, 16 bits lose nothing that shows.)
+template <typename T>
+struct Scaled;
+template <>
+struct Scaled<float> {
+  Operand<float> part;
+  __device__ __forceinline__ Scaled(const Operand<float>& z, const f32x4& w0, const f32x4& w1, bool) {
     f32x4 a, b;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { a[i] = z.at(i) * w0[i]; b[i] = z.at(i + 4) * w1[i]; }
-#pragma unroll
-    for (int t = 0; t < TERMS; ++t) {
-      part[t] = Operand<T>::of(a, b);
-      if (t + 1 < TERMS)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { a[i] -= part[t].at(i); b[i] -= part[t].at(i + 4); }
+    z.widen(&a, &b);
+    part = Operand<float>::of(a * w0, b * w1);
+  }
+  __device__ __forceinline__ f32x4 add(const Operand<float>& y, f32x4 s, bool) const { return Operand<float>::mma(y, part, s); }
+};
+template <>
+struct Scaled<bf16> {
+  Operand<bf16> part[3];
+  __device__ __forceinline__ Scaled(const Operand<bf16>& z, const f32x4& w0, const f32x4& w1, bool exact) {
+    f32x4 a, b, u, v;
+    z.widen(&a, &b);
+    a *= w0;
+    b *= w1;
+    part[0] = Operand<bf16>::of(a, b);
+    part[0].widen(&u, &v);
+    a -= u;
+    b -= v;
+    part[1] = Operand<bf16>::of(a, b);
+    if (exact) {
+      part[1].widen(&u, &v);
+      part[2] = Operand<bf16>::of(a - u, b - v);
     }
+  }
+  __device__ __forceinline__ f32x4 add(const Operand<bf16>& y, f32x4 s, bool exact) const {
+    if (exact) s = Operand<bf16>::mma(y, part[2], s);
+    return Operand<bf16>::mma(y, part[0], Operand<bf16>::mma(y, part[1], s));
   }
 };
 
-// decay^e for e >= 0 from its logarithm (which may be -infinity).
-__device__ __forceinline__ float decay_power(float g, int e) { return e == 0 ? 1.0f : expf((float)e * g); }
-
-// 32 rows of D elements on their way from memory to LDS, N pieces of 16 bytes in each thread's registers.
+// 32 rows of D elements on their way from memory to LDS through the threads' registers.
 template <typename T, int D, int THREADS>
-struct Piece {
-  static constexpr uint32_t W = Operand<T>::kWide, PER_ROW = D / W, PIECES = kChunk * PER_ROW, N = (PIECES + THREADS - 1) / THREADS;
+struct Staged {
+  static constexpr uint32_t W = Tile<T, D>::W, PER_ROW = D / W, PIECES = kChunk * PER_ROW, N = (PIECES + THREADS - 1) / THREADS;
   typedef T Vec __attribute__((ext_vector_type(W)));
   Vec v[N];
   // Rows first .. first + n of a head's sequence of `valid` tokens (against time: counted from its end), columns col0 .. col0 + D.
@@ -130,40 +192,96 @@ struct Piece {
       }
     }
   }
-  __device__ __forceinline__ void store(T* lds, uint32_t stride) const {
+  __device__ __forceinline__ void store(T* tile) const {
 #pragma unroll
     for (uint32_t k = 0; k < N; ++k) {
       const uint32_t at = threadIdx.x + k * THREADS;
-      if (PIECES % THREADS == 0 || at < PIECES) *reinterpret_cast<Vec*>(lds + at / PER_ROW * stride + at % PER_ROW * W) = v[k];
+      if (PIECES % THREADS == 0 || at < PIECES) *reinterpret_cast<Vec*>(tile + Tile<T, D>::at(at / PER_ROW, at % PER_ROW)) = v[k];
     }
   }
 };
 
-// Elements of one buffer of a chunk's rows.
+// The same straight into LDS.  A wave's instruction fills 64 places one behind the other: 1 KiB of the chunk's tiles, which lie one
+// behind the other too; the waves take these in turn.  Which piece belongs there is the lane's business: it asks for that one.
+struct Direct {
+  const uint8_t* base;   // (uniform) of the next chunk that is asked for
+  int64_t step;          // (uniform) bytes to the one after it
+  uint32_t offset;       // of the lane's piece within the chunk
+  uint32_t row;          // of the chunk; kNoRow: a column behind the width
+};
+constexpr uint32_t kNoRow = 1u << 16;
+
+template <typename T, int D>
+__device__ __forceinline__ void direct_piece(Direct* d, const SeqRows& r, const T* head, uint32_t place, int64_t token, bool back, uint32_t col0, uint32_t width) {
+  constexpr uint32_t PER_ROW = Tile<T, D>::PIECES, W = Tile<T, D>::W;
+  const uint32_t row = place / PER_ROW, piece = place % PER_ROW ^ Tile<T, D>::turn(row);
+  const int64_t bytes = r.token * (int64_t)sizeof(T);
+  d->base = reinterpret_cast<const uint8_t*>(head + col0) + token * bytes;
+  d->step = (back ? -(int64_t)kChunk : (int64_t)kChunk) * bytes;
+  d->offset = (back ? kChunk - 1 - row : row) * (uint32_t)bytes + piece * 16;
+  d->row = col0 + piece * W < width ? row : kNoRow;
+}
+
+// 16 bytes of every active lane to LDS bytes `to` + 16 lane: in flight until the wait below.  (M0 is the compiler's own only for
+// instructions that these kernels do not have.)
+__device__ __forceinline__ void load_to_lds(uint32_t to, const uint8_t* base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+// All but the wave's latest LEFT memory operations are done, its LDS operations too; then the workgroup's barrier.
+template <int LEFT>
+__device__ __forceinline__ void arrive() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// Bytes of a chunk's tiles, and how many chunks are held.  (The address that loads to LDS go to has 16 bits.)
 template <typename T, int DX, int DZ, bool OUT>
-constexpr uint32_t chunk_elements() {
-  return kChunk * ((OUT ? 2 : 1) * (DX + Operand<T>::kPadX) + DZ + Operand<T>::kPadZ);
+constexpr uint32_t chunk_bytes() { return kChunk * ((OUT ? 2 : 1) * DX + DZ) * sizeof(T); }
+template <typename T, int DX, int DZ, bool OUT, bool DIRECT>
+constexpr uint32_t ring() {
+  if (!DIRECT) return 2;
+  const uint32_t n = 65536 / chunk_bytes<T, DX, DZ, OUT>();
+  return n < 4 ? n : 4;
+}
+
+// A lane's outputs of one token, NT times four side by side, `left` elements before the end of the row.
+template <typename O, int NT>
+__device__ __forceinline__ void store_row(uint8_t* at, const f32x4 (&acc)[NT][2], int d, uint32_t left) {
+  typedef O Vec __attribute__((ext_vector_type(4 * NT)));
+  O* const to = reinterpret_cast<O*>(at);
+  if (left >= 4 * NT) {
+    Vec o;
+#pragma unroll
+    for (int i = 0; i < 4 * NT; ++i) o[i] = (O)acc[i / 4][d][i % 4];
+    *reinterpret_cast<Vec*>(to) = o;
+    return;
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < 4 * NT; ++i)
+    if (i < left) to[i] = (O)acc[i / 4][d][i % 4];
 }
 
 // OUT: the outputs are wanted too (else only the state that the piece of the sequence brings, from zeros).
-template <typename T, int DX, int NT, int WAVES, int TERMS, bool OUT>
+template <typename T, int DX, int NT, int WAVES, bool OUT, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
   constexpr int THREADS = 64 * WAVES, DZ = 16 * NT * WAVES, TX = DX / 16, KX = DX / 32;
-  constexpr uint32_t SX = DX + Operand<T>::kPadX, SZ = DZ + Operand<T>::kPadZ, BUFFER = chunk_elements<T, DX, DZ, OUT>();
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds_raw[];
+  constexpr uint32_t BUFFER = chunk_bytes<T, DX, DZ, OUT>() / sizeof(T), RING = ring<T, DX, DZ, OUT, DIRECT>();
+  extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   T* const lds = reinterpret_cast<T*>(lds_raw);
   // Workgroups go round the 8 dies by their number: the passes over the same rows sit on one die, one behind the other.
   const uint32_t which = blockIdx.x / 8 % all.count, item = blockIdx.x / (8 * all.count) * 8 + blockIdx.x % 8;
   if (item >= all.items) return;
   const AttentionPass& p = all.pass[which];
   const uint32_t slice = item % all.slices, seg = item / all.slices % all.segments, bh = item / all.slices / all.segments;
-  const uint32_t h = bh % p.H, b = bh / p.H, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
-  const uint32_t valid = valid_tokens(p.lengths, b, p.L), begin = seg * all.segment;
-  const uint32_t end = valid < begin ? begin : valid - begin < all.segment ? valid : begin + all.segment;
-  const uint32_t col0 = slice * DZ, col = col0 + wave * 16 * NT;   // first z column of the workgroup, of the wave
-  const float decay = p.log_decay[h];
-  const bool back = p.back != 0;
+  const uint32_t h = bh % p.H, b = bh / p.H, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // (what the loop needs of the arguments is taken out of them here: behind its barriers they would be loaded again)
+  const uint32_t L = p.L, dx = p.dx, dz = p.dz, segment = all.segment;
+  const float decay = p.log_decay[h], c_state = p.c_state;
+  const bool back = p.back != 0, out_f32 = p.out_f32 != 0, exact = p.exact != 0;
   const int lag = back ? 1 : 0;
+  const uint32_t valid = valid_tokens(p.lengths, b, L), begin = seg * segment;
+  const uint32_t end = valid < begin ? begin : valid - begin < segment ? valid : begin + segment;
+  const uint32_t col0 = slice * DZ, col = col0 + wave * 16 * NT;   // first z column of the workgroup, of the wave
 
   f32x4 S[TX][NT];
 #pragma unroll
@@ -171,31 +289,87 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
 #pragma unroll
     for (int c = 0; c < NT; ++c) S[a][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   if (OUT && p.in) {
+    // (all asked for at once: places behind a width take the last one's, and are cleared when all are there)
     const float* in = p.in + (int64_t)b * p.in_batch + (int64_t)h * p.in_head + (int64_t)seg * p.in_segment;
+    const uint32_t in_x = p.in_x, in_z = p.in_z;
 #pragma unroll
-    for (int a = 0; a < TX; ++a)
+    for (int c = 0; c < NT; ++c) {
+      const uint32_t j = col + state_column<NT>(c, m), at = (j < dz ? j : dz - 1) * in_z;
 #pragma unroll
-      for (int c = 0; c < NT; ++c)
+      for (int a = 0; a < TX; ++a)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const uint32_t i = 16 * a + 4 * g + r, j = col + 16 * c + m;
-          if (i < p.dx && j < p.dz) S[a][c][r] = in[i * p.in_x + j * p.in_z];
+          const uint32_t i = state_row(a, 4 * g + r);
+          S[a][c][r] = in[(i < dx ? i : dx - 1) * in_x + at];
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+      for (int a = 0; a < TX; ++a)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float s = S[a][c][r];
+          asm("" : "+v"(s));   // (the load stays above: moved into the choice each would be waited for by itself)
+          S[a][c][r] = state_row(a, 4 * g + r) < dx && col + state_column<NT>(c, m) < dz ? s : 0.0f;
         }
   }
 
   const T* const xh = OUT ? row_of<T>(p.x, b, 0, h) : nullptr;
   const T* const yh = row_of<T>(p.y, b, 0, h);
   const T* const zh = row_of<T>(p.z, b, 0, h);
-  Piece<T, DX, THREADS> px, py;
-  Piece<T, DZ, THREADS> pz;
-  auto fetch = [&](uint32_t first) {
+  const uint32_t out_size = out_f32 ? 4 : sizeof(T);
+  const int64_t out_step = p.out.token * (int64_t)out_size;
+  const bool out_wide = DIRECT || p.out.wide;
+  uint8_t* const oh = OUT ? static_cast<uint8_t*>(p.out.d) + ((int64_t)b * p.out.batch + (int64_t)(h / p.out.share) * p.out.head) * out_size : nullptr;
+  // Chunks on their way: staged in registers, or counted instructions that fill LDS.
+  Staged<T, DX, DIRECT ? 1 << 20 : THREADS> px, py;
+  Staged<T, DZ, DIRECT ? 1 << 20 : THREADS> pz;
+  constexpr uint32_t FILLS_X = OUT ? Tile<T, DX>::PIECES / 2 : 0, FILLS_Y = Tile<T, DX>::PIECES / 2, FILLS = FILLS_X + FILLS_Y + Tile<T, DZ>::PIECES / 2;
+  constexpr uint32_t MINE = (FILLS + WAVES - 1) / WAVES;
+  Direct fill[DIRECT ? MINE : 1];
+  const bool whole = dx == DX && dz - col0 >= DZ;   // no piece lies behind a width
+  const int64_t token0 = back ? (int64_t)valid - (int64_t)begin - (int64_t)kChunk : (int64_t)begin;   // lowest of the first chunk
+  if (DIRECT) {
+#pragma unroll
+    for (uint32_t k = 0; k < MINE; ++k) {
+      const uint32_t f = wave + WAVES * k;
+      fill[k].row = kNoRow;
+      if (f < FILLS_X) direct_piece<T, DX>(&fill[k], p.x, xh, f * 64 + lane, token0, back, 0, dx);
+      else if (f < FILLS_X + FILLS_Y) direct_piece<T, DX>(&fill[k], p.y, yh, (f - FILLS_X) * 64 + lane, token0, back, 0, dx);
+      else if (f < FILLS) direct_piece<T, DZ>(&fill[k], p.z, zh, (f - FILLS_X - FILLS_Y) * 64 + lane, token0, back, col0, dz);
+    }
+  }
+  // Asks for the chunk from token `first` on (the chunks one after the other), to go to a place of the ring.
+  auto fetch = [&](uint32_t first, uint32_t slot) {
     const uint32_t n = first < end ? (end - first < kChunk ? end - first : kChunk) : 0;
-    if (OUT) px.load(p.x, xh, first, n, valid, back, 0, p.dx);
-    py.load(p.y, yh, first, n, valid, back, 0, p.dx);
-    pz.load(p.z, zh, first, n, valid, back, col0, p.dz);
+    if (!DIRECT) {
+      if (OUT) px.load(p.x, xh, first, n, valid, back, 0, dx);
+      py.load(p.y, yh, first, n, valid, back, 0, dx);
+      pz.load(p.z, zh, first, n, valid, back, col0, dz);
+      return;
+    }
+    const uint32_t to = slot * BUFFER * (uint32_t)sizeof(T) + wave * 1024;
+    if (whole && n == kChunk) {
+#pragma unroll
+      for (uint32_t k = 0; k < MINE; ++k)
+        if (FILLS % WAVES == 0 || wave + WAVES * k < FILLS) load_to_lds(to + WAVES * k * 1024, fill[k].base, fill[k].offset);
+    } else {
+#pragma unroll
+      for (uint32_t k = 0; k < MINE; ++k) {
+        if (FILLS % WAVES && wave + WAVES * k >= FILLS) continue;
+        if (fill[k].row < n) load_to_lds(to + WAVES * k * 1024, fill[k].base, fill[k].offset);
+        else *reinterpret_cast<f32x4*>(lds_raw + to + WAVES * k * 1024 + 16 * lane) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < MINE; ++k) fill[k].base += fill[k].step;
   };
 
-  // Powers of the decay: between the tokens of a pair (same tile; a tile apart), to the chunk's tokens, from them, over the chunk.
+  // Powers of the decay: lane e works out decay^e, the others ask it for what they need.  Between the tokens of a pair (same tile; a
+  // tile apart), to the chunk's tokens, from them, over the chunk.
+  const float power = lane == 0 ? 1.0f : expf((float)lane * decay);
   f32x4 pair[2], into[2];
   float outof[2], keep = 0.0f;
   if (OUT) {
@@ -204,9 +378,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int e = 16 * d + (int)m - (int)(4 * g) - r;
-        pair[d][r] = e < 0 ? 0.0f : p.c_in * decay_power(decay, e);
+        const float w = p.c_in * __shfl(power, e < 0 ? 0 : e);
+        pair[d][r] = e < 0 ? 0.0f : w;
       }
-      outof[d] = p.c_out * decay_power(decay, 16 * d + (int)m + 1 - lag);
+      outof[d] = p.c_out * __shfl(power, 16 * d + (int)m + 1 - lag);
     }
   }
   auto weights = [&](int n) {
@@ -215,29 +390,46 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int e = n - 1 - 16 * d - (int)(4 * g) - r;
-        into[d][r] = e < 0 ? 0.0f : p.c_state * decay_power(decay, e + lag);
+        const float w = c_state * __shfl(power, e < 0 ? 0 : e + lag);
+        into[d][r] = e < 0 ? 0.0f : w;
       }
     // S + (decay^n - 1) S: the power itself, rounded to 32 bits, would be off by the same 2^-25 in every chunk of a slow decay
     keep = expm1f((float)n * decay);
   };
   weights(kChunk);
 
-  fetch(begin);
-  for (uint32_t first = begin, turn = 0; first < end; first += kChunk, turn ^= 1) {
-    T* const xs = lds + turn * BUFFER;
-    T* const ys = OUT ? xs + kChunk * SX : xs;
-    T* const zs = ys + kChunk * SX;
-    if (OUT) px.store(xs, SX);
-    py.store(ys, SX);
-    pz.store(zs, SZ);
-    __syncthreads();
-    if (first + kChunk < end) fetch(first + kChunk);
+  constexpr uint32_t AHEAD = RING - 1;   // chunks asked for before the one at hand
+  if (DIRECT) {
+#pragma unroll
+    for (uint32_t i = 0; i < AHEAD; ++i)
+      if (begin + i * kChunk < end) fetch(begin + i * kChunk, i);
+  } else {
+    fetch(begin, 0);
+  }
+  for (uint32_t first = begin, slot = 0; first < end; first += kChunk, slot = slot + 1 == RING ? 0 : slot + 1) {
+    T* const xs = lds + slot * BUFFER;
+    T* const ys = OUT ? xs + kChunk * DX : xs;
+    T* const zs = ys + kChunk * DX;
+    if (DIRECT) {
+      // The wave's parts of the chunks behind this one may still be on their way, at least FILLS / WAVES instructions for each whole
+      // chunk (the outputs stored meanwhile only add to what is left).  A part of a chunk may take fewer: then all are waited for.
+      if (end - first >= (RING - 1) * kChunk) arrive<(int)((RING - 2) * (FILLS / WAVES))>();
+      else arrive<0>();
+      // (this barrier: all are through with the chunk before, whose place the next one takes)
+      if (first + AHEAD * kChunk < end) fetch(first + AHEAD * kChunk, slot == 0 ? RING - 1 : slot - 1);
+    } else {
+      if (OUT) px.store(xs);
+      py.store(ys);
+      pz.store(zs);
+      __syncthreads();
+      if (first + kChunk < end) fetch(first + kChunk, 0);
+    }
     const uint32_t n = end - first < kChunk ? end - first : kChunk;
     if (n < kChunk) weights((int)n);
 
     Operand<T> z[NT];
 #pragma unroll
-    for (int c = 0; c < NT; ++c) z[c] = Operand<T>::across(zs + wave * 16 * NT + 16 * c, SZ, m, g);
+    for (int c = 0; c < NT; ++c) z[c] = Operand<T>::template across<DZ>(zs, [&](uint32_t i) { return wave * 16 * NT + state_column<NT>(c, i); }, m, g);
     if (OUT) {
       f32x4 acc[NT][2], pt[3];
       const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -246,8 +438,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
       pt[0] = pt[1] = pt[2] = zero;
 #pragma unroll
       for (int k = 0; k < KX; ++k) {
-        const Operand<T> x0 = Operand<T>::along(xs + m * SX + 32 * k, g), x1 = Operand<T>::along(xs + (16 + m) * SX + 32 * k, g);
-        const Operand<T> y0 = Operand<T>::along(ys + m * SX + 32 * k, g), y1 = Operand<T>::along(ys + (16 + m) * SX + 32 * k, g);
+        const Operand<T> x0 = Operand<T>::template along<DX>(xs, m, k, g), x1 = Operand<T>::template along<DX>(xs, 16 + m, k, g);
+        const Operand<T> y0 = Operand<T>::template along<DX>(ys, m, k, g), y1 = Operand<T>::template along<DX>(ys, 16 + m, k, g);
         pt[0] = Operand<T>::mma(y0, x0, pt[0]);
         pt[1] = Operand<T>::mma(y0, x1, pt[1]);
         pt[2] = Operand<T>::mma(y1, x1, pt[2]);
@@ -263,50 +455,74 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
       for (int c = 0; c < NT; ++c) {
         acc[c][0] = Operand<T>::mma(z[c], p0, acc[c][0] * outof[0]);
         acc[c][1] = Operand<T>::mma(z[c], p1, acc[c][1] * outof[1]);
+      }
+      // out: four columns of a token in each tile of a lane, eight side by side in two
+      if (out_wide) {
+        uint8_t* const base = oh + (back ? (int64_t)valid - (int64_t)first - (int64_t)kChunk : (int64_t)first) * out_step;
+        const uint32_t j = col + (NT == 2 ? 8 : 4) * g;
 #pragma unroll
         for (int d = 0; d < 2; ++d) {
-          const uint32_t row = 16 * d + m, j = col + 16 * c + 4 * g;
-          if (row >= n || j >= p.dz) continue;
-          const uint32_t i = first + row, t = back ? valid - 1 - i : i;
-          if (p.out_f32) store4(row_to<float>(p.out, b, t, h) + j, acc[c][d], p.out.wide, p.dz - j);
-          else store4(row_to<T>(p.out, b, t, h) + j, acc[c][d], p.out.wide, p.dz - j);
+          const uint32_t row = 16 * d + m;
+          uint8_t* const at = base + ((back ? kChunk - 1 - row : row) * (uint32_t)out_step + j * out_size);
+          if (row >= n || j >= dz) continue;
+          if (out_f32) store_row<float, NT>(at, acc, d, dz - j);
+          else store_row<T, NT>(at, acc, d, dz - j);
         }
+      } else {
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+          for (int d = 0; d < 2; ++d) {
+            const uint32_t row = 16 * d + m, i = first + row, t = back ? valid - 1 - i : i;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const uint32_t j = col + state_column<NT>(c, 4 * g + r);
+              if (row >= n || j >= dz) continue;
+              if (out_f32) row_to<float>(p.out, b, t, h)[j] = acc[c][d][r];
+              else row_to<T>(p.out, b, t, h)[j] = (T)acc[c][d][r];
+            }
+          }
       }
     }
+    {
+      Operand<T> y[TX];
 #pragma unroll
-    for (int c = 0; c < NT; ++c) {
-      const Scaled<T, TERMS> zw(z[c], into[0], into[1]);
+      for (int a = 0; a < TX; ++a) y[a] = Operand<T>::template across<DX>(ys, [&](uint32_t i) { return state_row(a, i); }, m, g);
 #pragma unroll
-      for (int a = 0; a < TX; ++a) {
-        const Operand<T> y = Operand<T>::across(ys + 16 * a, SX, m, g);
+      for (int c = 0; c < NT; ++c) {
+        const Scaled<T> zw(z[c], into[0], into[1], exact);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[a][c][r] = fmaf(S[a][c][r], keep, S[a][c][r]);
+        for (int a = 0; a < TX; ++a) {
 #pragma unroll
-        for (int t = TERMS - 1; t >= 0; --t) S[a][c] = Operand<T>::mma(y, zw.part[t], S[a][c]);
+          for (int r = 0; r < 4; ++r) S[a][c][r] = fmaf(S[a][c][r], keep, S[a][c][r]);
+          S[a][c] = zw.add(y[a], S[a][c], exact);
+        }
       }
     }
   }
 
   float* const to = OUT ? p.to : p.part;
   if (to) {
-    float* const S_out = OUT ? to + (int64_t)b * p.to_batch + (int64_t)h * p.to_head : to + ((size_t)bh * all.segments + seg) * p.dx * p.dz;
+    float* const S_out = OUT ? to + (int64_t)b * p.to_batch + (int64_t)h * p.to_head : to + ((size_t)bh * all.segments + seg) * dx * dz;
 #pragma unroll
-    for (int a = 0; a < TX; ++a)
+    for (int c = 0; c < NT; ++c) {
+      const uint32_t j = col + state_column<NT>(c, m);
+      if (j >= dz) continue;
+      float* const at = S_out + 8 * g * dz + j;
 #pragma unroll
-      for (int c = 0; c < NT; ++c)
+      for (int a = 0; a < TX; ++a)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const uint32_t i = 16 * a + 4 * g + r, j = col + 16 * c + m;
-          if (i < p.dx && j < p.dz) S_out[i * p.dz + j] = S[a][c][r];
-        }
+        for (int r = 0; r < 4; ++r)
+          if (dx == DX || state_row(a, 4 * g + r) < dx) at[state_row(a, r) * dz] = S[a][c][r];
+    }
   }
-  if (!OUT || valid >= p.L) return;
+  if (!OUT || valid >= L) return;
   // tokens behind the valid ones: zeros
-  const uint32_t width = p.dz - col0 < (uint32_t)DZ ? p.dz - col0 : DZ, from = begin > valid ? begin : valid;
-  const uint32_t until = p.L - begin < all.segment ? p.L : begin + all.segment;
+  const uint32_t width = dz - col0 < (uint32_t)DZ ? dz - col0 : DZ, from = begin > valid ? begin : valid;
+  const uint32_t until = L - begin < segment ? L : begin + segment;
   for (uint32_t t = from + wave; t < until; t += WAVES)
     for (uint32_t j = lane; j < width; j += 64) {
-      if (p.out_f32) row_to<float>(p.out, b, t, h)[col0 + j] = 0.0f;
+      if (out_f32) row_to<float>(p.out, b, t, h)[col0 + j] = 0.0f;
       else row_to<T>(p.out, b, t, h)[col0 + j] = (T)0.0f;
     }
 }

@@ -18,6 +18,7 @@ struct AttentionPass {
   uint32_t L, H, dx, dz;
   uint32_t back;                 // against time (and lag 1)
   uint32_t out_f32;              // out is fp32 whatever the rows' type
+  uint32_t exact;                // the state itself is an output (of this pass or behind it)
   float c_in, c_state, c_out;
   const float* log_decay;
   const int32_t* lengths;
@@ -49,22 +50,6 @@ struct JoinPasses {
   const int32_t* lengths;
 };
 
-// Four results side by side, `left` elements before the end of the row.
-template <typename O>
-__device__ __forceinline__ void store4(O* p, const float __attribute__((ext_vector_type(4))) & v, bool wide, uint32_t left) {
-  typedef O Four __attribute__((ext_vector_type(4)));
-  if (wide && left >= 4) {
-    Four o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = (O)v[i];
-    *reinterpret_cast<Four*>(p) = o;
-    return;
-  }
-#pragma unroll
-  for (uint32_t i = 0; i < 4; ++i)
-    if (i < left) p[i] = (O)v[i];
-}
-
 #include "k_attend.h"
 
 // Rows of heads that share one, added up: from [B][L][H][d] in fp32 to [B][L][G][d].
@@ -93,7 +78,9 @@ struct AttentionStep {
 
 SeqRows rows(const per_seq_rows& r, uint32_t dtype, uint32_t share) {
   const int64_t per16 = dtype == PER_SEQ_BF16 ? 8 : 4;
-  const bool wide = (reinterpret_cast<uintptr_t>(r.d) & 15) == 0 && r.batch % per16 == 0 && r.token % per16 == 0 && r.head % per16 == 0;
+  // (the tokens of a chunk lie within 2^31 bytes)
+  const bool wide = (reinterpret_cast<uintptr_t>(r.d) & 15) == 0 && r.batch % per16 == 0 && r.token % per16 == 0 && r.head % per16 == 0 &&
+                    r.token >= 0 && r.token < (1 << 24);
   return SeqRows{r.d, r.batch, r.token, r.head, share, wide ? 1u : 0u};
 }
 // Packed rows [B][L][H][d] in fp32.
@@ -153,10 +140,11 @@ size_t part_bytes(const AttentionSizes& a, const Cut& c) {
 }
 size_t fold_bytes(const AttentionSizes& a, uint32_t width) { return a.H == a.G ? 0 : align256((size_t)a.B * a.L * a.H * width * sizeof(float)); }
 
-template <typename T, int DX, int NT, int WAVES, int TERMS, bool OUT>
+template <typename T, int DX, int NT, int WAVES, bool OUT, bool DIRECT>
 hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
-  constexpr uint32_t lds = 2 * chunk_elements<T, DX, 16 * NT * WAVES, OUT>() * sizeof(T);
-  auto* kernel = k_attend<T, DX, NT, WAVES, TERMS, OUT>;
+  constexpr int DZ = 16 * NT * WAVES;
+  constexpr uint32_t lds = ring<T, DX, DZ, OUT, DIRECT>() * chunk_bytes<T, DX, DZ, OUT>();
+  auto* kernel = k_attend<T, DX, NT, WAVES, OUT, DIRECT>;
   if (lds > 64 * 1024) {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
@@ -164,22 +152,37 @@ hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
   kernel<<<(p.items + 7) / 8 * 8 * p.count, 64 * WAVES, lds, s>>>(p);
   return hipGetLastError();
 }
-template <typename T, int DX, int TERMS, bool OUT>
+// Straight into LDS where pieces of 16 bytes make up the rows, and where two chunks fit.
+template <typename T, int DX, int NT, int WAVES, bool OUT>
+hipError_t launch_way(const AttentionPasses& p, hipStream_t s) {
+  bool direct = true;
+  for (uint32_t i = 0; i < p.count; ++i) {
+    const AttentionPass& a = p.pass[i];
+    const uint32_t per16 = 16 / sizeof(T);
+    direct = direct && (!OUT || (a.x.wide && a.out.wide)) && a.y.wide && a.z.wide && a.dx % per16 == 0 && a.dz % per16 == 0;
+  }
+  if constexpr (ring<T, DX, 16 * NT * WAVES, OUT, true>() >= 2) {
+    if (direct) return launch_as<T, DX, NT, WAVES, OUT, true>(p, s);
+  }
+  return launch_as<T, DX, NT, WAVES, OUT, false>(p, s);
+}
+template <typename T, int DX, bool OUT>
 hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {
   const uint32_t dz = p.pass[0].dz;
   p.slices = 1;
   p.items = rows * p.segments;
-  if (dz <= 32) return launch_as<T, DX, 1, 2, TERMS, OUT>(p, s);
-  if (dz <= 64) return launch_as<T, DX, 1, 4, TERMS, OUT>(p, s);
-  return launch_as<T, DX, 2, 4, TERMS, OUT>(p, s);
+  if (dz <= 32) return launch_way<T, DX, 1, 2, OUT>(p, s);
+  if (dz <= 64) return launch_way<T, DX, 1, 4, OUT>(p, s);
+  return launch_way<T, DX, 2, 4, OUT>(p, s);
 }
-// Passes of the same widths, in one launch.
-template <typename T, int TERMS, bool OUT>
+// Passes of the same widths (as kernels go), in one launch.
+uint32_t kernel_width(uint32_t d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+template <typename T, bool OUT>
 hipError_t launch_passes(AttentionPasses p, uint32_t rows, hipStream_t s) {
   const uint32_t dx = p.pass[0].dx;
-  if (dx <= 32) return launch_dz<T, 32, TERMS, OUT>(p, rows, s);
-  if (dx <= 64) return launch_dz<T, 64, TERMS, OUT>(p, rows, s);
-  return launch_dz<T, 128, TERMS, OUT>(p, rows, s);
+  if (dx <= 32) return launch_dz<T, 32, OUT>(p, rows, s);
+  if (dx <= 64) return launch_dz<T, 64, OUT>(p, rows, s);
+  return launch_dz<T, 128, OUT>(p, rows, s);
 }
 
 void join_from(JoinPass* j, const per_seq_states* s) {
@@ -214,7 +217,6 @@ hipError_t launch_join(JoinPasses j, const AttentionSizes& a, const Cut& c, uint
 template <typename T>
 hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
                    const per_seq_states* state, const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
-  constexpr bool F = sizeof(T) == 4;
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
   const Cut c = cut(a);
   AttentionPasses all{};
@@ -230,10 +232,12 @@ hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq
   if (c.segments == 1) {
     from_states(&p, state, a.dv, false);
     to_states(&p, out_state);
-    return out_state ? launch_passes<T, F ? 1 : 3, true>(all, bh, s) : launch_passes<T, F ? 1 : 2, true>(all, bh, s);
+    p.exact = out_state != nullptr;
+    return launch_passes<T, true>(all, bh, s);
   }
   p.part = static_cast<float*>(work);
-  hipError_t e = launch_passes<T, F ? 1 : 3, false>(all, bh, s);
+  p.exact = out_state != nullptr;
+  hipError_t e = launch_passes<T, false>(all, bh, s);
   if (e != hipSuccess) return e;
   JoinPasses j{};
   j.pass[0] = JoinPass{p.part, nullptr, 0, 0, nullptr, 0, 0, a.dk, a.dv};
@@ -242,14 +246,14 @@ hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq
   e = launch_join(j, a, c, 1, s);
   if (e != hipSuccess) return e;
   from_parts(&p, p.part, a, c, false);
-  return launch_passes<T, F ? 1 : 2, true>(all, bh, s);
+  p.exact = 0;
+  return launch_passes<T, true>(all, bh, s);
 }
 
 template <typename T>
 hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per_seq_rows& q, const per_seq_rows& k,
                     const per_seq_rows& v, const per_seq_states* state, const per_seq_states* dstate, const per_seq_rows& dq,
                     const per_seq_rows& dk, const per_seq_rows& dv, const per_seq_states* dstate0, void* work, hipStream_t s) {
-  constexpr bool F = sizeof(T) == 4;
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
   const Cut c = cut(a);
   const SeqRows Q = rows(q, a.dtype, 1), K = rows(k, a.dtype, share), V = rows(v, a.dtype, share), D = rows(dout, a.dtype, 1);
@@ -276,14 +280,16 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
     from_states(&of_k, dstate, a.dv, true);
     from_states(&of_v, dstate, a.dv, false);
     to_states(&of_v, dstate0);
+    of_v.exact = dstate0 != nullptr;
   } else {
     all.count = 2;
     all.pass[0] = make_pass(a, false, a.dk, a.dv);
     all.pass[0].y = K;
     all.pass[0].z = V;
     all.pass[1] = of_v;
+    all.pass[1].exact = dstate0 != nullptr;
     for (int i = 0; i < 2; ++i) all.pass[i].part = part[i];
-    e = launch_passes<T, F ? 1 : 3, false>(all, bh, s);
+    e = launch_passes<T, false>(all, bh, s);
     if (e != hipSuccess) return e;
     JoinPasses j{};
     for (int i = 0; i < 2; ++i) j.pass[i] = JoinPass{part[i], nullptr, 0, 0, nullptr, 0, 0, a.dk, a.dv};
@@ -296,15 +302,18 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
     from_parts(&of_k, part[1], a, c, true);
     from_parts(&of_v, part[1], a, c, false);
   }
-  // (the gradient of k reads dstate, which that of v may write over: it comes first)
-  all.count = 2;
+  // All three in one launch where they take the same kernel; but the gradient of k reads dstate, which that of v may write over.
   all.pass[0] = of_q;
   all.pass[1] = of_k;
-  e = launch_passes<T, F ? 1 : 2, true>(all, bh, s);
-  if (e != hipSuccess) return e;
-  all.count = 1;
-  all.pass[0] = of_v;
-  e = of_v.to ? launch_passes<T, F ? 1 : 3, true>(all, bh, s) : launch_passes<T, F ? 1 : 2, true>(all, bh, s);
+  all.pass[2] = of_v;
+  const bool over = c.segments == 1 && dstate && dstate0 && dstate->d == dstate0->d;
+  all.count = !over && kernel_width(a.dk) == kernel_width(a.dv) ? 3 : 2;
+  e = launch_passes<T, true>(all, bh, s);
+  if (e == hipSuccess && all.count == 2) {
+    all.count = 1;
+    all.pass[0] = of_v;
+    e = launch_passes<T, true>(all, bh, s);
+  }
   if (e != hipSuccess || share == 1) return e;
   for (int i = 0; i < 2 && e == hipSuccess; ++i) {
     const uint32_t width = i ? a.dv : a.dk;
