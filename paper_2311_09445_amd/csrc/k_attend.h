@@ -279,8 +279,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
   const float decay = p.log_decay[h], c_state = p.c_state;
   const bool back = p.back != 0, out_f32 = p.out_f32 != 0, exact = p.exact != 0;
   const int lag = back ? 1 : 0;
-  const uint32_t valid = valid_tokens(p.lengths, b, L), begin = seg * segment;
-  const uint32_t end = valid < begin ? begin : valid - begin < segment ? valid : begin + segment;
+  const uint32_t valid = valid_tokens(p.lengths, b, L), start = seg * segment;
+  const uint32_t end = valid < start ? start : valid - start < segment ? valid : start + segment;
+  uint32_t begin = start;
+  if (!OUT && decay < 0.0f && end > start) {
+    // Tokens so far before the segment's end that their weight, decay^e, is zero in 32 bits (exp below -104) bring nothing to its state.
+    const float reach = 104.0f / -decay + 2.0f;
+    const uint32_t n = end - start;
+    if (reach < (float)n) begin += (n - (uint32_t)reach) / kChunk * kChunk;
+  }
   const uint32_t col0 = slice * DZ, col = col0 + wave * 16 * NT;   // first z column of the workgroup, of the wave
 
   f32x4 S[TX][NT];
@@ -518,8 +525,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
   }
   if (!OUT || valid >= L) return;
   // tokens behind the valid ones: zeros
-  const uint32_t width = dz - col0 < (uint32_t)DZ ? dz - col0 : DZ, from = begin > valid ? begin : valid;
-  const uint32_t until = L - begin < segment ? L : begin + segment;
+  const uint32_t width = dz - col0 < (uint32_t)DZ ? dz - col0 : DZ, from = start > valid ? start : valid;
+  const uint32_t until = L - start < segment ? L : start + segment;
   for (uint32_t t = from + wave; t < until; t += WAVES)
     for (uint32_t j = lane; j < width; j += 64) {
       if (out_f32) row_to<float>(p.out, b, t, h)[col0 + j] = 0.0f;

@@ -52,17 +52,35 @@ struct JoinPasses {
 
 #include "k_attend.h"
 
-// Rows of heads that share one, added up: from [B][L][H][d] in fp32 to [B][L][G][d].
-template <typename T>
-__global__ __launch_bounds__(256) void k_fold_heads(const float* from, SeqRows to, uint32_t L, uint32_t G, uint32_t share, uint32_t d, uint64_t n) {
-  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  const uint32_t e = (uint32_t)(i % d);
-  const uint64_t row = i / d;
-  const uint32_t g = (uint32_t)(row % G), t = (uint32_t)(row / G % L), b = (uint32_t)(row / G / L);
-  float sum = 0.0f;
-  for (uint32_t m = 0; m < share; ++m) sum += from[((row / G * G + g) * share + m) * d + e];
-  row_to<T>(to, b, t, g)[e] = (T)sum;
+// Rows of heads that share one, added up in the heads' order: from [B][L][H][d] in fp32 to [B][L][G][d].
+struct Fold {
+  const float* from;
+  SeqRows to;
+  uint32_t d;
+};
+struct Folds {
+  Fold fold[2];
+  uint32_t L, G, share;
+  uint64_t rows;   // B L G
+};
+// VEC elements to a lane; 32 lanes take a row.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void k_fold_heads(Folds all) {
+  typedef float Vec __attribute__((ext_vector_type(VEC)));
+  typedef T Out __attribute__((ext_vector_type(VEC)));
+  const Fold& f = all.fold[blockIdx.y];
+  const uint32_t lanes = (f.d + VEC - 1) / VEC, per = 256 / lanes, lane = threadIdx.x % lanes;
+  const uint64_t row = (uint64_t)blockIdx.x * per + threadIdx.x / lanes;
+  if (threadIdx.x / lanes >= per || row >= all.rows) return;
+  const uint32_t g = (uint32_t)(row % all.G);
+  const uint64_t tok = row / all.G;
+  const float* from = f.from + row * all.share * f.d + lane * VEC;
+  Vec sum = Vec(0.0f);
+  for (uint32_t m = 0; m < all.share; ++m) sum += *reinterpret_cast<const Vec*>(from + (size_t)m * f.d);
+  Out o;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) o[i] = (T)sum[i];
+  *reinterpret_cast<Out*>(row_to<T>(f.to, (uint32_t)(tok / all.L), (uint32_t)(tok % all.L), g) + lane * VEC) = o;
 }
 
 struct AttentionStep {
@@ -120,19 +138,37 @@ void to_states(AttentionPass* p, const per_seq_states* s) {
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 // How a sequence is cut.  A workgroup takes its tokens one chunk behind the other, so what cuts the time of few sequences is
-// workgroups: the sequence in segments, each from the state that those before it bring.  That costs another pass over keys and
-// values for those states, and a state in memory per segment.
+// workgroups: the sequence in segments, each from the state that those before it bring.  That costs another pass over keys and values
+// for those states, a state in memory per segment, and two launches.  The fewest microseconds by these measured figures are taken:
+//   a chunk of 64 x 64 takes 0.85 (fp32: 1.5), of 128 x 64 1.2 (2.7), of 128 x 128 1.9; two workgroups on a compute unit half as long
+//   again, more take turns; the pass for the states 0.55 of a pass with outputs; launches 12; states 4 TB/s.
+// Measured, whole against cut: 64 rows of 1024 tokens (64 x 64) 33 us and 25 in four; 4 rows of 1024 31 and 17 in sixteen; 4 rows of
+// 512 18 and 17; the gradient of 64 rows of 1024 34 and 37 in four; of 32 rows of 16384 (128 x 128) 426 in 5, 462 in 8, 455 in 16.
 struct Cut {
   uint32_t segments, segment;
 };
-Cut cut(const AttentionSizes& a) {
-  const uint64_t rows = (uint64_t)a.B * a.H;
-  uint64_t segments = 1;
-  if (rows && rows < 256) segments = (512 + rows - 1) / rows;
-  const uint64_t most = a.L / 256;
-  if (segments > most) segments = most;
-  if (segments < 2) return Cut{1, a.L ? a.L : 1};
-  const uint32_t segment = (uint32_t)((a.L + segments - 1) / segments + kChunk - 1) / kChunk * kChunk;
+uint32_t kernel_width(uint32_t d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+// Half of the columns to a workgroup: see launch_dz.
+bool halved(uint32_t dtype, uint32_t dz, uint64_t workgroups) { return dz > 64 && (dtype == PER_SEQ_F32 || workgroups <= 256); }
+Cut cut(const AttentionSizes& a, uint32_t passes) {
+  const uint64_t n = (uint64_t)a.B * a.H * passes;   // workgroups of whole sequences
+  const uint32_t most = a.L / 64 < 64 ? a.L / 64 : 64;
+  const float x = (float)kernel_width(a.dk) / 64.0f, z = (float)kernel_width(a.dv) / 64.0f, state = 4.0f * a.dk * a.dv;
+  float best = 0.0f;
+  uint32_t segments = 1;
+  for (uint32_t s = 1; n && s <= (most ? most : 1); ++s) {
+    const bool half = halved(a.dtype, a.dv, n * s);
+    const uint64_t each = (n * s * (half ? 2 : 1) + 255) / 256;   // workgroups to a compute unit
+    const float chunk = a.dtype == PER_SEQ_F32 ? 0.3f + 1.2f * x * (half ? z / 2 : z) : 0.5f + 0.35f * x * (half ? z / 2 : z);
+    float us = chunk * (float)((a.L / s + kChunk - 1) / kChunk) * ((float)(each / 2) * 1.5f + (float)(each % 2));
+    if (s > 1) us = us * (passes == 1 ? 1.55f : 1.37f) + 12.0f + state * (float)((uint64_t)a.B * a.H * s * (passes == 1 ? 4 : 8)) / 4e6f;
+    if (s == 1 || us < best) {
+      best = us;
+      segments = s;
+    }
+  }
+  if (segments == 1) return Cut{1, a.L ? a.L : 1};
+  const uint32_t segment = ((a.L + segments - 1) / segments + kChunk - 1) / kChunk * kChunk;
   return Cut{(a.L + segment - 1) / segment, segment};
 }
 size_t part_bytes(const AttentionSizes& a, const Cut& c) {
@@ -173,10 +209,18 @@ hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {
   p.items = rows * p.segments;
   if (dz <= 32) return launch_way<T, DX, 1, 2, OUT>(p, s);
   if (dz <= 64) return launch_way<T, DX, 1, 4, OUT>(p, s);
-  return launch_way<T, DX, 2, 4, OUT>(p, s);
+  // Wider states: two tiles of columns to a wave, or half of the columns to a workgroup where there are few (each then reads x and y:
+  // 16 rows of 1024 tokens of 128 x 128 61 us and 44, 128 rows of 512 37 and 29, but 16 of 65536 in 32 segments 371 and 434) and in
+  // fp32, where two tiles do not fit the registers (16 rows of 1024 333 us and 170).
+  if (halved(sizeof(T) == 4 ? PER_SEQ_F32 : PER_SEQ_BF16, dz, (uint64_t)p.items * p.count)) {
+    p.slices = 2;
+    p.items *= 2;
+    return launch_way<T, DX, 1, 4, OUT>(p, s);
+  }
+  if constexpr (sizeof(T) == 2) return launch_way<T, DX, 2, 4, OUT>(p, s);
+  return hipErrorInvalidValue;
 }
 // Passes of the same widths (as kernels go), in one launch.
-uint32_t kernel_width(uint32_t d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 template <typename T, bool OUT>
 hipError_t launch_passes(AttentionPasses p, uint32_t rows, hipStream_t s) {
   const uint32_t dx = p.pass[0].dx;
@@ -218,7 +262,7 @@ template <typename T>
 hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
                    const per_seq_states* state, const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
-  const Cut c = cut(a);
+  const Cut c = cut(a, 1);
   AttentionPasses all{};
   all.count = 1;
   all.segments = c.segments;
@@ -255,7 +299,7 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
                     const per_seq_rows& v, const per_seq_states* state, const per_seq_states* dstate, const per_seq_rows& dq,
                     const per_seq_rows& dk, const per_seq_rows& dv, const per_seq_states* dstate0, void* work, hipStream_t s) {
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
-  const Cut c = cut(a);
+  const Cut c = cut(a, 3);
   const SeqRows Q = rows(q, a.dtype, 1), K = rows(k, a.dtype, share), V = rows(v, a.dtype, share), D = rows(dout, a.dtype, 1);
   uint8_t* at = static_cast<uint8_t*>(work);
   float* part[2];   // of the states, of their gradients
@@ -315,20 +359,27 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
     e = launch_passes<T, true>(all, bh, s);
   }
   if (e != hipSuccess || share == 1) return e;
-  for (int i = 0; i < 2 && e == hipSuccess; ++i) {
-    const uint32_t width = i ? a.dv : a.dk;
-    const uint64_t n = (uint64_t)a.B * a.L * a.G * width;
-    if (!n) continue;
-    k_fold_heads<T><<<(uint32_t)((n + 255) / 256), 256, 0, s>>>(i ? fold_v : fold_k, rows(i ? dv : dk, a.dtype, 1), a.L, a.G, share, width, n);
-    e = hipGetLastError();
-  }
+  Folds f{};
+  f.fold[0] = Fold{fold_k, rows(dk, a.dtype, 1), a.dk};
+  f.fold[1] = Fold{fold_v, rows(dv, a.dtype, 1), a.dv};
+  f.L = a.L;
+  f.G = a.G;
+  f.share = share;
+  f.rows = (uint64_t)a.B * a.L * a.G;
+  if (!f.rows) return e;
+  const bool wide = a.dk % 4 == 0 && a.dv % 4 == 0 && f.fold[0].to.wide && f.fold[1].to.wide;
+  const uint32_t widest = a.dk > a.dv ? a.dk : a.dv, per = 256 / (wide ? (widest + 3) / 4 : widest);   // rows of a workgroup
+  const dim3 grid((uint32_t)((f.rows + per - 1) / per), 2);
+  if (wide) k_fold_heads<T, 4><<<grid, 256, 0, s>>>(f);
+  else k_fold_heads<T, 1><<<grid, 256, 0, s>>>(f);
+  e = hipGetLastError();
   return e;
 }
 
 }  // namespace
 
 size_t attention_work_bytes(const AttentionSizes& a, bool backward) {
-  const Cut c = cut(a);
+  const Cut c = cut(a, backward ? 3 : 1);
   return backward ? 2 * part_bytes(a, c) + fold_bytes(a, a.dk) + fold_bytes(a, a.dv) : part_bytes(a, c);
 }
 

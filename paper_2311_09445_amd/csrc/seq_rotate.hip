@@ -190,6 +190,8 @@ hipError_t launch(RotaryKind kind, RotaryArgs a, float* dqw, float* dkw, hipStre
     uint64_t n = 8 * 256 / lanes / heads;
     if (n > tokens / 1024) n = tokens / 1024;
     if (n > 4096 / (a.rot / 2 + 1)) n = 4096 / (a.rot / 2 + 1);
+    // (a gradient's workgroups are bounded by their sums: a few tokens more to each rather than a round more for some)
+    if (kind == NORM_ROTATE_BACK && n * most < tokens) n = (tokens + most - 1) / most < 4096 / (a.rot / 2 + 1) ? (tokens + most - 1) / most : n;
     a.tokens = n ? (uint32_t)n : 1;
     a.tiles = (uint32_t)((tokens + a.tokens - 1) / a.tokens);
     blocks = kind == NORM_ROTATE_BACK && a.tiles > most ? most : a.tiles;
