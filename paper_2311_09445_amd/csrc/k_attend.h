@@ -135,34 +135,45 @@ struct Scaled;
 template <>
 struct Scaled<float> {
   Operand<float> part;
-  __device__ __forceinline__ Scaled(const Operand<float>& z, const f32x4& w0, const f32x4& w1, bool) {
+  __device__ __forceinline__ Scaled(const Operand<float>& z, const f32x4& w0, const f32x4& w1) {
     f32x4 a, b;
     z.widen(&a, &b);
     part = Operand<float>::of(a * w0, b * w1);
   }
-  __device__ __forceinline__ f32x4 add(const Operand<float>& y, f32x4 s, bool) const { return Operand<float>::mma(y, part, s); }
+  template <int TX>
+  __device__ __forceinline__ void add(const Operand<float> (&y)[TX], f32x4 (&s)[TX], bool) const {
+#pragma unroll
+    for (int a = 0; a < TX; ++a) s[a] = Operand<float>::mma(y[a], part, s[a]);
+  }
 };
 template <>
 struct Scaled<bf16> {
-  Operand<bf16> part[3];
-  __device__ __forceinline__ Scaled(const Operand<bf16>& z, const f32x4& w0, const f32x4& w1, bool exact) {
-    f32x4 a, b, u, v;
-    z.widen(&a, &b);
-    a *= w0;
-    b *= w1;
-    part[0] = Operand<bf16>::of(a, b);
-    part[0].widen(&u, &v);
-    a -= u;
-    b -= v;
-    part[1] = Operand<bf16>::of(a, b);
-    if (exact) {
-      part[1].widen(&u, &v);
-      part[2] = Operand<bf16>::of(a - u, b - v);
+  Operand<bf16> part[2];
+  f32x4 rest0, rest1;
+  __device__ __forceinline__ Scaled(const Operand<bf16>& z, const f32x4& w0, const f32x4& w1) {
+    f32x4 u, v;
+    z.widen(&rest0, &rest1);
+    rest0 *= w0;
+    rest1 *= w1;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      part[t] = Operand<bf16>::of(rest0, rest1);
+      part[t].widen(&u, &v);
+      rest0 -= u;
+      rest1 -= v;
     }
   }
-  __device__ __forceinline__ f32x4 add(const Operand<bf16>& y, f32x4 s, bool exact) const {
-    if (exact) s = Operand<bf16>::mma(y, part[2], s);
-    return Operand<bf16>::mma(y, part[0], Operand<bf16>::mma(y, part[1], s));
+  template <int TX>
+  __device__ __forceinline__ void add(const Operand<bf16> (&y)[TX], f32x4 (&s)[TX], bool exact) const {
+    if (exact) {
+      const Operand<bf16> third = Operand<bf16>::of(rest0, rest1);
+#pragma unroll
+      for (int a = 0; a < TX; ++a) s[a] = Operand<bf16>::mma(y[a], third, s[a]);
+    }
+#pragma unroll
+    for (int a = 0; a < TX; ++a) s[a] = Operand<bf16>::mma(y[a], part[1], s[a]);
+#pragma unroll
+    for (int a = 0; a < TX; ++a) s[a] = Operand<bf16>::mma(y[a], part[0], s[a]);
   }
 };
 
@@ -223,9 +234,10 @@ __device__ __forceinline__ void direct_piece(Direct* d, const SeqRows& r, const 
 }
 
 // 16 bytes of every active lane to LDS bytes `to` + 16 lane: in flight until the wait below.  (M0 is the compiler's own only for
-// instructions that these kernels do not have.)
+// instructions that these kernels do not have.  The compiler does not see a memory instruction here, so the wait states between it
+// and what may have set its scalar registers, five, are here.)
 __device__ __forceinline__ void load_to_lds(uint32_t to, const uint8_t* base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
 // All but the wave's latest LEFT memory operations are done, its LDS operations too; then the workgroup's barrier.
 template <int LEFT>
@@ -259,6 +271,28 @@ __device__ __forceinline__ void store_row(uint8_t* at, const f32x4 (&acc)[NT][2]
   for (uint32_t i = 0; i < 4 * NT; ++i)
     if (i < left) to[i] = (O)acc[i / 4][d][i % 4];
 }
+// The same where rows are whole pieces, as one instruction (two in fp32 and NT = 2): they are counted.  The compiler does not see
+// that it is a store, so the wait states are here: behind it one, for its registers, which what follows may write; before it five, for
+// its scalar registers, or 16 where its values come straight out of a matrix instruction (8 passes and 3).
+template <bool STRAIGHT, typename V>
+__device__ __forceinline__ void store_counted(uint8_t* base, uint32_t offset, const V& v) {
+  if constexpr (STRAIGHT) asm volatile("s_nop 15\n\tglobal_store_dwordx4 %0, %1, %2\n\ts_nop 0" ::"v"(offset), "v"(v), "s"(base) : "memory");
+  else if constexpr (sizeof(V) == 16) asm volatile("s_nop 4\n\tglobal_store_dwordx4 %0, %1, %2\n\ts_nop 0" ::"v"(offset), "v"(v), "s"(base) : "memory");
+  else asm volatile("s_nop 4\n\tglobal_store_dwordx2 %0, %1, %2\n\ts_nop 0" ::"v"(offset), "v"(v), "s"(base) : "memory");
+}
+template <typename O, int NT>
+__device__ __forceinline__ void store_row_counted(uint8_t* base, uint32_t offset, const f32x4 (&acc)[NT][2], int d) {
+  if constexpr (sizeof(O) == 4) {
+#pragma unroll
+    for (int c = 0; c < NT; ++c) store_counted<true>(base, offset + 16 * c, acc[c][d]);
+  } else {
+    typedef O Vec __attribute__((ext_vector_type(4 * NT)));
+    Vec o;
+#pragma unroll
+    for (int i = 0; i < 4 * NT; ++i) o[i] = (O)acc[i / 4][d][i % 4];
+    store_counted<false>(base, offset, o);
+  }
+}
 
 // OUT: the outputs are wanted too (else only the state that the piece of the sequence brings, from zeros).
 template <typename T, int DX, int NT, int WAVES, bool OUT, bool DIRECT>
@@ -290,11 +324,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
   }
   const uint32_t col0 = slice * DZ, col = col0 + wave * 16 * NT;   // first z column of the workgroup, of the wave
 
-  f32x4 S[TX][NT];
+  f32x4 S[NT][TX];
 #pragma unroll
   for (int a = 0; a < TX; ++a)
 #pragma unroll
-    for (int c = 0; c < NT; ++c) S[a][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = 0; c < NT; ++c) S[c][a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   if (OUT && p.in) {
     // (all asked for at once: places behind a width take the last one's, and are cleared when all are there)
     const float* in = p.in + (int64_t)b * p.in_batch + (int64_t)h * p.in_head + (int64_t)seg * p.in_segment;
@@ -307,7 +341,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const uint32_t i = state_row(a, 4 * g + r);
-          S[a][c][r] = in[(i < dx ? i : dx - 1) * in_x + at];
+          S[c][a][r] = in[(i < dx ? i : dx - 1) * in_x + at];
         }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -317,9 +351,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
       for (int a = 0; a < TX; ++a)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float s = S[a][c][r];
+          float s = S[c][a][r];
           asm("" : "+v"(s));   // (the load stays above: moved into the choice each would be waited for by itself)
-          S[a][c][r] = state_row(a, 4 * g + r) < dx && col + state_column<NT>(c, m) < dz ? s : 0.0f;
+          S[c][a][r] = state_row(a, 4 * g + r) < dx && col + state_column<NT>(c, m) < dz ? s : 0.0f;
         }
   }
 
@@ -405,6 +439,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
   };
   weights(kChunk);
 
+  const bool stores = col < dz;           // the wave has outputs to store
   constexpr uint32_t AHEAD = RING - 1;   // chunks asked for before the one at hand
   if (DIRECT) {
 #pragma unroll
@@ -418,10 +453,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
     T* const ys = OUT ? xs + kChunk * DX : xs;
     T* const zs = ys + kChunk * DX;
     if (DIRECT) {
-      // The wave's parts of the chunks behind this one may still be on their way, at least FILLS / WAVES instructions for each whole
-      // chunk (the outputs stored meanwhile only add to what is left).  A part of a chunk may take fewer: then all are waited for.
-      if (end - first >= (RING - 1) * kChunk) arrive<(int)((RING - 2) * (FILLS / WAVES))>();
-      else arrive<0>();
+      // Behind the wave's parts of this chunk are those of the next RING - 2, at least FILLS / WAVES instructions each if they are
+      // whole, and the outputs of the last RING - 1, two rows each.  That many may be left; towards the end none.
+      constexpr int LOADS = (int)((RING - 2) * (FILLS / WAVES)), STORES = OUT ? 2 * (int)(RING - 1) : 0;
+      if (end - first < (RING - 1) * kChunk) arrive<0>();
+      else if (!OUT || !stores || first - begin < (RING - 1) * kChunk) arrive<LOADS>();
+      else if (NT == 2 && out_f32) arrive<LOADS + 2 * STORES>();
+      else arrive<LOADS + STORES>();
       // (this barrier: all are through with the chunk before, whose place the next one takes)
       if (first + AHEAD * kChunk < end) fetch(first + AHEAD * kChunk, slot == 0 ? RING - 1 : slot - 1);
     } else {
@@ -434,11 +472,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
     const uint32_t n = end - first < kChunk ? end - first : kChunk;
     if (n < kChunk) weights((int)n);
 
-    Operand<T> z[NT];
+    Operand<T> z[NT], y[TX];
 #pragma unroll
     for (int c = 0; c < NT; ++c) z[c] = Operand<T>::template across<DZ>(zs, [&](uint32_t i) { return wave * 16 * NT + state_column<NT>(c, i); }, m, g);
+    f32x4 acc[NT][2];
     if (OUT) {
-      f32x4 acc[NT][2], pt[3];
+      f32x4 pt[3];
       const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int c = 0; c < NT; ++c) acc[c][0] = acc[c][1] = zero;
@@ -452,7 +491,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
         pt[2] = Operand<T>::mma(y1, x1, pt[2]);
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
-          const Operand<T> s = Operand<T>::of(S[2 * k][c], S[2 * k + 1][c]);
+          const Operand<T> s = Operand<T>::of(S[c][2 * k], S[c][2 * k + 1]);
           acc[c][0] = Operand<T>::mma(s, x0, acc[c][0]);
           acc[c][1] = Operand<T>::mma(s, x1, acc[c][1]);
         }
@@ -463,48 +502,55 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
         acc[c][0] = Operand<T>::mma(z[c], p0, acc[c][0] * outof[0]);
         acc[c][1] = Operand<T>::mma(z[c], p1, acc[c][1] * outof[1]);
       }
-      // out: four columns of a token in each tile of a lane, eight side by side in two
-      if (out_wide) {
-        uint8_t* const base = oh + (back ? (int64_t)valid - (int64_t)first - (int64_t)kChunk : (int64_t)first) * out_step;
-        const uint32_t j = col + (NT == 2 ? 8 : 4) * g;
+    }
+#pragma unroll
+    for (int a = 0; a < TX; ++a) y[a] = Operand<T>::template across<DX>(ys, [&](uint32_t i) { return state_row(a, i); }, m, g);
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+      const Scaled<T> zw(z[c], into[0], into[1]);
+#pragma unroll
+      for (int a = 0; a < TX; ++a)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[c][a][r] = fmaf(S[c][a][r], keep, S[c][a][r]);
+      zw.add(y, S[c], exact);
+    }
+    if (!OUT) continue;
+    // out: four columns of a token in each tile of a lane, eight side by side in two
+    const uint32_t j = col + (NT == 2 ? 8 : 4) * g;
+    uint8_t* const base = oh + (back ? (int64_t)valid - (int64_t)first - (int64_t)kChunk : (int64_t)first) * out_step;
+    if (DIRECT) {
+      const uint32_t lower = (back ? kChunk - 1 - m : m) * (uint32_t)out_step + j * out_size;
+      const uint32_t upper = lower + (back ? -16 : 16) * (uint32_t)out_step;
+      if (out_f32) {
+        if (m < n && j < dz) store_row_counted<float, NT>(base, lower, acc, 0);
+        if (16 + m < n && j < dz) store_row_counted<float, NT>(base, upper, acc, 1);
+      } else {
+        if (m < n && j < dz) store_row_counted<T, NT>(base, lower, acc, 0);
+        if (16 + m < n && j < dz) store_row_counted<T, NT>(base, upper, acc, 1);
+      }
+    } else if (out_wide) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const uint32_t row = 16 * d + m;
+        uint8_t* const at = base + ((back ? kChunk - 1 - row : row) * (uint32_t)out_step + j * out_size);
+        if (row >= n || j >= dz) continue;
+        if (out_f32) store_row<float, NT>(at, acc, d, dz - j);
+        else store_row<T, NT>(at, acc, d, dz - j);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
 #pragma unroll
         for (int d = 0; d < 2; ++d) {
-          const uint32_t row = 16 * d + m;
-          uint8_t* const at = base + ((back ? kChunk - 1 - row : row) * (uint32_t)out_step + j * out_size);
-          if (row >= n || j >= dz) continue;
-          if (out_f32) store_row<float, NT>(at, acc, d, dz - j);
-          else store_row<T, NT>(at, acc, d, dz - j);
-        }
-      } else {
+          const uint32_t row = 16 * d + m, i = first + row, t = back ? valid - 1 - i : i;
 #pragma unroll
-        for (int c = 0; c < NT; ++c)
-#pragma unroll
-          for (int d = 0; d < 2; ++d) {
-            const uint32_t row = 16 * d + m, i = first + row, t = back ? valid - 1 - i : i;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const uint32_t j = col + state_column<NT>(c, 4 * g + r);
-              if (row >= n || j >= dz) continue;
-              if (out_f32) row_to<float>(p.out, b, t, h)[j] = acc[c][d][r];
-              else row_to<T>(p.out, b, t, h)[j] = (T)acc[c][d][r];
-            }
+          for (int r = 0; r < 4; ++r) {
+            const uint32_t e = col + state_column<NT>(c, 4 * g + r);
+            if (row >= n || e >= dz) continue;
+            if (out_f32) row_to<float>(p.out, b, t, h)[e] = acc[c][d][r];
+            else row_to<T>(p.out, b, t, h)[e] = (T)acc[c][d][r];
           }
-      }
-    }
-    {
-      Operand<T> y[TX];
-#pragma unroll
-      for (int a = 0; a < TX; ++a) y[a] = Operand<T>::template across<DX>(ys, [&](uint32_t i) { return state_row(a, i); }, m, g);
-#pragma unroll
-      for (int c = 0; c < NT; ++c) {
-        const Scaled<T> zw(z[c], into[0], into[1], exact);
-#pragma unroll
-        for (int a = 0; a < TX; ++a) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) S[a][c][r] = fmaf(S[a][c][r], keep, S[a][c][r]);
-          S[a][c] = zw.add(y[a], S[a][c], exact);
         }
-      }
     }
   }
 
@@ -520,7 +566,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
       for (int a = 0; a < TX; ++a)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (dx == DX || state_row(a, 4 * g + r) < dx) at[state_row(a, r) * dz] = S[a][c][r];
+          if (dx == DX || state_row(a, 4 * g + r) < dx) at[state_row(a, r) * dz] = S[c][a][r];
     }
   }
   if (!OUT || valid >= L) return;

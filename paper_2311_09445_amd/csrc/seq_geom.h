@@ -53,8 +53,10 @@ struct RotaryArgs {
   const float* freqs;
   float magnitude, sign;  // sign: -1 turns the other way
   float eps;
-  float* partial;         // gradients only: [blocks][2][dim] sums for the weights
-  uint32_t tokens, tiles; // heads in vectors: tokens that a workgroup takes at a time, and how often there are so many
+  float* partial;         // gradients only: the workgroups' sums for the weights
+  // heads in vectors: tokens that a workgroup takes at a time, how often there are so many; of a gradient by queries and keys, and
+  // the workgroups of either
+  uint32_t tokens[2], tiles[2], blocks[2];
 };
 
 enum RotaryKind { ROTATE, NORM_ROTATE, NORM_ROTATE_BACK };

@@ -113,15 +113,24 @@ __global__ __launch_bounds__(256) void k_rotate_any(RotaryArgs a) {
   }
 }
 
-// The weights' gradients from the workgroups' sums, in a fixed order: a workgroup takes 16 elements, 64 rows of sums at a time.
-__global__ __launch_bounds__(1024) void k_weight_sums(const float* partial, uint32_t blocks, uint32_t dim, float* dqw, float* dkw) {
+// The weights' gradients from the workgroups' sums, in their order: a workgroup takes 16 elements, 64 rows of sums at a time.
+struct WeightSums {
+  const float* from;
+  uint32_t rows, stride;
+  float* to;
+};
+struct WeightSumsOf {
+  WeightSums side[2];
+};
+__global__ __launch_bounds__(1024) void k_weight_sums(WeightSumsOf both, uint32_t dim) {
   __shared__ float all[64][16];
+  const WeightSums& w = both.side[blockIdx.y];
   const uint32_t e = threadIdx.x & 15, row = threadIdx.x >> 4, i = blockIdx.x * 16 + e;
   float sum = 0.0f;
-  if (i < 2 * dim) {
+  if (i < dim) {
     float s[kSums / 64];
 #pragma unroll
-    for (uint32_t k = 0; k < kSums / 64; ++k) s[k] = row + 64 * k < blocks ? partial[(size_t)(row + 64 * k) * 2 * dim + i] : 0.0f;
+    for (uint32_t k = 0; k < kSums / 64; ++k) s[k] = row + 64 * k < w.rows ? w.from[(size_t)(row + 64 * k) * w.stride + i] : 0.0f;
 #pragma unroll
     for (uint32_t k = 0; k < kSums / 64; ++k) sum += s[k];
   }
@@ -131,19 +140,19 @@ __global__ __launch_bounds__(1024) void k_weight_sums(const float* partial, uint
     if (row < m) all[row][e] += all[row + m][e];
     __syncthreads();
   }
-  float* out = i < dim ? dqw : dkw;
-  if (row == 0 && i < 2 * dim && out) out[i < dim ? i : i - dim] = all[0][e];
+  if (row == 0 && i < dim && w.to) w.to[i] = all[0][e];
 }
 
 // Workgroups of a gradient: as the workspace is sized, before it is known which kernel takes it.
 uint32_t sum_blocks(uint64_t tokens, uint32_t heads) {
   const uint64_t n = (tokens * heads + 3) / 4;
-  return (uint32_t)(n < kSums ? (n ? n : 1) : kSums);
+  return (uint32_t)(n < kSums ? (n > 2 ? n : 2) : kSums);
 }
 
 template <typename T, int W, RotaryKind KIND, bool INTERLEAVED>
 hipError_t launch_units(const RotaryArgs& a, uint32_t blocks, hipStream_t s) {
-  const uint32_t units = a.dim / (2 * W), lds = a.tokens * (a.rot / 2) * sizeof(float2);
+  const uint32_t units = a.dim / (2 * W), most = a.tokens[0] > a.tokens[1] ? a.tokens[0] : a.tokens[1];
+  const uint32_t lds = most * (a.rot / 2) * sizeof(float2);
   if (units <= 4) k_rotate_units<T, W, 4, KIND, INTERLEAVED><<<blocks, 256, lds, s>>>(a);
   else if (units <= 8) k_rotate_units<T, W, 8, KIND, INTERLEAVED><<<blocks, 256, lds, s>>>(a);
   else if (units <= 16) k_rotate_units<T, W, 16, KIND, INTERLEAVED><<<blocks, 256, lds, s>>>(a);
@@ -184,17 +193,29 @@ hipError_t launch(RotaryKind kind, RotaryArgs a, float* dqw, float* dkw, hipStre
   uint32_t blocks;
   hipError_t e;
   if (w) {
-    // As many tokens to a workgroup as give its lanes eight units each, but fewer where that would leave the chip without workgroups;
-    // their cosines take at most 32 KiB.
-    const uint32_t lanes = a.dim / (2 * w) <= 4 ? 4 : a.dim / (2 * w) <= 8 ? 8 : a.dim / (2 * w) <= 16 ? 16 : a.dim / (2 * w) <= 32 ? 32 : 64;
-    uint64_t n = 8 * 256 / lanes / heads;
-    if (n > tokens / 1024) n = tokens / 1024;
-    if (n > 4096 / (a.rot / 2 + 1)) n = 4096 / (a.rot / 2 + 1);
-    // (a gradient's workgroups are bounded by their sums: a few tokens more to each rather than a round more for some)
-    if (kind == NORM_ROTATE_BACK && n * most < tokens) n = (tokens + most - 1) / most < 4096 / (a.rot / 2 + 1) ? (tokens + most - 1) / most : n;
-    a.tokens = n ? (uint32_t)n : 1;
-    a.tiles = (uint32_t)((tokens + a.tokens - 1) / a.tokens);
-    blocks = kind == NORM_ROTATE_BACK && a.tiles > most ? most : a.tiles;
+    // As many tokens to a workgroup as give its lanes eight units each (a gradient's sixteen), but fewer where that would leave the
+    // chip without workgroups; their cosines take at most 32 KiB.
+    const uint32_t units = a.dim / (2 * w), lanes = units <= 4 ? 4 : units <= 8 ? 8 : units <= 16 ? 16 : units <= 32 ? 32 : 64;
+    const uint64_t fit = 4096 / (a.rot / 2 + 1);
+    blocks = 0;
+    for (int i = 0; i < 2; ++i) {
+      const bool back = kind == NORM_ROTATE_BACK;
+      const uint32_t of = back ? a.side[i].heads : heads;
+      if (!of) continue;
+      // (a gradient's workgroups are bounded by the room for their sums: shared out by heads, one at least)
+      uint64_t room = back ? (uint64_t)most * of / heads : tokens;
+      if (back && i == 1 && room + a.blocks[0] > most) room = most - a.blocks[0];
+      if (!room) room = 1;   // (there is one: `most` is two at least, and heads on the other side leave one)
+      uint64_t n = (back ? 16 : 8) * 256 / lanes / of;
+      const uint64_t share = back ? (tokens + room - 1) / room : tokens / 1024;
+      if (n > share) n = share;
+      if (n > fit) n = fit;
+      a.tokens[i] = n ? (uint32_t)n : 1;
+      a.tiles[i] = (uint32_t)((tokens + a.tokens[i] - 1) / a.tokens[i]);
+      a.blocks[i] = a.tiles[i] < room ? a.tiles[i] : (uint32_t)room;
+      blocks += a.blocks[i];
+      if (!back) break;
+    }
     e = w * sizeof(T) == 16 ? launch_units<T, 16 / sizeof(T)>(kind, a, blocks, s) : launch_units<T, 8 / sizeof(T)>(kind, a, blocks, s);
   } else {
     const uint64_t n = (tokens * heads + 3) / 4;
@@ -205,7 +226,11 @@ hipError_t launch(RotaryKind kind, RotaryArgs a, float* dqw, float* dkw, hipStre
     e = hipGetLastError();
   }
   if (e != hipSuccess || kind != NORM_ROTATE_BACK || (!dqw && !dkw)) return e;
-  k_weight_sums<<<(2 * a.dim + 15) / 16, 1024, 0, s>>>(a.partial, blocks, a.dim, dqw, dkw);
+  WeightSumsOf sums{};
+  for (int i = 0; i < 2; ++i)
+    sums.side[i] = w ? WeightSums{a.partial + (i ? (size_t)a.blocks[0] * a.dim : 0), a.blocks[i], a.dim, i ? dkw : dqw}
+                     : WeightSums{a.partial + i * a.dim, blocks, 2 * a.dim, i ? dkw : dqw};
+  k_weight_sums<<<dim3((a.dim + 15) / 16, 2), 1024, 0, s>>>(sums, a.dim);
   return hipGetLastError();
 }
 
