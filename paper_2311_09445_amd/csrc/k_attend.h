@@ -573,11 +573,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
   // tokens behind the valid ones: zeros
   const uint32_t width = dz - col0 < (uint32_t)DZ ? dz - col0 : DZ, from = start > valid ? start : valid;
   const uint32_t until = L - start < segment ? L : start + segment;
-  for (uint32_t t = from + wave; t < until; t += WAVES)
-    for (uint32_t j = lane; j < width; j += 64) {
-      if (out_f32) row_to<float>(p.out, b, t, h)[col0 + j] = 0.0f;
-      else row_to<T>(p.out, b, t, h)[col0 + j] = (T)0.0f;
-    }
+  const uint32_t piece = 16 / out_size, pieces = out_wide && width % piece == 0 ? width / piece : 0;
+  if (pieces) {
+    const uint32_t rows = THREADS / pieces, row = threadIdx.x / pieces;
+    uint8_t* at = oh + (int64_t)(from + row) * out_step + (col0 * out_size + threadIdx.x % pieces * 16);
+    if (row < rows)
+      for (uint32_t t = from + row; t < until; t += rows, at += rows * out_step) *reinterpret_cast<f32x4*>(at) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  } else {
+    for (uint32_t t = from + wave; t < until; t += WAVES)
+      for (uint32_t j = lane; j < width; j += 64) {
+        if (out_f32) row_to<float>(p.out, b, t, h)[col0 + j] = 0.0f;
+        else row_to<T>(p.out, b, t, h)[col0 + j] = (T)0.0f;
+      }
+  }
 }
 
 // The states that the segments of a sequence start from, from what each of them brings, in place; and the last state.
