@@ -16,7 +16,8 @@
 //
 // Rows lie in LDS in pieces of 16 bytes, piece p of row r at place p ^ turn(r), so that reads along rows and across them meet the
 // banks evenly without padding; memory can then be loaded straight into LDS, 64 pieces an instruction, several chunks ahead
-// (DIRECT).  Rows that cannot (odd widths, alignments or strides) go through registers, one chunk ahead.
+// (DIRECT: bfloat16).  Rows in fp32, which are taken apart on the way, go through registers, two chunks ahead (PIECES); rows of odd
+// widths, alignments or strides too, one ahead (ELEMENTS).
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -25,18 +26,19 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kChunk = 32;
 
-// Where row, piece of 32 rows of D elements lies in LDS, in elements.
-template <typename T, int D>
+enum Way { ELEMENTS, PIECES, DIRECT };
+
+// Where row, piece of 32 rows of D elements of two bytes lies in LDS, in elements.
+template <int D>
 struct Tile {
-  static constexpr uint32_t W = 16 / sizeof(T), PIECES = D / W;
+  static constexpr uint32_t PIECES = D / 8, SIZE = kChunk * D;
   // What is read at once: 16 rows of one piece (along), for which the turns of 16 rows (those that share 256 bytes aside) differ; or
-  // (across) rows 0 .. 7 of four pieces in a row, in 2 bytes an element, and rows i, 4 + i, 8 + i, 12 + i of every other piece, in 4.
+  // (across) rows 0 .. 7 of four pieces in a row.
   __device__ __forceinline__ static uint32_t turn(uint32_t row) {
     const uint32_t q = (row & 15) / (PIECES < 16 ? 16 / PIECES : 1);
-    if (sizeof(T) == 2) return PIECES >= 16 ? (q & 3) << 2 | q >> 2 : PIECES == 8 ? (q & 1) << 2 | q >> 1 : q;
-    return PIECES >= 16 ? (q & 3) << 1 | (q >> 2 & 1) | (q >> 3) << 3 : (q & 1) << 1 | (q >> 1 & 1) | (q >> 2) << 2;
+    return PIECES >= 16 ? (q & 3) << 2 | q >> 2 : PIECES == 8 ? (q & 1) << 2 | q >> 1 : q;
   }
-  __device__ __forceinline__ static uint32_t at(uint32_t row, uint32_t piece) { return row * D + (piece ^ turn(row)) * W; }
+  __device__ __forceinline__ static uint32_t at(uint32_t row, uint32_t piece) { return row * D + (piece ^ turn(row)) * 8; }
 };
 
 // The place of dx that row m of tile a of the state is; the column of the wave's that column m of tile c is.
@@ -44,86 +46,92 @@ __device__ __forceinline__ uint32_t state_row(uint32_t a, uint32_t m) { return 3
 template <int NT>
 __device__ __forceinline__ uint32_t state_column(uint32_t c, uint32_t m) { return NT == 2 ? 8 * (m >> 2) + 4 * c + (m & 3) : 16 * c + m; }
 
-// Operand of 16 x 32 places: 8 of the inner dimension per lane.
+// Operand of 16 x 32 places: 8 of the inner dimension per lane.  Values in fp32 are taken apart into three in bfloat16, whose sum they
+// are (8 bits each, cut off, not rounded: no part overflows), and products into six matrix instructions; the two products of 2^-24
+// that are left out are of the size of fp32's own rounding.  (The matrix instructions of fp32 itself take 32 times as long as those of
+// bfloat16, 5.3 times as long as six: a chunk of 64 x 64 took 3.1 us and takes 2.6, of 128 x 64 5.0 and 4.0.)  In LDS the parts are three tiles, one
+// behind the other.
 template <typename T>
-struct Operand;
+constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-template <>
-struct Operand<bf16> {
-  bf16x8 v;
+template <typename T>
+struct Operand {
+  static constexpr int PARTS = kParts<T>;
+  bf16x8 v[PARTS];
   // A row of the tile, the inner dimension along it: 32 k + 8 g ..
   template <int D>
   __device__ __forceinline__ static Operand along(const bf16* tile, uint32_t row, uint32_t k, uint32_t g) {
-    return {*reinterpret_cast<const bf16x8*>(tile + Tile<bf16, D>::at(row, 4 * k + g))};
+    Operand o;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) o.v[i] = *reinterpret_cast<const bf16x8*>(tile + i * Tile<D>::SIZE + Tile<D>::at(row, 4 * k + g));
+    return o;
   }
   // Columns column(0) .. column(15), of which four in a row are neighbours, the inner dimension across the 32 rows: a transposing
   // read, in which 16 lanes read 4 rows of 4 x 4 elements.
   template <int D, typename F>
   __device__ __forceinline__ static Operand across(const bf16* tile, F column, uint32_t m, uint32_t g) {
     typedef __attribute__((address_space(3))) s16x4 Lds;
-    const uint32_t first = column(4 * (m & 3));
-    const bf16* at = tile + Tile<bf16, D>::at(4 * g + (m >> 2), first >> 3) + (first & 4);
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + 16 * D));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
-    const s16x8 v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    return {__builtin_bit_cast(bf16x8, v)};
-  }
-  __device__ __forceinline__ static Operand of(f32x4 a, f32x4 b) {
     Operand o;
+    const uint32_t first = column(4 * (m & 3));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { o.v[i] = (bf16)a[i]; o.v[i + 4] = (bf16)b[i]; }
-    return o;
-  }
-  // The elements in fp32, two by two from their 32 bits.
-  __device__ __forceinline__ void widen(f32x4* a, f32x4* b) const {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    const u32x4 u = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      (*a)[2 * i] = __builtin_bit_cast(float, u[i] << 16);
-      (*a)[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xFFFF0000u);
-      (*b)[2 * i] = __builtin_bit_cast(float, u[i + 2] << 16);
-      (*b)[2 * i + 1] = __builtin_bit_cast(float, u[i + 2] & 0xFFFF0000u);
-    }
-  }
-  __device__ __forceinline__ static f32x4 mma(const Operand& a, const Operand& b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
-  }
-};
-
-template <>
-struct Operand<float> {
-  float v[8];
-  template <int D>
-  __device__ __forceinline__ static Operand along(const float* tile, uint32_t row, uint32_t k, uint32_t g) {
-    return of(*reinterpret_cast<const f32x4*>(tile + Tile<float, D>::at(row, 8 * k + 2 * g)),
-              *reinterpret_cast<const f32x4*>(tile + Tile<float, D>::at(row, 8 * k + 2 * g + 1)));
-  }
-  template <int D, typename F>
-  __device__ __forceinline__ static Operand across(const float* tile, F column, uint32_t m, uint32_t g) {
-    Operand o;
-    const uint32_t c = column(m);
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-      const float* at = tile + Tile<float, D>::at(4 * g + i, c >> 2) + (c & 3);
-      o.v[i] = at[0];
-      o.v[i + 4] = at[16 * D];
+    for (int i = 0; i < PARTS; ++i) {
+      const bf16* at = tile + i * Tile<D>::SIZE + Tile<D>::at(4 * g + (m >> 2), first >> 3) + (first & 4);
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + 16 * D));
+      const s16x8 both = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+      o.v[i] = __builtin_bit_cast(bf16x8, both);
     }
     return o;
   }
   __device__ __forceinline__ static Operand of(f32x4 a, f32x4 b) {
     Operand o;
+    if constexpr (PARTS == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { o.v[i] = a[i]; o.v[i + 4] = b[i]; }
+      for (int i = 0; i < 4; ++i) { o.v[0][i] = (bf16)a[i]; o.v[0][i + 4] = (bf16)b[i]; }
+    } else {
+#pragma unroll
+      for (int t = 0; t < PARTS; ++t) {
+        u32x4 packed;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          packed[i] = upper_halves(a[2 * i], a[2 * i + 1]);
+          packed[i + 2] = upper_halves(b[2 * i], b[2 * i + 1]);
+        }
+        if (t + 1 < PARTS)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { a[i] -= upper(a[i]); b[i] -= upper(b[i]); }
+        o.v[t] = __builtin_bit_cast(bf16x8, packed);
+      }
+    }
     return o;
   }
+  __device__ __forceinline__ static float upper(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xFFFF0000u); }
+  __device__ __forceinline__ static uint32_t upper_halves(float x, float y) {   // packed
+    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
+  }
+  // The values in fp32.
   __device__ __forceinline__ void widen(f32x4* a, f32x4* b) const {
+    *a = *b = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { (*a)[i] = v[i]; (*b)[i] = v[i + 4]; }
+    for (int t = PARTS - 1; t >= 0; --t) {
+      const u32x4 u = __builtin_bit_cast(u32x4, v[t]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float x[4] = {__builtin_bit_cast(float, u[i] << 16), __builtin_bit_cast(float, u[i] & 0xFFFF0000u),
+                            __builtin_bit_cast(float, u[i + 2] << 16), __builtin_bit_cast(float, u[i + 2] & 0xFFFF0000u)};
+        (*a)[2 * i] = t + 1 < PARTS ? (*a)[2 * i] + x[0] : x[0];
+        (*a)[2 * i + 1] = t + 1 < PARTS ? (*a)[2 * i + 1] + x[1] : x[1];
+        (*b)[2 * i] = t + 1 < PARTS ? (*b)[2 * i] + x[2] : x[2];
+        (*b)[2 * i + 1] = t + 1 < PARTS ? (*b)[2 * i + 1] + x[3] : x[3];
+      }
+    }
   }
   __device__ __forceinline__ static f32x4 mma(const Operand& a, const Operand& b, f32x4 c) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
+    for (int s = PARTS - 1; s >= 0; --s)   // parts s apart from the first of both, the smallest first
+#pragma unroll
+      for (int i = 0; i <= s; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[s - i], c, 0, 0, 0);
     return c;
   }
 };
@@ -180,7 +188,7 @@ struct Scaled<bf16> {
 // 32 rows of D elements on their way from memory to LDS through the threads' registers.
 template <typename T, int D, int THREADS>
 struct Staged {
-  static constexpr uint32_t W = Tile<T, D>::W, PER_ROW = D / W, PIECES = kChunk * PER_ROW, N = (PIECES + THREADS - 1) / THREADS;
+  static constexpr uint32_t W = 16 / sizeof(T), PER_ROW = D / W, ALL = kChunk * PER_ROW, N = (ALL + THREADS - 1) / THREADS;
   typedef T Vec __attribute__((ext_vector_type(W)));
   Vec v[N];
   // Rows first .. first + n of a head's sequence of `valid` tokens (against time: counted from its end), columns col0 .. col0 + D.
@@ -190,7 +198,7 @@ struct Staged {
       const uint32_t at = threadIdx.x + k * THREADS;
       const uint32_t row = at / PER_ROW, col = col0 + at % PER_ROW * W;
       v[k] = Vec(T(0.0f));
-      if ((PIECES % THREADS == 0 || at < PIECES) && row < n && col < width) {
+      if ((ALL % THREADS == 0 || at < ALL) && row < n && col < width) {
         const uint32_t i = first + row, t = back ? valid - 1 - i : i;
         const T* p = head + (int64_t)t * r.token + col;
         if (r.wide && col + W <= width) {
@@ -203,18 +211,48 @@ struct Staged {
       }
     }
   }
-  __device__ __forceinline__ void store(T* tile) const {
+  // The same where rows are whole pieces, without a branch (a load in one is waited for at its end): rows behind the last, of which
+  // there is at least one, and pieces behind the width take the last ones, and are cleared on their way to LDS.
+  __device__ __forceinline__ void load_whole(const SeqRows& r, const T* head, uint32_t first, uint32_t end, uint32_t valid, bool back, uint32_t col0, uint32_t width) {
 #pragma unroll
     for (uint32_t k = 0; k < N; ++k) {
       const uint32_t at = threadIdx.x + k * THREADS;
-      if (PIECES % THREADS == 0 || at < PIECES) *reinterpret_cast<Vec*>(tile + Tile<T, D>::at(at / PER_ROW, at % PER_ROW)) = v[k];
+      const uint32_t row = at / PER_ROW % kChunk, col = col0 + at % PER_ROW * W;
+      const uint32_t i = first + row < end ? first + row : end - 1, t = back ? valid - 1 - i : i;
+      v[k] = *reinterpret_cast<const Vec*>(head + (int64_t)t * r.token + (col < width ? col : width - W));
+    }
+  }
+  __device__ __forceinline__ void clear(uint32_t n, uint32_t col0, uint32_t width) {
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) {
+      const uint32_t at = threadIdx.x + k * THREADS;
+      const bool on = at / PER_ROW < n && col0 + at % PER_ROW * W < width;
+#pragma unroll
+      for (uint32_t e = 0; e < W; ++e) v[k][e] = on ? v[k][e] : T(0.0f);
+    }
+  }
+  __device__ __forceinline__ void store(bf16* tile) const {
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) {
+      const uint32_t at = threadIdx.x + k * THREADS;
+      if (ALL % THREADS != 0 && at >= ALL) continue;
+      const uint32_t row = at / PER_ROW, col = at % PER_ROW * W;
+      bf16* to = tile + Tile<D>::at(row, col / 8) + col % 8;
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<Vec*>(to) = v[k];
+      } else {
+        const Operand<T> parts = Operand<T>::of(v[k], v[k]);
+#pragma unroll
+        for (int t = 0; t < kParts<T>; ++t)
+          *reinterpret_cast<bf16x4*>(to + t * Tile<D>::SIZE) = __builtin_shufflevector(parts.v[t], parts.v[t], 0, 1, 2, 3);
+      }
     }
   }
 };
 
-// The same straight into LDS.  A wave's instruction fills 64 places one behind the other: 1 KiB of the chunk's tiles, which lie one
+// The same straight into LDS, in bfloat16.  A wave's instruction fills 64 places one behind the other: 1 KiB of the chunk's tiles, which lie one
 // behind the other too; the waves take these in turn.  Which piece belongs there is the lane's business: it asks for that one.
-struct Direct {
+struct Fill {
   const uint8_t* base;   // (uniform) of the next chunk that is asked for
   int64_t step;          // (uniform) bytes to the one after it
   uint32_t offset;       // of the lane's piece within the chunk
@@ -223,9 +261,9 @@ struct Direct {
 constexpr uint32_t kNoRow = 1u << 16;
 
 template <typename T, int D>
-__device__ __forceinline__ void direct_piece(Direct* d, const SeqRows& r, const T* head, uint32_t place, int64_t token, bool back, uint32_t col0, uint32_t width) {
-  constexpr uint32_t PER_ROW = Tile<T, D>::PIECES, W = Tile<T, D>::W;
-  const uint32_t row = place / PER_ROW, piece = place % PER_ROW ^ Tile<T, D>::turn(row);
+__device__ __forceinline__ void fill_piece(Fill* d, const SeqRows& r, const T* head, uint32_t place, int64_t token, bool back, uint32_t col0, uint32_t width) {
+  constexpr uint32_t PER_ROW = Tile<D>::PIECES, W = 8;
+  const uint32_t row = place / PER_ROW, piece = place % PER_ROW ^ Tile<D>::turn(row);
   const int64_t bytes = r.token * (int64_t)sizeof(T);
   d->base = reinterpret_cast<const uint8_t*>(head + col0) + token * bytes;
   d->step = (back ? -(int64_t)kChunk : (int64_t)kChunk) * bytes;
@@ -247,10 +285,10 @@ __device__ __forceinline__ void arrive() {
 
 // Bytes of a chunk's tiles, and how many chunks are held.  (The address that loads to LDS go to has 16 bits.)
 template <typename T, int DX, int DZ, bool OUT>
-constexpr uint32_t chunk_bytes() { return kChunk * ((OUT ? 2 : 1) * DX + DZ) * sizeof(T); }
-template <typename T, int DX, int DZ, bool OUT, bool DIRECT>
+constexpr uint32_t chunk_bytes() { return kChunk * ((OUT ? 2 : 1) * DX + DZ) * kParts<T> * sizeof(bf16); }
+template <typename T, int DX, int DZ, bool OUT, Way WAY>
 constexpr uint32_t ring() {
-  if (!DIRECT) return 2;
+  if (WAY != DIRECT) return 2;
   const uint32_t n = 65536 / chunk_bytes<T, DX, DZ, OUT>();
   return n < 4 ? n : 4;
 }
@@ -295,12 +333,12 @@ __device__ __forceinline__ void store_row_counted(uint8_t* base, uint32_t offset
 }
 
 // OUT: the outputs are wanted too (else only the state that the piece of the sequence brings, from zeros).
-template <typename T, int DX, int NT, int WAVES, bool OUT, bool DIRECT>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
+template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY>
+__global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 : 2) void k_attend(AttentionPasses all) {
   constexpr int THREADS = 64 * WAVES, DZ = 16 * NT * WAVES, TX = DX / 16, KX = DX / 32;
-  constexpr uint32_t BUFFER = chunk_bytes<T, DX, DZ, OUT>() / sizeof(T), RING = ring<T, DX, DZ, OUT, DIRECT>();
+  constexpr uint32_t BUFFER = chunk_bytes<T, DX, DZ, OUT>() / sizeof(bf16), RING = ring<T, DX, DZ, OUT, WAY>();
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
-  T* const lds = reinterpret_cast<T*>(lds_raw);
+  bf16* const lds = reinterpret_cast<bf16*>(lds_raw);
   // Workgroups go round the 8 dies by their number: the passes over the same rows sit on one die, one behind the other.
   const uint32_t which = blockIdx.x / 8 % all.count, item = blockIdx.x / (8 * all.count) * 8 + blockIdx.x % 8;
   if (item >= all.items) return;
@@ -362,36 +400,44 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
   const T* const zh = row_of<T>(p.z, b, 0, h);
   const uint32_t out_size = out_f32 ? 4 : sizeof(T);
   const int64_t out_step = p.out.token * (int64_t)out_size;
-  const bool out_wide = DIRECT || p.out.wide;
+  const bool out_wide = WAY != ELEMENTS || p.out.wide;
   uint8_t* const oh = OUT ? static_cast<uint8_t*>(p.out.d) + ((int64_t)b * p.out.batch + (int64_t)(h / p.out.share) * p.out.head) * out_size : nullptr;
   // Chunks on their way: staged in registers, or counted instructions that fill LDS.
-  Staged<T, DX, DIRECT ? 1 << 20 : THREADS> px, py;
-  Staged<T, DZ, DIRECT ? 1 << 20 : THREADS> pz;
-  constexpr uint32_t FILLS_X = OUT ? Tile<T, DX>::PIECES / 2 : 0, FILLS_Y = Tile<T, DX>::PIECES / 2, FILLS = FILLS_X + FILLS_Y + Tile<T, DZ>::PIECES / 2;
+  struct Rows {
+    Staged<T, DX, WAY == DIRECT ? 1 << 20 : THREADS> x, y;
+    Staged<T, DZ, WAY == DIRECT ? 1 << 20 : THREADS> z;
+  } staged[2];
+  constexpr uint32_t FILLS_X = OUT ? Tile<DX>::PIECES / 2 : 0, FILLS_Y = Tile<DX>::PIECES / 2, FILLS = FILLS_X + FILLS_Y + Tile<DZ>::PIECES / 2;
   constexpr uint32_t MINE = (FILLS + WAVES - 1) / WAVES;
-  Direct fill[DIRECT ? MINE : 1];
+  Fill fill[WAY == DIRECT ? MINE : 1];
   const bool whole = dx == DX && dz - col0 >= DZ;   // no piece lies behind a width
   const int64_t token0 = back ? (int64_t)valid - (int64_t)begin - (int64_t)kChunk : (int64_t)begin;   // lowest of the first chunk
-  if (DIRECT) {
+  if (WAY == DIRECT) {
 #pragma unroll
     for (uint32_t k = 0; k < MINE; ++k) {
       const uint32_t f = wave + WAVES * k;
       fill[k].row = kNoRow;
-      if (f < FILLS_X) direct_piece<T, DX>(&fill[k], p.x, xh, f * 64 + lane, token0, back, 0, dx);
-      else if (f < FILLS_X + FILLS_Y) direct_piece<T, DX>(&fill[k], p.y, yh, (f - FILLS_X) * 64 + lane, token0, back, 0, dx);
-      else if (f < FILLS) direct_piece<T, DZ>(&fill[k], p.z, zh, (f - FILLS_X - FILLS_Y) * 64 + lane, token0, back, col0, dz);
+      if (f < FILLS_X) fill_piece<T, DX>(&fill[k], p.x, xh, f * 64 + lane, token0, back, 0, dx);
+      else if (f < FILLS_X + FILLS_Y) fill_piece<T, DX>(&fill[k], p.y, yh, (f - FILLS_X) * 64 + lane, token0, back, 0, dx);
+      else if (f < FILLS) fill_piece<T, DZ>(&fill[k], p.z, zh, (f - FILLS_X - FILLS_Y) * 64 + lane, token0, back, col0, dz);
     }
   }
-  // Asks for the chunk from token `first` on (the chunks one after the other), to go to a place of the ring.
-  auto fetch = [&](uint32_t first, uint32_t slot) {
+  // Asks for the chunk from token `first` on (the chunks one after the other), to go to registers or to a place of the ring.
+  auto fetch = [&](uint32_t first, uint32_t slot, Rows& to_rows) {
     const uint32_t n = first < end ? (end - first < kChunk ? end - first : kChunk) : 0;
-    if (!DIRECT) {
-      if (OUT) px.load(p.x, xh, first, n, valid, back, 0, dx);
-      py.load(p.y, yh, first, n, valid, back, 0, dx);
-      pz.load(p.z, zh, first, n, valid, back, col0, dz);
+    if (WAY == ELEMENTS) {
+      if (OUT) to_rows.x.load(p.x, xh, first, n, valid, back, 0, dx);
+      to_rows.y.load(p.y, yh, first, n, valid, back, 0, dx);
+      to_rows.z.load(p.z, zh, first, n, valid, back, col0, dz);
       return;
     }
-    const uint32_t to = slot * BUFFER * (uint32_t)sizeof(T) + wave * 1024;
+    if (WAY == PIECES) {
+      if (OUT) to_rows.x.load_whole(p.x, xh, first, end, valid, back, 0, dx);
+      to_rows.y.load_whole(p.y, yh, first, end, valid, back, 0, dx);
+      to_rows.z.load_whole(p.z, zh, first, end, valid, back, col0, dz);
+      return;
+    }
+    const uint32_t to = slot * BUFFER * (uint32_t)sizeof(bf16) + wave * 1024;
     if (whole && n == kChunk) {
 #pragma unroll
       for (uint32_t k = 0; k < MINE; ++k)
@@ -440,19 +486,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
   weights(kChunk);
 
   const bool stores = col < dz;           // the wave has outputs to store
-  constexpr uint32_t AHEAD = RING - 1;   // chunks asked for before the one at hand
-  if (DIRECT) {
-#pragma unroll
-    for (uint32_t i = 0; i < AHEAD; ++i)
-      if (begin + i * kChunk < end) fetch(begin + i * kChunk, i);
-  } else {
-    fetch(begin, 0);
-  }
-  for (uint32_t first = begin, slot = 0; first < end; first += kChunk, slot = slot + 1 == RING ? 0 : slot + 1) {
-    T* const xs = lds + slot * BUFFER;
-    T* const ys = OUT ? xs + kChunk * DX : xs;
-    T* const zs = ys + kChunk * DX;
-    if (DIRECT) {
+  // One chunk: its rows into LDS, or in LDS, and those of a later one asked for; then its products.
+  constexpr uint32_t AHEAD = WAY == DIRECT ? RING - 1 : WAY == PIECES ? 2 : 1;   // chunks asked for before the one at hand
+  auto chunk = [&](uint32_t first, uint32_t slot, Rows& rows) __attribute__((always_inline)) {
+    bf16* const xs = lds + slot * BUFFER;
+    bf16* const ys = OUT ? xs + kParts<T> * Tile<DX>::SIZE : xs;
+    bf16* const zs = ys + kParts<T> * Tile<DX>::SIZE;
+    if (WAY == DIRECT) {
       // Behind the wave's parts of this chunk are those of the next RING - 2, at least FILLS / WAVES instructions each if they are
       // whole, and the outputs of the last RING - 1, two rows each.  That many may be left; towards the end none.
       constexpr int LOADS = (int)((RING - 2) * (FILLS / WAVES)), STORES = OUT ? 2 * (int)(RING - 1) : 0;
@@ -461,13 +501,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
       else if (NT == 2 && out_f32) arrive<LOADS + 2 * STORES>();
       else arrive<LOADS + STORES>();
       // (this barrier: all are through with the chunk before, whose place the next one takes)
-      if (first + AHEAD * kChunk < end) fetch(first + AHEAD * kChunk, slot == 0 ? RING - 1 : slot - 1);
+      if (first + AHEAD * kChunk < end) fetch(first + AHEAD * kChunk, slot == 0 ? RING - 1 : slot - 1, rows);
     } else {
-      if (OUT) px.store(xs);
-      py.store(ys);
-      pz.store(zs);
+      if (WAY == PIECES && (!whole || end - first < kChunk)) {
+        if (OUT) rows.x.clear(end - first, 0, dx);
+        rows.y.clear(end - first, 0, dx);
+        rows.z.clear(end - first, col0, dz);
+      }
+      if (OUT) rows.x.store(xs);
+      rows.y.store(ys);
+      rows.z.store(zs);
       __syncthreads();
-      if (first + kChunk < end) fetch(first + kChunk, 0);
+      if (WAY == PIECES || first + AHEAD * kChunk < end) fetch(first + AHEAD * kChunk, 0, rows);
     }
     const uint32_t n = end - first < kChunk ? end - first : kChunk;
     if (n < kChunk) weights((int)n);
@@ -514,11 +559,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
         for (int r = 0; r < 4; ++r) S[c][a][r] = fmaf(S[c][a][r], keep, S[c][a][r]);
       zw.add(y, S[c], exact);
     }
-    if (!OUT) continue;
+    if (!OUT) return;
     // out: four columns of a token in each tile of a lane, eight side by side in two
     const uint32_t j = col + (NT == 2 ? 8 : 4) * g;
     uint8_t* const base = oh + (back ? (int64_t)valid - (int64_t)first - (int64_t)kChunk : (int64_t)first) * out_step;
-    if (DIRECT) {
+    if (WAY == DIRECT) {
       const uint32_t lower = (back ? kChunk - 1 - m : m) * (uint32_t)out_step + j * out_size;
       const uint32_t upper = lower + (back ? -16 : 16) * (uint32_t)out_step;
       if (out_f32) {
@@ -534,8 +579,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
         const uint32_t row = 16 * d + m;
         uint8_t* const at = base + ((back ? kChunk - 1 - row : row) * (uint32_t)out_step + j * out_size);
         if (row >= n || j >= dz) continue;
-        if (out_f32) store_row<float, NT>(at, acc, d, dz - j);
-        else store_row<T, NT>(at, acc, d, dz - j);
+        const uint32_t left = WAY == PIECES ? 4 * NT : dz - j;
+        if (out_f32) store_row<float, NT>(at, acc, d, left);
+        else store_row<T, NT>(at, acc, d, left);
       }
     } else {
 #pragma unroll
@@ -552,6 +598,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend(AttentionPasses all) {
           }
         }
     }
+  };
+
+  if (WAY == DIRECT) {
+#pragma unroll
+    for (uint32_t i = 0; i < AHEAD; ++i)
+      if (begin + i * kChunk < end) fetch(begin + i * kChunk, i, staged[0]);
+    for (uint32_t first = begin, slot = 0; first < end; first += kChunk, slot = slot + 1 == RING ? 0 : slot + 1) chunk(first, slot, staged[0]);
+  } else if (WAY == PIECES) {
+    if (begin < end) {
+      fetch(begin, 0, staged[0]);
+      fetch(begin + kChunk, 0, staged[1]);
+    }
+    for (uint32_t first = begin; first < end; first += 2 * kChunk) {
+      chunk(first, 0, staged[0]);
+      if (first + kChunk < end) chunk(first + kChunk, 1, staged[1]);
+    }
+  } else {
+    fetch(begin, 0, staged[0]);
+    for (uint32_t first = begin, slot = 0; first < end; first += kChunk, slot ^= 1) chunk(first, slot, staged[0]);
   }
 
   float* const to = OUT ? p.to : p.part;

@@ -176,11 +176,11 @@ size_t part_bytes(const AttentionSizes& a, const Cut& c) {
 }
 size_t fold_bytes(const AttentionSizes& a, uint32_t width) { return a.H == a.G ? 0 : align256((size_t)a.B * a.L * a.H * width * sizeof(float)); }
 
-template <typename T, int DX, int NT, int WAVES, bool OUT, bool DIRECT>
+template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY>
 hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
   constexpr int DZ = 16 * NT * WAVES;
-  constexpr uint32_t lds = ring<T, DX, DZ, OUT, DIRECT>() * chunk_bytes<T, DX, DZ, OUT>();
-  auto* kernel = k_attend<T, DX, NT, WAVES, OUT, DIRECT>;
+  constexpr uint32_t lds = ring<T, DX, DZ, OUT, WAY>() * chunk_bytes<T, DX, DZ, OUT>();
+  auto* kernel = k_attend<T, DX, NT, WAVES, OUT, WAY>;
   if (lds > 64 * 1024) {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
@@ -188,19 +188,16 @@ hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
   kernel<<<(p.items + 7) / 8 * 8 * p.count, 64 * WAVES, lds, s>>>(p);
   return hipGetLastError();
 }
-// Straight into LDS where pieces of 16 bytes make up the rows, and where two chunks fit.
+// Rows that are made up of pieces of 16 bytes: in bfloat16 straight into LDS, in fp32 taken apart on the way.
 template <typename T, int DX, int NT, int WAVES, bool OUT>
 hipError_t launch_way(const AttentionPasses& p, hipStream_t s) {
-  bool direct = true;
+  constexpr uint32_t W = 16 / sizeof(T);
+  bool pieces = true;
   for (uint32_t i = 0; i < p.count; ++i) {
     const AttentionPass& a = p.pass[i];
-    const uint32_t per16 = 16 / sizeof(T);
-    direct = direct && (!OUT || (a.x.wide && a.out.wide)) && a.y.wide && a.z.wide && a.dx % per16 == 0 && a.dz % per16 == 0;
+    pieces = pieces && (!OUT || (a.x.wide && a.out.wide)) && a.y.wide && a.z.wide && a.dx % W == 0 && a.dz % W == 0;
   }
-  if constexpr (ring<T, DX, 16 * NT * WAVES, OUT, true>() >= 2) {
-    if (direct) return launch_as<T, DX, NT, WAVES, OUT, true>(p, s);
-  }
-  return launch_as<T, DX, NT, WAVES, OUT, false>(p, s);
+  return pieces ? launch_as<T, DX, NT, WAVES, OUT, sizeof(T) == 4 ? PIECES : DIRECT>(p, s) : launch_as<T, DX, NT, WAVES, OUT, ELEMENTS>(p, s);
 }
 template <typename T, int DX, bool OUT>
 hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {
