@@ -16,8 +16,8 @@
 //
 // Rows lie in LDS in pieces of 16 bytes, piece p of row r at place p ^ turn(r), so that reads along rows and across them meet the
 // banks evenly without padding; memory can then be loaded straight into LDS, 64 pieces an instruction, several chunks ahead
-// (DIRECT: bfloat16).  Rows in fp32, which are taken apart on the way, go through registers, two chunks ahead (PIECES); rows of odd
-// widths, alignments or strides too, one ahead (ELEMENTS).
+// (DIRECT: bfloat16, rows made of pieces).  Rows in fp32, which are taken apart on the way, and rows of odd widths or alignments go
+// through registers in pieces, two chunks ahead (PIECES); rows narrower than a piece or far apart one by one (ELEMENTS).
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -105,6 +105,21 @@ struct Operand {
       }
     }
     return o;
+  }
+  // A piece of 16 bytes, taken apart.
+  typedef bf16 Piece __attribute__((ext_vector_type(16 / sizeof(T))));
+  struct Pieces {
+    Piece v[PARTS];
+  };
+  template <typename V>
+  __device__ __forceinline__ static void cut(const V& piece, Pieces* p) {
+    if constexpr (PARTS == 1) {
+      p->v[0] = piece;
+    } else {
+      const Operand o = of(piece, piece);
+#pragma unroll
+      for (int t = 0; t < PARTS; ++t) p->v[t] = __builtin_shufflevector(o.v[t], o.v[t], 0, 1, 2, 3);
+    }
   }
   __device__ __forceinline__ static float upper(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xFFFF0000u); }
   __device__ __forceinline__ static uint32_t upper_halves(float x, float y) {   // packed
@@ -211,15 +226,16 @@ struct Staged {
       }
     }
   }
-  // The same where rows are whole pieces, without a branch (a load in one is waited for at its end): rows behind the last, of which
-  // there is at least one, and pieces behind the width take the last ones, and are cleared on their way to LDS.
-  __device__ __forceinline__ void load_whole(const SeqRows& r, const T* head, uint32_t first, uint32_t end, uint32_t valid, bool back, uint32_t col0, uint32_t width) {
+  // The same in pieces, without a branch (a load in one is waited for at its end).  Rows behind the last, of which there is at least
+  // one, take that one and are cleared on their way to LDS; pieces that reach behind the width end with it instead.
+  __device__ __forceinline__ void load_pieces(const SeqRows& r, const T* head, uint32_t first, uint32_t end, uint32_t valid, bool back, uint32_t col0, uint32_t width) {
+    typedef Vec Loose __attribute__((aligned(sizeof(T))));   // (memory is read at any address that its elements may have)
 #pragma unroll
     for (uint32_t k = 0; k < N; ++k) {
       const uint32_t at = threadIdx.x + k * THREADS;
       const uint32_t row = at / PER_ROW % kChunk, col = col0 + at % PER_ROW * W;
       const uint32_t i = first + row < end ? first + row : end - 1, t = back ? valid - 1 - i : i;
-      v[k] = *reinterpret_cast<const Vec*>(head + (int64_t)t * r.token + (col < width ? col : width - W));
+      v[k] = *reinterpret_cast<const Loose*>(head + (int64_t)t * r.token + (col + W <= width ? col : width - W));
     }
   }
   __device__ __forceinline__ void clear(uint32_t n, uint32_t col0, uint32_t width) {
@@ -231,6 +247,28 @@ struct Staged {
       for (uint32_t e = 0; e < W; ++e) v[k][e] = on ? v[k][e] : T(0.0f);
     }
   }
+  // A piece that ended with the width (columns width - W ..): its last `width % W` elements to the front of their place, zeros behind.
+  __device__ __forceinline__ void store_ends(bf16* tile, uint32_t width) const {
+    const uint32_t rest = width % W;
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) {
+      const uint32_t at = threadIdx.x + k * THREADS;
+      if (ALL % THREADS != 0 && at >= ALL) continue;
+      const uint32_t row = at / PER_ROW, col = at % PER_ROW * W;
+      if (col / W != width / W) continue;
+      bf16* to = tile + Tile<D>::at(row, col / 8) + col % 8;
+      typename Operand<T>::Pieces parts;
+      Operand<T>::cut(v[k], &parts);
+#pragma unroll
+      for (int t = 0; t < kParts<T>; ++t) {
+#pragma unroll
+        for (uint32_t e = 0; e < W; ++e) to[t * Tile<D>::SIZE + e] = (bf16)0.0f;
+#pragma unroll
+        for (uint32_t e = 0; e < W; ++e)
+          if (e + rest >= W) to[t * Tile<D>::SIZE + e + rest - W] = parts.v[t][e];
+      }
+    }
+  }
   __device__ __forceinline__ void store(bf16* tile) const {
 #pragma unroll
     for (uint32_t k = 0; k < N; ++k) {
@@ -238,14 +276,10 @@ struct Staged {
       if (ALL % THREADS != 0 && at >= ALL) continue;
       const uint32_t row = at / PER_ROW, col = at % PER_ROW * W;
       bf16* to = tile + Tile<D>::at(row, col / 8) + col % 8;
-      if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<Vec*>(to) = v[k];
-      } else {
-        const Operand<T> parts = Operand<T>::of(v[k], v[k]);
+      typename Operand<T>::Pieces parts;
+      Operand<T>::cut(v[k], &parts);
 #pragma unroll
-        for (int t = 0; t < kParts<T>; ++t)
-          *reinterpret_cast<bf16x4*>(to + t * Tile<D>::SIZE) = __builtin_shufflevector(parts.v[t], parts.v[t], 0, 1, 2, 3);
-      }
+      for (int t = 0; t < kParts<T>; ++t) *reinterpret_cast<decltype(&parts.v[t])>(to + t * Tile<D>::SIZE) = parts.v[t];
     }
   }
 };
@@ -297,12 +331,13 @@ constexpr uint32_t ring() {
 template <typename O, int NT>
 __device__ __forceinline__ void store_row(uint8_t* at, const f32x4 (&acc)[NT][2], int d, uint32_t left) {
   typedef O Vec __attribute__((ext_vector_type(4 * NT)));
+  typedef Vec Loose __attribute__((aligned(sizeof(O))));
   O* const to = reinterpret_cast<O*>(at);
   if (left >= 4 * NT) {
     Vec o;
 #pragma unroll
     for (int i = 0; i < 4 * NT; ++i) o[i] = (O)acc[i / 4][d][i % 4];
-    *reinterpret_cast<Vec*>(to) = o;
+    *reinterpret_cast<Loose*>(to) = o;
     return;
   }
 #pragma unroll
@@ -400,7 +435,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
   const T* const zh = row_of<T>(p.z, b, 0, h);
   const uint32_t out_size = out_f32 ? 4 : sizeof(T);
   const int64_t out_step = p.out.token * (int64_t)out_size;
-  const bool out_wide = WAY != ELEMENTS || p.out.wide;
+  const bool out_near = WAY != ELEMENTS || p.out.near, out_wide = WAY == DIRECT || p.out.wide;
   uint8_t* const oh = OUT ? static_cast<uint8_t*>(p.out.d) + ((int64_t)b * p.out.batch + (int64_t)(h / p.out.share) * p.out.head) * out_size : nullptr;
   // Chunks on their way: staged in registers, or counted instructions that fill LDS.
   struct Rows {
@@ -411,6 +446,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
   constexpr uint32_t MINE = (FILLS + WAVES - 1) / WAVES;
   Fill fill[WAY == DIRECT ? MINE : 1];
   const bool whole = dx == DX && dz - col0 >= DZ;   // no piece lies behind a width
+  const bool ends = dx % (16 / sizeof(T)) || dz % (16 / sizeof(T));
   const int64_t token0 = back ? (int64_t)valid - (int64_t)begin - (int64_t)kChunk : (int64_t)begin;   // lowest of the first chunk
   if (WAY == DIRECT) {
 #pragma unroll
@@ -432,9 +468,9 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
       return;
     }
     if (WAY == PIECES) {
-      if (OUT) to_rows.x.load_whole(p.x, xh, first, end, valid, back, 0, dx);
-      to_rows.y.load_whole(p.y, yh, first, end, valid, back, 0, dx);
-      to_rows.z.load_whole(p.z, zh, first, end, valid, back, col0, dz);
+      if (OUT) to_rows.x.load_pieces(p.x, xh, first, end, valid, back, 0, dx);
+      to_rows.y.load_pieces(p.y, yh, first, end, valid, back, 0, dx);
+      to_rows.z.load_pieces(p.z, zh, first, end, valid, back, col0, dz);
       return;
     }
     const uint32_t to = slot * BUFFER * (uint32_t)sizeof(bf16) + wave * 1024;
@@ -511,6 +547,11 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
       if (OUT) rows.x.store(xs);
       rows.y.store(ys);
       rows.z.store(zs);
+      if (WAY == PIECES && ends) {   // (behind the whole places, by the same lanes)
+        if (OUT) rows.x.store_ends(xs, dx);
+        rows.y.store_ends(ys, dx);
+        rows.z.store_ends(zs, dz - col0);
+      }
       __syncthreads();
       if (WAY == PIECES || first + AHEAD * kChunk < end) fetch(first + AHEAD * kChunk, 0, rows);
     }
@@ -573,15 +614,14 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
         if (m < n && j < dz) store_row_counted<T, NT>(base, lower, acc, 0);
         if (16 + m < n && j < dz) store_row_counted<T, NT>(base, upper, acc, 1);
       }
-    } else if (out_wide) {
+    } else if (out_near) {
 #pragma unroll
       for (int d = 0; d < 2; ++d) {
         const uint32_t row = 16 * d + m;
         uint8_t* const at = base + ((back ? kChunk - 1 - row : row) * (uint32_t)out_step + j * out_size);
         if (row >= n || j >= dz) continue;
-        const uint32_t left = WAY == PIECES ? 4 * NT : dz - j;
-        if (out_f32) store_row<float, NT>(at, acc, d, left);
-        else store_row<T, NT>(at, acc, d, left);
+        if (out_f32) store_row<float, NT>(at, acc, d, dz - j);
+        else store_row<T, NT>(at, acc, d, dz - j);
       }
     } else {
 #pragma unroll

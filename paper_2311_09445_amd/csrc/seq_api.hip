@@ -73,7 +73,7 @@ RotarySide side(const per_rotary_config* c, uint32_t heads, const per_seq_rows* 
     const per_seq_rows& q = or_none(r);
     const uint32_t per16 = 16 / element(c->dtype);
     const bool wide = !misaligned(q.d, 16) && q.batch % per16 == 0 && q.token % per16 == 0 && q.head % per16 == 0;
-    return SeqRows{q.d, q.batch, q.token, q.head, 1, wide ? 1u : 0u};
+    return SeqRows{q.d, q.batch, q.token, q.head, 1, wide ? 1u : 0u, 0};
   };
   return RotarySide{rows(x), rows(out), rows(dout), weight, heads};
 }

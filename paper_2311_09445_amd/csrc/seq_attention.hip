@@ -9,6 +9,8 @@
 //     gradient of k:           v, dout, q;  the same, transposed;   against time, lag 1
 #include "dev_seq.h"
 
+#include <atomic>
+
 namespace per {
 
 namespace {
@@ -96,14 +98,13 @@ struct AttentionStep {
 
 SeqRows rows(const per_seq_rows& r, uint32_t dtype, uint32_t share) {
   const int64_t per16 = dtype == PER_SEQ_BF16 ? 8 : 4;
-  // (the tokens of a chunk lie within 2^31 bytes)
-  const bool wide = (reinterpret_cast<uintptr_t>(r.d) & 15) == 0 && r.batch % per16 == 0 && r.token % per16 == 0 && r.head % per16 == 0 &&
-                    r.token >= 0 && r.token < (1 << 24);
-  return SeqRows{r.d, r.batch, r.token, r.head, share, wide ? 1u : 0u};
+  const bool near = r.token >= 0 && r.token < (1 << 24);
+  const bool wide = near && (reinterpret_cast<uintptr_t>(r.d) & 15) == 0 && r.batch % per16 == 0 && r.token % per16 == 0 && r.head % per16 == 0;
+  return SeqRows{r.d, r.batch, r.token, r.head, share, wide ? 1u : 0u, near ? 1u : 0u};
 }
 // Packed rows [B][L][H][d] in fp32.
 SeqRows packed(float* d, const AttentionSizes& a, uint32_t width) {
-  return SeqRows{d, (int64_t)a.L * a.H * width, (int64_t)a.H * width, (int64_t)width, 1, width % 4 == 0};
+  return SeqRows{d, (int64_t)a.L * a.H * width, (int64_t)a.H * width, (int64_t)width, 1, width % 4 == 0, (uint64_t)a.H * width < (1 << 24)};
 }
 
 AttentionPass make_pass(const AttentionSizes& a, bool back, uint32_t dx, uint32_t dz) {
@@ -181,23 +182,35 @@ hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
   constexpr int DZ = 16 * NT * WAVES;
   constexpr uint32_t lds = ring<T, DX, DZ, OUT, WAY>() * chunk_bytes<T, DX, DZ, OUT>();
   auto* kernel = k_attend<T, DX, NT, WAVES, OUT, WAY>;
-  if (lds > 64 * 1024) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if constexpr (lds > 64 * 1024) {   // granted once per kernel and device
+    static std::atomic<uint64_t> granted{0};
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (!(granted.load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+      granted.fetch_or(bit, std::memory_order_relaxed);
+    }
   }
   kernel<<<(p.items + 7) / 8 * 8 * p.count, 64 * WAVES, lds, s>>>(p);
   return hipGetLastError();
 }
-// Rows that are made up of pieces of 16 bytes: in bfloat16 straight into LDS, in fp32 taken apart on the way.
+// In bfloat16 straight into LDS where rows are made up of pieces of 16 bytes; through registers in pieces where they hold one.
 template <typename T, int DX, int NT, int WAVES, bool OUT>
 hipError_t launch_way(const AttentionPasses& p, hipStream_t s) {
   constexpr uint32_t W = 16 / sizeof(T);
-  bool pieces = true;
+  bool direct = sizeof(T) == 2, pieces = true;
   for (uint32_t i = 0; i < p.count; ++i) {
     const AttentionPass& a = p.pass[i];
-    pieces = pieces && (!OUT || (a.x.wide && a.out.wide)) && a.y.wide && a.z.wide && a.dx % W == 0 && a.dz % W == 0;
+    direct = direct && (!OUT || (a.x.wide && a.out.wide)) && a.y.wide && a.z.wide && a.dx % W == 0 && a.dz % W == 0;
+    pieces = pieces && (!OUT || a.out.near) && a.dx >= W && a.dz >= W;
   }
-  return pieces ? launch_as<T, DX, NT, WAVES, OUT, sizeof(T) == 4 ? PIECES : DIRECT>(p, s) : launch_as<T, DX, NT, WAVES, OUT, ELEMENTS>(p, s);
+  if constexpr (sizeof(T) == 2) {
+    if (direct) return launch_as<T, DX, NT, WAVES, OUT, DIRECT>(p, s);
+  }
+  return pieces ? launch_as<T, DX, NT, WAVES, OUT, PIECES>(p, s) : launch_as<T, DX, NT, WAVES, OUT, ELEMENTS>(p, s);
 }
 template <typename T, int DX, bool OUT>
 hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {

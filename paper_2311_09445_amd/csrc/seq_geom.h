@@ -12,7 +12,8 @@ struct SeqRows {
   void* d;
   int64_t batch, token, head;
   uint32_t share;
-  uint32_t wide;   // address and strides are multiples of 16 bytes
+  uint32_t wide;   // address and strides are multiples of 16 bytes (and near)
+  uint32_t near;   // the tokens of a chunk lie within 2^31 bytes of the first
 };
 
 struct SeqStates {
