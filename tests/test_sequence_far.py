@@ -1,0 +1,111 @@
+"""The sequence operators where rows lie far apart or a tensor holds more than 2^31 elements, and long ragged sequences of odd widths.
+Bounds as in test_sequence.py."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import sequence_oracle as oracle  # noqa: E402
+from sequence_oracle import U_BF16, U_F32  # noqa: E402
+from test_sequence import BF16, F32, absolute, attention_inputs, check_attention, normal, out_bound, spread, state_bound, within  # noqa: E402
+from paper_2311_09445_amd import sequence as seq  # noqa: E402
+
+TAIL = 300   # tokens that the last ones can depend on, at a decay of e^-3: e^-300 is nothing in 64 bits beside what is near
+
+
+def long_rows(seed, L, H, d):
+    """[1, L, H, d] in bfloat16 that repeats 4096 tokens."""
+    return normal(seed, 1, 4096, H, d, dtype=BF16).repeat(1, L // 4096 + 1, 1, 1)[:, :L]
+
+
+def test_more_than_2_to_31_elements():
+    L, H, d = (1 << 20) + 77, 16, 128
+    q, k, v = (long_rows(i, L, H, d) for i in range(3))
+    assert q.numel() > 1 << 31
+    g = torch.full((H,), -3.0, device="cuda")
+    out, last = seq.linear_attention(q, k, v, g, scale=0.3)
+    tail = [t[:, -TAIL:].contiguous() for t in (q, k, v)]
+    want, want_state = oracle.attention(*tail, g, None, None, 0.3)
+    A, A_state = oracle.attention(*absolute(*tail), g, None, None, 0.3)
+    part = slice(TAIL // 2, None)
+    within(out[:, -TAIL:][:, part], want[:, part], out_bound(BF16, want, A, d, L)[:, part], "out")
+    within(last, want_state, state_bound(A_state, 32), "state")
+    del last
+    dout = out.copy_(v)   # (the same memory again)
+    dq, dk, dv, _ = seq.linear_attention_backward(dout, q, k, v, g, scale=0.3, want_dstate=False)
+    want = oracle.attention_backward(tail[2], *tail, g, None, None, None, 0.3)
+    A = oracle.attention_backward(*absolute(tail[2], *tail), g, None, None, None, 0.3)
+    for name, x, w, a in zip(("dq", "dk", "dv"), (dq, dk, dv), want, A):
+        within(x[:, -TAIL:][:, part], w[:, part], out_bound(BF16, w, a, d, L)[:, part], name)
+    del dq, dk, dv, dout
+    f, _ = seq.rotary_frequencies(d)
+    w = 1 + 0.1 * normal(9, d)
+    at = torch.arange(L - 5, L, dtype=torch.int32)[None]
+    turned = seq.rotate(q, None, f)
+    want = oracle.turned(q[:, -5:], at, f.cpu(), "half", 1.0)
+    within(turned[:, -5:], want, U_BF16 * want.abs() + 32 * U_F32 * spread(q[:, -5:], at, f, "half", 1.0), "rotated")
+    seq.norm_rotate(q, k[:, :, :1], w, w, None, f, q_out=turned)
+    want = oracle.norm_rotate(q[:, -5:], w, at, f.cpu(), 1e-6, "half", 1.0)
+    A = spread(oracle.normed(q[:, -5:], w, 1e-6), at, f, "half", 1.0)
+    within(turned[:, -5:], want, U_BF16 * want.abs() + (d + 32) * U_F32 * A, "normed and rotated")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_tokens_far_apart(dtype):
+    """Tokens 2^24 elements apart and more: a chunk spans more than 2^31 bytes in fp32."""
+    B, L, H, d = 1, 33, 1, 32
+    apart = (1 << 24) + 8
+    pool = torch.empty(L * apart, dtype=dtype, device="cuda")
+    views = [torch.as_strided(pool, (B, L, H, d), (0, apart, d, 1), i * 64) for i in range(4)]
+    near = [normal(i, B, L, H, d, dtype=dtype) for i in range(3)]
+    for far, t in zip(views, near):
+        far.copy_(t)
+    g, S = torch.tensor([-0.1], device="cuda"), normal(5, B, H, d, d)
+    out, last = seq.linear_attention(*views[:3], g, S, out=views[3])
+    want = seq.linear_attention(*near, g, S)
+    assert torch.equal(out, want[0]) and torch.equal(last, want[1])
+    f, _ = seq.rotary_frequencies(d)
+    assert torch.equal(seq.rotate(views[0], None, f, out=views[3]), seq.rotate(near[0], None, f))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(61, 127), (128, 72), (36, 20)])
+def test_long_ragged_odd(dk, dv, dtype):
+    B, L, H, G = 3, 1100, 2, 1
+    q, k, v, _, S, _ = attention_inputs(B, L, H, G, dk, dv, dtype)
+    g = torch.tensor([-0.003, -1.5], device="cuda")
+    lengths = torch.tensor([1100, 0, 771], dtype=torch.int32, device="cuda")
+    out, last = seq.linear_attention(q, k, v, g, S, lengths, scale=0.1)
+    check_attention(q, k, v, g, S, lengths, 0.1, out, last)
+    dout, dS = normal(11, B, L, H, dv, dtype=dtype), normal(12, B, H, dk, dv)
+    got = seq.linear_attention_backward(dout, q, k, v, g, S, dS, lengths, scale=0.1)
+    want = oracle.attention_backward(dout, q, k, v, g, S, dS, lengths.cpu(), 0.1)
+    A = oracle.attention_backward(*absolute(dout, q, k, v), g, *absolute(S, dS), lengths.cpu(), 0.1)
+    for name, x, w, a, width in zip(("dq", "dk", "dv"), got, want, A, (dv, dv, dk)):
+        within(x, w, out_bound(dtype, w, a, width, L), name)
+    within(got[3], want[3], state_bound(A[3], L), "dstate0")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_rows_at_every_alignment(dtype):
+    """The same rows at addresses that are multiples of 2, 4 and 8 bytes only, outputs too."""
+    B, L, H, d = 2, 70, 2, 40
+    near = [normal(i, B, L, H, d, dtype=dtype) for i in range(3)]
+    g, S = torch.tensor([-0.05, -0.5], device="cuda"), normal(5, B, H, d, d)
+    want, want_state = oracle.attention(*near, g, S, None, 0.2)
+    A, A_state = oracle.attention(*absolute(*near), g, S.abs(), None, 0.2)
+    for shift in (1, 2, 4):
+        moved = []
+        for t in near + [torch.zeros_like(near[0])]:
+            room = torch.full((t.numel() + 16,), 7.0, dtype=dtype, device="cuda")
+            moved.append(room[shift:shift + t.numel()].view_as(t))
+            moved[-1].copy_(t)
+        out, last = seq.linear_attention(*moved[:3], g, S, scale=0.2, out=moved[3])
+        within(out, want, out_bound(dtype, want, A, d, L), f"shift {shift}")
+        within(last, want_state, state_bound(A_state, L), f"state, shift {shift}")
+        lead = torch.as_strided(moved[3], (shift,), (1,), moved[3].storage_offset() - shift)
+        tail = torch.as_strided(moved[3], (16 - shift,), (1,), moved[3].storage_offset() + moved[3].numel())
+        assert bool((lead == 7.0).all()) and bool((tail == 7.0).all())     # nothing written around it
