@@ -408,16 +408,21 @@ hipError_t launch_attention_backward(const AttentionSizes& a, const per_seq_rows
                                  : backward<float>(a, dout, q, k, v, state, dstate, dq, dk, dv, dstate0, work, s);
 }
 
+template <typename T, int VEC, int R>
+static hipError_t step(const AttentionStep& p, uint32_t rows, hipStream_t s) {
+  const uint64_t bytes = (uint64_t)rows * p.dk * p.dv * 4;
+  if (bytes <= 256ull << 20) k_attend_step<T, VEC, R, KEPT><<<rows, 256, 0, s>>>(p);
+  else if (bytes <= 768ull << 20) k_attend_step<T, VEC, R, STORES_PAST><<<rows, 256, 0, s>>>(p);
+  else k_attend_step<T, VEC, R, ALL_PAST><<<rows, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
 template <typename T>
 static hipError_t step(AttentionStep p, uint32_t rows, hipStream_t s) {
   const bool wide = p.dv % 4 == 0 && (reinterpret_cast<uintptr_t>(p.state.d) & 15) == 0 && p.state.batch % 4 == 0 && p.state.head % 4 == 0;
   const uint32_t columns = wide ? p.dv / 4 : p.dv;
   p.groups = 256 / columns < p.dk ? 256 / columns : p.dk;
   const bool few = (p.dk + p.groups - 1) / p.groups <= 4;   // rows of a thread
-  if (wide && few) k_attend_step<T, 4, 4><<<rows, 256, 0, s>>>(p);
-  else if (wide) k_attend_step<T, 4, 16><<<rows, 256, 0, s>>>(p);
-  else k_attend_step<T, 1, 16><<<rows, 256, 0, s>>>(p);
-  return hipGetLastError();
+  return !wide ? step<T, 1, 16>(p, rows, s) : few ? step<T, 4, 4>(p, rows, s) : step<T, 4, 16>(p, rows, s);
 }
 
 hipError_t launch_attention_step(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,

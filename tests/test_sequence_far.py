@@ -109,3 +109,17 @@ def test_rows_at_every_alignment(dtype):
         lead = torch.as_strided(moved[3], (shift,), (1,), moved[3].storage_offset() - shift)
         tail = torch.as_strided(moved[3], (16 - shift,), (1,), moved[3].storage_offset() + moved[3].numel())
         assert bool((lead == 7.0).all()) and bool((tail == 7.0).all())     # nothing written around it
+
+
+@pytest.mark.parametrize("B", [300, 800])
+def test_steps_of_states_that_do_not_fit_the_cache(B):
+    """More than 256 and 768 MiB of states: the same as batch by batch."""
+    H, d = 16, 128
+    q, k, v = (normal(i, B, 1, H, d, dtype=BF16) for i in range(3))
+    g, S = -torch.linspace(0.001, 1.0, H, device="cuda"), torch.randn(B, H, d, d, device="cuda")
+    T = S.clone()
+    out = seq.linear_attention_step(q, k, v, g, T)
+    for lo in range(0, B, 100):
+        part = S[lo:lo + 100].clone()
+        want = seq.linear_attention_step(q[lo:lo + 100], k[lo:lo + 100], v[lo:lo + 100], g, part)
+        assert torch.equal(out[lo:lo + 100], want) and torch.equal(T[lo:lo + 100], part)
