@@ -396,6 +396,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
     if (reach < (float)n) begin += (n - (uint32_t)reach) / kChunk * kChunk;
   }
   const uint32_t col0 = slice * DZ, col = col0 + wave * 16 * NT;   // first z column of the workgroup, of the wave
+  if (col0 >= dz) return;   // (a pass narrower than the launch's widest)
 
   f32x4 S[NT][TX];
 #pragma unroll

@@ -140,37 +140,48 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 // How a sequence is cut.  A workgroup takes its tokens one chunk behind the other, so what cuts the time of few sequences is
 // workgroups: the sequence in segments, each from the state that those before it bring.  That costs another pass over keys and values
-// for those states, a state in memory per segment, and two launches.  The fewest microseconds by these measured figures are taken:
-//   a chunk of 64 x 64 takes 0.85 (fp32: 1.5), of 128 x 64 1.2 (2.7), of 128 x 128 1.9; two workgroups on a compute unit half as long
-//   again, more take turns; the pass for the states 0.55 of a pass with outputs; launches 12; states 4 TB/s.
+// for those states, a state in memory per segment, and two launches.  A gradient of unlike widths is two launches, or one as wide as
+// the widest.  The fewest microseconds by these measured figures are taken:
+//   a chunk of 64 x 64 takes 0.85 (fp32: 1.9), of 128 x 64 1.2 (2.8), of 128 x 128 1.9; two workgroups on a compute unit 1.45 times
+//   that, more take turns; the pass for the states 0.55 of that for outputs (0.42 where it serves a gradient's); states move at 4 TB/s.
 // Measured, whole against cut: 64 rows of 1024 tokens (64 x 64) 33 us and 25 in four; 4 rows of 1024 31 and 17 in sixteen; 4 rows of
 // 512 18 and 17; the gradient of 64 rows of 1024 34 and 37 in four; of 32 rows of 16384 (128 x 128) 426 in 5, 462 in 8, 455 in 16.
 struct Cut {
   uint32_t segments, segment;
+  bool one;   // a gradient's passes in one launch
 };
 uint32_t kernel_width(uint32_t d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 // Half of the columns to a workgroup: see launch_dz.
 bool halved(uint32_t dtype, uint32_t dz, uint64_t workgroups) { return dz > 64 && (dtype == PER_SEQ_F32 || workgroups <= 256); }
-Cut cut(const AttentionSizes& a, uint32_t passes) {
-  const uint64_t n = (uint64_t)a.B * a.H * passes;   // workgroups of whole sequences
-  const uint32_t most = a.L / 64 < 64 ? a.L / 64 : 64;
-  const float x = (float)kernel_width(a.dk) / 64.0f, z = (float)kernel_width(a.dv) / 64.0f, state = 4.0f * a.dk * a.dv;
+float launch_us(uint32_t dtype, uint64_t workgroups, uint32_t dx, uint32_t dz, uint32_t chunks) {
+  const bool half = halved(dtype, dz, workgroups);
+  const float area = (float)(dx * (half ? dz / 2 : dz)) / 4096.0f, each = (float)((workgroups * (half ? 2 : 1) + 255) / 256);
+  return (dtype == PER_SEQ_F32 ? 0.97f + 0.93f * area : 0.5f + 0.35f * area) * (float)chunks * (each <= 1 ? 1.0f : each <= 2 ? 1.45f : 0.25f + 0.8f * each);
+}
+Cut cut(const AttentionSizes& a, bool backward) {
+  const uint64_t rows = (uint64_t)a.B * a.H;
+  const uint32_t wk = kernel_width(a.dk), wv = kernel_width(a.dv), widest = wk > wv ? wk : wv, most = a.L / 64 < 64 ? a.L / 64 : 64;
   float best = 0.0f;
-  uint32_t segments = 1;
-  for (uint32_t s = 1; n && s <= (most ? most : 1); ++s) {
-    const bool half = halved(a.dtype, a.dv, n * s);
-    const uint64_t each = (n * s * (half ? 2 : 1) + 255) / 256;   // workgroups to a compute unit
-    const float chunk = a.dtype == PER_SEQ_F32 ? 0.3f + 1.2f * x * (half ? z / 2 : z) : 0.5f + 0.35f * x * (half ? z / 2 : z);
-    float us = chunk * (float)((a.L / s + kChunk - 1) / kChunk) * ((float)(each / 2) * 1.5f + (float)(each % 2));
-    if (s > 1) us = us * (passes == 1 ? 1.55f : 1.37f) + 12.0f + state * (float)((uint64_t)a.B * a.H * s * (passes == 1 ? 4 : 8)) / 4e6f;
+  Cut c{1, a.L ? a.L : 1, true};
+  for (uint32_t s = 1; rows && a.L && (s == 1 || s <= most); ++s) {
+    const uint64_t n = rows * s;
+    const uint32_t segment = ((a.L + s - 1) / s + kChunk - 1) / kChunk * kChunk, chunks = segment / kChunk;
+    bool one = true;
+    float us = backward ? launch_us(a.dtype, 3 * n, widest, widest, chunks) : launch_us(a.dtype, n, wk, wv, chunks);
+    if (backward && wk != wv) {
+      const float apart = launch_us(a.dtype, 2 * n, wv, wk, chunks) + launch_us(a.dtype, n, wk, wv, chunks) + 3.0f;
+      one = us <= apart;
+      if (!one) us = apart;
+    }
+    if (s > 1)
+      us += (backward ? 0.42f : 0.55f) * launch_us(a.dtype, backward ? 2 * n : n, wk, wv, chunks) + 10.0f +
+            4.0f * a.dk * a.dv * (float)(n * (backward ? 8 : 4)) / 4e6f;
     if (s == 1 || us < best) {
       best = us;
-      segments = s;
+      c = s == 1 ? Cut{1, a.L, one} : Cut{(a.L + segment - 1) / segment, segment, one};
     }
   }
-  if (segments == 1) return Cut{1, a.L ? a.L : 1};
-  const uint32_t segment = ((a.L + segments - 1) / segments + kChunk - 1) / kChunk * kChunk;
-  return Cut{(a.L + segment - 1) / segment, segment};
+  return c;
 }
 size_t part_bytes(const AttentionSizes& a, const Cut& c) {
   return c.segments < 2 ? 0 : align256((size_t)a.B * a.H * c.segments * a.dk * a.dv * sizeof(float));
@@ -214,7 +225,8 @@ hipError_t launch_way(const AttentionPasses& p, hipStream_t s) {
 }
 template <typename T, int DX, bool OUT>
 hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {
-  const uint32_t dz = p.pass[0].dz;
+  uint32_t dz = 0;
+  for (uint32_t i = 0; i < p.count; ++i) dz = dz < p.pass[i].dz ? p.pass[i].dz : dz;
   p.slices = 1;
   p.items = rows * p.segments;
   if (dz <= 32) return launch_way<T, DX, 1, 2, OUT>(p, s);
@@ -230,10 +242,11 @@ hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {
   if constexpr (sizeof(T) == 2) return launch_way<T, DX, 2, 4, OUT>(p, s);
   return hipErrorInvalidValue;
 }
-// Passes of the same widths (as kernels go), in one launch.
+// Passes in one launch, as wide as the widest.
 template <typename T, bool OUT>
 hipError_t launch_passes(AttentionPasses p, uint32_t rows, hipStream_t s) {
-  const uint32_t dx = p.pass[0].dx;
+  uint32_t dx = 0;
+  for (uint32_t i = 0; i < p.count; ++i) dx = dx < p.pass[i].dx ? p.pass[i].dx : dx;
   if (dx <= 32) return launch_dz<T, 32, OUT>(p, rows, s);
   if (dx <= 64) return launch_dz<T, 64, OUT>(p, rows, s);
   return launch_dz<T, 128, OUT>(p, rows, s);
@@ -272,7 +285,7 @@ template <typename T>
 hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
                    const per_seq_states* state, const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
-  const Cut c = cut(a, 1);
+  const Cut c = cut(a, false);
   AttentionPasses all{};
   all.count = 1;
   all.segments = c.segments;
@@ -309,7 +322,7 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
                     const per_seq_rows& v, const per_seq_states* state, const per_seq_states* dstate, const per_seq_rows& dq,
                     const per_seq_rows& dk, const per_seq_rows& dv, const per_seq_states* dstate0, void* work, hipStream_t s) {
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
-  const Cut c = cut(a, 3);
+  const Cut c = cut(a, true);
   const SeqRows Q = rows(q, a.dtype, 1), K = rows(k, a.dtype, share), V = rows(v, a.dtype, share), D = rows(dout, a.dtype, 1);
   uint8_t* at = static_cast<uint8_t*>(work);
   float* part[2];   // of the states, of their gradients
@@ -356,12 +369,12 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
     from_parts(&of_k, part[1], a, c, true);
     from_parts(&of_v, part[1], a, c, false);
   }
-  // All three in one launch where they take the same kernel; but the gradient of k reads dstate, which that of v may write over.
+  // All three in one launch, if that is best; but the gradient of k reads dstate, which that of v may write over.
   all.pass[0] = of_q;
   all.pass[1] = of_k;
   all.pass[2] = of_v;
   const bool over = c.segments == 1 && dstate && dstate0 && dstate->d == dstate0->d;
-  all.count = !over && kernel_width(a.dk) == kernel_width(a.dv) ? 3 : 2;
+  all.count = c.one && !over ? 3 : 2;
   e = launch_passes<T, true>(all, bh, s);
   if (e == hipSuccess && all.count == 2) {
     all.count = 1;
@@ -389,7 +402,7 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
 }  // namespace
 
 size_t attention_work_bytes(const AttentionSizes& a, bool backward) {
-  const Cut c = cut(a, backward ? 3 : 1);
+  const Cut c = cut(a, backward);
   return backward ? 2 * part_bytes(a, c) + fold_bytes(a, a.dk) + fold_bytes(a, a.dv) : part_bytes(a, c);
 }
 
