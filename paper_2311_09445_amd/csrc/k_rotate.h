@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256, KIND == NORM_ROTATE_BACK ? 4 : 2) void k_rotat
           }
         }
         if (side == from && it == group) {   // (every wave comes here once per tile)
-          if (BACK && tile != block) __syncthreads();
+          if (tile != block) __syncthreads();   // (all are through with the tile before)
           for (uint32_t i = threadIdx.x; i < n * half; i += 256) {
             const uint32_t tok = first + i / half, b = tok / a.L, t = tok % a.L;
             const int32_t pos = a.at ? a.at[(int64_t)b * a.at_batch + (int64_t)t * a.at_token] : (int32_t)t;

@@ -41,12 +41,13 @@ const per_seq_rows& or_none(const per_seq_rows* r) {
   return r ? *r : empty;
 }
 
-int check_attention(const per_attention_config* c) {
+// most: sequences times heads, so that a launch stays within 2^32 threads
+int check_attention(const per_attention_config* c, uint32_t most = 1u << 21) {
   if (!c || c->struct_size != sizeof(per_attention_config)) return PER_EINVAL;
   if (c->dtype != PER_SEQ_BF16 && c->dtype != PER_SEQ_F32) return PER_EINVAL;
   if (c->dk < 1 || c->dk > 128 || c->dv < 1 || c->dv > 128) return PER_ERANGE;
   if (c->heads && (!c->kv_heads || c->heads % c->kv_heads)) return PER_EINVAL;
-  if (c->length > (1u << 30) || (uint64_t)c->batch * c->heads > (1u << 24)) return PER_ERANGE;
+  if (c->length > (1u << 30) || (uint64_t)c->batch * c->heads > most) return PER_ERANGE;
   if (!isfinite(c->scale)) return PER_EINVAL;
   return PER_OK;
 }
@@ -215,7 +216,7 @@ int per_linear_attention_backward(const per_attention_config* c, const per_seq_r
 int per_linear_attention_step(const per_attention_config* c, const per_seq_rows* q, const per_seq_rows* k,
                               const per_seq_rows* v, const float* d_log_decay, const int32_t* d_lengths,
                               const per_seq_states* state, const per_seq_rows* out, void* stream) {
-  int rc = check_attention(c);
+  int rc = check_attention(c, 1u << 23);
   if (rc != PER_OK) return rc;
   if (c->length != 1) return PER_ERANGE;
   const Extent nq{c->batch, 1, c->heads}, nk{c->batch, 1, c->kv_heads};

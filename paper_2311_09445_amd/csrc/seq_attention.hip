@@ -65,24 +65,25 @@ struct Folds {
   uint32_t L, G, share;
   uint64_t rows;   // B L G
 };
-// VEC elements to a lane; 32 lanes take a row.
+// VEC elements to a lane.
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void k_fold_heads(Folds all) {
   typedef float Vec __attribute__((ext_vector_type(VEC)));
   typedef T Out __attribute__((ext_vector_type(VEC)));
   const Fold& f = all.fold[blockIdx.y];
   const uint32_t lanes = (f.d + VEC - 1) / VEC, per = 256 / lanes, lane = threadIdx.x % lanes;
-  const uint64_t row = (uint64_t)blockIdx.x * per + threadIdx.x / lanes;
-  if (threadIdx.x / lanes >= per || row >= all.rows) return;
-  const uint32_t g = (uint32_t)(row % all.G);
-  const uint64_t tok = row / all.G;
-  const float* from = f.from + row * all.share * f.d + lane * VEC;
-  Vec sum = Vec(0.0f);
-  for (uint32_t m = 0; m < all.share; ++m) sum += *reinterpret_cast<const Vec*>(from + (size_t)m * f.d);
-  Out o;
+  if (threadIdx.x / lanes >= per) return;
+  for (uint64_t row = (uint64_t)blockIdx.x * per + threadIdx.x / lanes; row < all.rows; row += (uint64_t)gridDim.x * per) {
+    const uint32_t g = (uint32_t)(row % all.G);
+    const uint64_t tok = row / all.G;
+    const float* from = f.from + row * all.share * f.d + lane * VEC;
+    Vec sum = Vec(0.0f);
+    for (uint32_t m = 0; m < all.share; ++m) sum += *reinterpret_cast<const Vec*>(from + (size_t)m * f.d);
+    Out o;
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) o[i] = (T)sum[i];
-  *reinterpret_cast<Out*>(row_to<T>(f.to, (uint32_t)(tok / all.L), (uint32_t)(tok % all.L), g) + lane * VEC) = o;
+    for (int i = 0; i < VEC; ++i) o[i] = (T)sum[i];
+    *reinterpret_cast<Out*>(row_to<T>(f.to, (uint32_t)(tok / all.L), (uint32_t)(tok % all.L), g) + lane * VEC) = o;
+  }
 }
 
 struct AttentionStep {
@@ -392,7 +393,8 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
   if (!f.rows) return e;
   const bool wide = a.dk % 4 == 0 && a.dv % 4 == 0 && f.fold[0].to.wide && f.fold[1].to.wide;
   const uint32_t widest = a.dk > a.dv ? a.dk : a.dv, per = 256 / (wide ? (widest + 3) / 4 : widest);   // rows of a workgroup
-  const dim3 grid((uint32_t)((f.rows + per - 1) / per), 2);
+  const uint64_t blocks = (f.rows + per - 1) / per;
+  const dim3 grid((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), 2);
   if (wide) k_fold_heads<T, 4><<<grid, 256, 0, s>>>(f);
   else k_fold_heads<T, 1><<<grid, 256, 0, s>>>(f);
   e = hipGetLastError();

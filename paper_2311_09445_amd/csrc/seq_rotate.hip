@@ -203,7 +203,7 @@ hipError_t launch(RotaryKind kind, RotaryArgs a, float* dqw, float* dkw, hipStre
       const uint32_t of = back ? a.side[i].heads : heads;
       if (!of) continue;
       // (a gradient's workgroups are bounded by the room for their sums: shared out by heads, one at least)
-      uint64_t room = back ? (uint64_t)most * of / heads : tokens;
+      uint64_t room = back ? (uint64_t)most * of / heads : 1u << 20;
       if (back && i == 1 && room + a.blocks[0] > most) room = most - a.blocks[0];
       if (!room) room = 1;   // (there is one: `most` is two at least, and heads on the other side leave one)
       uint64_t n = (back ? 16 : 8) * 256 / lanes / of;

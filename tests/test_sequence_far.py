@@ -123,3 +123,40 @@ def test_steps_of_states_that_do_not_fit_the_cache(B):
         part = S[lo:lo + 100].clone()
         want = seq.linear_attention_step(q[lo:lo + 100], k[lo:lo + 100], v[lo:lo + 100], g, part)
         assert torch.equal(out[lo:lo + 100], want) and torch.equal(T[lo:lo + 100], part)
+
+
+def test_more_tiles_than_workgroups():
+    """300 heads of 32 on 1.1 million tokens: a workgroup takes one token after another."""
+    x = torch.empty(1, 1_100_000, 300, 32, dtype=BF16, device="cuda")
+    x.copy_(normal(1, 1, 1, 300, 32, dtype=BF16).expand_as(x))
+    f, _ = seq.rotary_frequencies(32)
+    head = x[:, :1].clone()
+    seq.rotate(x, None, f, out=x)
+    for t in (0, 1, 524_288, 1_048_576, 1_048_577, 1_099_999):
+        at = torch.tensor([[t]], dtype=torch.int32)
+        want = oracle.turned(head, at, f.cpu(), "half", 1.0)
+        within(x[:, t:t + 1], want, U_BF16 * want.abs() + 32 * U_F32 * spread(head, at, f, "half", 1.0), f"token {t}")
+
+
+def test_what_is_masked_may_hold_anything():
+    """Actors that stand still, and elements behind the rotated ones."""
+    B, H, d = 4, 2, 32
+    q, k, v = (normal(i, B, 1, H, d, dtype=BF16) for i in range(3))
+    g, S = torch.tensor([-0.1, -1.0], device="cuda"), normal(5, B, H, d, d)
+    active = torch.tensor([1, 0, 1, 0], dtype=torch.int32, device="cuda")
+    T = S.clone()
+    want = seq.linear_attention_step(q, k, v, g, T, active)
+    for t in (q, k, v, S):
+        t[1] = float("nan")
+        t[3] = float("inf")
+    U = S.clone()
+    got = seq.linear_attention_step(q, k, v, g, U, active)
+    assert torch.equal(got, want) and torch.equal(U[::2], T[::2])
+    assert bool(U[1].isnan().all()) and bool(U[3].isinf().all())
+    x = normal(7, 1, 3, 2, 64, dtype=F32)
+    f, _ = seq.rotary_frequencies(32)
+    want = seq.rotate(x, None, f)
+    x[..., 33] = float("nan")
+    x[..., 40] = float("inf")
+    got = seq.rotate(x, None, f)
+    assert torch.equal(got[..., :32], want[..., :32]) and torch.equal(got[..., 34:40], want[..., 34:40]) and torch.equal(got[..., 41:], want[..., 41:])
