@@ -19,6 +19,11 @@
 // (DIRECT: bfloat16, rows made of pieces).  Rows in fp32, which are taken apart on the way, and rows of odd widths or alignments go
 // through registers in pieces, two chunks ahead (PIECES); rows narrower than a piece or far apart one by one (ELEMENTS).
 
+// What bounds it.  A workgroup by itself takes 0.8 us a chunk of 64 x 64 in bfloat16, 1.9 of 128 x 128: the chain from its barrier
+// through LDS and two rounds of matrix instructions.  With the chip full it is memory: 768 workgroups of 64 x 64, three to a compute
+// unit, take 2.8 us for a chunk each (4.5 TB/s), 2.7 without any of the products, 1.6 without the outputs; 65536 tokens of 16 heads of
+// 128 x 128 229 us (4.7 TB/s).
+
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
