@@ -383,13 +383,14 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
   const uint32_t which = blockIdx.x / 8 % all.count, item = blockIdx.x / (8 * all.count) * 8 + blockIdx.x % 8;
   if (item >= all.items) return;
   const AttentionPass& p = all.pass[which];
-  const uint32_t slice = item % all.slices, seg = item / all.slices % all.segments, bh = item / all.slices / all.segments;
+  const uint32_t slice = item % all.slices, seg = item / all.slices % all.run, bh = item / all.slices / all.run;
   const uint32_t h = bh % p.H, b = bh / p.H, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // (what the loop needs of the arguments is taken out of them here: behind its barriers they would be loaded again)
   const uint32_t L = p.L, dx = p.dx, dz = p.dz, segment = all.segment;
   const float decay = p.log_decay[h], c_state = p.c_state;
-  const bool back = p.back != 0, out_f32 = p.out_f32 != 0, exact = p.exact != 0;
+  const bool back = p.back != 0, out_f32 = p.out_f32 != 0;
+  const bool last = OUT && p.to && seg + 1 == all.segments, exact = p.exact && (last || !OUT);   // (its state is an output)
   const int lag = back ? 1 : 0;
   const uint32_t valid = valid_tokens(p.lengths, b, L), start = seg * segment;
   const uint32_t end = valid < start ? start : valid - start < segment ? valid : start + segment;
@@ -408,9 +409,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
   for (int a = 0; a < TX; ++a)
 #pragma unroll
     for (int c = 0; c < NT; ++c) S[c][a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  if (OUT && p.in) {
-    // (all asked for at once: places behind a width take the last one's, and are cleared when all are there)
-    const float* in = p.in + (int64_t)b * p.in_batch + (int64_t)h * p.in_head + (int64_t)seg * p.in_segment;
+  // A state out of memory (all asked for at once: places behind a width take the last one's, and are cleared when all are there).
+  auto load = [&](const float* in, f32x4 (&to)[NT][TX]) __attribute__((always_inline)) {
     const uint32_t in_x = p.in_x, in_z = p.in_z;
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const uint32_t i = state_row(a, 4 * g + r);
-          S[c][a][r] = in[(i < dx ? i : dx - 1) * in_x + at];
+          to[c][a][r] = in[(i < dx ? i : dx - 1) * in_x + at];
         }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -430,11 +430,12 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
       for (int a = 0; a < TX; ++a)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float s = S[c][a][r];
+          float s = to[c][a][r];
           asm("" : "+v"(s));   // (the load stays above: moved into the choice each would be waited for by itself)
-          S[c][a][r] = state_row(a, 4 * g + r) < dx && col + state_column<NT>(c, m) < dz ? s : 0.0f;
+          to[c][a][r] = state_row(a, 4 * g + r) < dx && col + state_column<NT>(c, m) < dz ? s : 0.0f;
         }
-  }
+  };
+  if (OUT && p.in) load(p.in + (int64_t)b * p.in_batch + (int64_t)h * p.in_head + (int64_t)seg * p.in_segment, S);
 
   const T* const xh = OUT ? row_of<T>(p.x, b, 0, h) : nullptr;
   const T* const yh = row_of<T>(p.y, b, 0, h);
@@ -665,9 +666,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
     for (uint32_t first = begin, slot = 0; first < end; first += kChunk, slot ^= 1) chunk(first, slot, staged[0]);
   }
 
-  float* const to = OUT ? p.to : p.part;
-  if (to) {
-    float* const S_out = OUT ? to + (int64_t)b * p.to_batch + (int64_t)h * p.to_head : to + ((size_t)bh * all.segments + seg) * dx * dz;
+  if (last || !OUT) {
+    float* const S_out = OUT ? p.to + (int64_t)b * p.to_batch + (int64_t)h * p.to_head : p.part + ((size_t)bh * all.segments + seg) * dx * dz;
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
       const uint32_t j = col + state_column<NT>(c, m);
@@ -699,29 +699,29 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
   }
 }
 
-// The states that the segments of a sequence start from, from what each of them brings, in place; and the last state.
+// The states that the segments of a sequence start from, from what each of those before brings, in place.
 __global__ __launch_bounds__(256) void k_join(JoinPasses all) {
   const JoinPass& p = all.pass[blockIdx.y];
   const uint32_t per = p.dx * p.dz;
   const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= (uint64_t)all.BH * per) return;
   const uint32_t bh = (uint32_t)(at / per), e = (uint32_t)(at % per), h = bh % all.H, b = bh / all.H;
-  const uint32_t valid = valid_tokens(all.lengths, b, all.L);
+  const uint32_t valid = valid_tokens(all.lengths, b, all.L), last = all.segments - 1;
   const float g = all.log_decay[h];
   float S = p.in ? p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + e] : 0.0f;
   float* part = p.part + (size_t)bh * all.segments * per + e;
-  for (uint32_t s0 = 0; s0 < all.segments; s0 += 8) {
+  for (uint32_t s0 = 0; s0 < last; s0 += 8) {
     float brought[8];
 #pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) brought[k] = s0 + k < all.segments ? part[(size_t)(s0 + k) * per] : 0.0f;
+    for (uint32_t k = 0; k < 8; ++k) brought[k] = s0 + k < last ? part[(size_t)(s0 + k) * per] : 0.0f;
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) {
-      if (s0 + k >= all.segments) break;
+      if (s0 + k >= last) break;
       part[(size_t)(s0 + k) * per] = S;
       const uint32_t begin = (s0 + k) * all.segment;
       const uint32_t n = valid <= begin ? 0 : valid - begin < all.segment ? valid - begin : all.segment;
       if (n) S = fmaf(S, expm1f((float)n * g), S) + brought[k];
     }
   }
-  if (p.to) p.to[(int64_t)b * p.to_batch + (int64_t)h * p.to_head + e] = S;
+  part[(size_t)last * per] = S;
 }

@@ -34,15 +34,13 @@ struct AttentionPass {
 };
 struct AttentionPasses {
   AttentionPass pass[3];
-  uint32_t count, items, slices, segments, segment;   // items: workgroups of a pass; segment: tokens
+  uint32_t count, items, slices, segments, run, segment;   // items: workgroups of a pass; run: segments taken; segment: tokens
 };
 
 struct JoinPass {
   float* part;
   const float* in;
   int64_t in_batch, in_head;
-  float* to;
-  int64_t to_batch, to_head;
   uint32_t dx, dz;
 };
 struct JoinPasses {
@@ -141,12 +139,12 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 // How a sequence is cut.  A workgroup takes its tokens one chunk behind the other, so what cuts the time of few sequences is
 // workgroups: the sequence in segments, each from the state that those before it bring.  That costs another pass over keys and values
-// for those states, a state in memory per segment, and two launches.  A gradient of unlike widths is two launches, or one as wide as
-// the widest.  The fewest microseconds by these measured figures are taken:
+// for those states (the last segment's is not needed), a state in memory per segment, and two launches.  A gradient of unlike
+// widths is two launches, or one as wide as the widest.  The fewest microseconds by these measured figures are taken:
 //   a chunk of 64 x 64 takes 0.85 (fp32: 1.9), of 128 x 64 1.2 (2.8), of 128 x 128 1.9; two workgroups on a compute unit 1.45 times
 //   that, more take turns; the pass for the states 0.55 of that for outputs (0.42 where it serves a gradient's); states move at 4 TB/s.
 // Measured, whole against cut: 64 rows of 1024 tokens (64 x 64) 33 us and 25 in four; 4 rows of 1024 31 and 17 in sixteen; 4 rows of
-// 512 18 and 17; the gradient of 64 rows of 1024 34 and 37 in four; of 32 rows of 16384 (128 x 128) 426 in 5, 462 in 8, 455 in 16.
+// 512 18 and 17; the gradient of 64 rows of 1024 34 and 37 in four; of 32 rows of 16384 (128 x 128) 388 in 5, 423 in 8, 403 in 10.
 struct Cut {
   uint32_t segments, segment;
   bool one;   // a gradient's passes in one launch
@@ -175,7 +173,7 @@ Cut cut(const AttentionSizes& a, bool backward) {
       if (!one) us = apart;
     }
     if (s > 1)
-      us += (backward ? 0.42f : 0.55f) * launch_us(a.dtype, backward ? 2 * n : n, wk, wv, chunks) + 10.0f +
+      us += (backward ? 0.42f : 0.55f) * launch_us(a.dtype, (backward ? 2 : 1) * (n - rows), wk, wv, chunks) + 10.0f +
             4.0f * a.dk * a.dv * (float)(n * (backward ? 8 : 4)) / 4e6f;
     if (s == 1 || us < best) {
       best = us;
@@ -229,7 +227,7 @@ hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {
   uint32_t dz = 0;
   for (uint32_t i = 0; i < p.count; ++i) dz = dz < p.pass[i].dz ? p.pass[i].dz : dz;
   p.slices = 1;
-  p.items = rows * p.segments;
+  p.items = rows * p.run;
   if (dz <= 32) return launch_way<T, DX, 1, 2, OUT>(p, s);
   if (dz <= 64) return launch_way<T, DX, 1, 4, OUT>(p, s);
   // Wider states: two tiles of columns to a wave, or half of the columns to a workgroup where there are few (each then reads x and y:
@@ -255,9 +253,6 @@ hipError_t launch_passes(AttentionPasses p, uint32_t rows, hipStream_t s) {
 
 void join_from(JoinPass* j, const per_seq_states* s) {
   if (s) { j->in = s->d; j->in_batch = s->batch; j->in_head = s->head; }
-}
-void join_to(JoinPass* j, const per_seq_states* s) {
-  if (s) { j->to = s->d; j->to_batch = s->batch; j->to_head = s->head; }
 }
 // A pass whose segments start from the joined states.
 void from_parts(AttentionPass* p, float* part, const AttentionSizes& a, const Cut& c, bool transposed) {
@@ -297,24 +292,25 @@ hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq
   p.y = rows(k, a.dtype, share);
   p.z = rows(v, a.dtype, share);
   p.out = rows(out, a.dtype, 1);
+  to_states(&p, out_state);
+  p.exact = out_state != nullptr;
   if (c.segments == 1) {
+    all.run = 1;
     from_states(&p, state, a.dv, false);
-    to_states(&p, out_state);
-    p.exact = out_state != nullptr;
     return launch_passes<T, true>(all, bh, s);
   }
-  p.part = static_cast<float*>(work);
-  p.exact = out_state != nullptr;
+  float* const part = static_cast<float*>(work);
+  all.run = c.segments - 1;
+  p.part = part;
   hipError_t e = launch_passes<T, false>(all, bh, s);
   if (e != hipSuccess) return e;
+  all.run = c.segments;
   JoinPasses j{};
-  j.pass[0] = JoinPass{p.part, nullptr, 0, 0, nullptr, 0, 0, a.dk, a.dv};
+  j.pass[0] = JoinPass{part, nullptr, 0, 0, a.dk, a.dv};
   join_from(&j.pass[0], state);
-  join_to(&j.pass[0], out_state);
   e = launch_join(j, a, c, 1, s);
   if (e != hipSuccess) return e;
-  from_parts(&p, p.part, a, c, false);
-  p.exact = 0;
+  from_parts(&p, part, a, c, false);
   return launch_passes<T, true>(all, bh, s);
 }
 
@@ -342,34 +338,34 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
   AttentionPasses all{};
   all.segments = c.segments;
   all.segment = c.segment;
+  to_states(&of_v, dstate0);
+  of_v.exact = dstate0 != nullptr;
   hipError_t e;
   if (c.segments == 1) {
     from_states(&of_q, state, a.dv, true);
     from_states(&of_k, dstate, a.dv, true);
     from_states(&of_v, dstate, a.dv, false);
-    to_states(&of_v, dstate0);
-    of_v.exact = dstate0 != nullptr;
   } else {
+    all.run = c.segments - 1;
     all.count = 2;
     all.pass[0] = make_pass(a, false, a.dk, a.dv);
     all.pass[0].y = K;
     all.pass[0].z = V;
     all.pass[1] = of_v;
-    all.pass[1].exact = dstate0 != nullptr;
     for (int i = 0; i < 2; ++i) all.pass[i].part = part[i];
     e = launch_passes<T, false>(all, bh, s);
     if (e != hipSuccess) return e;
     JoinPasses j{};
-    for (int i = 0; i < 2; ++i) j.pass[i] = JoinPass{part[i], nullptr, 0, 0, nullptr, 0, 0, a.dk, a.dv};
+    for (int i = 0; i < 2; ++i) j.pass[i] = JoinPass{part[i], nullptr, 0, 0, a.dk, a.dv};
     join_from(&j.pass[0], state);
     join_from(&j.pass[1], dstate);
-    join_to(&j.pass[1], dstate0);
     e = launch_join(j, a, c, 2, s);
     if (e != hipSuccess) return e;
     from_parts(&of_q, part[0], a, c, true);
     from_parts(&of_k, part[1], a, c, true);
     from_parts(&of_v, part[1], a, c, false);
   }
+  all.run = c.segments;
   // All three in one launch, if that is best; but the gradient of k reads dstate, which that of v may write over.
   all.pass[0] = of_q;
   all.pass[1] = of_k;

@@ -160,3 +160,28 @@ def test_what_is_masked_may_hold_anything():
     x[..., 40] = float("inf")
     got = seq.rotate(x, None, f)
     assert torch.equal(got[..., :32], want[..., :32]) and torch.equal(got[..., 34:40], want[..., 34:40]) and torch.equal(got[..., 41:], want[..., 41:])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B,L,H,d", [(2, 300, 4, 64), (3, 1001, 6, 64), (8, 2000, 4, 128), (1, 4099, 2, 32)])
+def test_cut_sequences_with_and_without_states(B, L, H, d, dtype):
+    """Few rows, which are computed in segments: no first state, no last one, and the last in the first one's place."""
+    q, k, v, g, S, _ = attention_inputs(B, L, H, H, d, d, dtype)
+    lengths = torch.tensor([max(0, L - 277 * b * b) for b in range(B)], dtype=torch.int32, device="cuda")
+    zero = torch.zeros_like(S)
+    out, last = seq.linear_attention(q, k, v, g, None, lengths, scale=0.2)
+    check_attention(q, k, v, g, zero, lengths, 0.2, out, last)
+    out, last = seq.linear_attention(q, k, v, g, S, lengths, scale=0.2)
+    check_attention(q, k, v, g, S, lengths, 0.2, out, last)
+    alone, none = seq.linear_attention(q, k, v, g, S, lengths, scale=0.2, want_state=False)
+    assert none is None
+    check_attention(q, k, v, g, S, lengths, 0.2, alone, last)
+    T = S.clone()
+    over, same = seq.linear_attention(q, k, v, g, T, lengths, scale=0.2, out_state=T)
+    assert same is T
+    check_attention(q, k, v, g, S, lengths, 0.2, over, T)
+    dout, dS = normal(11, B, L, H, d, dtype=dtype), normal(12, *S.shape)
+    want = seq.linear_attention_backward(dout, q, k, v, g, S, dS, lengths, scale=0.2)
+    D = dS.clone()
+    for x, y in zip(seq.linear_attention_backward(dout, q, k, v, g, S, D, lengths, scale=0.2, dstate0=D), want):
+        assert torch.equal(x, y)
