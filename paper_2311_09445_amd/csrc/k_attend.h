@@ -372,6 +372,13 @@ __device__ __forceinline__ void store_row_counted(uint8_t* base, uint32_t offset
   }
 }
 
+// What is left of a state over tokens whose decays' logarithms add up to x: S + (e^x - 1) S where more than half is (the power itself,
+// rounded to 32 bits, would be off by the same 2^-25 in every chunk of a slow decay), e^x S where less is (the other form would be off
+// by 2^-25 of what there was).
+struct Keep { float factor; bool half; };
+__device__ __forceinline__ Keep keeps(float x) { return x > -0.6931472f ? Keep{expm1f(x), true} : Keep{expf(x), false}; }
+__device__ __forceinline__ float kept(float S, const Keep& k) { return k.half ? fmaf(S, k.factor, S) : S * k.factor; }
+
 // OUT: the outputs are wanted too (else only the state that the piece of the sequence brings, from zeros).
 template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY>
 __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 : 2) void k_attend(AttentionPasses all) {
@@ -501,7 +508,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
   // tile apart), to the chunk's tokens, from them, over the chunk.
   const float power = lane == 0 ? 1.0f : expf((float)lane * decay);
   f32x4 pair[2], into[2];
-  float outof[2], keep = 0.0f;
+  float outof[2];
+  Keep keep{0.0f, false};
   if (OUT) {
 #pragma unroll
     for (int d = 0; d < 2; ++d) {
@@ -523,8 +531,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
         const float w = c_state * __shfl(power, e < 0 ? 0 : e + lag);
         into[d][r] = e < 0 ? 0.0f : w;
       }
-    // S + (decay^n - 1) S: the power itself, rounded to 32 bits, would be off by the same 2^-25 in every chunk of a slow decay
-    keep = expm1f((float)n * decay);
+    keep = keeps((float)n * decay);
+    keep.half = __builtin_amdgcn_readfirstlane(keep.half);   // (the same in all lanes: a branch, not a choice for each element)
   };
   weights(kChunk);
 
@@ -601,10 +609,17 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
       const Scaled<T> zw(z[c], into[0], into[1]);
+      if (keep.half) {
 #pragma unroll
-      for (int a = 0; a < TX; ++a)
+        for (int a = 0; a < TX; ++a)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[c][a][r] = fmaf(S[c][a][r], keep, S[c][a][r]);
+          for (int r = 0; r < 4; ++r) S[c][a][r] = kept(S[c][a][r], Keep{keep.factor, true});
+      } else {
+#pragma unroll
+        for (int a = 0; a < TX; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) S[c][a][r] = kept(S[c][a][r], Keep{keep.factor, false});
+      }
       zw.add(y, S[c], exact);
     }
     if (!OUT) return;
@@ -720,7 +735,7 @@ __global__ __launch_bounds__(256) void k_join(JoinPasses all) {
       part[(size_t)(s0 + k) * per] = S;
       const uint32_t begin = (s0 + k) * all.segment;
       const uint32_t n = valid <= begin ? 0 : valid - begin < all.segment ? valid - begin : all.segment;
-      if (n) S = fmaf(S, expm1f((float)n * g), S) + brought[k];
+      if (n) S = kept(S, keeps((float)n * g)) + brought[k];
     }
   }
   part[(size_t)last * per] = S;

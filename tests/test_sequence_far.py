@@ -185,3 +185,19 @@ def test_cut_sequences_with_and_without_states(B, L, H, d, dtype):
     D = dS.clone()
     for x, y in zip(seq.linear_attention_backward(dout, q, k, v, g, S, D, lengths, scale=0.2, dstate0=D), want):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("L", [11, 32, 75, 1500])
+def test_states_that_decay_fast(L, dtype):
+    """With nothing added, a state is its decay^L: exact to 32 bits of what is left, however little."""
+    q, k, v, _, S, _ = attention_inputs(2, L, 5, 5, 64, 48, dtype)
+    g = torch.tensor([-1.0, -0.3, -0.02, -2.0 ** -9, -5.0], device="cuda")
+    k.zero_()
+    out, last = seq.linear_attention(q, k, v, g, S, scale=0.2)
+    check_attention(q, k, v, g, S, None, 0.2, out, last)
+    dout, dS = torch.zeros_like(v), normal(12, *S.shape)
+    got = seq.linear_attention_backward(dout, q, k, v, g, S, dS, scale=0.2)
+    want = oracle.attention_backward(dout, q, k, v, g, S, dS, None, 0.2)
+    A = oracle.attention_backward(*absolute(dout, q, k, v), g, *absolute(S, dS), None, 0.2)
+    within(got[3], want[3], state_bound(A[3], L), "dstate0")
