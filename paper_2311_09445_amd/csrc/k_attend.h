@@ -12,7 +12,9 @@
 // wave's two tiles are mixed likewise, so that a lane ends up with eight outputs in a row.
 //
 // A wave holds 16 NT columns of the state for all of dx in registers; the waves of a workgroup share the chunk's rows in LDS, and
-// each works out the products of pairs for itself (3 tiles; sharing them would cost a barrier).
+// each works out the products of pairs for itself (3 tiles; sharing them would cost a barrier).  A gradient's workgroup may hold
+// several heads that share a key and value, a team of waves each with rows of its own in LDS; what they bring to the shared output is
+// added up in LDS, in the heads' order, behind one more barrier.
 //
 // Rows lie in LDS in pieces of 16 bytes, piece p of row r at place p ^ turn(r), so that reads along rows and across them meet the
 // banks evenly without padding; memory can then be loaded straight into LDS, 64 pieces an instruction, several chunks ahead
@@ -379,18 +381,27 @@ struct Keep { float factor; bool half; };
 __device__ __forceinline__ Keep keeps(float x) { return x > -0.6931472f ? Keep{expm1f(x), true} : Keep{expf(x), false}; }
 __device__ __forceinline__ float kept(float S, const Keep& k) { return k.half ? fmaf(S, k.factor, S) : S * k.factor; }
 
-// OUT: the outputs are wanted too (else only the state that the piece of the sequence brings, from zeros).
+// Bytes of LDS: of a team's chunks, and of the outputs that teams add up.
 template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY>
-__global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 : 2) void k_attend(AttentionPasses all) {
+constexpr uint32_t team_bytes() { return ring<T, DX, 16 * NT * WAVES, OUT, WAY>() * chunk_bytes<T, DX, 16 * NT * WAVES, OUT>(); }
+template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY, int TEAMS>
+constexpr uint32_t lds_bytes() { return TEAMS * (team_bytes<T, DX, NT, WAVES, OUT, WAY>() + (TEAMS > 1 ? 2 * NT * WAVES * 1024 : 0)); }
+
+// OUT: the outputs are wanted too (else only the state that the piece of the sequence brings, from zeros).
+// TEAMS: heads of a workgroup, each a team of WAVES waves; a pass that is `summed` has one output for them.
+template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY, int TEAMS>
+__global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && OUT ? 1 : 2) void k_attend(AttentionPasses all) {
   constexpr int THREADS = 64 * WAVES, DZ = 16 * NT * WAVES, TX = DX / 16, KX = DX / 32;
   constexpr uint32_t BUFFER = chunk_bytes<T, DX, DZ, OUT>() / sizeof(bf16), RING = ring<T, DX, DZ, OUT, WAY>();
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
-  bf16* const lds = reinterpret_cast<bf16*>(lds_raw);
+  const uint32_t team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.y) : 0;
+  bf16* const lds = reinterpret_cast<bf16*>(lds_raw + team * team_bytes<T, DX, NT, WAVES, OUT, WAY>());
+  f32x4* const sums = reinterpret_cast<f32x4*>(lds_raw + TEAMS * team_bytes<T, DX, NT, WAVES, OUT, WAY>());
   // Workgroups go round the 8 dies by their number: the passes over the same rows sit on one die, one behind the other.
   const uint32_t which = blockIdx.x / 8 % all.count, item = blockIdx.x / (8 * all.count) * 8 + blockIdx.x % 8;
   if (item >= all.items) return;
   const AttentionPass& p = all.pass[which];
-  const uint32_t slice = item % all.slices, seg = item / all.slices % all.run, bh = item / all.slices / all.run;
+  const uint32_t slice = item % all.slices, seg = item / all.slices % all.run, bh = item / all.slices / all.run * TEAMS + team;
   const uint32_t h = bh % p.H, b = bh / p.H, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // (what the loop needs of the arguments is taken out of them here: behind its barriers they would be loaded again)
@@ -398,6 +409,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
   const float decay = p.log_decay[h], c_state = p.c_state;
   const bool back = p.back != 0, out_f32 = p.out_f32 != 0;
   const bool last = OUT && p.to && seg + 1 == all.segments, exact = p.exact && (last || !OUT);   // (its state is an output)
+  const bool summed = TEAMS > 1 && p.summed;
   const int lag = back ? 1 : 0;
   const uint32_t valid = valid_tokens(p.lengths, b, L), start = seg * segment;
   const uint32_t end = valid < start ? start : valid - start < segment ? valid : start + segment;
@@ -623,6 +635,25 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
       zw.add(y, S[c], exact);
     }
     if (!OUT) return;
+    if (TEAMS > 1 && summed) {   // (the next chunk's barrier is between these reads and its sums)
+      f32x4* const mine = sums + wave * 64 + lane;
+      constexpr uint32_t TILE = WAVES * 64, TEAM = 2 * NT * TILE;
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) mine[team * TEAM + (2 * c + d) * TILE] = acc[c][d];
+      __syncthreads();
+      if (team >= 2) return;   // the first two teams add up and store a tile of tokens each
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          if (team != (uint32_t)d) continue;
+          acc[c][d] = mine[(2 * c + d) * TILE];
+#pragma unroll
+          for (int other = 1; other < TEAMS; ++other) acc[c][d] += mine[other * TEAM + (2 * c + d) * TILE];
+        }
+    }
     // out: four columns of a token in each tile of a lane, eight side by side in two
     const uint32_t j = col + (NT == 2 ? 8 : 4) * g;
     uint8_t* const base = oh + (back ? (int64_t)valid - (int64_t)first - (int64_t)kChunk : (int64_t)first) * out_step;
@@ -641,7 +672,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
       for (int d = 0; d < 2; ++d) {
         const uint32_t row = 16 * d + m;
         uint8_t* const at = base + ((back ? kChunk - 1 - row : row) * (uint32_t)out_step + j * out_size);
-        if (row >= n || j >= dz) continue;
+        if (row >= n || j >= dz || (summed && team != (uint32_t)d)) continue;
         if (out_f32) store_row<float, NT>(at, acc, d, dz - j);
         else store_row<T, NT>(at, acc, d, dz - j);
       }
@@ -654,7 +685,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const uint32_t e = col + state_column<NT>(c, 4 * g + r);
-            if (row >= n || e >= dz) continue;
+            if (row >= n || e >= dz || (summed && team != (uint32_t)d)) continue;
             if (out_f32) row_to<float>(p.out, b, t, h)[e] = acc[c][d][r];
             else row_to<T>(p.out, b, t, h)[e] = (T)acc[c][d][r];
           }
@@ -695,7 +726,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 4 && DX == 128 && OUT ? 1 
           if (dx == DX || state_row(a, 4 * g + r) < dx) at[state_row(a, r) * dz] = S[c][a][r];
     }
   }
-  if (!OUT || valid >= L) return;
+  if (!OUT || valid >= L || (summed && team > 0)) return;
   // tokens behind the valid ones: zeros
   const uint32_t width = dz - col0 < (uint32_t)DZ ? dz - col0 : DZ, from = start > valid ? start : valid;
   const uint32_t until = L - start < segment ? L : start + segment;

@@ -20,6 +20,7 @@ struct AttentionPass {
   uint32_t L, H, dx, dz;
   uint32_t back;                 // against time (and lag 1)
   uint32_t out_f32;              // out is fp32 whatever the rows' type
+  uint32_t summed;               // out is the sum over a workgroup's heads
   uint32_t exact;                // the state itself is an output (of this pass or behind it)
   float c_in, c_state, c_out;
   const float* log_decay;
@@ -34,7 +35,7 @@ struct AttentionPass {
 };
 struct AttentionPasses {
   AttentionPass pass[3];
-  uint32_t count, items, slices, segments, run, segment;   // items: workgroups of a pass; run: segments taken; segment: tokens
+  uint32_t count, teams, items, slices, segments, run, segment;   // items: workgroups of a pass; run: segments taken; segment: tokens
 };
 
 struct JoinPass {
@@ -101,9 +102,9 @@ SeqRows rows(const per_seq_rows& r, uint32_t dtype, uint32_t share) {
   const bool wide = near && (reinterpret_cast<uintptr_t>(r.d) & 15) == 0 && r.batch % per16 == 0 && r.token % per16 == 0 && r.head % per16 == 0;
   return SeqRows{r.d, r.batch, r.token, r.head, share, wide ? 1u : 0u, near ? 1u : 0u};
 }
-// Packed rows [B][L][H][d] in fp32.
-SeqRows packed(float* d, const AttentionSizes& a, uint32_t width) {
-  return SeqRows{d, (int64_t)a.L * a.H * width, (int64_t)a.H * width, (int64_t)width, 1, width % 4 == 0, (uint64_t)a.H * width < (1 << 24)};
+// Packed rows [B][L][heads][d] in fp32.
+SeqRows packed(float* d, uint32_t L, uint32_t heads, uint32_t width, uint32_t share) {
+  return SeqRows{d, (int64_t)L * heads * width, (int64_t)heads * width, (int64_t)width, share, width % 4 == 0, (uint64_t)heads * width < (1 << 24)};
 }
 
 AttentionPass make_pass(const AttentionSizes& a, bool back, uint32_t dx, uint32_t dz) {
@@ -137,22 +138,41 @@ void to_states(AttentionPass* p, const per_seq_states* s) {
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
+// Rows in fp32 of the heads of workgroups, where several of these share one.
+size_t fold_bytes(const AttentionSizes& a, uint32_t teams, uint32_t width) {
+  const uint32_t from = a.H / teams;
+  return from == a.G ? 0 : align256((size_t)a.B * a.L * from * width * sizeof(float));
+}
+
 // How a sequence is cut.  A workgroup takes its tokens one chunk behind the other, so what cuts the time of few sequences is
 // workgroups: the sequence in segments, each from the state that those before it bring.  That costs another pass over keys and values
 // for those states (the last segment's is not needed), a state in memory per segment, and two launches.  A gradient of unlike
 // widths is two launches, or one as wide as the widest.  The fewest microseconds by these measured figures are taken:
 //   a chunk of 64 x 64 takes 0.85 (fp32: 1.9), of 128 x 64 1.2 (2.8), of 128 x 128 1.9; two workgroups on a compute unit 1.45 times
 //   that, more take turns; the pass for the states 0.55 of that for outputs (0.42 where it serves a gradient's); states move at 4 TB/s.
+// Heads that share a key and value bring gradients of their own, in fp32, which are added up behind; in bfloat16, up to 64 wide, a
+// gradient's workgroup may take two or four of them, a team of waves each, and add up in LDS.  That spares most of this memory, but
+// keeps a compute unit busy longer: a chunk takes 1.6 with two teams (2.4 for two workgroups on a compute unit, 1.2 for each of more)
+// and 2.6 with four (each; 3.1 where none waits for another, since then sequences of unlike lengths do not even out), and their starts
+// are one and two chunks longer.  The memory moves at 8 TB/s up to 128 MB, at 4 above.
+// Measured, teams of 1, 2, 4 (64 x 64, 8 heads): that share 2, 32 x 512 tokens 51, 53, 46 us, 64 x 512 108, 81, 86, 256 x 512 441, 313,
+// 262, 48 x 80 28, 30, 33, 8 x 1024 41, 61, 80; that share 4 64 x 512 111, 65, 16 x 80 17, 14, 8 x 512 27, 31.
 // Measured, whole against cut: 64 rows of 1024 tokens (64 x 64) 33 us and 25 in four; 4 rows of 1024 31 and 17 in sixteen; 4 rows of
 // 512 18 and 17; the gradient of 64 rows of 1024 34 and 37 in four; of 32 rows of 16384 (128 x 128) 388 in 5, 423 in 8, 403 in 10.
 struct Cut {
   uint32_t segments, segment;
   bool one;   // a gradient's passes in one launch
+  uint32_t teams;
 };
 uint32_t kernel_width(uint32_t d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 // Half of the columns to a workgroup: see launch_dz.
 bool halved(uint32_t dtype, uint32_t dz, uint64_t workgroups) { return dz > 64 && (dtype == PER_SEQ_F32 || workgroups <= 256); }
-float launch_us(uint32_t dtype, uint64_t workgroups, uint32_t dx, uint32_t dz, uint32_t chunks) {
+float launch_us(uint32_t dtype, uint64_t workgroups, uint32_t dx, uint32_t dz, uint32_t chunks, uint32_t teams = 1) {
+  if (teams > 1) {
+    const float area = (float)(dx * dz) / 4096.0f, each = (float)((workgroups / teams + 255) / 256);
+    return teams == 2 ? (0.8f + 0.8f * area) * (float)(chunks + 1) * (each <= 1 ? 1.0f : each <= 2 ? 1.5f : 0.75f * each)
+                      : (0.7f + 1.9f * area) * (float)(chunks + 2) * (each <= 1 ? 1.2f : each);
+  }
   const bool half = halved(dtype, dz, workgroups);
   const float area = (float)(dx * (half ? dz / 2 : dz)) / 4096.0f, each = (float)((workgroups * (half ? 2 : 1) + 255) / 256);
   return (dtype == PER_SEQ_F32 ? 0.97f + 0.93f * area : 0.5f + 0.35f * area) * (float)chunks * (each <= 1 ? 1.0f : each <= 2 ? 1.45f : 0.25f + 0.8f * each);
@@ -160,24 +180,32 @@ float launch_us(uint32_t dtype, uint64_t workgroups, uint32_t dx, uint32_t dz, u
 Cut cut(const AttentionSizes& a, bool backward) {
   const uint64_t rows = (uint64_t)a.B * a.H;
   const uint32_t wk = kernel_width(a.dk), wv = kernel_width(a.dv), widest = wk > wv ? wk : wv, most = a.L / 64 < 64 ? a.L / 64 : 64;
+  const uint32_t share = a.G ? a.H / a.G : 1;
+  const uint32_t teams = !backward || a.dtype != PER_SEQ_BF16 || widest > 64 ? 1 : share % 4 == 0 ? 4 : share % 2 == 0 ? 2 : 1;
   float best = 0.0f;
-  Cut c{1, a.L ? a.L : 1, true};
+  Cut c{1, a.L ? a.L : 1, true, 1};
   for (uint32_t s = 1; rows && a.L && (s == 1 || s <= most); ++s) {
     const uint64_t n = rows * s;
     const uint32_t segment = ((a.L + s - 1) / s + kChunk - 1) / kChunk * kChunk, chunks = segment / kChunk;
-    bool one = true;
-    float us = backward ? launch_us(a.dtype, 3 * n, widest, widest, chunks) : launch_us(a.dtype, n, wk, wv, chunks);
-    if (backward && wk != wv) {
-      const float apart = launch_us(a.dtype, 2 * n, wv, wk, chunks) + launch_us(a.dtype, n, wk, wv, chunks) + 3.0f;
-      one = us <= apart;
-      if (!one) us = apart;
-    }
-    if (s > 1)
-      us += (backward ? 0.42f : 0.55f) * launch_us(a.dtype, (backward ? 2 : 1) * (n - rows), wk, wv, chunks) + 10.0f +
-            4.0f * a.dk * a.dv * (float)(n * (backward ? 8 : 4)) / 4e6f;
-    if (s == 1 || us < best) {
-      best = us;
-      c = s == 1 ? Cut{1, a.L, one} : Cut{(a.L + segment - 1) / segment, segment, one};
+    for (uint32_t t = 1; t <= teams; t *= 2) {
+      bool one = true;
+      float us = backward ? launch_us(a.dtype, 3 * n, widest, widest, chunks, t) : launch_us(a.dtype, n, wk, wv, chunks);
+      if (backward && wk != wv) {
+        const float apart = launch_us(a.dtype, 2 * n, wv, wk, chunks, t) + launch_us(a.dtype, n, wk, wv, chunks, t) + 3.0f;
+        one = us <= apart;
+        if (!one) us = apart;
+      }
+      if (s > 1)
+        us += (backward ? 0.42f : 0.55f) * launch_us(a.dtype, (backward ? 2 : 1) * (n - rows), wk, wv, chunks) + 10.0f +
+              4.0f * a.dk * a.dv * (float)(n * (backward ? 8 : 4)) / 4e6f;
+      if (backward && share > t) {
+        const float bytes = (float)(fold_bytes(a, t, a.dk) + fold_bytes(a, t, a.dv));
+        us += 4.0f + bytes / (bytes <= 128e6f ? 8e6f : 4e6f);
+      }
+      if ((s == 1 && t == 1) || us < best) {
+        best = us;
+        c = s == 1 ? Cut{1, a.L, one, t} : Cut{(a.L + segment - 1) / segment, segment, one, t};
+      }
     }
   }
   return c;
@@ -185,13 +213,11 @@ Cut cut(const AttentionSizes& a, bool backward) {
 size_t part_bytes(const AttentionSizes& a, const Cut& c) {
   return c.segments < 2 ? 0 : align256((size_t)a.B * a.H * c.segments * a.dk * a.dv * sizeof(float));
 }
-size_t fold_bytes(const AttentionSizes& a, uint32_t width) { return a.H == a.G ? 0 : align256((size_t)a.B * a.L * a.H * width * sizeof(float)); }
 
-template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY>
+template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY, int TEAMS = 1>
 hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
-  constexpr int DZ = 16 * NT * WAVES;
-  constexpr uint32_t lds = ring<T, DX, DZ, OUT, WAY>() * chunk_bytes<T, DX, DZ, OUT>();
-  auto* kernel = k_attend<T, DX, NT, WAVES, OUT, WAY>;
+  constexpr uint32_t lds = lds_bytes<T, DX, NT, WAVES, OUT, WAY, TEAMS>();
+  auto* kernel = k_attend<T, DX, NT, WAVES, OUT, WAY, TEAMS>;
   if constexpr (lds > 64 * 1024) {   // granted once per kernel and device
     static std::atomic<uint64_t> granted{0};
     int device = 0;
@@ -204,7 +230,7 @@ hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
       granted.fetch_or(bit, std::memory_order_relaxed);
     }
   }
-  kernel<<<(p.items + 7) / 8 * 8 * p.count, 64 * WAVES, lds, s>>>(p);
+  kernel<<<(p.items + 7) / 8 * 8 * p.count, dim3(64 * WAVES, TEAMS), lds, s>>>(p);
   return hipGetLastError();
 }
 // In bfloat16 straight into LDS where rows are made up of pieces of 16 bytes; through registers in pieces where they hold one.
@@ -222,12 +248,24 @@ hipError_t launch_way(const AttentionPasses& p, hipStream_t s) {
   }
   return pieces ? launch_as<T, DX, NT, WAVES, OUT, PIECES>(p, s) : launch_as<T, DX, NT, WAVES, OUT, ELEMENTS>(p, s);
 }
+// Teams of two waves: more columns to a wave, so that the waves read less LDS (of four waves each, 64 x 64, 128 x 512 tokens with 8
+// heads that share 2: 166 us, of two 139).
+template <int DX, int NT>
+hipError_t launch_teams(const AttentionPasses& p, hipStream_t s) {
+  bool pieces = true;
+  for (uint32_t i = 0; i < p.count; ++i) pieces = pieces && p.pass[i].out.near && p.pass[i].dx >= 8 && p.pass[i].dz >= 8;
+  if (p.teams == 4) return pieces ? launch_as<bf16, DX, NT, 2, true, PIECES, 4>(p, s) : launch_as<bf16, DX, NT, 2, true, ELEMENTS, 4>(p, s);
+  return pieces ? launch_as<bf16, DX, NT, 2, true, PIECES, 2>(p, s) : launch_as<bf16, DX, NT, 2, true, ELEMENTS, 2>(p, s);
+}
 template <typename T, int DX, bool OUT>
 hipError_t launch_dz(AttentionPasses& p, uint32_t rows, hipStream_t s) {
   uint32_t dz = 0;
   for (uint32_t i = 0; i < p.count; ++i) dz = dz < p.pass[i].dz ? p.pass[i].dz : dz;
   p.slices = 1;
-  p.items = rows * p.run;
+  p.items = rows / p.teams * p.run;
+  if constexpr (sizeof(T) == 2 && DX <= 64 && OUT) {
+    if (p.teams > 1) return dz <= 32 ? launch_teams<DX, 1>(p, s) : launch_teams<DX, 2>(p, s);
+  }
   if (dz <= 32) return launch_way<T, DX, 1, 2, OUT>(p, s);
   if (dz <= 64) return launch_way<T, DX, 1, 4, OUT>(p, s);
   // Wider states: two tiles of columns to a wave, or half of the columns to a workgroup where there are few (each then reads x and y:
@@ -283,7 +321,7 @@ hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
   const Cut c = cut(a, false);
   AttentionPasses all{};
-  all.count = 1;
+  all.count = all.teams = 1;
   all.segments = c.segments;
   all.segment = c.segment;
   AttentionPass& p = all.pass[0];
@@ -320,21 +358,23 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
                     const per_seq_rows& dk, const per_seq_rows& dv, const per_seq_states* dstate0, void* work, hipStream_t s) {
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
   const Cut c = cut(a, true);
+  const uint32_t team = c.teams, left = share / team;   // left: to be added up behind
   const SeqRows Q = rows(q, a.dtype, 1), K = rows(k, a.dtype, share), V = rows(v, a.dtype, share), D = rows(dout, a.dtype, 1);
   uint8_t* at = static_cast<uint8_t*>(work);
   float* part[2];   // of the states, of their gradients
   for (int i = 0; i < 2; ++i, at += part_bytes(a, c)) part[i] = reinterpret_cast<float*>(at);
   float* const fold_k = reinterpret_cast<float*>(at);
-  float* const fold_v = reinterpret_cast<float*>(at + fold_bytes(a, a.dk));
+  float* const fold_v = reinterpret_cast<float*>(at + fold_bytes(a, team, a.dk));
 
   AttentionPass of_q = make_pass(a, false, a.dv, a.dk), of_k = make_pass(a, true, a.dv, a.dk), of_v = make_pass(a, true, a.dk, a.dv);
   of_q.x = D; of_q.y = V; of_q.z = K;
   of_k.x = V; of_k.y = D; of_k.z = Q;
   of_v.x = K; of_v.y = Q; of_v.z = D;
   of_q.out = rows(dq, a.dtype, 1);
-  of_k.out = share == 1 ? rows(dk, a.dtype, 1) : packed(fold_k, a, a.dk);
-  of_v.out = share == 1 ? rows(dv, a.dtype, 1) : packed(fold_v, a, a.dv);
-  of_k.out_f32 = of_v.out_f32 = share > 1;
+  of_k.out = left == 1 ? rows(dk, a.dtype, team) : packed(fold_k, a.L, a.H / team, a.dk, team);
+  of_v.out = left == 1 ? rows(dv, a.dtype, team) : packed(fold_v, a.L, a.H / team, a.dv, team);
+  of_k.out_f32 = of_v.out_f32 = left > 1;
+  of_k.summed = of_v.summed = team > 1;
   AttentionPasses all{};
   all.segments = c.segments;
   all.segment = c.segment;
@@ -347,6 +387,7 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
     from_states(&of_v, dstate, a.dv, false);
   } else {
     all.run = c.segments - 1;
+    all.teams = 1;
     all.count = 2;
     all.pass[0] = make_pass(a, false, a.dk, a.dv);
     all.pass[0].y = K;
@@ -366,6 +407,7 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
     from_parts(&of_v, part[1], a, c, false);
   }
   all.run = c.segments;
+  all.teams = team;
   // All three in one launch, if that is best; but the gradient of k reads dstate, which that of v may write over.
   all.pass[0] = of_q;
   all.pass[1] = of_k;
@@ -378,13 +420,13 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
     all.pass[0] = of_v;
     e = launch_passes<T, true>(all, bh, s);
   }
-  if (e != hipSuccess || share == 1) return e;
+  if (e != hipSuccess || left == 1) return e;
   Folds f{};
   f.fold[0] = Fold{fold_k, rows(dk, a.dtype, 1), a.dk};
   f.fold[1] = Fold{fold_v, rows(dv, a.dtype, 1), a.dv};
   f.L = a.L;
   f.G = a.G;
-  f.share = share;
+  f.share = left;
   f.rows = (uint64_t)a.B * a.L * a.G;
   if (!f.rows) return e;
   const bool wide = a.dk % 4 == 0 && a.dv % 4 == 0 && f.fold[0].to.wide && f.fold[1].to.wide;
@@ -401,7 +443,10 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
 
 size_t attention_work_bytes(const AttentionSizes& a, bool backward) {
   const Cut c = cut(a, backward);
-  return backward ? 2 * part_bytes(a, c) + fold_bytes(a, a.dk) + fold_bytes(a, a.dv) : part_bytes(a, c);
+  if (!backward) return part_bytes(a, c);
+  const size_t need = 2 * part_bytes(a, c) + fold_bytes(a, c.teams, a.dk) + fold_bytes(a, c.teams, a.dv);
+  // (a gradient of shared heads always has a workspace: what a caller passes does not depend on who adds up)
+  return need || a.H == a.G || !a.B || !a.L ? need : 256;
 }
 
 hipError_t launch_attention(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,

@@ -201,3 +201,49 @@ def test_states_that_decay_fast(L, dtype):
     want = oracle.attention_backward(dout, q, k, v, g, S, dS, None, 0.2)
     A = oracle.attention_backward(*absolute(dout, q, k, v), g, *absolute(S, dS), None, 0.2)
     within(got[3], want[3], state_bound(A[3], L), "dstate0")
+
+
+@pytest.mark.parametrize("B,L,H,G,dk,dv", [
+    (6, 45, 4, 2, 40, 64), (3, 1, 4, 2, 64, 64), (4, 50, 4, 2, 5, 7), (20, 70, 12, 2, 33, 17), (2, 2000, 4, 2, 64, 64),
+    (40, 80, 8, 2, 64, 64), (40, 96, 8, 2, 32, 48), (40, 96, 8, 2, 5, 7), (2, 2000, 4, 1, 32, 32), (32, 96, 8, 1, 64, 64)])
+def test_gradients_of_shared_heads(B, L, H, G, dk, dv):
+    """Sums over the heads that share a key and value, within a workgroup and behind it: dense rows, and rows in larger buffers."""
+    q, k, v, g, S, lengths = attention_inputs(B, L, H, G, dk, dv, BF16, ragged=True)
+    dout, dS = normal(11, B, L, H, dv, dtype=BF16), normal(12, B, H, dk, dv)
+    want = oracle.attention_backward(dout, q, k, v, g, S, dS, lengths.cpu(), 0.3)
+    A = oracle.attention_backward(*absolute(dout, q, k, v), g, *absolute(S, dS), lengths.cpu(), 0.3)
+
+    def check(got, what):
+        for name, x, w, a, width in zip(("dq", "dk", "dv"), got, want, A, (dv, dv, dk)):
+            within(x, w, out_bound(BF16, w, a, width, L), f"{name}, {what}")
+        within(got[3], want[3], state_bound(A[3], L), f"dstate0, {what}")
+
+    got = seq.linear_attention_backward(dout, q, k, v, g, S, dS, lengths, scale=0.3)
+    check(got, "dense")
+    for x, y in zip(seq.linear_attention_backward(dout, q, k, v, g, S, dS, lengths, scale=0.3), got):
+        assert torch.equal(x, y)
+    views, rooms = [], []
+    for t in got[:3]:
+        room = torch.full((B, L + 2, t.shape[2] + 1, t.shape[3] + 3), 7.0, dtype=BF16, device="cuda")
+        views.append(room[:, 1:L + 1, 1:, 1:t.shape[3] + 1])
+        rooms.append(room)
+    check(seq.linear_attention_backward(dout, q, k, v, g, S, dS, lengths, scale=0.3, dq=views[0], dk=views[1], dv=views[2]), "views")
+    for room, view in zip(rooms, views):
+        view.fill_(7.0)
+        assert bool((room == 7.0).all())   # nothing written around them
+
+
+@pytest.mark.parametrize("B,L,H,G,dk,dv", [(192, 384, 4, 1, 64, 64), (128, 512, 8, 1, 64, 40), (170, 480, 8, 2, 64, 64)])
+def test_gradients_of_shared_heads_in_full_batches(B, L, H, G, dk, dv):
+    """Batches that fill the machine several times over: some of their sequences against the definition."""
+    q, k, v, g, S, _ = attention_inputs(B, L, H, G, dk, dv, BF16)
+    dout, dS = normal(11, B, L, H, dv, dtype=BF16), normal(12, B, H, dk, dv)
+    lengths = torch.tensor([L - (37 * b) % (L + 1) if b % 3 else L for b in range(B)], dtype=torch.int32, device="cuda")
+    got = seq.linear_attention_backward(dout, q, k, v, g, S, dS, lengths, scale=0.3)
+    for b in (0, 1, B // 2, B - 1):
+        few = [t[b:b + 1] for t in (dout, q, k, v)]
+        want = oracle.attention_backward(*few, g, S[b:b + 1], dS[b:b + 1], lengths[b:b + 1].cpu(), 0.3)
+        A = oracle.attention_backward(*absolute(*few), g, *absolute(S[b:b + 1], dS[b:b + 1]), lengths[b:b + 1].cpu(), 0.3)
+        for name, x, w, a, width in zip(("dq", "dk", "dv"), got, want, A, (dv, dv, dk)):
+            within(x[b:b + 1], w, out_bound(BF16, w, a, width, L), f"{name}, sequence {b}")
+        within(got[3][b:b + 1], want[3], state_bound(A[3], L), f"dstate0, sequence {b}")

@@ -136,3 +136,11 @@ def test_calls_without_their_tensors_raise():
             call(*([None] * n))
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+@pytest.mark.parametrize("sizes", [dict(heads=0, kv_heads=0), dict(batch=0), dict(length=0)])
+def test_empty_sizes_need_no_workspace(sizes, backward):
+    c, n = attention(**sizes), C.c_size_t(7)
+    assert per._lib().per_linear_attention_workspace(C.byref(c), backward, C.byref(n)) == 0
+    assert n.value == 0
