@@ -413,13 +413,6 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
   const int lag = back ? 1 : 0;
   const uint32_t valid = valid_tokens(p.lengths, b, L), start = seg * segment;
   const uint32_t end = valid < start ? start : valid - start < segment ? valid : start + segment;
-  uint32_t begin = start;
-  if (!OUT && decay < 0.0f && end > start) {
-    // Tokens so far before the segment's end that their weight, decay^e, is zero in 32 bits (exp below -104) bring nothing to its state.
-    const float reach = 104.0f / -decay + 2.0f;
-    const uint32_t n = end - start;
-    if (reach < (float)n) begin += (n - (uint32_t)reach) / kChunk * kChunk;
-  }
   const uint32_t col0 = slice * DZ, col = col0 + wave * 16 * NT;   // first z column of the workgroup, of the wave
   if (col0 >= dz) return;   // (a pass narrower than the launch's widest)
 
@@ -473,7 +466,7 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
   Fill fill[WAY == DIRECT ? MINE : 1];
   const bool whole = dx == DX && dz - col0 >= DZ;   // no piece lies behind a width
   const bool ends = dx % (16 / sizeof(T)) || dz % (16 / sizeof(T));
-  const int64_t token0 = back ? (int64_t)valid - (int64_t)begin - (int64_t)kChunk : (int64_t)begin;   // lowest of the first chunk
+  const int64_t token0 = back ? (int64_t)valid - (int64_t)start - (int64_t)kChunk : (int64_t)start;   // lowest of the first chunk
   if (WAY == DIRECT) {
 #pragma unroll
     for (uint32_t k = 0; k < MINE; ++k) {
@@ -560,7 +553,7 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
       // whole, and the outputs of the last RING - 1, two rows each.  That many may be left; towards the end none.
       constexpr int LOADS = (int)((RING - 2) * (FILLS / WAVES)), STORES = OUT ? 2 * (int)(RING - 1) : 0;
       if (end - first < (RING - 1) * kChunk) arrive<0>();
-      else if (!OUT || !stores || first - begin < (RING - 1) * kChunk) arrive<LOADS>();
+      else if (!OUT || !stores || first - start < (RING - 1) * kChunk) arrive<LOADS>();
       else if (NT == 2 && out_f32) arrive<LOADS + 2 * STORES>();
       else arrive<LOADS + STORES>();
       // (this barrier: all are through with the chunk before, whose place the next one takes)
@@ -696,20 +689,20 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
   if (WAY == DIRECT) {
 #pragma unroll
     for (uint32_t i = 0; i < AHEAD; ++i)
-      if (begin + i * kChunk < end) fetch(begin + i * kChunk, i, staged[0]);
-    for (uint32_t first = begin, slot = 0; first < end; first += kChunk, slot = slot + 1 == RING ? 0 : slot + 1) chunk(first, slot, staged[0]);
+      if (start + i * kChunk < end) fetch(start + i * kChunk, i, staged[0]);
+    for (uint32_t first = start, slot = 0; first < end; first += kChunk, slot = slot + 1 == RING ? 0 : slot + 1) chunk(first, slot, staged[0]);
   } else if (WAY == PIECES) {
-    if (begin < end) {
-      fetch(begin, 0, staged[0]);
-      fetch(begin + kChunk, 0, staged[1]);
+    if (start < end) {
+      fetch(start, 0, staged[0]);
+      fetch(start + kChunk, 0, staged[1]);
     }
-    for (uint32_t first = begin; first < end; first += 2 * kChunk) {
+    for (uint32_t first = start; first < end; first += 2 * kChunk) {
       chunk(first, 0, staged[0]);
       if (first + kChunk < end) chunk(first + kChunk, 1, staged[1]);
     }
   } else {
-    fetch(begin, 0, staged[0]);
-    for (uint32_t first = begin, slot = 0; first < end; first += kChunk, slot ^= 1) chunk(first, slot, staged[0]);
+    fetch(start, 0, staged[0]);
+    for (uint32_t first = start, slot = 0; first < end; first += kChunk, slot ^= 1) chunk(first, slot, staged[0]);
   }
 
   if (last || !OUT) {
