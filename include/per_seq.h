@@ -109,8 +109,8 @@ typedef struct per_attention_config {
  *   d_lengths   : [batch] valid tokens of each sequence (values outside 0..length are taken as the nearest of these), or
  *                 NULL: all.  Tokens behind them are not read; their outputs are zeros.
  *   out_state   : S behind the last valid token, or NULL.  It may be state.
- * A value among the valid tokens that is not finite makes all outputs and states that depend on it, and the outputs of up
- * to 31 tokens before it, not finite. */
+ * A value among the valid tokens, or of the state, that is not finite makes all outputs and states that depend on it not
+ * finite (those of tokens before it do not). */
 int per_linear_attention_workspace(const per_attention_config* c, int backward, size_t* bytes);
 int per_linear_attention(const per_attention_config* c, const per_seq_rows* q, const per_seq_rows* k, const per_seq_rows* v,
                          const float* d_log_decay, const int32_t* d_lengths, const per_seq_states* state,
@@ -118,7 +118,7 @@ int per_linear_attention(const per_attention_config* c, const per_seq_rows* q, c
 
 /* Its gradient, the decays being constants: from dout (of out) and dstate (of out_state; NULL: zeros) to dq, dk, dv and
  * dstate0 (of state; NULL where not wanted).  Gradients of keys and values that several heads share are sums in a fixed
- * order.  dstate0 may be dstate, and not state. */
+ * order.  dstate0 may be dstate, and not state.  Of values that are not finite the same holds as above. */
 int per_linear_attention_backward(const per_attention_config* c, const per_seq_rows* dout, const per_seq_rows* q,
                                   const per_seq_rows* k, const per_seq_rows* v, const float* d_log_decay,
                                   const int32_t* d_lengths, const per_seq_states* state, const per_seq_states* dstate,

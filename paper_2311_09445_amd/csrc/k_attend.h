@@ -542,6 +542,7 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
   weights(kChunk);
 
   const bool stores = col < dz;           // the wave has outputs to store
+  float worst = 0.0f;                     // not a number: one of the wave's outputs was none
   // One chunk: its rows into LDS, or in LDS, and those of a later one asked for; then its products.
   constexpr uint32_t AHEAD = WAY == DIRECT ? RING - 1 : WAY == PIECES ? 2 : 1;   // chunks asked for before the one at hand
   auto chunk = [&](uint32_t first, uint32_t slot, Rows& rows) __attribute__((always_inline)) {
@@ -647,6 +648,12 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
           for (int other = 1; other < TEAMS; ++other) acc[c][d] += mine[other * TEAM + (2 * c + d) * TILE];
         }
     }
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) worst = __builtin_elementwise_maximum(worst, acc[c][d][r]);
     // out: four columns of a token in each tile of a lane, eight side by side in two
     const uint32_t j = col + (NT == 2 ? 8 : 4) * g;
     uint8_t* const base = oh + (back ? (int64_t)valid - (int64_t)first - (int64_t)kChunk : (int64_t)first) * out_step;
@@ -686,6 +693,75 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
     }
   };
 
+  // The recurrence itself, token by token, over what the chunks have computed: for pieces of a sequence with values that are not
+  // finite.  The product with Z takes each token of a chunk to all of them, with weight zero to those before it, and zero times such a
+  // value is not zero.  That shows as outputs that are not numbers, which a chunk takes a maximum of (1 % of its time; looking at Z
+  // before the product instead held up each chunk by up to 0.1 us).
+  auto recur = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the stores that the compiler does not see)
+#pragma unroll
+    for (int a = 0; a < TX; ++a)
+#pragma unroll
+      for (int c = 0; c < NT; ++c) S[c][a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (p.in) load(p.in + (int64_t)b * p.in_batch + (int64_t)h * p.in_head + (int64_t)seg * p.in_segment, S);
+    const Keep once = keeps(decay);
+    float* const shared = reinterpret_cast<float*>(sums);
+    for (uint32_t i = start; i < end; ++i) {
+      const uint32_t t = back ? valid - 1 - i : i;
+      const T *xr = xh + (int64_t)t * p.x.token, *yr = yh + (int64_t)t * p.y.token, *zr = zh + (int64_t)t * p.z.token;
+      float zc[NT], sum[NT];
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        const uint32_t j = col + state_column<NT>(c, m);
+        zc[c] = j < dz ? c_state * (float)zr[j] : 0.0f;
+        sum[c] = 0.0f;
+      }
+#pragma unroll
+      for (int a = 0; a < TX; ++a) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t row = state_row(a, 4 * g + r);
+          if (row >= dx) continue;
+          const float xv = (float)xr[row], yv = (float)yr[row];
+#pragma unroll
+          for (int c = 0; c < NT; ++c) {   // (against time what a token adds is decayed with the rest, behind its output)
+            const float now = fmaf(yv, zc[c], back ? S[c][a][r] : kept(S[c][a][r], once));
+            sum[c] = fmaf(xv, now, sum[c]);
+            S[c][a][r] = back ? kept(now, once) : now;
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        sum[c] += __shfl_xor(sum[c], 16);
+        sum[c] = p.c_out * (sum[c] + __shfl_xor(sum[c], 32));
+      }
+      const uint32_t place = wave * 16 * NT;
+      if (TEAMS > 1 && summed) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+          if (g == 0) shared[team * DZ + place + state_column<NT>(c, m)] = sum[c];
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+          sum[c] = shared[place + state_column<NT>(c, m)];
+#pragma unroll
+          for (int other = 1; other < TEAMS; ++other) sum[c] += shared[other * DZ + place + state_column<NT>(c, m)];
+        }
+        __syncthreads();
+        if (team > 0) continue;
+      }
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        const uint32_t j = col + state_column<NT>(c, m);
+        if (g != 0 || j >= dz) continue;
+        if (out_f32) row_to<float>(p.out, b, t, h)[j] = sum[c];
+        else row_to<T>(p.out, b, t, h)[j] = (T)sum[c];
+      }
+    }
+  };
+
   if (WAY == DIRECT) {
 #pragma unroll
     for (uint32_t i = 0; i < AHEAD; ++i)
@@ -705,6 +781,20 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
     for (uint32_t first = start, slot = 0; first < end; first += kChunk, slot ^= 1) chunk(first, slot, staged[0]);
   }
 
+  if (OUT) {
+    bool again = __any(worst != worst);
+    if (TEAMS > 1 && summed) {   // (the teams' outputs are one: all or none)
+      uint32_t* const seen = reinterpret_cast<uint32_t*>(sums);
+      arrive<0>();
+      if (lane == 0) seen[team * WAVES + wave] = again;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < TEAMS * WAVES; ++i) again = again || seen[i];
+      again = __builtin_amdgcn_readfirstlane(again);
+      __syncthreads();
+    }
+    if (__builtin_expect(again, 0)) recur();
+  }
   if (last || !OUT) {
     float* const S_out = OUT ? p.to + (int64_t)b * p.to_batch + (int64_t)h * p.to_head : p.part + ((size_t)bh * all.segments + seg) * dx * dz;
 #pragma unroll
