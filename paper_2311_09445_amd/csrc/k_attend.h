@@ -375,7 +375,7 @@ __device__ __forceinline__ void store_row_counted(uint8_t* base, uint32_t offset
 }
 
 // What is left of a state over tokens whose decays' logarithms add up to x: S + (e^x - 1) S where more than half is (the power itself,
-// rounded to 32 bits, would be off by the same 2^-25 in every chunk of a slow decay), e^x S where less is (the other form would be off
+// rounded to 32 bits, would be off by the same 2^-25 in every chunk, or token, of a slow decay), e^x S where less is (the other form would be off
 // by 2^-25 of what there was).
 struct Keep { float factor; bool half; };
 __device__ __forceinline__ Keep keeps(float x) { return x > -0.6931472f ? Keep{expm1f(x), true} : Keep{expf(x), false}; }
