@@ -96,17 +96,6 @@ struct AttentionStep {
 
 #include "k_attend_step.h"
 
-SeqRows rows(const per_seq_rows& r, uint32_t dtype, uint32_t share) {
-  const int64_t per16 = dtype == PER_SEQ_BF16 ? 8 : 4;
-  const bool near = r.token >= 0 && r.token < (1 << 24);
-  const bool wide = near && (reinterpret_cast<uintptr_t>(r.d) & 15) == 0 && r.batch % per16 == 0 && r.token % per16 == 0 && r.head % per16 == 0;
-  return SeqRows{r.d, r.batch, r.token, r.head, share, wide ? 1u : 0u, near ? 1u : 0u};
-}
-// Packed rows [B][L][heads][d] in fp32.
-SeqRows packed(float* d, uint32_t L, uint32_t heads, uint32_t width, uint32_t share) {
-  return SeqRows{d, (int64_t)L * heads * width, (int64_t)heads * width, (int64_t)width, share, width % 4 == 0, (uint64_t)heads * width < (1 << 24)};
-}
-
 AttentionPass make_pass(const AttentionSizes& a, bool back, uint32_t dx, uint32_t dz) {
   AttentionPass p{};
   p.L = a.L;
