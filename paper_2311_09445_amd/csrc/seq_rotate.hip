@@ -58,7 +58,8 @@ __global__ __launch_bounds__(256) void k_rotate_any(RotaryArgs a) {
       }
       own[i] = as_float(x[e]);
       if (KIND == NORM_ROTATE_BACK) {
-        dy[i] = as_float(d[e]) * cs[i] + as_float(d[partner]) * sn[i];
+        dy[i] = as_float(d[e]);
+        if (e < a.rot) dy[i] = dy[i] * cs[i] + as_float(d[partner]) * sn[i];
       } else {
         other[i] = as_float(x[partner]);
         if (KIND == NORM_ROTATE && sd.weight) other[i] *= sd.weight[partner];
@@ -95,7 +96,8 @@ __global__ __launch_bounds__(256) void k_rotate_any(RotaryArgs a) {
         const uint32_t e = lane + 64 * i;
         if (e >= a.dim) continue;
         if (KIND == NORM_ROTATE && sd.weight) own[i] *= sd.weight[e];
-        out[e] = (T)((own[i] * cs[i] + other[i] * sn[i]) * r);
+        if (e < a.rot) own[i] = own[i] * cs[i] + other[i] * sn[i];   // (those behind pass: zero times infinity would not be zero)
+        out[e] = (T)(own[i] * r);
       }
     }
   }

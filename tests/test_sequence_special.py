@@ -78,3 +78,21 @@ def test_values_that_are_not_finite_reach_nothing_else(B, L, H, G, dk, dv, dtype
     same_places(got[3][:5], want[3], state_bound(A[3], L), "dstate0")
     for x in (out, last, *got):
         assert bool(x[5:].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("D,rot,shift", [(37, 20, 0), (64, 32, 1), (64, 32, 0), (200, 64, 0), (201, 66, 0)])
+def test_elements_behind_the_rotated_ones_pass(D, rot, shift, layout, dtype):
+    """Whatever they are, bit for bit; widths, pairs and addresses that go in vectors and that do not."""
+    B, L, H = 2, 5, 3
+    x = normal(1, B * L * H * D + 1, dtype=dtype)[shift:shift + B * L * H * D].view(B, L, H, D)
+    for i, value in enumerate((float("inf"), float("-inf"), float("nan"), -0.0, 0.0, torch.finfo(dtype).max)):
+        x[..., rot + 2 * i] = value
+    f, _ = seq.rotary_frequencies(rot)
+    bits = torch.int16 if dtype == BF16 else torch.int32
+    for inverse in (False, True):
+        y = seq.rotate(x, None, f, layout=layout, magnitude=1.5, inverse=inverse)
+        same = y[..., rot:].contiguous().view(bits) == x[..., rot:].contiguous().view(bits)
+        assert bool((same | (y[..., rot:].isnan() & x[..., rot:].isnan())).all())
+        assert bool(y[..., :rot].isfinite().all())
