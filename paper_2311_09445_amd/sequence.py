@@ -149,6 +149,7 @@ def linear_attention_step(q, k, v, log_decay, state, active=None, scale=None, ou
 # ------------------------------------------------------------------------------------------------------------- autograd
 def _functions():
     import torch
+    from torch.autograd.function import once_differentiable
 
     class NormRotate(torch.autograd.Function):
         @staticmethod
@@ -158,6 +159,7 @@ def _functions():
             return norm_rotate(q, k, q_weight, k_weight, positions, freqs, eps, layout, magnitude)
 
         @staticmethod
+        @once_differentiable
         def backward(ctx, dq_out, dk_out):
             q, k, qw, kw, positions, freqs = ctx.saved_tensors
             want = ctx.needs_input_grad[2] or ctx.needs_input_grad[3]
@@ -173,6 +175,7 @@ def _functions():
             return linear_attention(q, k, v, log_decay, state, lengths, scale)
 
         @staticmethod
+        @once_differentiable
         def backward(ctx, dout, dstate):
             q, k, v, log_decay, state, lengths = ctx.saved_tensors
             want = ctx.needs_input_grad[4]
@@ -194,10 +197,10 @@ def _function(i):
 
 
 def norm_rotate_autograd(q, k, q_weight, k_weight, positions, freqs, eps: float = 1e-6, layout: str = "half", magnitude: float = 1.0):
-    """``norm_rotate`` as a node of torch's graph: gradients of q, k and the weights."""
+    """``norm_rotate`` as a node of torch's graph: gradients of q, k and the weights, once."""
     return _function(0).apply(q, k, q_weight, k_weight, positions, freqs, eps, layout, magnitude)
 
 
 def linear_attention_autograd(q, k, v, log_decay, state=None, lengths=None, scale=None):
-    """``linear_attention`` as a node of torch's graph: gradients of q, k, v and ``state``."""
+    """``linear_attention`` as a node of torch's graph: gradients of q, k, v and ``state``, once."""
     return _function(1).apply(q, k, v, log_decay, state, lengths, scale)
