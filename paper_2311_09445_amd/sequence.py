@@ -196,11 +196,19 @@ def _function(i):
     return _FUNCTIONS[i]
 
 
+def _constant(t, name):
+    import torch
+    if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: no gradient of it is formed; detach it")
+
+
 def norm_rotate_autograd(q, k, q_weight, k_weight, positions, freqs, eps: float = 1e-6, layout: str = "half", magnitude: float = 1.0):
-    """``norm_rotate`` as a node of torch's graph: gradients of q, k and the weights, once."""
+    """``norm_rotate`` as a node of torch's graph: gradients of q, k and the weights, once (``freqs`` are constants)."""
+    _constant(freqs, "freqs")
     return _function(0).apply(q, k, q_weight, k_weight, positions, freqs, eps, layout, magnitude)
 
 
 def linear_attention_autograd(q, k, v, log_decay, state=None, lengths=None, scale=None):
-    """``linear_attention`` as a node of torch's graph: gradients of q, k, v and ``state``, once."""
+    """``linear_attention`` as a node of torch's graph: gradients of q, k, v and ``state``, once (the decays are constants)."""
+    _constant(log_decay, "log_decay")
     return _function(1).apply(q, k, v, log_decay, state, lengths, scale)

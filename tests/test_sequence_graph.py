@@ -26,3 +26,20 @@ def test_no_second_derivatives():
         first, = torch.autograd.grad(loss, a, create_graph=True)
         with pytest.raises(RuntimeError):
             first.square().sum().backward()
+
+
+def test_constants_that_ask_for_a_gradient_are_refused():
+    """No gradient of decays and frequencies is formed: None for it would be a wrong one."""
+    q, k, v, g, S, _ = attention_inputs(2, 20, 2, 2, 16, 16, F32)
+    f, _ = seq.rotary_frequencies(16)
+    asked_g, asked_f = leaves(g, f)
+    a, b = leaves(q, k)
+    with pytest.raises(ValueError, match="log_decay"):
+        seq.linear_attention_autograd(a, b, v, asked_g, S)
+    with pytest.raises(ValueError, match="freqs"):
+        seq.norm_rotate_autograd(a, b, None, None, None, asked_f)
+    with torch.no_grad():       # nothing is asked for here
+        out, _ = seq.linear_attention_autograd(a, b, v, asked_g, S)
+        x, _ = seq.norm_rotate_autograd(a, b, None, None, None, asked_f)
+    assert torch.equal(out, seq.linear_attention_autograd(q, k, v, g, S)[0]) and torch.equal(x, seq.norm_rotate_autograd(q, k, None, None, None, f)[0])
+    assert not out.requires_grad and not x.requires_grad
