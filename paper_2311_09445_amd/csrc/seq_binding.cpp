@@ -149,6 +149,16 @@ at::Tensor result(PyObject* given, const char* name, const Need& n, at::ScalarTy
   return *t;
 }
 
+// The caller's tensors (or None) that a call has written: if torch has kept one of them for a gradient, it finds out by its version.
+void written(int rc, std::initializer_list<PyObject*> given) {
+  if (rc) return;
+  for (PyObject* o : given) {
+    if (!THPVariable_Check(o)) continue;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  }
+}
+
 struct Attention {
   per_attention_config c{};
   Need n;
@@ -223,6 +233,7 @@ PyObject* do_attention(Args a, Py_ssize_t n_args) {
     rc = unlocked([&] {
       return per_linear_attention(&p.c, &p.q, &p.k, &p.v, p.decay, p.lengths, in ? &si : nullptr, &ro, last.defined() ? &so : nullptr, data(work), bytes, s);
     });
+  written(rc, {a[7], last.defined() ? a[8] : Py_None});
   return answer(rc, {&out, &last});
 }
 
@@ -252,6 +263,7 @@ PyObject* do_attention_backward(Args a, Py_ssize_t n_args) {
       return per_linear_attention_backward(&p.c, &dout, &p.q, &p.k, &p.v, p.decay, p.lengths, in ? &si : nullptr, din ? &sd : nullptr, &rq, &rk, &rv,
                                            first.defined() ? &so : nullptr, data(work), bytes, s);
     });
+  written(rc, {a[9], a[10], a[11], first.defined() ? a[12] : Py_None});
   return answer(rc, {&dq, &dk, &dv, &first});
 }
 
@@ -265,6 +277,7 @@ PyObject* do_attention_step(Args a, Py_ssize_t n_args) {
   const per_seq_rows ro = p.rows_of(out, "out", p.H, p.dv);
   void* s = stream_of(p.n);
   const int rc = unlocked([&] { return per_linear_attention_step(&p.c, &p.q, &p.k, &p.v, p.decay, p.lengths, &st, &ro, s); });
+  written(rc, {a[4], a[7]});
   return answer(rc, {&out});
 }
 
@@ -311,6 +324,7 @@ PyObject* do_rotate(Args a, Py_ssize_t n_args) {
   const per_seq_rows rx = rows(x, "x"), ro = rows(out, "out");
   void* s = stream_of(p.n);
   const int rc = unlocked([&] { return per_rotate(&p.c, &rx, &p.at, p.freqs, &ro, s); });
+  written(rc, {a[6]});
   return answer(rc, {&out});
 }
 
@@ -329,6 +343,7 @@ PyObject* do_norm_rotate(Args a, Py_ssize_t n_args) {
   const per_seq_rows rq = rows(q, "q"), rk = rows(k, "k"), oq = rows(qo, "q_out"), ok = rows(ko, "k_out");
   void* s = stream_of(p.n);
   const int rc = unlocked([&] { return per_norm_rotate(&p.c, &rq, &rk, qw, kw, &p.at, p.freqs, &oq, &ok, s); });
+  written(rc, {a[9], a[10]});
   return answer(rc, {&qo, &ko});
 }
 
@@ -361,6 +376,7 @@ PyObject* do_norm_rotate_backward(Args a, Py_ssize_t n_args) {
       return per_norm_rotate_backward(&p.c, &rgq, &rgk, &rq, &rk, qw, kw, &p.at, p.freqs, &oq, &ok, static_cast<float*>(data(wq)),
                                       static_cast<float*>(data(wk)), data(work), bytes, s);
     });
+  written(rc, {a[11], a[12]});
   return answer(rc, {&dq, &dk, &wq, &wk});
 }
 

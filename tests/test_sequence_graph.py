@@ -43,3 +43,56 @@ def test_constants_that_ask_for_a_gradient_are_refused():
         x, _ = seq.norm_rotate_autograd(a, b, None, None, None, asked_f)
     assert torch.equal(out, seq.linear_attention_autograd(q, k, v, g, S)[0]) and torch.equal(x, seq.norm_rotate_autograd(q, k, None, None, None, f)[0])
     assert not out.requires_grad and not x.requires_grad
+
+
+def test_tensors_written_in_place_are_noticed():
+    """Torch's check of what it has kept for a gradient sees every tensor of the caller's that a call writes."""
+    q, k, v, g, S, _ = attention_inputs(2, 1, 2, 2, 16, 16, F32)
+    f, _ = seq.rotary_frequencies(16)
+    dout, dS = normal(11, *q.shape), normal(12, *S.shape)
+    room = torch.empty_like
+    writes = {
+        "step": (lambda: S, lambda t: seq.linear_attention_step(q, k, v, g, t)),
+        "step's out": (lambda: q, lambda t: seq.linear_attention_step(k, k, v, g, S.clone(), out=t)),
+        "out": (lambda: q, lambda t: seq.linear_attention(k, k, v, g, S, out=t)),
+        "out_state": (lambda: S, lambda t: seq.linear_attention(q, k, v, g, t, out_state=t)),
+        "dq": (lambda: q, lambda t: seq.linear_attention_backward(dout, k, k, v, g, S, dS, dq=t)),
+        "dk": (lambda: q, lambda t: seq.linear_attention_backward(dout, k, k, v, g, S, dS, dk=t)),
+        "dv": (lambda: q, lambda t: seq.linear_attention_backward(dout, k, k, v, g, S, dS, dv=t)),
+        "dstate0": (lambda: S, lambda t: seq.linear_attention_backward(dout, q, k, v, g, None, dS, dstate0=t)),
+        "rotate": (lambda: q, lambda t: seq.rotate(t, None, f, out=t)),
+        "q_out": (lambda: q, lambda t: seq.norm_rotate(t, k, None, None, None, f, q_out=t)),
+        "k_out": (lambda: q, lambda t: seq.norm_rotate(k, t, None, None, None, f, k_out=t)),
+        "norm's dq": (lambda: q, lambda t: seq.norm_rotate_backward(dout, dout, k, k, None, None, None, f, dq=t)),
+        "norm's dk": (lambda: q, lambda t: seq.norm_rotate_backward(dout, dout, k, k, None, None, None, f, dk=t)),
+    }
+    for name, (make, write) in writes.items():
+        kept = make().clone()
+        x, = leaves(room(kept).fill_(2.0))
+        loss = (x * kept).sum()
+        write(kept)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+            print("not noticed:", name)
+    T = S.clone()
+    a, b = leaves(q, k)
+    out, _ = seq.linear_attention_autograd(a, b, v, g, T)
+    seq.linear_attention_step(q, k, v, g, T)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+
+
+def test_what_is_only_read_stays_as_it_is_for_the_graph():
+    q, k, v, g, S, _ = attention_inputs(2, 9, 2, 2, 16, 16, BF16)
+    f, _ = seq.rotary_frequencies(16)
+    before = [t._version for t in (q, k, v, g, S, f)]
+    out, last = seq.linear_attention(q, k, v, g, S)
+    seq.linear_attention_backward(out, q, k, v, g, S, last)
+    seq.norm_rotate(q, k, None, None, None, f)
+    assert [t._version for t in (q, k, v, g, S, f)] == before
+    with pytest.raises(seq.PerError):       # refused: nothing is written
+        seq.linear_attention(q, k, v, g, S, out=q)
+    assert q._version == before[0]
+    with torch.inference_mode():
+        T = S.clone()
+    seq.linear_attention_step(*(t[:, :1] for t in (q, k, v)), g, T)     # (these have no versions)
