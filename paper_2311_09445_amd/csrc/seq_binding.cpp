@@ -4,6 +4,7 @@
 
 #include <ATen/Functions.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -135,6 +136,23 @@ PyObject* answer(int rc, std::initializer_list<const at::Tensor*> results) {
 
 using Args = PyObject* const*;
 
+bool asks(std::initializer_list<PyObject*> tensors) {
+  for (PyObject* o : tensors)
+    if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad()) return true;
+  return false;
+}
+// Whether a gradient of the inputs is asked for: the call has to be made as a node of torch's graph then (its caller is told by None),
+// and results that are given, which may hold what another node has kept, have no place in it.
+bool differentiated(std::initializer_list<PyObject*> inputs, std::initializer_list<PyObject*> given) {
+  if (!c10::GradMode::is_enabled()) return false;
+  bool any = false;
+  for (PyObject* o : given) any = any || o != Py_None;
+  if (!asks(inputs) && !(any && asks(given))) return false;
+  if (!any) return true;
+  PyErr_SetString(PyExc_RuntimeError, "no gradient is formed where results are written over given tensors: call it under no_grad, or without them");
+  throw Raised{};
+}
+
 void expect(Py_ssize_t n, Py_ssize_t want) {
   if (n == want) return;
   PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, n);
@@ -211,9 +229,10 @@ struct Attention {
 
 void* data(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
-// (q, k, v, log_decay, state, lengths, scale, out, out_state, want_state) -> (code, out, out_state)
+// (q, k, v, log_decay, state, lengths, scale, out, out_state, want_state) -> (code, out, out_state), or None
 PyObject* do_attention(Args a, Py_ssize_t n_args) {
   expect(n_args, 10);
+  if (differentiated({a[0], a[1], a[2], a[3], a[4]}, {a[7], a[8]})) Py_RETURN_NONE;
   const Attention p(a[0], a[1], a[2], a[3], a[5], a[6]);
   const c10::DeviceGuard guard(p.n.device);
   const at::Tensor* in = maybe(a[4], "state");
@@ -270,6 +289,7 @@ PyObject* do_attention_backward(Args a, Py_ssize_t n_args) {
 // (q, k, v, log_decay, state, active, scale, out) -> (code, out)
 PyObject* do_attention_step(Args a, Py_ssize_t n_args) {
   expect(n_args, 8);
+  differentiated({a[0], a[1], a[2], a[3]}, {a[4], a[7]});   // (the state is a given result)
   const Attention p(a[0], a[1], a[2], a[3], a[5], a[6]);
   const c10::DeviceGuard guard(p.n.device);
   const per_seq_states st = p.states_of(tensor(a[4], "state"), "state");
@@ -313,9 +333,10 @@ struct Rotary {
   }
 };
 
-// (x, positions, freqs, layout, magnitude, inverse, out) -> (code, out)
+// (x, positions, freqs, layout, magnitude, inverse, out) -> (code, out), or None
 PyObject* do_rotate(Args a, Py_ssize_t n_args) {
   expect(n_args, 7);
+  if (differentiated({a[0], a[2]}, {a[6]})) Py_RETURN_NONE;
   Rotary p(a[0], a[1], a[2], a[3], a[4], "x");
   const c10::DeviceGuard guard(p.n.device);
   p.c.inverse = truth(a[5]);
@@ -328,9 +349,10 @@ PyObject* do_rotate(Args a, Py_ssize_t n_args) {
   return answer(rc, {&out});
 }
 
-// (q, k, q_weight, k_weight, positions, freqs, layout, magnitude, eps, q_out, k_out) -> (code, q_out, k_out)
+// (q, k, q_weight, k_weight, positions, freqs, layout, magnitude, eps, q_out, k_out) -> (code, q_out, k_out), or None
 PyObject* do_norm_rotate(Args a, Py_ssize_t n_args) {
   expect(n_args, 11);
+  if (differentiated({a[0], a[1], a[2], a[3], a[5]}, {a[9], a[10]})) Py_RETURN_NONE;
   Rotary p(a[0], a[4], a[5], a[6], a[7], "q");
   const c10::DeviceGuard guard(p.n.device);
   const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k");

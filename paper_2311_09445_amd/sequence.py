@@ -5,6 +5,10 @@ Rows are device tensors [batch, length, heads, width] in bfloat16 or float32; ev
 dimension has to be contiguous.  Work is enqueued on the current stream; nothing synchronises.  Tensors are taken apart, and
 results allocated, in ``_seq_binding.so`` (``csrc/seq_binding.cpp``: the checks and their messages are there).
 
+Inputs that ask for a gradient get one: the calls of sequences are then nodes of torch's graph (with no tensors given for their
+results, which could not be).  Gradients of gradients are refused but for the rotation's, and so are gradients of decays and frequencies;
+the calls that form gradients, and single tokens, are no nodes.
+
 There is no CPU fallback.
 """
 from __future__ import annotations
@@ -86,7 +90,11 @@ def rotate(x, positions, freqs, layout: str = "half", magnitude: float = 1.0, in
 
     ``positions``: int32 [B, L], or None (0, 1, ...).  ``layout``: "half" (pair p: elements p and p + rot/2) or
     "interleaved" (2p and 2p + 1).  ``inverse`` turns the other way, which is also the gradient.  ``out`` may be ``x``."""
-    rc, out = _calls().rotate(x, positions, freqs, _layout(layout), magnitude, inverse, out)
+    done = _calls().rotate(x, positions, freqs, _layout(layout), magnitude, inverse, out)
+    if done is None:
+        _constant(freqs, "freqs")
+        return _function(2).apply(x, positions, freqs, layout, magnitude, inverse)
+    rc, out = done
     if rc:
         raise PerError(rc, "per_rotate")
     return out
@@ -96,7 +104,10 @@ def norm_rotate(q, k, q_weight, k_weight, positions, freqs, eps: float = 1e-6, l
                 q_out=None, k_out=None):
     """Queries and keys divided by the root of the mean square (plus ``eps``) of each head, times their weights (fp32 [D],
     or None), then turned as by ``rotate``, in one pass.  Returns (q_out, k_out), which may be q and k."""
-    rc, q_out, k_out = _calls().norm_rotate(q, k, q_weight, k_weight, positions, freqs, _layout(layout), magnitude, eps, q_out, k_out)
+    done = _calls().norm_rotate(q, k, q_weight, k_weight, positions, freqs, _layout(layout), magnitude, eps, q_out, k_out)
+    if done is None:
+        return norm_rotate_autograd(q, k, q_weight, k_weight, positions, freqs, eps, layout, magnitude)
+    rc, q_out, k_out = done
     if rc:
         raise PerError(rc, "per_norm_rotate")
     return q_out, k_out
@@ -120,7 +131,11 @@ def linear_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, o
     q [B, L, H, dk]; k [B, L, G, dk] and v [B, L, G, dv] with G dividing H; ``log_decay`` fp32 [H], at most 0; ``state`` fp32
     [B, H, dk, dv] or None (zeros); ``lengths`` int32 [B] or None: valid tokens of each sequence (behind them nothing is read
     and the outputs are zeros); ``scale``: 1 / sqrt(dk) if None."""
-    rc, out, last = _calls().linear_attention(q, k, v, log_decay, state, lengths, scale, out, out_state, want_state or out_state is not None)
+    done = _calls().linear_attention(q, k, v, log_decay, state, lengths, scale, out, out_state, want_state or out_state is not None)
+    if done is None:
+        out, last = linear_attention_autograd(q, k, v, log_decay, state, lengths, scale)
+        return out, last if want_state else None
+    rc, out, last = done
     if rc:
         raise PerError(rc, "per_linear_attention")
     return out, last
@@ -139,7 +154,7 @@ def linear_attention_backward(dout, q, k, v, log_decay, state=None, dstate=None,
 
 def linear_attention_step(q, k, v, log_decay, state, active=None, scale=None, out=None):
     """One token (length 1) of ``linear_attention`` with the states [B, H, dk, dv] updated in place.  ``active`` int32 [B] or None:
-    where it is 0 the state is not touched and the output is zero.  Returns out."""
+    where it is 0 the state is not touched and the output is zero.  No gradient is formed: refused where one is asked for.  Returns out."""
     rc, out = _calls().linear_attention_step(q, k, v, log_decay, state, active, scale, out)
     if rc:
         raise PerError(rc, "per_linear_attention_step")
@@ -183,7 +198,18 @@ def _functions():
                                                           lengths, ctx.scale, want_dstate=want)
             return dq, dk, dv, None, first, None, None
 
-    return NormRotate, LinearAttention
+    class Rotate(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, positions, freqs, layout, magnitude, inverse):
+            ctx.save_for_backward(positions, freqs)
+            ctx.how = (layout, magnitude, not inverse)
+            return rotate(x, positions, freqs, layout, magnitude, inverse)
+
+        @staticmethod
+        def backward(ctx, dout):
+            return rotate(dout.contiguous(), *ctx.saved_tensors, *ctx.how), None, None, None, None, None
+
+    return NormRotate, LinearAttention, Rotate
 
 
 _FUNCTIONS = None

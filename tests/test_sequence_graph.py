@@ -96,3 +96,82 @@ def test_what_is_only_read_stays_as_it_is_for_the_graph():
     with torch.inference_mode():
         T = S.clone()
     seq.linear_attention_step(*(t[:, :1] for t in (q, k, v)), g, T)     # (these have no versions)
+
+
+def test_inputs_that_ask_for_gradients_get_them():
+    """The plain calls are nodes of the graph too where an input asks for a gradient: no result is detached without an error."""
+    B, L, H, G, d = 2, 21, 4, 2, 32
+    q, k, v, g, S, lengths = attention_inputs(B, L, H, G, d, d, F32, ragged=True)
+    f, _ = seq.rotary_frequencies(d)
+    w = 1 + 0.1 * normal(9, d)
+    at = torch.arange(L, dtype=torch.int32, device="cuda").expand(B, L) + 7
+    for i in range(4):      # one at a time
+        ts = [q, k, v, S]
+        ts[i], = leaves(ts[i])
+        out, last = seq.linear_attention(*ts[:3], g, ts[3], lengths, scale=0.3)
+        dout, dS = normal(11, *out.shape), normal(12, *S.shape)
+        torch.autograd.backward((out, last), (dout, dS))
+        assert torch.equal(ts[i].grad, seq.linear_attention_backward(dout, q, k, v, g, S, dS, lengths, scale=0.3)[i])
+    a, = leaves(q)
+    out, none = seq.linear_attention(a, k, v, g, S, lengths, want_state=False)
+    assert none is None and torch.equal(out.detach(), seq.linear_attention(q, k, v, g, S, lengths)[0])
+    out.sum().backward()
+    assert torch.equal(a.grad, seq.linear_attention_backward(torch.ones_like(q), q, k, v, g, S, None, lengths)[0])
+    for i in range(4):
+        ts = [q, k, w, w]
+        ts[i], = leaves(ts[i])
+        x, y = seq.norm_rotate(*ts, at, f, eps=1e-3, layout="interleaved", magnitude=1.2)
+        torch.autograd.backward((x, y), (normal(13, *q.shape), normal(14, *k.shape)))
+        want = seq.norm_rotate_backward(normal(13, *q.shape), normal(14, *k.shape), q, k, w, w, at, f, eps=1e-3, layout="interleaved", magnitude=1.2)
+        assert torch.equal(ts[i].grad, want[i])
+    # (values below 6, two turns that round by 4 e each way: within 1e-5)
+    for inverse in (False, True):
+        for layout in ("half", "interleaved"):
+            x, = leaves(q)
+            y = seq.rotate(x, at, f, layout, 1.2, inverse)
+            assert torch.equal(y.detach(), seq.rotate(q, at, f, layout, 1.2, inverse))
+            first, = torch.autograd.grad((y * y).sum() / 2, x, create_graph=True)     # the magnitude twice, turned and back
+            assert float((first.detach() - 1.2 ** 2 * q).abs().max()) < 1e-5
+            again, = torch.autograd.grad(first, x, normal(13, *q.shape))
+            assert float((again - 1.2 ** 2 * normal(13, *q.shape)).abs().max()) < 1e-5
+    x, = leaves(q)
+    seq.rotate(x, at, f).sum().backward()       # (a gradient whose last dimension is not contiguous)
+    assert torch.equal(x.grad, seq.rotate(torch.ones_like(q), at, f, inverse=True))
+
+
+def test_no_gradient_is_formed_where_none_is_asked_for():
+    q, k, v, g, S, _ = attention_inputs(2, 9, 2, 2, 16, 16, F32)
+    f, _ = seq.rotary_frequencies(16)
+    with torch.no_grad():
+        a, b, c = leaves(q, k, v)
+        for t in (*seq.linear_attention(a, b, c, g, S), *seq.norm_rotate(a, b, None, None, None, f), seq.rotate(a, None, f),
+                  seq.linear_attention_step(*(t[:, :1] for t in (a, b, c)), g, S)):
+            assert not t.requires_grad
+        seq.rotate(a, None, f, out=a)
+    for t in (*seq.linear_attention(q, k, v, g, S), seq.rotate(q, None, f)):
+        assert not t.requires_grad
+
+
+def test_results_that_are_given_take_no_part_in_a_gradient():
+    """Written over, they cannot be nodes of the graph: refused, as torch refuses it."""
+    q, k, v, g, S, _ = attention_inputs(2, 1, 2, 2, 16, 16, F32)
+    f, _ = seq.rotary_frequencies(16)
+    a, T = leaves(q, S)
+    room, room_state, b = torch.empty_like(q), torch.empty_like(S), a * 1.0
+    before = b.detach().clone()
+    refused = {
+        "out": lambda: seq.linear_attention(a, k, v, g, S, out=room),
+        "out_state": lambda: seq.linear_attention(a, k, v, g, S, out_state=room_state),
+        "out itself": lambda: seq.linear_attention(q, k, v, g, S, out=a),
+        "a step": lambda: seq.linear_attention_step(a, k, v, g, S),
+        "a step's state": lambda: seq.linear_attention_step(q, k, v, g, T),
+        "a step's out": lambda: seq.linear_attention_step(q, k, v, g, S, out=a),
+        "rotate": lambda: seq.rotate(b, None, f, out=b),
+        "q_out": lambda: seq.norm_rotate(a, k, None, None, None, f, q_out=room),
+        "k_out": lambda: seq.norm_rotate(k, q, None, None, None, f, k_out=a),
+    }
+    for name, call in refused.items():
+        with pytest.raises(RuntimeError, match="gradient"):
+            call()
+            print("not refused:", name)
+    assert torch.equal(b, before)
