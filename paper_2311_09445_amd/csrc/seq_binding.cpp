@@ -185,7 +185,8 @@ struct Attention {
   const float* decay;
   const int32_t* lengths;
   // (q, k, v, log_decay, lengths, scale); scale None: 1 / sqrt(dk)
-  Attention(PyObject* oq, PyObject* ok, PyObject* ov, PyObject* odecay, PyObject* olengths, PyObject* oscale) : n(need_of(tensor(oq, "q"), "q")) {
+  Attention(PyObject* oq, PyObject* ok, PyObject* ov, PyObject* odecay, PyObject* olengths, PyObject* oscale, const char* lengths_name = "lengths")
+      : n(need_of(tensor(oq, "q"), "q")) {
     const at::Tensor &tq = tensor(oq, "q"), &tk = tensor(ok, "k"), &tv = tensor(ov, "v");
     if (tq.dim() != 4 || tk.dim() != 4 || tv.dim() != 4) raise_value("q, k and v must be [batch, length, heads, width]");
     B = tq.size(0);
@@ -210,7 +211,7 @@ struct Attention {
     k = rows(tk, "k");
     v = rows(tv, "v");
     decay = vector<float>(&tensor(odecay, "log_decay"), "log_decay", n, at::kFloat, H);
-    lengths = vector<int32_t>(maybe(olengths, "lengths"), "lengths", n, at::kInt, B);
+    lengths = vector<int32_t>(maybe(olengths, lengths_name), lengths_name, n, at::kInt, B);
   }
   per_seq_rows rows_of(const at::Tensor& t, const char* name, int64_t heads, int64_t width) const {
     check(t, name, n, n.type, {B, L, heads, width});
@@ -290,7 +291,7 @@ PyObject* do_attention_backward(Args a, Py_ssize_t n_args) {
 PyObject* do_attention_step(Args a, Py_ssize_t n_args) {
   expect(n_args, 8);
   differentiated({a[0], a[1], a[2], a[3]}, {a[4], a[7]});   // (the state is a given result)
-  const Attention p(a[0], a[1], a[2], a[3], a[5], a[6]);
+  const Attention p(a[0], a[1], a[2], a[3], a[5], a[6], "active");
   const c10::DeviceGuard guard(p.n.device);
   const per_seq_states st = p.states_of(tensor(a[4], "state"), "state");
   at::Tensor out = result(a[7], "out", p.n, p.n.type, {p.B, p.L, p.H, p.dv});

@@ -48,3 +48,15 @@ def test_steps_reach_the_state_that_the_sequence_does(dtype):
         A = A * decay + k[:, t].cpu().double().abs()[..., None] * v[:, t].cpu().double().abs()[..., None, :]
     _, last = seq.linear_attention(q, k, v, g, S)
     within(T, last.cpu().double(), (8 * (2 * n) ** 0.5 + 64 + n / 16) * U_F32 * A, "state")
+
+
+def test_refusals_name_the_argument():
+    q, S = normal(2, 3, 1, 2, 16), normal(1, 3, 2, 16, 16)
+    g = torch.tensor([-0.1, -0.2], device="cuda")
+    for active in (torch.ones(2, dtype=torch.int32, device="cuda"), torch.ones(3, device="cuda"), torch.ones(3, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="active"):
+            seq.linear_attention_step(q, q, q, g, S, active)
+        with pytest.raises(ValueError, match="lengths"):
+            seq.linear_attention(q, q, q, g, S, active)
+    with pytest.raises(TypeError, match="active"):
+        seq.linear_attention_step(q, q, q, g, S, [1, 0, 1])
