@@ -16,8 +16,9 @@
  *    found on the host before anything is enqueued.  The library allocates nothing: the caller provides the workspace
  *    where one is needed (sized by the *_workspace function, 256-byte aligned; its contents need not be kept).  Calls hold
  *    no state between them and may be captured into a HIP graph and replayed.
- *  - Element type of rows: PER_SEQ_BF16 or PER_SEQ_F32.  Sums, norms, states and weights are fp32; a result is rounded to
- *    its type once, at the end.
+ *  - Element type of rows: PER_SEQ_BF16 or PER_SEQ_F32.  Sums, norms, states and weights are fp32.  A result is rounded to
+ *    its type once, at the end; only sequences of linear attention and their gradients in bfloat16 round inside as well,
+ *    where it says so.
  *  - Outputs must not overlap inputs or each other, except where a call says so.
  *  - A batch, a length or a number of heads of 0 is valid: nothing is written but states (which are then copied).
  */
@@ -109,6 +110,11 @@ typedef struct per_attention_config {
  *   d_lengths   : [batch] valid tokens of each sequence (values outside 0..length are taken as the nearest of these), or
  *                 NULL: all.  Tokens behind them are not read; their outputs are zeros.
  *   out_state   : S behind the last valid token, or NULL.  It may be state.
+ * Rows in fp32 are computed to fp32's accuracy throughout.  Rows in bfloat16 are multiplied in bfloat16: the state that a
+ * chunk of 32 tokens starts from and the decayed products of pairs of its tokens are rounded to it where they are factors
+ * (each held, and summed, in fp32), so that an output carries up to three roundings of 2^-8, of its parts and of itself:
+ * 2.3e-3 of the outputs by the 2-norm, where one rounding is 1.7e-3.  What a token adds to a state is rounded to 16 bits
+ * where the state itself is no result, and to 24 where it is; outputs may differ by that much with out_state.
  * A value among the valid tokens, or of the state, that is not finite makes all outputs and states that depend on it not
  * finite (those of tokens before it do not). */
 int per_linear_attention_workspace(const per_attention_config* c, int backward, size_t* bytes);
@@ -118,7 +124,8 @@ int per_linear_attention(const per_attention_config* c, const per_seq_rows* q, c
 
 /* Its gradient, the decays being constants: from dout (of out) and dstate (of out_state; NULL: zeros) to dq, dk, dv and
  * dstate0 (of state; NULL where not wanted).  Gradients of keys and values that several heads share are sums in a fixed
- * order.  dstate0 may be dstate, and not state.  Of values that are not finite the same holds as above. */
+ * order.  dstate0 may be dstate, and not state.  Of roundings, and of values that are not
+ * finite, the same holds as above. */
 int per_linear_attention_backward(const per_attention_config* c, const per_seq_rows* dout, const per_seq_rows* q,
                                   const per_seq_rows* k, const per_seq_rows* v, const float* d_log_decay,
                                   const int32_t* d_lengths, const per_seq_states* state, const per_seq_states* dstate,

@@ -53,7 +53,10 @@ __device__ __forceinline__ uint32_t state_row(uint32_t a, uint32_t m) { return 3
 template <int NT>
 __device__ __forceinline__ uint32_t state_column(uint32_t c, uint32_t m) { return NT == 2 ? 8 * (m >> 2) + 4 * c + (m & 3) : 16 * c + m; }
 
-// Operand of 16 x 32 places: 8 of the inner dimension per lane.  Values in fp32 are taken apart into three in bfloat16, whose sum they
+// Operand of 16 x 32 places: 8 of the inner dimension per lane.  Where rows are bfloat16, what meets them (the state, the decayed
+// products of pairs) is rounded to it once more as it becomes an operand.  In two parts each, outputs are off by 1.7e-3 as after one
+// rounding, not 2.3e-3, but there are a third more matrix instructions and over half as many again of the others: 16 rows of 1024 tokens of 8
+// heads of 128 x 128 45 -> 54 us and the gradient 89 -> 112, 2 x 16384 of 16 heads 395 -> 472, 32 x 512 of 64 x 64 21 -> 23.  Values in fp32 are taken apart into three in bfloat16, whose sum they
 // are (8 bits each, cut off, not rounded: no part overflows), and products into six matrix instructions; the two products of 2^-24
 // that are left out are of the size of fp32's own rounding.  (The matrix instructions of fp32 itself take 32 times as long as those of
 // bfloat16, 5.3 times as long as six: a chunk of 64 x 64 took 3.1 us and takes 2.6, of 128 x 64 5.0 and 4.0.)  In LDS the parts are three tiles, one

@@ -130,7 +130,8 @@ def linear_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, o
 
     q [B, L, H, dk]; k [B, L, G, dk] and v [B, L, G, dv] with G dividing H; ``log_decay`` fp32 [H], at most 0; ``state`` fp32
     [B, H, dk, dv] or None (zeros); ``lengths`` int32 [B] or None: valid tokens of each sequence (behind them nothing is read
-    and the outputs are zeros); ``scale``: 1 / sqrt(dk) if None."""
+    and the outputs are zeros); ``scale``: 1 / sqrt(dk) if None.  In bfloat16 two factors inside are rounded to it, besides the
+    outputs (``include/per_seq.h``); states are fp32 sums."""
     done = _calls().linear_attention(q, k, v, log_decay, state, lengths, scale, out, out_state, want_state or out_state is not None)
     if done is None:
         out, last = linear_attention_autograd(q, k, v, log_decay, state, lengths, scale)
