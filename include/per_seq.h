@@ -20,7 +20,8 @@
  *    its type once, at the end; only sequences of linear attention and their gradients in bfloat16 round inside as well,
  *    where it says so.
  *  - Outputs must not overlap inputs or each other, except where a call says so.
- *  - A batch, a length or a number of heads of 0 is valid: nothing is written but states (which are then copied).
+ *  - A batch, a length or a number of heads of 0 is valid: nothing is written but states (which are then copied), and zeros
+ *    for gradients of keys and values that no head reads.
  */
 #ifndef PER_SEQ_H_
 #define PER_SEQ_H_

@@ -195,12 +195,12 @@ int per_linear_attention_backward(const per_attention_config* c, const per_seq_r
   int rc = check_attention(c);
   if (rc != PER_OK) return rc;
   const Extent nq{c->batch, c->length, c->heads}, nk{c->batch, c->length, c->kv_heads};
-  if (!c->batch || !c->heads) return PER_OK;
+  if (!c->batch || (!c->heads && nk.empty())) return PER_OK;
   if (!readable(dout, nq, c->dtype) || !readable(q, nq, c->dtype) || !readable(k, nk, c->dtype) || !readable(v, nk, c->dtype)) return PER_EINVAL;
   if (!writable(dq, nq, c->dtype) || !writable(dk, nk, c->dtype) || !writable(dv, nk, c->dtype)) return PER_EINVAL;
-  if (!d_log_decay || misaligned(d_log_decay, 4) || misaligned(d_lengths, 4)) return PER_EINVAL;
+  if ((c->heads && !d_log_decay) || misaligned(d_log_decay, 4) || misaligned(d_lengths, 4)) return PER_EINVAL;
   if ((state && !state_ok(state, c, false)) || (dstate && !state_ok(dstate, c, false)) || (dstate0 && !state_ok(dstate0, c, true))) return PER_EINVAL;
-  if (state && dstate0 && state->d == dstate0->d) return PER_EINVAL;
+  if (c->heads && state && dstate0 && state->d == dstate0->d) return PER_EINVAL;
   for (const per_seq_rows* o : {dq, dk, dv})
     for (const per_seq_rows* i : {dout, q, k, v})
       if (same(o, i)) return PER_EINVAL;

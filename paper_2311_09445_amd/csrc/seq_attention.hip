@@ -342,9 +342,29 @@ hipError_t forward(const AttentionSizes& a, const per_seq_rows& q, const per_seq
 }
 
 template <typename T>
+hipError_t launch_fold(const Folds& f, hipStream_t s) {
+  if (!f.rows) return hipSuccess;
+  const uint32_t dk = f.fold[0].d, dv = f.fold[1].d;
+  const bool wide = dk % 4 == 0 && dv % 4 == 0 && f.fold[0].to.wide && f.fold[1].to.wide;
+  const uint32_t widest = dk > dv ? dk : dv, per = 256 / (wide ? (widest + 3) / 4 : widest);   // rows of a workgroup
+  const uint64_t blocks = (f.rows + per - 1) / per;
+  const dim3 grid((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), 2);
+  if (wide) k_fold_heads<T, 4><<<grid, 256, 0, s>>>(f);
+  else k_fold_heads<T, 1><<<grid, 256, 0, s>>>(f);
+  return hipGetLastError();
+}
+
+template <typename T>
 hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per_seq_rows& q, const per_seq_rows& k,
                     const per_seq_rows& v, const per_seq_states* state, const per_seq_states* dstate, const per_seq_rows& dq,
                     const per_seq_rows& dk, const per_seq_rows& dv, const per_seq_states* dstate0, void* work, hipStream_t s) {
+  Folds f{};
+  f.fold[0] = Fold{nullptr, rows(dk, a.dtype, 1), a.dk};
+  f.fold[1] = Fold{nullptr, rows(dv, a.dtype, 1), a.dv};
+  f.L = a.L;
+  f.G = a.G;
+  f.rows = (uint64_t)a.B * a.L * a.G;
+  if (!a.H) return launch_fold<T>(f, s);   // (sums over no heads)
   const uint32_t share = a.H / a.G, bh = a.B * a.H;
   const Cut c = cut(a, true);
   const uint32_t team = c.teams, left = share / team;   // left: to be added up behind
@@ -410,22 +430,10 @@ hipError_t backward(const AttentionSizes& a, const per_seq_rows& dout, const per
     e = launch_passes<T, true>(all, bh, s);
   }
   if (e != hipSuccess || left == 1) return e;
-  Folds f{};
-  f.fold[0] = Fold{fold_k, rows(dk, a.dtype, 1), a.dk};
-  f.fold[1] = Fold{fold_v, rows(dv, a.dtype, 1), a.dv};
-  f.L = a.L;
-  f.G = a.G;
+  f.fold[0].from = fold_k;
+  f.fold[1].from = fold_v;
   f.share = left;
-  f.rows = (uint64_t)a.B * a.L * a.G;
-  if (!f.rows) return e;
-  const bool wide = a.dk % 4 == 0 && a.dv % 4 == 0 && f.fold[0].to.wide && f.fold[1].to.wide;
-  const uint32_t widest = a.dk > a.dv ? a.dk : a.dv, per = 256 / (wide ? (widest + 3) / 4 : widest);   // rows of a workgroup
-  const uint64_t blocks = (f.rows + per - 1) / per;
-  const dim3 grid((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), 2);
-  if (wide) k_fold_heads<T, 4><<<grid, 256, 0, s>>>(f);
-  else k_fold_heads<T, 1><<<grid, 256, 0, s>>>(f);
-  e = hipGetLastError();
-  return e;
+  return launch_fold<T>(f, s);
 }
 
 }  // namespace
@@ -435,7 +443,7 @@ size_t attention_work_bytes(const AttentionSizes& a, bool backward) {
   if (!backward) return part_bytes(a, c);
   const size_t need = 2 * part_bytes(a, c) + fold_bytes(a, c.teams, a.dk) + fold_bytes(a, c.teams, a.dv);
   // (a gradient of shared heads always has a workspace: what a caller passes does not depend on who adds up)
-  return need || a.H == a.G || !a.B || !a.L ? need : 256;
+  return need || !a.H || a.H == a.G || !a.B || !a.L ? need : 256;
 }
 
 hipError_t launch_attention(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,

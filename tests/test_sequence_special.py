@@ -96,3 +96,23 @@ def test_elements_behind_the_rotated_ones_pass(D, rot, shift, layout, dtype):
         same = y[..., rot:].contiguous().view(bits) == x[..., rot:].contiguous().view(bits)
         assert bool((same | (y[..., rot:].isnan() & x[..., rot:].isnan())).all())
         assert bool(y[..., :rot].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(16, 32), (5, 7)])
+def test_keys_and_values_that_no_query_reads_have_a_gradient_of_zero(dk, dv, dtype):
+    """No heads of queries at all: the sum over none of them, in tensors of the call's and of the caller's (other strides, too)."""
+    B, L, G = 2, 9, 3
+    q, k, v = normal(1, B, L, 0, dk, dtype=dtype), normal(2, B, L, G, dk, dtype=dtype), normal(3, B, L, G, dv, dtype=dtype)
+    dout, g = normal(4, B, L, 0, dv, dtype=dtype), torch.zeros(0, device="cuda")
+    out, last = seq.linear_attention(q, k, v, g)
+    assert out.shape == (B, L, 0, dv) and last.shape == (B, 0, dk, dv)
+    room = torch.full((B, L, G + 1, dk), 7.0, dtype=dtype, device="cuda")
+    given_v = torch.full((B, L, G, dv), 7.0, dtype=dtype, device="cuda")
+    dq, gk, gv, first = seq.linear_attention_backward(dout, q, k, v, g, dk=room[:, :, 1:], dv=given_v)
+    assert dq.shape == q.shape and first.shape == (B, 0, dk, dv)
+    assert not gk.any() and not gv.any() and bool((room[:, :, 0] == 7.0).all())
+    dirty = [torch.full_like(t, 7.0) for t in (k, v)]
+    del dirty       # (memory that a new tensor may well get)
+    for t in seq.linear_attention_backward(dout, q, k, v, g, last, last)[1:3]:
+        assert not t.any()
