@@ -24,7 +24,7 @@
 // What bounds it.  A workgroup by itself takes 0.8 us a chunk of 64 x 64 in bfloat16, 1.9 of 128 x 128: the chain from its barrier
 // through LDS and two rounds of matrix instructions.  With the chip full it is memory: 768 workgroups of 64 x 64, three to a compute
 // unit, take 2.8 us for a chunk each (4.5 TB/s), 2.7 without any of the products, 1.6 without the outputs; 65536 tokens of 16 heads of
-// 128 x 128 229 us (4.7 TB/s).
+// 128 x 128 take 255 us (4.2 TB/s; the least of 40 launches 231) behind 155 for their segments' states.
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -400,7 +400,9 @@ __global__ __launch_bounds__(64 * WAVES * TEAMS, sizeof(T) == 4 && DX == 128 && 
   const uint32_t team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.y) : 0;
   bf16* const lds = reinterpret_cast<bf16*>(lds_raw + team * team_bytes<T, DX, NT, WAVES, OUT, WAY>());
   f32x4* const sums = reinterpret_cast<f32x4*>(lds_raw + TEAMS * team_bytes<T, DX, NT, WAVES, OUT, WAY>());
-  // Workgroups go round the 8 dies by their number: the passes over the same rows sit on one die, one behind the other.
+  // Workgroups go round the 8 dies by their number: the passes over the same rows sit on one die.  (That spares little reading: those of
+  // keys and values run against time, that of queries with it, and 2 x 16384 tokens of 16 heads of 128 x 128 miss L2 for 1.5 GB, where
+  // nine readings and three writings by themselves are 1.6.)
   const uint32_t which = blockIdx.x / 8 % all.count, item = blockIdx.x / (8 * all.count) * 8 + blockIdx.x % 8;
   if (item >= all.items) return;
   const AttentionPass& p = all.pass[which];

@@ -144,10 +144,10 @@ size_t fold_bytes(const AttentionSizes& a, uint32_t teams, uint32_t width) {
 // keeps a compute unit busy longer: a chunk takes 1.6 with two teams (2.4 for two workgroups on a compute unit, 1.2 for each of more)
 // and 2.6 with four (each; 3.1 where none waits for another, since then sequences of unlike lengths do not even out), and their starts
 // are one and two chunks longer.  The memory moves at 8 TB/s up to 128 MB, at 4 above.
-// Measured, teams of 1, 2, 4 (64 x 64, 8 heads): that share 2, 32 x 512 tokens 51, 53, 46 us, 64 x 512 108, 81, 86, 256 x 512 441, 313,
-// 262, 48 x 80 28, 30, 33, 8 x 1024 41, 61, 80; that share 4 64 x 512 111, 65, 16 x 80 17, 14, 8 x 512 27, 31.
-// Measured, whole against cut: 64 rows of 1024 tokens (64 x 64) 33 us and 25 in four; 4 rows of 1024 31 and 17 in sixteen; 4 rows of
-// 512 18 and 17; the gradient of 64 rows of 1024 34 and 37 in four; of 32 rows of 16384 (128 x 128) 388 in 5, 423 in 8, 403 in 10.
+// Measured, teams of 1, 2, 4 (64 x 64, 8 heads): that share 2, 32 x 512 tokens 50, 52, 49 us, 64 x 512 102, 82, 91, 256 x 512 445, 315,
+// 278, 48 x 80 26, 30, 33; that share 4 64 x 512 110, 67, 16 x 80 16, 13, 8 x 512 27, 33.
+// Measured, whole against cut: 64 rows of 1024 tokens (64 x 64) 33 us and 26 in four; 4 rows of 1024 32 and 17 in sixteen; 4 rows of
+// 512 18 and 16; the gradient of 64 rows of 1024 33 and 37 in four; of 32 rows of 16384 (128 x 128) 429 in 5, 456 in 8, 462 in 10.
 struct Cut {
   uint32_t segments, segment;
   bool one;   // a gradient's passes in one launch
@@ -238,7 +238,7 @@ hipError_t launch_way(const AttentionPasses& p, hipStream_t s) {
   return pieces ? launch_as<T, DX, NT, WAVES, OUT, PIECES>(p, s) : launch_as<T, DX, NT, WAVES, OUT, ELEMENTS>(p, s);
 }
 // Teams of two waves: more columns to a wave, so that the waves read less LDS (of four waves each, 64 x 64, 128 x 512 tokens with 8
-// heads that share 2: 166 us, of two 139).
+// heads that share 2: 166 us, of two 142).
 template <int DX, int NT>
 hipError_t launch_teams(const AttentionPasses& p, hipStream_t s) {
   bool pieces = true;
