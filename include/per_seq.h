@@ -10,6 +10,9 @@
  *   keys with the rotation
  *   linear attention with a  per_linear_attention (sequences), per_linear_attention_backward (their gradient),
  *   decay for each head      per_linear_attention_step (one token)
+ *   the gated delta rule     per_gated_delta (sequences), per_gated_delta_backward (their gradient), per_gated_delta_step (one token)
+ *   layer norm               per_layer_norm, per_layer_norm_backward
+ *   dropout                  per_dropout (added to a residual if there is one; also its own gradient)
  *
  * Conventions (where they are not those of per.h)
  *  - No handle: every call stands for itself.  It only enqueues work on `stream`; errors are the PER_E* codes of per.h,
@@ -52,6 +55,12 @@ typedef struct per_seq_states {
   float* d;
   int64_t batch, head;
 } per_seq_states;
+
+/* Gates [batch][token][head] in fp32: strides in elements, any of them. */
+typedef struct per_seq_gates {
+  float* d;
+  int64_t batch, token, head;
+} per_seq_gates;
 
 /* Positions [batch][token]; d == NULL: token t is at position t. */
 typedef struct per_seq_positions {
@@ -138,6 +147,79 @@ int per_linear_attention_backward(const per_attention_config* c, const per_seq_r
 int per_linear_attention_step(const per_attention_config* c, const per_seq_rows* q, const per_seq_rows* k,
                               const per_seq_rows* v, const float* d_log_decay, const int32_t* d_lengths,
                               const per_seq_states* state, const per_seq_rows* out, void* stream);
+
+/* ------------------------------------------------------------------------------------------------ gated delta rule */
+typedef struct per_delta_config {
+  uint32_t struct_size;               /* sizeof(per_delta_config)                                                 */
+  uint32_t dtype;
+  uint32_t batch, length;
+  uint32_t heads;                     /* of outputs, states and gates; batch * heads at most 2^22, with the chunks of 32 tokens below 2^24 (one token: 2^23) */
+  uint32_t q_heads, k_heads, v_heads; /* of queries, keys, values: each divides heads, head h reads h / (heads / of them) */
+  uint32_t dk, dv;                    /* widths, 1..128                                                           */
+  float    scale;                     /* of the queries                                                           */
+} per_delta_config;
+
+/* D = exp(log_decay[t]) S[t-1],  u[t] = beta[t] (v[t] - D^T k[t]),  S[t] = D + k[t] u[t]^T,  out[t] = scale * S[t]^T q[t]
+ * for t = 0 .. d_lengths[b]-1 of each sequence and head, from S[-1] = state (NULL: zeros).
+ *   log_decay : natural logarithms, at most 0; -infinity keeps nothing of the state
+ *   beta      : strengths; the rule forgets along k[t], and stays bounded, where 0 <= beta k.k <= 2 (keys of length 1, say)
+ *   d_lengths : as for linear attention.  Tokens behind a sequence's are not read; their outputs are zeros.
+ *   out_state : S behind the last valid token, or NULL.  It may be state.
+ * Rows, states and gates in fp32 are computed to fp32's accuracy whatever the rows' type; results in bfloat16 carry their own rounding and
+ * up to 2^-16 inside.  A value among the valid tokens, or of the state, that is not finite makes all that depends on it not
+ * finite, and may do so to outputs of the up to 31 tokens before it that it shares a chunk of 32 with; sequences and heads do not
+ * reach each other. */
+int per_gated_delta_workspace(const per_delta_config* c, int backward, size_t* bytes);
+int per_gated_delta(const per_delta_config* c, const per_seq_rows* q, const per_seq_rows* k, const per_seq_rows* v,
+                    const per_seq_gates* log_decay, const per_seq_gates* beta, const int32_t* d_lengths, const per_seq_states* state,
+                    const per_seq_rows* out, const per_seq_states* out_state, void* d_work, size_t work_bytes, void* stream);
+
+/* Its gradient: from dout (of out) and dstate (of out_state; NULL: zeros) to dq, dk, dv, the gates' dlog_decay and dbeta, and dstate0 (of
+ * state; NULL where not wanted).  Gradients of rows that several heads share are sums in a fixed order; behind a sequence's end all are
+ * zeros.  In bfloat16 the products of rows round the states (once, to 2^-9) and what else they take (to 2^-17).  dstate0 may be dstate, and not
+ * state. */
+int per_gated_delta_backward(const per_delta_config* c, const per_seq_rows* dout, const per_seq_rows* q, const per_seq_rows* k,
+                             const per_seq_rows* v, const per_seq_gates* log_decay, const per_seq_gates* beta,
+                             const int32_t* d_lengths, const per_seq_states* state, const per_seq_states* dstate,
+                             const per_seq_rows* dq, const per_seq_rows* dk, const per_seq_rows* dv,
+                             const per_seq_gates* dlog_decay, const per_seq_gates* dbeta, const per_seq_states* dstate0,
+                             void* d_work, size_t work_bytes, void* stream);
+
+/* One token for every sequence (length must be 1), the states updated in place.  d_lengths[b] < 1: sequence b stands still
+ * (its state is not touched, its output is zero). */
+int per_gated_delta_step(const per_delta_config* c, const per_seq_rows* q, const per_seq_rows* k, const per_seq_rows* v,
+                         const per_seq_gates* log_decay, const per_seq_gates* beta, const int32_t* d_lengths,
+                         const per_seq_states* state, const per_seq_rows* out, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------- rows of a block */
+/* For these `dim` is the width of a row, and batch, length, heads count rows (heads of 1: plain rows of a sequence). */
+typedef struct per_block_config {
+  uint32_t struct_size;   /* sizeof(per_block_config)                                                             */
+  uint32_t dtype;
+  uint32_t batch, length, heads;   /* at most 2^31 rows                                                           */
+  uint32_t dim;           /* layer norm: 1..65536; dropout: at least 1                                                */
+  float    eps;           /* layer norm: added to the variance                                                     */
+  float    p;             /* dropout: the share that is dropped, 0 <= p < 1, to the nearest 1/65536 (at most 65535 of them) */
+  uint64_t seed, offset;  /* dropout                                                                               */
+} per_block_config;
+
+/* out = (x - mean) / sqrt(variance + eps) * d_weight + d_bias over each row; the variance is that of all dim values.  d_weight, d_bias:
+ * dim values, or NULL for ones and zeros.  out may be x. */
+int per_layer_norm(const per_block_config* c, const per_seq_rows* x, const float* d_weight, const float* d_bias,
+                   const per_seq_rows* out, void* stream);
+
+/* Its gradient: from dout to dx, and d_dweight, d_dbias (dim values each, sums over all rows in a fixed order; NULL where not wanted).
+ * dx may be dout. */
+int per_layer_norm_workspace(const per_block_config* c, size_t* bytes);
+int per_layer_norm_backward(const per_block_config* c, const per_seq_rows* dout, const per_seq_rows* x, const float* d_weight,
+                            const per_seq_rows* dx, float* d_dweight, float* d_dbias, void* d_work, size_t work_bytes, void* stream);
+
+/* out = x kept / (1 - p) (+ residual, if not NULL).  Element i, counted over [batch][length][heads][dim], has the 16 bits i % 8, from the lowest, of
+ * the four words that Philox4x32-10 makes of counter (i / 8, offset + *d_offset) and key seed, and is dropped if they are below 65536 p.  The
+ * same call without a residual on dout is the gradient of x.  d_offset: one value on the device, or NULL for 0; a captured graph that
+ * advances it drops other elements at each replay.  out may be x or residual. */
+int per_dropout(const per_block_config* c, const per_seq_rows* x, const per_seq_rows* residual, const int64_t* d_offset,
+                const per_seq_rows* out, void* stream);
 
 #ifdef __cplusplus
 }

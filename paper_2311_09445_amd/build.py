@@ -12,7 +12,7 @@ OBJECTS = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libper_hip.so")
 BINDING = os.path.join(HERE, "_per_binding.so")
 SEQ_BINDING = os.path.join(HERE, "_seq_binding.so")
-SOURCES = ["per_kernels.hip", "per_api.hip", "seq_api.hip", "seq_rotate.hip", "seq_attention.hip"]
+SOURCES = ["per_kernels.hip", "per_api.hip", "seq_api.hip", "seq_rotate.hip", "seq_attention.hip", "seq_delta.hip", "seq_block.hip"]
 
 # -ffp-contract=off: the tree arithmetic must round after every add and multiply.
 # packed-fp32 ops are switched off for the device pass.

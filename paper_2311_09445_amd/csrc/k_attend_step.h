@@ -11,7 +11,6 @@
 // PAST: states that do not fit the last cache (256 MB) would only push each other out of it: the stores go past it, of more than
 // three times as much the loads too.  Us by size, kept / stores past / both: 128 MB 40 / 43 / 49, 256 MB 82 / 81 / 100, 512 MB
 // 219 / 171 / 205, 1 GB 434 / 433 / 415.
-enum Past { KEPT, STORES_PAST, ALL_PAST };
 
 template <typename T, int VEC, int R, Past PAST>
 __global__ __launch_bounds__(256) void k_attend_step(AttentionStep p) {

@@ -1,0 +1,222 @@
+// The gated delta rule within a chunk: what its tokens make of each other.  Part of seq_delta.hip (included inside namespace per).
+//
+// With G the sums of the decays' logarithms up to each of the 32 tokens, e_ij = exp(G_i - G_j) and
+//   N_ij = e_ij k_i.k_j (i > j),   M_ij = scale e_ij q_i.k_j (i >= j),
+// the tokens write U = diag(beta) Y with Y = (1 + N diag(beta))^-1 (V - e^G K S), and read  scale e^G Q S + M U.  The inverse is what
+// makes the tokens of a chunk independent of each other.  It does not depend on the state, so it is formed for all chunks at once: a wave
+// takes one chunk, the products on the matrix cores straight from memory, the inverse by substitution, a column to a lane (the upper
+// half of the wave forms (1 + diag(beta) N)^-1, which a gradient runs backwards through).
+//
+// What goes into the record of a chunk is laid out as the operands that the passes over the sequence take: places {4 g .. 4 g + 3, 16 + 4 g ..} of
+// the inner dimension in lane 16 g + m, in three parts.
+
+struct Gates {
+  const float* d;
+  int64_t batch, token, head;
+  __device__ __forceinline__ float at(uint32_t b, uint32_t t, uint32_t h) const { return d[(int64_t)b * batch + (int64_t)t * token + (int64_t)h * head]; }
+};
+
+struct DeltaRecord {
+  bf16x8 solve[3][2][64], pairs[3][2][64];
+  float gamma[32], left[32], beta[32];   // e^G, e^(G at the end - G), strengths
+  Keep keep;
+  float pad[30];
+};
+struct DeltaRecordBack {
+  DeltaRecord of;
+  bf16x8 solve_t[3][2][64], pairs_t[3][2][64];
+};
+template <bool BACK>
+struct RecordOf { typedef DeltaRecord type; };
+template <>
+struct RecordOf<true> { typedef DeltaRecordBack type; };
+
+struct DeltaPairs {
+  SeqRows q, k;
+  Gates log_decay, beta;
+  const int32_t* lengths;
+  void* records;
+  uint32_t L, H, dk, chunks, items;
+  float scale;
+};
+
+// Elements col .. col + 7 of a row, zeros behind `width` and where the row is not `on`.  FAST: rows are made of pieces of 16 bytes.
+template <typename T, bool FAST>
+__device__ __forceinline__ Operand<T> row_piece(const T* row, bool on, uint32_t col, uint32_t width) {
+  typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T))));
+  T x[8];
+  if constexpr (FAST) {
+    const bool in = on && col < width;
+    const Vec* at = reinterpret_cast<const Vec*>(row + (col < width ? col : 0));
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      const bool there = sizeof(T) == 2 || (int)col + 4 * i < (int)width;
+      const Vec v = at[there ? i : 0];
+#pragma unroll
+      for (int e = 0; e < 16 / (int)sizeof(T); ++e) x[i * (16 / sizeof(T)) + e] = in && there ? v[e] : T(0.0f);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = on && col + e < width ? row[col + e] : T(0.0f);
+  }
+  if constexpr (sizeof(T) == 2) {
+    Operand<T> o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.v[0][e] = x[e];
+    return o;
+  } else {
+    return Operand<T>::of(f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]});
+  }
+}
+
+// Sums of the logarithms up to each token of a chunk, in 64 bits: differences of far sums keep what a slow decay adds.  A decay that keeps
+// nothing in fp32 anyway (e^-104) counts as e^-10000, so that differences stay numbers.
+__device__ __forceinline__ double decay_sums(const Gates& log_decay, uint32_t b, uint32_t h, uint32_t t, bool on, uint32_t lane) {
+  float x = on ? log_decay.at(b, t, h) : 0.0f;
+  x = x < -1e4f ? -1e4f : x;
+  double G = x;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const double before = __shfl_up(G, d);
+    if ((lane & 31) >= (uint32_t)d) G += before;
+  }
+  return G;
+}
+
+constexpr uint32_t kPairRow = 36;   // floats of a row of 32 in LDS
+
+template <typename T, int DK, bool BACK, bool FAST>
+__device__ __forceinline__ void pair_products(const DeltaPairs& p, uint32_t b, uint32_t h, uint32_t first, uint32_t valid, uint32_t m, uint32_t g,
+                                              f32x4 (&kk)[3], f32x4 (&qk)[3]) {
+  const T *qr[2], *kr[2];
+  bool on[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t t = first + 16 * i + m;
+    on[i] = t < valid;
+    const uint32_t at = on[i] ? t : valid - 1;
+    qr[i] = row_of<T>(p.q, b, at, h);
+    kr[i] = row_of<T>(p.k, b, at, h);
+  }
+#pragma unroll
+  for (int s = 0; s < DK / 32; ++s) {
+    Operand<T> q[2], k[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      q[i] = row_piece<T, FAST>(qr[i], on[i], 32 * s + 8 * g, p.dk);
+      k[i] = row_piece<T, FAST>(kr[i], on[i], 32 * s + 8 * g, p.dk);
+    }
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {   // tiles (0, 0), (1, 0), (1, 1)
+      kk[x] = mma(k[x > 0].v, k[x > 1].v, kk[x]);
+      qk[x] = mma(q[x > 0].v, k[x > 1].v, qk[x]);
+    }
+  }
+}
+
+template <typename T, int DK, bool BACK>
+__global__ __launch_bounds__(256) void k_delta_pairs(DeltaPairs p) {
+  __shared__ __attribute__((aligned(16))) float lds_a[4][32 * kPairRow], lds_b[4][32 * kPairRow], lds_beta[4][32];
+  __shared__ double lds_g[4][32];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const uint32_t item = blockIdx.x * 4 + wave;
+  if (item >= p.items) return;
+  const uint32_t chunk = item % p.chunks, bh = item / p.chunks, h = bh % p.H, b = bh / p.H;
+  const uint32_t valid = valid_tokens(p.lengths, b, p.L), first = chunk * kChunk;
+  if (first >= valid) return;
+  typename RecordOf<BACK>::type* const whole = static_cast<typename RecordOf<BACK>::type*>(p.records) + item;
+  DeltaRecord* const record = reinterpret_cast<DeltaRecord*>(whole);
+  float *const A = lds_a[wave], *const B = lds_b[wave], *const beta = lds_beta[wave];
+  double* const G = lds_g[wave];
+
+  const uint32_t column = lane & 31;
+  const bool here = first + column < valid;
+  const double sum = decay_sums(p.log_decay, b, h, here ? first + column : first, here, lane);
+  const float strength = here ? p.beta.at(b, first + column, h) : 0.0f;
+  if (lane < 32) {
+    G[lane] = sum;
+    beta[lane] = strength;
+  }
+  f32x4 kk[3] = {}, qk[3] = {};
+  if (p.q.wide && p.k.wide && p.dk % (16 / sizeof(T)) == 0) pair_products<T, DK, BACK, true>(p, b, h, first, valid, m, g, kk, qk);
+  else pair_products<T, DK, BACK, false>(p, b, h, first, valid, m, g, kk, qk);
+  wave_sync();
+  const double total = G[31];
+  if (lane < 32) {
+    record->gamma[lane] = expf((float)sum);
+    record->left[lane] = expf((float)(total - sum));
+    record->beta[lane] = strength;
+  }
+  if (lane == 0) record->keep = keeps((float)total);
+#pragma unroll
+  for (int x = 0; x < 3; ++x) {
+    const uint32_t row = 16 * (x > 0) + 4 * g, col = 16 * (x > 1) + m;
+    const double Gj = G[col];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint32_t i = row + r;
+      const float e = expf((float)(G[i] - Gj));
+      kk[x][r] = i > col ? e * kk[x][r] : 0.0f;
+      qk[x][r] = i >= col ? p.scale * e * qk[x][r] : 0.0f;
+      A[i * kPairRow + col] = kk[x][r];
+      B[i * kPairRow + col] = qk[x][r];
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) B[(4 * g + r) * kPairRow + 16 + m] = 0.0f;
+  wave_sync();
+  auto put = [&](bf16x8 (&to)[3][2][64], int tile, f32x4 a, f32x4 c) {
+    const Parts<3> o = Parts<3>::of(a, c);
+#pragma unroll
+    for (int t = 0; t < 3; ++t) to[t][tile][lane] = o.v[t];
+  };
+  auto put_rows = [&](bf16x8 (&to)[3][2][64], const float* from) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float* row = from + (16 * i + m) * kPairRow + 4 * g;
+      put(to, i, *reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + 16));
+    }
+  };
+  put_rows(record->pairs, B);
+  if constexpr (BACK) {
+    put(whole->pairs_t, 0, qk[0], qk[1]);
+    put(whole->pairs_t, 1, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, qk[2]);
+  }
+  const bool other = BACK && lane >= 32;   // (1 + diag(beta) N)^-1
+  float x[32], w[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int l = 0; l + 3 < i + 3; l += 4) {
+      const f32x4 n = *reinterpret_cast<const f32x4*>(A + i * kPairRow + l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (l + e < i) {
+          if (e & 1) s1 = fmaf(n[e], w[l + e], s1);
+          else s0 = fmaf(n[e], w[l + e], s0);
+        }
+    }
+    const float all = s0 + s1, bi = beta[i];
+    x[i] = ((uint32_t)i == column ? 1.0f : 0.0f) - (other ? bi * all : all);
+    w[i] = other ? x[i] : bi * x[i];
+  }
+  wave_sync();
+  float* const X = other ? B : A;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) X[i * kPairRow + column] = x[i];
+  wave_sync();
+  put_rows(record->solve, A);
+  if constexpr (BACK) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      f32x4 a, c;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        a[r] = B[(4 * g + r) * kPairRow + 16 * j + m];
+        c[r] = B[(16 + 4 * g + r) * kPairRow + 16 * j + m];
+      }
+      put(whole->solve_t, j, a, c);
+    }
+  }
+}

@@ -7,7 +7,7 @@
 //     gradient of q:           dout, v, k;  S the state, transposed;              lag 0
 //     gradient of v:           k, q, dout;  S the state's gradient; against time, lag 1
 //     gradient of k:           v, dout, q;  the same, transposed;   against time, lag 1
-#include "dev_seq.h"
+#include "dev_tiles.h"
 
 #include <atomic>
 
@@ -463,9 +463,9 @@ hipError_t launch_attention_backward(const AttentionSizes& a, const per_seq_rows
 
 template <typename T, int VEC, int R>
 static hipError_t step(const AttentionStep& p, uint32_t rows, hipStream_t s) {
-  const uint64_t bytes = (uint64_t)rows * p.dk * p.dv * 4;
-  if (bytes <= 256ull << 20) k_attend_step<T, VEC, R, KEPT><<<rows, 256, 0, s>>>(p);
-  else if (bytes <= 768ull << 20) k_attend_step<T, VEC, R, STORES_PAST><<<rows, 256, 0, s>>>(p);
+  const Past way = past((uint64_t)rows * p.dk * p.dv * 4);
+  if (way == KEPT) k_attend_step<T, VEC, R, KEPT><<<rows, 256, 0, s>>>(p);
+  else if (way == STORES_PAST) k_attend_step<T, VEC, R, STORES_PAST><<<rows, 256, 0, s>>>(p);
   else k_attend_step<T, VEC, R, ALL_PAST><<<rows, 256, 0, s>>>(p);
   return hipGetLastError();
 }

@@ -403,6 +403,257 @@ PyObject* do_norm_rotate_backward(Args a, Py_ssize_t n_args) {
   return answer(rc, {&dq, &dk, &wq, &wk});
 }
 
+struct Delta {
+  per_delta_config c{};
+  Need n;
+  int64_t B, L, H, Q, K, V, dk, dv;
+  per_seq_rows q, k, v;
+  per_seq_gates decay, beta;
+  const int32_t* lengths;
+  // (q, k, v, log_decay, beta, lengths, scale); scale None: 1 / sqrt(dk)
+  Delta(PyObject* oq, PyObject* ok, PyObject* ov, PyObject* odecay, PyObject* obeta, PyObject* olengths, PyObject* oscale, const char* lengths_name = "lengths")
+      : n(need_of(tensor(oq, "q"), "q")) {
+    const at::Tensor &tq = tensor(oq, "q"), &tk = tensor(ok, "k"), &tv = tensor(ov, "v"), &tg = tensor(odecay, "log_decay"), &tb = tensor(obeta, "beta");
+    if (tq.dim() != 4 || tk.dim() != 4 || tv.dim() != 4) raise_value("q, k and v must be [batch, length, heads, width]");
+    if (tg.dim() != 3) raise_value("log_decay: expected [batch, length, heads], got " + shape_of(tg));
+    B = tq.size(0);
+    L = tq.size(1);
+    H = tg.size(2);
+    Q = tq.size(2);
+    K = tk.size(2);
+    V = tv.size(2);
+    dk = tq.size(3);
+    dv = tv.size(3);
+    check(tk, "k", n, n.type, {B, L, K, dk});
+    check(tv, "v", n, n.type, {B, L, V, dv});
+    decay = gates_of(tg, "log_decay");
+    beta = gates_of(tb, "beta");
+    for (int64_t heads : {Q, K, V})
+      if (H ? !heads || H % heads : heads != 0) raise_value("the heads of q, k and v must divide those of log_decay");
+    c.struct_size = sizeof(c);
+    c.dtype = dtype_of(n);
+    c.batch = count(B, "batch");
+    c.length = count(L, "length");
+    c.heads = count(H, "heads");
+    c.q_heads = count(Q, "heads");
+    c.k_heads = count(K, "heads");
+    c.v_heads = count(V, "heads");
+    c.dk = count(dk, "dk");
+    c.dv = count(dv, "dv");
+    c.scale = oscale == Py_None ? 1.0f / sqrtf((float)(dk ? dk : 1)) : (float)real(oscale);
+    q = rows(tq, "q");
+    k = rows(tk, "k");
+    v = rows(tv, "v");
+    lengths = vector<int32_t>(maybe(olengths, lengths_name), lengths_name, n, at::kInt, B);
+  }
+  per_seq_gates gates_of(const at::Tensor& t, const char* name) const {
+    check(t, name, n, at::kFloat, {B, L, H});
+    return per_seq_gates{static_cast<float*>(t.data_ptr()), step_of(t, 0), step_of(t, 1), step_of(t, 2)};
+  }
+  per_seq_rows rows_of(const at::Tensor& t, const char* name, int64_t heads, int64_t width) const {
+    check(t, name, n, n.type, {B, L, heads, width});
+    return rows(t, name);
+  }
+  per_seq_states states_of(const at::Tensor& t, const char* name) const {
+    check(t, name, n, at::kFloat, {B, H, dk, dv});
+    return states(t, name);
+  }
+  at::Tensor work(int backward, size_t* bytes, int* rc) const {
+    *bytes = 0;
+    *rc = per_gated_delta_workspace(&c, backward, bytes);
+    return *rc == 0 && *bytes ? make(n, at::kByte, {(int64_t)*bytes}) : at::Tensor();
+  }
+};
+
+// (q, k, v, log_decay, beta, state, lengths, scale, out, out_state, want_state) -> (code, out, out_state), or None
+PyObject* do_delta(Args a, Py_ssize_t n_args) {
+  expect(n_args, 11);
+  if (differentiated({a[0], a[1], a[2], a[3], a[4], a[5]}, {a[8], a[9]})) Py_RETURN_NONE;
+  const Delta p(a[0], a[1], a[2], a[3], a[4], a[6], a[7]);
+  const c10::DeviceGuard guard(p.n.device);
+  const at::Tensor* in = maybe(a[5], "state");
+  per_seq_states si{}, so{};
+  if (in) si = p.states_of(*in, "state");
+  at::Tensor out = result(a[8], "out", p.n, p.n.type, {p.B, p.L, p.H, p.dv}), last;
+  const per_seq_rows ro = p.rows_of(out, "out", p.H, p.dv);
+  if (truth(a[10])) {
+    last = result(a[9], "out_state", p.n, at::kFloat, {p.B, p.H, p.dk, p.dv});
+    so = p.states_of(last, "out_state");
+  }
+  size_t bytes;
+  int rc;
+  const at::Tensor work = p.work(0, &bytes, &rc);
+  void* s = stream_of(p.n);
+  if (rc == 0)
+    rc = unlocked([&] {
+      return per_gated_delta(&p.c, &p.q, &p.k, &p.v, &p.decay, &p.beta, p.lengths, in ? &si : nullptr, &ro, last.defined() ? &so : nullptr, data(work), bytes, s);
+    });
+  written(rc, {a[8], last.defined() ? a[9] : Py_None});
+  return answer(rc, {&out, &last});
+}
+
+// (dout, q, k, v, log_decay, beta, state, dstate, lengths, scale, dq, dk, dv, dlog_decay, dbeta, dstate0, want_dstate)
+//   -> (code, dq, dk, dv, dlog_decay, dbeta, dstate0)
+PyObject* do_delta_backward(Args a, Py_ssize_t n_args) {
+  expect(n_args, 17);
+  const Delta p(a[1], a[2], a[3], a[4], a[5], a[8], a[9]);
+  const c10::DeviceGuard guard(p.n.device);
+  const per_seq_rows dout = p.rows_of(tensor(a[0], "dout"), "dout", p.H, p.dv);
+  const at::Tensor *in = maybe(a[6], "state"), *din = maybe(a[7], "dstate");
+  per_seq_states si{}, sd{}, so{};
+  if (in) si = p.states_of(*in, "state");
+  if (din) sd = p.states_of(*din, "dstate");
+  at::Tensor dq = result(a[10], "dq", p.n, p.n.type, {p.B, p.L, p.Q, p.dk}), dk = result(a[11], "dk", p.n, p.n.type, {p.B, p.L, p.K, p.dk}),
+             dv = result(a[12], "dv", p.n, p.n.type, {p.B, p.L, p.V, p.dv}), dg = result(a[13], "dlog_decay", p.n, at::kFloat, {p.B, p.L, p.H}),
+             db = result(a[14], "dbeta", p.n, at::kFloat, {p.B, p.L, p.H}), first;
+  const per_seq_rows rq = p.rows_of(dq, "dq", p.Q, p.dk), rk = p.rows_of(dk, "dk", p.K, p.dk), rv = p.rows_of(dv, "dv", p.V, p.dv);
+  const per_seq_gates gg = p.gates_of(dg, "dlog_decay"), gb = p.gates_of(db, "dbeta");
+  if (truth(a[16])) {
+    first = result(a[15], "dstate0", p.n, at::kFloat, {p.B, p.H, p.dk, p.dv});
+    so = p.states_of(first, "dstate0");
+  }
+  size_t bytes;
+  int rc;
+  const at::Tensor work = p.work(1, &bytes, &rc);
+  void* s = stream_of(p.n);
+  if (rc == 0)
+    rc = unlocked([&] {
+      return per_gated_delta_backward(&p.c, &dout, &p.q, &p.k, &p.v, &p.decay, &p.beta, p.lengths, in ? &si : nullptr, din ? &sd : nullptr, &rq, &rk, &rv,
+                                      &gg, &gb, first.defined() ? &so : nullptr, data(work), bytes, s);
+    });
+  written(rc, {a[10], a[11], a[12], a[13], a[14], first.defined() ? a[15] : Py_None});
+  return answer(rc, {&dq, &dk, &dv, &dg, &db, &first});
+}
+
+// (q, k, v, log_decay, beta, state, active, scale, out) -> (code, out)
+PyObject* do_delta_step(Args a, Py_ssize_t n_args) {
+  expect(n_args, 9);
+  differentiated({a[0], a[1], a[2], a[3], a[4]}, {a[5], a[8]});   // (the state is a given result)
+  const Delta p(a[0], a[1], a[2], a[3], a[4], a[6], a[7], "active");
+  const c10::DeviceGuard guard(p.n.device);
+  const per_seq_states st = p.states_of(tensor(a[5], "state"), "state");
+  at::Tensor out = result(a[8], "out", p.n, p.n.type, {p.B, p.L, p.H, p.dv});
+  const per_seq_rows ro = p.rows_of(out, "out", p.H, p.dv);
+  void* s = stream_of(p.n);
+  const int rc = unlocked([&] { return per_gated_delta_step(&p.c, &p.q, &p.k, &p.v, &p.decay, &p.beta, p.lengths, &st, &ro, s); });
+  written(rc, {a[5], a[8]});
+  return answer(rc, {&out});
+}
+
+// Rows [..., dim] of up to four dimensions.
+struct Block {
+  per_block_config c{};
+  Need n;
+  at::IntArrayRef shape;
+  Block(const at::Tensor& x) : n(need_of(x, "x")), shape(x.sizes()) {
+    if (x.dim() < 1 || x.dim() > 4) raise_value("x: expected one to four dimensions, got " + shape_of(x));
+    const int64_t d = x.dim();
+    c.struct_size = sizeof(c);
+    c.dtype = dtype_of(n);
+    c.batch = d > 3 ? count(x.size(d - 4), "x") : 1;
+    c.length = d > 2 ? count(x.size(d - 3), "x") : 1;
+    c.heads = d > 1 ? count(x.size(d - 2), "x") : 1;
+    c.dim = count(x.size(d - 1), "x");
+  }
+  per_seq_rows rows_of(const at::Tensor& t, const char* name) const {
+    if (t.device() != n.device) raise_value(std::string(name) + ": expected a tensor on " + n.device.str() + ", got one on " + t.device().str());
+    if (t.scalar_type() != n.type) raise_value(std::string(name) + ": expected type " + c10::toString(n.type) + ", got " + c10::toString(t.scalar_type()));
+    if (t.sizes() != shape) raise_value(std::string(name) + ": its shape is " + shape_of(t) + ", not that of x");
+    const int64_t d = t.dim();
+    if (t.numel() && t.size(d - 1) > 1 && t.stride(d - 1) != 1) raise_value(std::string(name) + ": the last dimension must be contiguous");
+    return per_seq_rows{t.data_ptr(), d > 3 ? step_of(t, d - 4) : 0, d > 2 ? step_of(t, d - 3) : 0, d > 1 ? step_of(t, d - 2) : 0};
+  }
+  at::Tensor result_of(PyObject* given, const char* name) const {
+    const at::Tensor* t = maybe(given, name);
+    return t ? *t : make(n, n.type, shape);
+  }
+};
+
+// (x, weight, bias, eps, out) -> (code, out), or None
+PyObject* do_layer_norm(Args a, Py_ssize_t n_args) {
+  expect(n_args, 5);
+  if (differentiated({a[0], a[1], a[2]}, {a[4]})) Py_RETURN_NONE;
+  const at::Tensor& x = tensor(a[0], "x");
+  Block p(x);
+  const c10::DeviceGuard guard(p.n.device);
+  p.c.eps = (float)real(a[3]);
+  const float *w = vector<float>(maybe(a[1], "weight"), "weight", p.n, at::kFloat, p.c.dim), *b = vector<float>(maybe(a[2], "bias"), "bias", p.n, at::kFloat, p.c.dim);
+  at::Tensor out = p.result_of(a[4], "out");
+  const per_seq_rows rx = p.rows_of(x, "x"), ro = p.rows_of(out, "out");
+  void* s = stream_of(p.n);
+  const int rc = unlocked([&] { return per_layer_norm(&p.c, &rx, w, b, &ro, s); });
+  written(rc, {a[4]});
+  return answer(rc, {&out});
+}
+
+// (dout, x, weight, eps, dx, want_weights) -> (code, dx, dweight, dbias)
+PyObject* do_layer_norm_backward(Args a, Py_ssize_t n_args) {
+  expect(n_args, 6);
+  const at::Tensor &dout = tensor(a[0], "dout"), &x = tensor(a[1], "x");
+  Block p(x);
+  const c10::DeviceGuard guard(p.n.device);
+  p.c.eps = (float)real(a[3]);
+  const float* w = vector<float>(maybe(a[2], "weight"), "weight", p.n, at::kFloat, p.c.dim);
+  at::Tensor dx = p.result_of(a[4], "dx"), dw, db;
+  const per_seq_rows rd = p.rows_of(dout, "dout"), rx = p.rows_of(x, "x"), ro = p.rows_of(dx, "dx");
+  if (truth(a[5])) {
+    dw = make(p.n, at::kFloat, {(int64_t)p.c.dim});
+    db = make(p.n, at::kFloat, {(int64_t)p.c.dim});
+  }
+  size_t bytes = 0;
+  int rc = per_layer_norm_workspace(&p.c, &bytes);
+  const at::Tensor work = rc == 0 && bytes ? make(p.n, at::kByte, {(int64_t)bytes}) : at::Tensor();
+  void* s = stream_of(p.n);
+  if (rc == 0)
+    rc = unlocked([&] {
+      return per_layer_norm_backward(&p.c, &rd, &rx, w, &ro, static_cast<float*>(data(dw)), static_cast<float*>(data(db)), data(work), bytes, s);
+    });
+  written(rc, {a[4]});
+  return answer(rc, {&dx, &dw, &db});
+}
+
+uint64_t whole(PyObject* o, const char* name) {
+  if (!PyLong_Check(o)) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a whole number, got %.100s", name, Py_TYPE(o)->tp_name);
+    throw Raised{};
+  }
+  const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    raise_value(std::string(name) + ": expected 0 <= " + name + " < 2^64");
+  }
+  return v;
+}
+
+// (x, p, seed, offset, residual, out) -> (code, out), or None.  offset: a number, or an int64 tensor of one value on the device
+PyObject* do_dropout(Args a, Py_ssize_t n_args) {
+  expect(n_args, 6);
+  if (differentiated({a[0], a[4]}, {a[5]})) Py_RETURN_NONE;
+  const at::Tensor& x = tensor(a[0], "x");
+  Block p(x);
+  const c10::DeviceGuard guard(p.n.device);
+  p.c.p = (float)real(a[1]);
+  if (!(p.c.p >= 0.0f && p.c.p < 1.0f)) raise_value("p: expected 0 <= p < 1");
+  p.c.seed = whole(a[2], "seed");
+  const int64_t* at_offset = nullptr;
+  if (THPVariable_Check(a[3])) {
+    const at::Tensor& o = THPVariable_Unpack(a[3]);
+    if (o.device() != p.n.device || o.scalar_type() != at::kLong || o.numel() != 1) raise_value("offset: expected a number, or an int64 tensor of one value on " + p.n.device.str());
+    at_offset = static_cast<const int64_t*>(o.data_ptr());
+  } else {
+    p.c.offset = whole(a[3], "offset");
+  }
+  const at::Tensor* residual = maybe(a[4], "residual");
+  per_seq_rows rr{};
+  if (residual) rr = p.rows_of(*residual, "residual");
+  at::Tensor out = p.result_of(a[5], "out");
+  const per_seq_rows rx = p.rows_of(x, "x"), ro = p.rows_of(out, "out");
+  void* s = stream_of(p.n);
+  const int rc = unlocked([&] { return per_dropout(&p.c, &rx, residual ? &rr : nullptr, at_offset, &ro, s); });
+  written(rc, {a[5]});
+  return answer(rc, {&out});
+}
+
 // Every function: C++ and library errors become Python exceptions, nothing is thrown past the interpreter.
 template <PyObject* (*F)(Args, Py_ssize_t)>
 PyObject* function(PyObject*, Args a, Py_ssize_t n) {
@@ -420,7 +671,10 @@ constexpr PyMethodDef entry(const char* name) {
 }
 PyMethodDef functions[] = {entry<do_attention>("linear_attention"), entry<do_attention_backward>("linear_attention_backward"),
                            entry<do_attention_step>("linear_attention_step"), entry<do_rotate>("rotate"), entry<do_norm_rotate>("norm_rotate"),
-                           entry<do_norm_rotate_backward>("norm_rotate_backward"), {nullptr, nullptr, 0, nullptr}};
+                           entry<do_norm_rotate_backward>("norm_rotate_backward"), entry<do_delta>("gated_delta"),
+                           entry<do_delta_backward>("gated_delta_backward"), entry<do_delta_step>("gated_delta_step"),
+                           entry<do_layer_norm>("layer_norm"), entry<do_layer_norm_backward>("layer_norm_backward"),
+                           entry<do_dropout>("dropout"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_seq_binding", "The sequence operators, tensors in, C-ABI calls out.", -1, functions};
 
 }  // namespace

@@ -1,0 +1,262 @@
+// The gated delta rule: a state that is decayed, corrected and read.
+//
+//   D = exp(g_t) S[t-1],  u_t = beta_t (v_t - D^T k_t),  S[t] = D + k_t u_t^T,  out_t = scale S[t]^T q_t.
+//
+// Sequences are taken in chunks of 32 tokens (k_gated_pairs.h: what a chunk's tokens make of each other, all chunks at once; k_gated_run.h: the
+// states one chunk behind the other; k_gated_back.h: the gradient, against time and then all chunks at once), single tokens in k_gated_step.h.
+#include <atomic>
+
+#include "dev_parts.h"
+
+namespace per {
+
+namespace {
+
+#include "k_gated_pairs.h"
+#include "k_gated_run.h"
+#include "k_gated_back.h"
+#include "k_gated_step.h"
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+Gates gates(const per_seq_gates& g) { return Gates{g.d, g.batch, g.token, g.head}; }
+uint32_t chunks_of(uint32_t L) { return (L + kChunk - 1) / kChunk; }
+// (256 divides every chunk's part of a workspace, so that the parts stay aligned)
+uint32_t padded(uint32_t dk) { return dk <= 64 ? 64 : 128; }
+
+// Where a gradient's intermediate results lie in the workspace.
+struct BackWork {
+  size_t records, states, dstates, y, dz, along, strength, border, fold_q, fold_k, bytes;
+};
+BackWork back_work(const DeltaSizes& a) {
+  const uint64_t bh = (uint64_t)a.B * a.H, chunks = bh * chunks_of(a.L), tokens = chunks * kChunk;
+  const uint64_t blocks = (a.dv + 31) / 32, parts = blocks * 2, e = a.dtype == PER_SEQ_BF16;
+  BackWork w{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += align256(bytes);
+    return here;
+  };
+  const uint64_t state = blocks * 32 * padded(a.dk) * sizeof(bf16);
+  w.records = take(chunks * sizeof(DeltaRecordBack));
+  w.states = take(chunks * state * (e ? 2 : 3));
+  w.dstates = take(chunks * state * (e ? 1 : 3));
+  w.y = take(tokens * blocks * 32 * sizeof(float));
+  w.dz = take(tokens * blocks * 32 * sizeof(float));
+  w.along = take(tokens * parts * sizeof(float));
+  w.strength = take(tokens * parts * sizeof(float));
+  w.border = take(chunks * parts * sizeof(float));
+  w.fold_q = take(a.Q == a.H ? 0 : tokens * a.dk * sizeof(float));
+  w.fold_k = take(a.K == a.H ? 0 : tokens * a.dk * sizeof(float));
+  w.bytes = at;
+  return w;
+}
+
+// A launch with more than 64 KB of LDS: granted once per kernel and device.
+template <typename Args>
+hipError_t launch(void (*kernel)(Args), std::atomic<uint64_t>* granted, uint32_t grid, uint32_t lds, const Args& args, hipStream_t s) {
+  if (lds > 64 * 1024) {
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (!(granted->load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+      granted->fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  kernel<<<grid, 256, lds, s>>>(args);
+  return hipGetLastError();
+}
+template <typename T, int DK, DeltaMode MODE>
+hipError_t launch_run(const DeltaRun& p, uint32_t bh, hipStream_t s) {
+  static std::atomic<uint64_t> granted{0};
+  return launch(k_delta_run<T, DK, MODE>, &granted, bh * p.slices, run_lds<T, DK>(), p, s);
+}
+template <typename T, int DK>
+hipError_t launch_back(const DeltaBack& p, uint32_t bh, hipStream_t s) {
+  static std::atomic<uint64_t> granted{0};
+  return launch(k_delta_back<T, DK>, &granted, bh * p.slices, run_lds<T, DK>(), p, s);
+}
+template <typename T, int DK>
+hipError_t launch_grads(const DeltaGrads& p, uint32_t bh, hipStream_t s) {
+  static std::atomic<uint64_t> granted{0};
+  return launch(k_delta_grads<T, DK>, &granted, bh * p.chunks, grads_lds<T, DK>(), p, s);
+}
+template <typename T, int DK, bool BACK>
+hipError_t launch_pairs(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, void* records, hipStream_t s) {
+  const uint32_t items = a.B * a.H * chunks_of(a.L);
+  if (!items) return hipSuccess;
+  const DeltaPairs p{rows(q, a.dtype, a.H / a.Q), rows(k, a.dtype, a.H / a.K), gates(a.log_decay), gates(a.beta), a.lengths, records,
+                     a.L, a.H, a.dk, chunks_of(a.L), items, a.scale};
+  k_delta_pairs<T, DK, BACK><<<(items + 3) / 4, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+DeltaRun make_run(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state, const void* records) {
+  DeltaRun p{};
+  p.q = rows(q, a.dtype, a.H / a.Q);
+  p.k = rows(k, a.dtype, a.H / a.K);
+  p.v = rows(v, a.dtype, a.H / a.V);
+  p.records = records;
+  p.lengths = a.lengths;
+  if (state) { p.in = state->d; p.in_batch = state->batch; p.in_head = state->head; }
+  p.L = a.L;
+  p.H = a.H;
+  p.dk = a.dk;
+  p.dv = a.dv;
+  p.chunks = chunks_of(a.L);
+  p.slices = (a.dv + 63) / 64;
+  p.scale = a.scale;
+  return p;
+}
+
+template <typename T, int DK>
+hipError_t forward(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state,
+                   const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
+  const hipError_t e = launch_pairs<T, DK, false>(a, q, k, work, s);
+  if (e != hipSuccess) return e;
+  DeltaRun p = make_run(a, q, k, v, state, work);
+  p.out = rows(out, a.dtype, 1);
+  if (out_state) { p.to = out_state->d; p.to_batch = out_state->batch; p.to_head = out_state->head; }
+  return launch_run<T, DK, FORWARD>(p, a.B * a.H, s);
+}
+
+template <typename T>
+hipError_t fold(const DeltaSizes& a, const float* from, const per_seq_rows& to, uint32_t n, uint32_t width, uint32_t stride, hipStream_t s) {
+  const DeltaFold f{from, rows(to, a.dtype, 1), a.lengths, (uint64_t)a.B * a.L * n, a.L, a.H, n, width, stride, chunks_of(a.L) * kChunk};
+  if (!f.rows) return hipSuccess;
+  const uint32_t per = 256 / ((width + 3) / 4);
+  const uint64_t blocks = (f.rows + per - 1) / per;
+  k_delta_fold<T><<<(uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), 256, 0, s>>>(f);
+  return hipGetLastError();
+}
+
+template <typename T, int DK>
+hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
+                    const per_seq_states* state, const per_seq_states* dstate, const per_seq_rows& dq, const per_seq_rows& dk,
+                    const per_seq_rows& dv, const per_seq_gates& dlog_decay, const per_seq_gates& dbeta, const per_seq_states* dstate0,
+                    void* work, hipStream_t s) {
+  const BackWork w = back_work(a);
+  uint8_t* const at = static_cast<uint8_t*>(work);
+  auto floats = [&](size_t o) { return reinterpret_cast<float*>(at + o); };
+  const uint32_t bh = a.B * a.H;
+  hipError_t e = launch_pairs<T, DK, true>(a, q, k, at + w.records, s);
+  if (e != hipSuccess) return e;
+  DeltaRun run = make_run(a, q, k, v, state, at + w.records);
+  run.dout = rows(dout, a.dtype, 1);
+  run.states = reinterpret_cast<bf16*>(at + w.states);
+  run.y = floats(w.y);
+  run.along = floats(w.along);
+  if (run.chunks) e = launch_run<T, DK, KEEPING>(run, bh, s);
+  if (e != hipSuccess) return e;
+  DeltaBack b{};
+  b.q = run.q;
+  b.k = run.k;
+  b.v = run.v;
+  b.dout = run.dout;
+  b.dv = rows(dv, a.dtype, 1);
+  b.records = run.records;
+  b.lengths = a.lengths;
+  if (dstate) { b.in = dstate->d; b.in_batch = dstate->batch; b.in_head = dstate->head; }
+  if (dstate0) { b.to = dstate0->d; b.to_batch = dstate0->batch; b.to_head = dstate0->head; }
+  b.L = a.L;
+  b.H = a.H;
+  b.dk = a.dk;
+  b.dvw = a.dv;
+  b.chunks = run.chunks;
+  b.slices = run.slices;
+  b.scale = a.scale;
+  b.direct = a.V == a.H;
+  b.states = run.states;
+  b.y = run.y;
+  b.dstates = reinterpret_cast<bf16*>(at + w.dstates);
+  b.dz = floats(w.dz);
+  b.along = run.along;
+  b.strength = floats(w.strength);
+  b.border = floats(w.border);
+  e = launch_back<T, DK>(b, bh, s);
+  if (e != hipSuccess || !run.chunks) return e;
+  DeltaGrads g{};
+  g.q = run.q;
+  g.k = run.k;
+  g.dout = run.dout;
+  g.dq = rows(dq, a.dtype, 1);
+  g.dk = rows(dk, a.dtype, 1);
+  g.log_decay = gates(a.log_decay);
+  g.beta = gates(a.beta);
+  g.dlog_decay = gates(dlog_decay);
+  g.dbeta = gates(dbeta);
+  g.lengths = a.lengths;
+  g.L = a.L;
+  g.H = a.H;
+  g.dkw = a.dk;
+  g.dv = a.dv;
+  g.chunks = run.chunks;
+  g.scale = a.scale;
+  g.direct_q = a.Q == a.H;
+  g.direct_k = a.K == a.H;
+  g.fold_q = floats(w.fold_q);
+  g.fold_k = floats(w.fold_k);
+  g.states = run.states;
+  g.dstates = b.dstates;
+  g.y = run.y;
+  g.dz = b.dz;
+  g.along = run.along;
+  g.strength = b.strength;
+  g.border = b.border;
+  e = launch_grads<T, DK>(g, bh, s);
+  if (e == hipSuccess && !g.direct_q) e = fold<T>(a, g.fold_q, dq, a.Q, a.dk, a.dk, s);
+  if (e == hipSuccess && !g.direct_k) e = fold<T>(a, g.fold_k, dk, a.K, a.dk, a.dk, s);
+  if (e == hipSuccess && !b.direct) e = fold<T>(a, b.dz, dv, a.V, a.dv, (a.dv + 31) / 32 * 32, s);
+  return e;
+}
+
+template <typename T, int VEC, int R>
+hipError_t step(const DeltaStep& p, uint32_t rows, hipStream_t s) {
+  const Past way = past((uint64_t)rows * p.dk * p.dv * 4);
+  if (way == KEPT) k_delta_step<T, VEC, R, KEPT><<<rows, 256, 0, s>>>(p);
+  else if (way == STORES_PAST) k_delta_step<T, VEC, R, STORES_PAST><<<rows, 256, 0, s>>>(p);
+  else k_delta_step<T, VEC, R, ALL_PAST><<<rows, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t step(DeltaStep p, uint32_t rows, hipStream_t s) {
+  const bool wide = p.dv % 4 == 0 && (reinterpret_cast<uintptr_t>(p.state.d) & 15) == 0 && p.state.batch % 4 == 0 && p.state.head % 4 == 0;
+  const uint32_t columns = wide ? p.dv / 4 : p.dv;
+  p.groups = 256 / columns < p.dk ? 256 / columns : p.dk;
+  const uint32_t held = (p.dk + p.groups - 1) / p.groups;   // rows of a thread
+  if (!wide) return held <= 16 ? step<T, 1, 16>(p, rows, s) : step<T, 1, 64>(p, rows, s);
+  return held <= 4 ? step<T, 4, 4>(p, rows, s) : step<T, 4, 16>(p, rows, s);
+}
+
+}  // namespace
+
+size_t delta_work_bytes(const DeltaSizes& a, bool backward) {
+  if (!a.B || !a.H || !a.L) return 0;
+  return backward ? back_work(a).bytes : (size_t)a.B * a.H * chunks_of(a.L) * sizeof(DeltaRecord);
+}
+
+hipError_t launch_delta(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state,
+                        const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
+  auto* call = a.dtype == PER_SEQ_BF16 ? (a.dk <= 64 ? forward<bf16, 64> : forward<bf16, 128>) : (a.dk <= 64 ? forward<float, 64> : forward<float, 128>);
+  return call(a, q, k, v, state, out, out_state, work, s);
+}
+
+hipError_t launch_delta_backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
+                                 const per_seq_states* state, const per_seq_states* dstate, const per_seq_rows& dq, const per_seq_rows& dk,
+                                 const per_seq_rows& dv, const per_seq_gates& dlog_decay, const per_seq_gates& dbeta,
+                                 const per_seq_states* dstate0, void* work, hipStream_t s) {
+  auto* call = a.dtype == PER_SEQ_BF16 ? (a.dk <= 64 ? backward<bf16, 64> : backward<bf16, 128>) : (a.dk <= 64 ? backward<float, 64> : backward<float, 128>);
+  return call(a, dout, q, k, v, state, dstate, dq, dk, dv, dlog_decay, dbeta, dstate0, work, s);
+}
+
+hipError_t launch_delta_step(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
+                             const per_seq_states& state, const per_seq_rows& out, hipStream_t s) {
+  const DeltaStep p{rows(q, a.dtype, a.H / a.Q), rows(k, a.dtype, a.H / a.K), rows(v, a.dtype, a.H / a.V), rows(out, a.dtype, 1),
+                    gates(a.log_decay), gates(a.beta), SeqStates{state.d, state.batch, state.head}, a.H, a.dk, a.dv, 0, a.scale, a.lengths};
+  return a.dtype == PER_SEQ_BF16 ? step<bf16>(p, a.B * a.H, s) : step<float>(p, a.B * a.H, s);
+}
+
+}  // namespace per

@@ -34,6 +34,10 @@ struct SeqStates {
   int64_t batch, head;
 };
 
+// How states larger than the last cache are read and written (see k_attend_step.h).
+enum Past { KEPT, STORES_PAST, ALL_PAST };
+inline Past past(uint64_t state_bytes) { return state_bytes <= 256ull << 20 ? KEPT : state_bytes <= 768ull << 20 ? STORES_PAST : ALL_PAST; }
+
 // Sizes of a linear attention.
 struct AttentionSizes {
   uint32_t dtype, B, L, H, G, dk, dv;
@@ -52,6 +56,24 @@ hipError_t launch_attention_backward(const AttentionSizes& a, const per_seq_rows
                                      const per_seq_rows& dv, const per_seq_states* dstate0, void* work, hipStream_t s);
 hipError_t launch_attention_step(const AttentionSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
                                  const per_seq_states& state, const per_seq_rows& out, hipStream_t s);
+
+// Sizes of a gated delta rule; its gates [batch][token][head].
+struct DeltaSizes {
+  uint32_t dtype, B, L, H, Q, K, V, dk, dv;
+  float scale;
+  per_seq_gates log_decay, beta;
+  const int32_t* lengths;
+};
+
+size_t delta_work_bytes(const DeltaSizes& a, bool backward);
+hipError_t launch_delta(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state,
+                        const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s);
+hipError_t launch_delta_backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
+                                 const per_seq_states* state, const per_seq_states* dstate, const per_seq_rows& dq, const per_seq_rows& dk,
+                                 const per_seq_rows& dv, const per_seq_gates& dlog_decay, const per_seq_gates& dbeta,
+                                 const per_seq_states* dstate0, void* work, hipStream_t s);
+hipError_t launch_delta_step(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v,
+                             const per_seq_states& state, const per_seq_rows& out, hipStream_t s);
 
 // One tensor of a rotation: its rows, where they go, the norm's weight.
 struct RotarySide {
@@ -72,6 +94,22 @@ struct RotaryArgs {
   // the workgroups of either
   uint32_t tokens[2], tiles[2], blocks[2];
 };
+
+// Rows of a block: layer norm and dropout.
+struct BlockArgs {
+  SeqRows x, more, out;   // more: dout, or the residual
+  const float *weight, *bias;
+  float *dweight, *dbias, *partial;
+  uint32_t B, L, H, dim;
+  float eps;
+  uint32_t border;        // of 65536: dropped below
+  uint64_t seed, offset;
+  const int64_t* d_offset;
+};
+size_t norm_work_bytes(uint32_t dtype, const BlockArgs& a);
+hipError_t launch_layer_norm(uint32_t dtype, const BlockArgs& a, hipStream_t s);
+hipError_t launch_layer_norm_backward(uint32_t dtype, const BlockArgs& a, hipStream_t s);
+hipError_t launch_dropout(uint32_t dtype, const BlockArgs& a, hipStream_t s);
 
 enum RotaryKind { ROTATE, NORM_ROTATE, NORM_ROTATE_BACK };
 size_t rotary_work_bytes(uint64_t tokens, uint32_t heads, uint32_t dim);

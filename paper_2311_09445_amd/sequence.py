@@ -25,6 +25,8 @@ BINDING_PATH = os.path.join(_HERE, "_seq_binding.so")
 EXPORTS = [
     "per_rotate", "per_norm_rotate", "per_norm_rotate_workspace", "per_norm_rotate_backward", "per_linear_attention_workspace",
     "per_linear_attention", "per_linear_attention_backward", "per_linear_attention_step",
+    "per_gated_delta_workspace", "per_gated_delta", "per_gated_delta_backward", "per_gated_delta_step",
+    "per_layer_norm", "per_layer_norm_workspace", "per_layer_norm_backward", "per_dropout",
 ]
 LAYOUTS = {"half": 0, "interleaved": 1}
 
@@ -162,6 +164,81 @@ def linear_attention_step(q, k, v, log_decay, state, active=None, scale=None, ou
     return out
 
 
+# ------------------------------------------------------------------------------------------------------ gated delta rule
+def gated_delta(q, k, v, log_decay, beta, state=None, lengths=None, scale=None, out=None, out_state=None, want_state: bool = True):
+    """D = exp(log_decay[t]) S[t-1];  u[t] = beta[t] (v[t] - D^T k[t]);  S[t] = D + k[t] u[t]^T;  out[t] = scale S[t]^T q[t].
+    Returns (out, last state or None).
+
+    q [B, L, Q, dk], k [B, L, K, dk], v [B, L, V, dv] with Q, K and V dividing H; ``log_decay`` (at most 0) and ``beta`` fp32
+    [B, L, H] of any strides; ``state`` fp32 [B, H, dk, dv] or None (zeros); ``lengths`` int32 [B] or None: valid tokens of each
+    sequence (behind them nothing is read and the outputs are zeros); ``scale``: 1 / sqrt(dk) if None.  States are computed to
+    fp32's accuracy whatever the type of the rows."""
+    done = _calls().gated_delta(q, k, v, log_decay, beta, state, lengths, scale, out, out_state, want_state or out_state is not None)
+    if done is None:
+        out, last = _function(3).apply(q, k, v, log_decay, beta, state, lengths, scale)
+        return out, last if want_state else None
+    rc, out, last = done
+    if rc:
+        raise PerError(rc, "per_gated_delta")
+    return out, last
+
+
+def gated_delta_backward(dout, q, k, v, log_decay, beta, state=None, dstate=None, lengths=None, scale=None, dq=None, dk=None, dv=None,
+                         dlog_decay=None, dbeta=None, dstate0=None, want_dstate: bool = True):
+    """Gradient of ``gated_delta``: from ``dout`` and ``dstate`` (of the last state; None: zeros) to (dq, dk, dv, dlog_decay, dbeta,
+    gradient of ``state`` or None)."""
+    rc, dq, dk, dv, dg, db, first = _calls().gated_delta_backward(dout, q, k, v, log_decay, beta, state, dstate, lengths, scale, dq, dk, dv, dlog_decay,
+                                                                  dbeta, dstate0, want_dstate or dstate0 is not None)
+    if rc:
+        raise PerError(rc, "per_gated_delta_backward")
+    return dq, dk, dv, dg, db, first
+
+
+def gated_delta_step(q, k, v, log_decay, beta, state, active=None, scale=None, out=None):
+    """One token (length 1) of ``gated_delta`` with the states [B, H, dk, dv] updated in place.  ``active`` int32 [B] or None:
+    where it is 0 the state is not touched and the output is zero.  No gradient is formed: refused where one is asked for.  Returns out."""
+    rc, out = _calls().gated_delta_step(q, k, v, log_decay, beta, state, active, scale, out)
+    if rc:
+        raise PerError(rc, "per_gated_delta_step")
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------- rows of a block
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None):
+    """(x - mean) / sqrt(variance + eps) * weight + bias over the last dimension of ``x`` (one to four dimensions, any strides but
+    the last); ``weight`` and ``bias`` fp32 [D], or None.  ``out`` may be ``x``."""
+    done = _calls().layer_norm(x, weight, bias, eps, out)
+    if done is None:
+        return _function(4).apply(x, weight, bias, eps)
+    rc, out = done
+    if rc:
+        raise PerError(rc, "per_layer_norm")
+    return out
+
+
+def layer_norm_backward(dout, x, weight=None, eps: float = 1e-5, dx=None, want_weights: bool = True):
+    """Gradient of ``layer_norm``: (dx, dweight, dbias), the last two (fp32 [D]) None without ``want_weights``.  dx may be dout."""
+    rc, dx, dw, db = _calls().layer_norm_backward(dout, x, weight, eps, dx, want_weights)
+    if rc:
+        raise PerError(rc, "per_layer_norm_backward")
+    return dx, dw, db
+
+
+def dropout(x, p: float, seed: int, offset=0, residual=None, out=None):
+    """``x`` with the share ``p`` of its elements dropped (to the nearest 1/65536) and the others divided by 1 - p, plus ``residual``
+    if there is one.  What is dropped is a function of ``seed``, ``offset`` and the element's place alone (``include/per_seq.h``):
+    nothing is stored for the gradient, which is the same call on that of the output.  ``offset`` is a number, or an int64 tensor
+    of one value on the device, which a captured graph may advance; it must not change between a call and its gradient.  ``out``
+    may be ``x`` or ``residual``."""
+    done = _calls().dropout(x, p, seed, offset, residual, out)
+    if done is None:
+        return _function(5).apply(x, p, seed, offset, residual)
+    rc, out = done
+    if rc:
+        raise PerError(rc, "per_dropout")
+    return out
+
+
 # ------------------------------------------------------------------------------------------------------------- autograd
 def _functions():
     import torch
@@ -210,7 +287,53 @@ def _functions():
         def backward(ctx, dout):
             return rotate(dout.contiguous(), *ctx.saved_tensors, *ctx.how), None, None, None, None, None
 
-    return NormRotate, LinearAttention, Rotate
+    class GatedDelta(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, log_decay, beta, state, lengths, scale):
+            ctx.save_for_backward(q, k, v, log_decay, beta, state, lengths)
+            ctx.scale = scale
+            return gated_delta(q, k, v, log_decay, beta, state, lengths, scale)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dout, dstate):
+            q, k, v, log_decay, beta, state, lengths = ctx.saved_tensors
+            want = ctx.needs_input_grad[5]
+            dq, dk, dv, dg, db, first = gated_delta_backward(dout.contiguous(), q, k, v, log_decay, beta, state,
+                                                             None if dstate is None else dstate.contiguous(), lengths, ctx.scale, want_dstate=want)
+            return dq, dk, dv, dg, db, first, None, None
+
+    class LayerNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, eps):
+            ctx.save_for_backward(x, weight)
+            ctx.eps, ctx.bias = eps, bias is not None
+            return layer_norm(x, weight, bias, eps)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dout):
+            x, weight = ctx.saved_tensors
+            want = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
+            dx, dw, db = layer_norm_backward(dout.contiguous(), x, weight, ctx.eps, want_weights=want)
+            return dx, dw if weight is not None else None, db if ctx.bias else None, None
+
+    class Dropout(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, p, seed, offset, residual):
+            moves = isinstance(offset, torch.Tensor)
+            ctx.save_for_backward(offset if moves else None)
+            ctx.how = (p, seed, None if moves else offset)
+            return dropout(x, p, seed, offset, residual)
+
+        @staticmethod
+        def backward(ctx, dout):
+            p, seed, offset = ctx.how
+            offset = ctx.saved_tensors[0] if offset is None else offset
+            dx = dropout(dout.contiguous(), p, seed, offset) if ctx.needs_input_grad[0] else None
+            return dx, None, None, None, dout if ctx.needs_input_grad[4] else None
+
+    return NormRotate, LinearAttention, Rotate, GatedDelta, LayerNorm, Dropout
 
 
 _FUNCTIONS = None

@@ -1,0 +1,510 @@
+"""The gated delta rule on the GPU against its definition in 64 bits.
+
+How far results may be off.  Unit roundoffs: 2^-24 in fp32, 2^-8 in bfloat16.  A state goes through one round of products for each 32
+tokens: sums over dk and 32 terms in fp32 (roundings of either sign: about the root of their number of them in 2-norm), of factors taken
+apart into 24 bits; with keys of length 1 and strengths up to 1 what one round is off is not enlarged by the next.  So states, and all that is
+fp32, are held to  u(T, d) = 2^-24 (6 + sqrt(d)) (1 + sqrt(T / 32))  of themselves by the 2-norm, and gradients, which take states and
+the states' gradients, to four times that.  A single element may be off by 16 times the root mean square of that.
+Results in bfloat16 are rounded once, 2^-8 of an element at most; inside, outputs and gradients of values keep 2^-16.  Gradients
+of queries and keys take states rounded to bfloat16: each product is then off by up to 2^-8 of its terms, of either sign, that is by
+2^-8 of the root mean square in 2-norm and a few times that in an element.  The terms of an element are those of its token: with R the state's
+gradient, of which an element is off by up to 2^-8 of itself, dk = R u is off by sqrt(sum over j of (2^-8 R_ij u_j)^2) in the mean, as large as 2^-8 of
+the root mean square of R u over the token's row, and rows differ by more than ten times (tokens next to the end see a dstate of
+size 1 in each element).  So an element is held to its row's root mean square where that is the larger one.
+
+Where there is one token of one element nothing is averaged: the state is D + k u, two terms that may cancel, each off by its roundings.  So
+there the state, and the output and dq that it is a factor of, are held to (|D| + |k u|) / |D + k u| times as much."""
+import math
+
+import pytest
+import torch
+
+import block_oracle as oracle
+from paper_2311_09445_amd import sequence as seq
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+TYPES = pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+
+
+def normal(seed, *shape, dtype=F32):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g, dtype=torch.float32).to(dtype).cuda()
+
+
+def unit(t):
+    return t / t.norm(dim=-1, keepdim=True)
+
+
+def inputs(B, L, H, Q, K, V, dk, dv, dtype, seed=1, ragged=False, fast=0.5):
+    q, k = (unit(normal(seed + i, B, L, n, dk)).to(dtype) for i, n in enumerate((Q, K)))
+    v = normal(seed + 2, B, L, V, dv, dtype=dtype)
+    g = -fast * torch.nn.functional.softplus(normal(seed + 3, B, L, H))
+    beta = torch.sigmoid(normal(seed + 4, B, L, H))
+    S = 0.3 * normal(seed + 5, B, H, dk, dv)
+    lengths = None
+    if ragged:
+        lengths = torch.randint(0, L + 1, (B,), generator=torch.Generator().manual_seed(seed), dtype=torch.int32)
+        lengths[0] = L
+        lengths = lengths.cuda()
+    return q, k, v, g, beta, S, lengths
+
+
+def u32(T, d):
+    return oracle.U_F32 * (6 + math.sqrt(d)) * (1 + math.sqrt(T / 32))
+
+
+def cancelled(k, v, g, beta, S, T, dk, dv):
+    """(|D| + |k u|) / |D + k u| of one token of one element, else 1."""
+    if (T, dk, dv) != (1, 1, 1):
+        return 1.0
+    k, v, a, beta, S = (float(oracle.f64(t).flatten()[0]) for t in (k, v, g.exp(), beta, S))
+    D = a * S
+    u = beta * (v - D * k)
+    return (abs(D) + abs(k * u)) / abs(D + k * u)
+
+
+def near(got, want, rel, what, element=0.0):
+    """Within `rel` of the 2-norm, elements within 16 times that of the root mean square (of all, or of their row) and `element` of themselves."""
+    got = oracle.f64(got)
+    assert got.shape == want.shape, what
+    assert torch.isfinite(got).all(), what
+    if not want.numel():
+        return
+    rms = float(want.norm()) / math.sqrt(want.numel())
+    rows = (want.norm(dim=-1, keepdim=True) / math.sqrt(want.shape[-1])).clamp(min=rms)
+    off = got - want
+    size = float(want.norm()) or 1.0
+    assert float(off.norm()) <= (rel + element) * size + 1e-30, f"{what}: 2-norm off by {float(off.norm()) / size:.3g}, allowed {rel + element:.3g}"
+    worst = float(((off.abs() - element * want.abs()) / (rows + 1e-30)).max())
+    assert worst <= 16 * rel, f"{what}: an element off by {worst:.3g} of the root mean square, allowed {16 * rel:.3g}"
+
+
+def check_out(got, want, T, d, dtype, what="out", more=1.0):
+    if dtype == BF16:
+        near(got, want, more * 2 ** -15, what, element=oracle.U_BF16)
+    else:
+        near(got, want, more * u32(T, d), what)
+
+
+def check_grads(got, want, T, d, dtype, more=1.0):
+    for name, x, y in zip(("dq", "dk", "dv", "dlog_decay", "dbeta", "dstate"), got, want):
+        if name == "dq" and more > 1:
+            near(x, y, more * (oracle.U_BF16 if dtype == BF16 else 4 * u32(T, d)), name)
+        elif dtype == BF16 and name in ("dq", "dk"):
+            near(x, y, oracle.U_BF16 / 2, name, element=oracle.U_BF16)
+        elif dtype == BF16 and name == "dv":
+            near(x, y, 2 ** -14, name, element=oracle.U_BF16)
+        else:
+            near(x, y, 4 * u32(T, d), name)
+
+
+SHAPES = [(1, 1, 1, 1, 1, 1, 1, 1), (2, 31, 2, 2, 2, 2, 64, 64), (2, 32, 2, 1, 1, 2, 64, 64), (3, 33, 4, 4, 2, 2, 32, 16), (2, 65, 2, 2, 2, 1, 128, 128),
+          (1, 100, 6, 6, 2, 2, 48, 80), (2, 97, 4, 2, 2, 4, 17, 5), (5, 64, 3, 3, 3, 3, 128, 40), (2, 130, 6, 2, 3, 1, 61, 127), (1, 257, 2, 2, 2, 2, 65, 33),
+          (4, 40, 2, 2, 2, 2, 3, 128)]
+
+
+@TYPES
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("B,L,H,Q,K,V,dk,dv", SHAPES)
+def test_sequences(B, L, H, Q, K, V, dk, dv, ragged, dtype):
+    q, k, v, g, beta, S, lengths = inputs(B, L, H, Q, K, V, dk, dv, dtype, ragged=ragged)
+    out, last = seq.gated_delta(q, k, v, g, beta, S, lengths, scale=0.7)
+    want, state = oracle.delta_of(q, k, v, g, beta, S, lengths, 0.7)
+    more = cancelled(k, v, g, beta, S, L, dk, dv)
+    check_out(out, want, L, dk, dtype, more=more)
+    near(last, state, more * u32(L, dk), "state")
+
+
+@TYPES
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("B,L,H,Q,K,V,dk,dv", SHAPES)
+def test_gradients(B, L, H, Q, K, V, dk, dv, ragged, dtype):
+    q, k, v, g, beta, S, lengths = inputs(B, L, H, Q, K, V, dk, dv, dtype, ragged=ragged)
+    dout, dS = normal(21, B, L, H, dv, dtype=dtype), 0.3 * normal(22, B, H, dk, dv)
+    got = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths, scale=0.7)
+    want = oracle.delta_backward(dout, q, k, v, g, beta, S, dS, lengths, 0.7)
+    check_grads(got, want, L, max(dk, dv), dtype, cancelled(k, v, g, beta, S, L, dk, dv))
+
+
+@TYPES
+def test_gradient_against_differences(dtype):
+    """The directional derivative of a sum over all results: central differences of the definition in 64 bits, of third order in the step."""
+    B, L, H, d = 2, 70, 2, 32
+    q, k, v, g, beta, S, lengths = inputs(B, L, H, 1, 2, 1, d, d, dtype, ragged=True)
+    dout, dS = normal(21, B, L, H, d, dtype=dtype), normal(22, B, H, d, d)
+    grads = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths)
+    scale = d ** -0.5
+
+    def value(step, along):
+        moved = [oracle.cleared(t, lengths) if t.dim() < 5 and t is not S else oracle.f64(t) for t in (q, k, v, g, beta)] + [oracle.f64(S)]
+        moved = [x + step * y for x, y in zip(moved, along)]
+        out, last = oracle.delta(*moved, lengths, scale)
+        return float((out * oracle.cleared(dout, lengths)).sum() + (last * oracle.f64(dS)).sum())
+
+    for i, name in enumerate(("q", "k", "v", "log_decay", "beta", "state")):
+        along = [torch.zeros(t.shape, dtype=torch.float64) for t in (q, k, v, g, beta, S)]
+        along[i] = torch.randn(along[i].shape, generator=torch.Generator().manual_seed(50 + i), dtype=torch.float64)
+        step = 1e-4
+        want = (value(step, along) - value(-step, along)) / (2 * step)
+        got = float((oracle.f64(grads[i]) * along[i]).sum())
+        size = float(oracle.f64(grads[i]).norm())      # (a sum of as many terms of either sign, each off by its own rounding)
+        rel = 2 * oracle.U_BF16 if dtype == BF16 and i < 3 else 1e-5
+        assert abs(got - want) <= 5 * rel * size + 1e-6 * abs(want), (name, got, want)
+
+
+@TYPES
+@pytest.mark.parametrize("B,H,Q,K,V,dk,dv", [(1, 1, 1, 1, 1, 1, 1), (64, 4, 4, 4, 4, 64, 64), (3, 8, 4, 4, 8, 128, 128), (5, 6, 6, 2, 3, 48, 80), (4, 2, 1, 2, 1, 127, 101),
+                                               (2, 3, 3, 3, 1, 5, 3), (300, 16, 16, 16, 16, 128, 128), (800, 16, 8, 8, 16, 128, 128)])
+def test_steps(B, H, Q, K, V, dk, dv, dtype):
+    q, k, v, g, beta, S, _ = inputs(B, 1, H, Q, K, V, dk, dv, dtype)
+    active = (torch.arange(B, dtype=torch.int32) % 3 != 1).int().cuda()
+    T = S.clone()
+    out = seq.gated_delta_step(q, k, v, g, beta, T, active)
+    want, state = oracle.delta_of(q, k, v, g, beta, S, active, dk ** -0.5)
+    more = cancelled(k, v, g, beta, S, B, dk, dv)
+    check_out(out, want, 1, dk, dtype, more=more)
+    near(T, state, more * u32(1, dk), "state")
+    assert torch.equal(T[active == 0], S[active == 0]) and not out[active == 0].any()
+
+
+@TYPES
+def test_steps_follow_the_sequence(dtype):
+    B, L, H, d = 3, 75, 2, 64
+    q, k, v, g, beta, S, _ = inputs(B, L, H, 1, 2, 2, d, d, dtype, fast=0.05)
+    T = S.clone()
+    steps = torch.cat([seq.gated_delta_step(q[:, t:t + 1], k[:, t:t + 1], v[:, t:t + 1], g[:, t:t + 1], beta[:, t:t + 1], T) for t in range(L)], 1)
+    out, last = seq.gated_delta(q, k, v, g, beta, S)
+    want, state = oracle.delta_of(q, k, v, g, beta, S, scale=d ** -0.5)
+    check_out(steps, want, L, d, dtype)
+    near(T, state, u32(L, d), "state of the steps")
+    near(last, state, u32(L, d), "state of the sequence")
+
+
+@TYPES
+def test_long_sequences(dtype):
+    """4000 tokens: a stretch at a time through the definition would take the same states."""
+    B, L, H, dk, dv = 1, 4000, 2, 64, 48
+    q, k, v, g, beta, S, _ = inputs(B, L, H, 1, 1, 2, dk, dv, dtype, fast=0.01)
+    dout, dS = normal(21, B, L, H, dv, dtype=dtype), normal(22, B, H, dk, dv)
+    out, last = seq.gated_delta(q, k, v, g, beta, S)
+    want, state = oracle.delta_of(q, k, v, g, beta, S, scale=dk ** -0.5)
+    check_out(out, want, L, dk, dtype)
+    near(last, state, u32(L, dk), "state")
+    got = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS)
+    check_grads(got, oracle.delta_backward(dout, q, k, v, g, beta, S, dS, scale=dk ** -0.5), L, dk, dtype)
+
+
+@TYPES
+@pytest.mark.parametrize("B,L", [(3, 90), (1, 2000)])
+def test_what_lies_behind_the_length_is_not_read(B, L, dtype):
+    q, k, v, g, beta, S, _ = inputs(B, L, 2, 2, 1, 2, 40, 24, dtype)
+    lengths = torch.tensor([L - 1, 0, 37][:B], dtype=torch.int32).cuda()
+    dout, dS = normal(21, B, L, 2, 24, dtype=dtype), normal(22, *S.shape)
+    call = lambda *t: [*seq.gated_delta(*t, S, lengths), *seq.gated_delta_backward(dout, *t, S, dS, lengths)]  # noqa: E731
+    want = call(q, k, v, g, beta)
+    here = (torch.arange(L).cuda() < lengths[:, None])
+    for bad in (math.nan, math.inf, torch.finfo(torch.bfloat16).min):
+        spoilt = [torch.where(here.reshape(B, L, *([1] * (t.dim() - 2))), t, torch.full_like(t, bad)) for t in (q, k, v, g, beta)]
+        for x, y in zip(call(*spoilt), want):
+            assert torch.equal(x, y)
+    for x in (want[0], *want[2:7]):
+        assert not x[~here].any()
+    assert torch.equal(want[1][lengths == 0], S[lengths == 0]) and torch.equal(want[7][lengths == 0], dS[lengths == 0])
+
+
+def test_lengths_outside_the_range_are_taken_as_its_ends():
+    q, k, v, g, beta, S, _ = inputs(2, 20, 2, 2, 2, 2, 32, 32, BF16)
+    far = torch.tensor([-5, 99], dtype=torch.int32).cuda()
+    ends = torch.tensor([0, 20], dtype=torch.int32).cuda()
+    for x, y in zip(seq.gated_delta(q, k, v, g, beta, S, far), seq.gated_delta(q, k, v, g, beta, S, ends)):
+        assert torch.equal(x, y)
+
+
+@TYPES
+@pytest.mark.parametrize("rate", [0.0, -1e-6, -30.0, -104.0, -1e5, -math.inf, "mixed"])
+def test_decays_at_their_ends(rate, dtype):
+    B, L, H, d = 2, 70, 2, 32
+    q, k, v, g, beta, S, _ = inputs(B, L, H, 2, 2, 2, d, d, dtype)
+    if rate == "mixed":      # between slow decays some that keep nothing
+        g = torch.where(torch.rand(g.shape, generator=torch.Generator().manual_seed(3)).cuda() < 0.1, torch.full_like(g, -math.inf), 0.01 * g)
+    else:
+        g = torch.full_like(g, rate)
+    dout, dS = normal(21, B, L, H, d, dtype=dtype), normal(22, *S.shape)
+    out, last = seq.gated_delta(q, k, v, g, beta, S)
+    want, state = oracle.delta_of(q, k, v, g, beta, S, scale=d ** -0.5)
+    check_out(out, want, L, d, dtype)
+    near(last, state, u32(L, d), "state")
+    got = list(seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS))
+    T = seq.gated_delta_step(q[:, :1], k[:, :1], v[:, :1], g[:, :1], beta[:, :1], S.clone())
+    check_out(T, want[:, :1], 1, d, dtype, "one token")
+    # the definition's own gradient of a decay that keeps nothing is 0 times infinity: it counts as e^-10000, of which nothing is left either
+    exact = oracle.delta_backward(dout, q, k, v, g.clamp(min=-1e4), beta, S, dS, scale=d ** -0.5)
+    # where the gradient of a decay is small, it is what is left of outputs times their gradients: held to those
+    size = float((oracle.f64(dout).abs() * want.abs()).sum(-1).max()) * (1 + 32)
+    off = float((oracle.f64(got[3]) - exact[3]).abs().max())
+    assert off <= u32(L, d) * size, (off, size)
+    got[3], exact[3] = got[4], exact[4]
+    check_grads(got, exact, L, d, dtype)
+
+
+@TYPES
+def test_strengths_of_zero_and_two(dtype):
+    """A strength of 0 leaves the state alone, but has a gradient; one of 2 turns it around along the key."""
+    B, L, H, d = 2, 50, 2, 32
+    q, k, v, g, beta, S, _ = inputs(B, L, H, 2, 2, 2, d, d, dtype)
+    beta = torch.where(beta > 0.6, torch.full_like(beta, 2.0), torch.where(beta < 0.4, torch.zeros_like(beta), beta))
+    dout, dS = normal(21, B, L, H, d, dtype=dtype), normal(22, *S.shape)
+    want, state = oracle.delta_of(q, k, v, g, beta, S, scale=d ** -0.5)
+    out, last = seq.gated_delta(q, k, v, g, beta, S)
+    check_out(out, want, L, d, dtype)
+    near(last, state, 2 * u32(L, d), "state")
+    check_grads(seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS), oracle.delta_backward(dout, q, k, v, g, beta, S, dS, scale=d ** -0.5), 4 * L, d, dtype)
+
+
+def test_keys_that_repeat():
+    """The same key at every token of strength 1: each value replaces the one before, and the triangular system is as full as it gets."""
+    B, L, H, d = 1, 96, 1, 64
+    q, k, v, g, beta, S, _ = inputs(B, L, H, 1, 1, 1, d, d, F32)
+    k = k[:, :1].expand(-1, L, -1, -1).contiguous()
+    g, beta = torch.zeros_like(g), torch.ones_like(beta)
+    out, last = seq.gated_delta(q, k, v, g, beta, S)
+    want, state = oracle.delta_of(q, k, v, g, beta, S, scale=d ** -0.5)
+    check_out(out, want, L, d, F32)
+    near(last, state, u32(L, d), "state")
+
+
+def test_empty_sizes():
+    for B, L, H in [(0, 5, 2), (2, 0, 2), (2, 5, 0), (2, 0, 0)]:
+        q, k, v, g, beta, S, _ = inputs(B, L, H, H, H, H, 8, 8, BF16)
+        out, last = seq.gated_delta(q, k, v, g, beta, S)
+        assert out.shape == (B, L, H, 8) and torch.equal(last, S)
+        got = seq.gated_delta_backward(out, q, k, v, g, beta, S, 2 * S)
+        assert [t.shape for t in got] == [t.shape for t in (q, k, v, g, beta, S)] and torch.equal(got[5], 2 * S)
+    assert not seq.gated_delta(*inputs(2, 0, 2, 2, 2, 2, 8, 8, F32)[:5])[1].any()      # (no state: zeros)
+
+
+def test_without_state_and_in_place():
+    B, L, H, d = 2, 50, 2, 64
+    q, k, v, g, beta, S, lengths = inputs(B, L, H, 2, 2, 2, d, d, BF16, ragged=True)
+    zeros = seq.gated_delta(q, k, v, g, beta, torch.zeros_like(S), lengths)
+    for x, y in zip(seq.gated_delta(q, k, v, g, beta, None, lengths), zeros):
+        assert torch.equal(x, y)
+    out, none = seq.gated_delta(q, k, v, g, beta, S, lengths, want_state=False)
+    want, last = seq.gated_delta(q, k, v, g, beta, S, lengths)
+    assert none is None and torch.equal(out, want)
+    T, O = S.clone(), torch.empty_like(out)
+    seq.gated_delta(q, k, v, g, beta, T, lengths, out=O, out_state=T)
+    assert torch.equal(T, last) and torch.equal(O, out)
+    dout, dS = normal(21, *out.shape, dtype=BF16), normal(22, *S.shape)
+    want = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths)
+    D = dS.clone()
+    got = seq.gated_delta_backward(dout, q, k, v, g, beta, S, D, lengths, dstate0=D)
+    assert all(torch.equal(x, y) for x, y in zip(got, want)) and got[5] is D
+    assert seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths, want_dstate=False)[5] is None
+
+
+@TYPES
+def test_strided_views(dtype):
+    """Rows out of one projection, gates out of another, states out of a pool, results into views."""
+    B, L, H, d = 2, 75, 2, 32
+    wide = normal(1, B, L, 3 * H, d + 3, dtype=dtype)
+    q, k, v = (unit(wide[:, :, i * H:(i + 1) * H, 1:d + 1].float()).to(dtype) for i in range(3))
+    views = []
+    for i, t in enumerate((q, k, v)):
+        wide[:, :, i * H:(i + 1) * H, 1:d + 1] = t
+        views.append(wide[:, :, i * H:(i + 1) * H, 1:d + 1])
+    gates = torch.stack((-normal(2, L, B, H).abs(), torch.sigmoid(normal(3, L, B, H))), -1)
+    g, beta = gates[..., 0].transpose(0, 1), gates[..., 1].transpose(0, 1)
+    pool = normal(4, 5, H + 1, d, d)
+    S = pool[1:4:2, 1:]
+    want = seq.gated_delta(q, k, v, g.contiguous(), beta.contiguous(), S.contiguous())
+    out = torch.full((L, B, H, d + 1), 7.0, dtype=dtype, device="cuda")
+    got = seq.gated_delta(*views, g, beta, S, out=out.transpose(0, 1)[..., :d])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and (out[..., d] == 7).all()
+    dout = normal(5, B, L, H, d + 5, dtype=dtype)[..., 2:d + 2]
+    want = seq.gated_delta_backward(dout.contiguous(), q, k, v, g.contiguous(), beta.contiguous(), S.contiguous())
+    grads = torch.full((B, L, 3 * H, d + 3), 7.0, dtype=dtype, device="cuda")
+    dgates = torch.full((L, B, H, 3), 7.0, device="cuda")
+    parts = [grads[:, :, i * H:(i + 1) * H, 1:d + 1] for i in range(3)]
+    got = seq.gated_delta_backward(dout, *views, g, beta, S, dq=parts[0], dk=parts[1], dv=parts[2], dlog_decay=dgates[..., 0].transpose(0, 1),
+                                   dbeta=dgates[..., 2].transpose(0, 1))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert (grads[..., 0] == 7).all() and (grads[..., d + 1:] == 7).all() and (dgates[..., 1] == 7).all()
+    before = pool.clone()
+    o = seq.gated_delta_step(*(t[:, :1] for t in views), g[:, :1], beta[:, :1], S)
+    want, last = seq.gated_delta(q[:, :1], k[:, :1], v[:, :1], g[:, :1], beta[:, :1], before[1:4:2, 1:].contiguous())
+    near(S, oracle.f64(last), 2 * u32(1, d), "pool")
+    near(o, oracle.f64(want), 2 * u32(1, d), "out", element=2 * oracle.U_BF16 if dtype == BF16 else 0.0)
+    pool[1:4:2, 1:] = before[1:4:2, 1:]
+    assert torch.equal(pool, before)
+
+
+def test_broadcast_inputs():
+    """Strides of zero repeat an input; its gradient has rows of its own for each place."""
+    B, L, H, d = 3, 40, 2, 32
+    q, k, v, g, beta, S, _ = inputs(1, L, 1, 1, 1, 1, d, d, F32)
+    many = [q.expand(B, L, H, d), k.expand(B, L, H, d), v.expand(B, L, H, d), g.expand(B, L, H), beta.expand(B, L, H), S.expand(B, H, d, d)]
+    plain = [t.contiguous() for t in many]
+    dout = normal(21, B, L, H, d)
+    for x, y in zip([*seq.gated_delta(*many), *seq.gated_delta_backward(dout, *many)], [*seq.gated_delta(*plain), *seq.gated_delta_backward(dout, *plain)]):
+        assert torch.equal(x, y)
+
+
+def test_results_do_not_change_from_call_to_call():
+    q, k, v, g, beta, S, lengths = inputs(4, 300, 4, 2, 1, 4, 64, 64, BF16, ragged=True)
+    dout = normal(21, 4, 300, 4, 64, dtype=BF16)
+    call = lambda: [*seq.gated_delta(q, k, v, g, beta, S, lengths), *seq.gated_delta_backward(dout, q, k, v, g, beta, S, S, lengths)]  # noqa: E731
+    first = call()
+    for _ in range(5):
+        assert all(torch.equal(x, y) for x, y in zip(call(), first))
+
+
+@TYPES
+def test_values_that_are_not_finite(dtype):
+    """They reach what depends on them, tokens of their own chunk of 32 at most before them, and no other sequence or head."""
+    B, L, H, d = 2, 200, 2, 32
+    clean = inputs(B, L, H, H, H, H, d, d, dtype)[:6]
+    want, last = seq.gated_delta(*clean)
+    for i in range(6):
+        spoilt = [t.clone() for t in clean]
+        at = (1, 100, 1) if i < 5 else (1, 1)
+        spoilt[i][at] = math.nan
+        out, state = seq.gated_delta(*spoilt)
+        other = torch.ones(B, H, dtype=torch.bool)
+        other[1, 1] = False
+        for b in range(B):
+            for h in range(H):
+                if other[b, h]:
+                    assert torch.equal(out[b, :, h], want[b, :, h]) and torch.equal(state[b, h], last[b, h])
+        if i == 5:
+            assert out[1, :, 1].isnan().all()
+        else:
+            assert torch.equal(out[1, :96, 1], want[1, :96, 1])
+            assert out[1, 100, 1].isnan().all()
+            assert i == 0 or (out[1, 100:, 1].isnan().all() and state[1, 1].isnan().all())
+
+
+# ------------------------------------------------------------------------------------------- streams, graphs, torch's graph
+def test_on_a_stream_of_its_own():
+    q, k, v, g, beta, S, lengths = inputs(3, 500, 2, 2, 1, 2, 64, 64, BF16, ragged=True)
+    dout = normal(21, 3, 500, 2, 64, dtype=BF16)
+    call = lambda: [*seq.gated_delta(q, k, v, g, beta, S, lengths), *seq.gated_delta_backward(dout, q, k, v, g, beta, S, S, lengths)]  # noqa: E731
+    want = call()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = call()
+    s.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_a_block_in_a_graph():
+    """Norm, memory, dropout and their gradients, captured once and replayed on new data and random numbers, eager calls in between."""
+    B, L, H, d = 2, 100, 2, 32
+    D = H * d
+    x, w, b = normal(1, B, L, D, dtype=BF16), 1 + 0.1 * normal(2, D), 0.1 * normal(3, D)
+    dout = normal(4, B, L, D, dtype=BF16)
+    g, beta = -normal(5, B, L, H).abs(), torch.sigmoid(normal(6, B, L, H))
+    S = normal(7, B, H, d, d)
+    T, offset = S.clone(), torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def work(T, offset):
+        y = seq.layer_norm(x, w, b)
+        rows = y.unflatten(-1, (H, d))
+        o, last = seq.gated_delta(rows, rows, rows, g, beta, S, scale=0.1)
+        z = seq.dropout(o.flatten(-2), 0.3, 5, offset, residual=x)
+        do = seq.dropout(dout, 0.3, 5, offset)
+        grads = seq.gated_delta_backward(do.unflatten(-1, (H, d)), rows, rows, rows, g, beta, S, last, scale=0.1)
+        dy = (grads[0] + grads[1] + grads[2]).flatten(-2)
+        back = seq.layer_norm_backward(dy, x, w)
+        step = seq.gated_delta_step(rows[:, :1], rows[:, :1], rows[:, :1], g[:, :1], beta[:, :1], T)
+        offset += 1
+        return [z, last, *grads, *back, step]
+
+    work(T, offset)
+    torch.cuda.synchronize()
+    T.copy_(S)
+    offset.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = work(T, offset)
+    E, eager = S.clone(), torch.zeros_like(offset)
+    kept = []
+    for i in range(4):
+        x.copy_(normal(20 + i, *x.shape, dtype=BF16))
+        g.copy_(-normal(30 + i, *g.shape).abs())
+        dout.copy_(normal(40 + i, *dout.shape, dtype=BF16))
+        graph.replay()
+        want = work(E, eager)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), f"replay {i}"
+        assert torch.equal(T, E) and int(offset) == i + 1
+        kept.append((got[0] != x).clone())
+    assert not torch.equal(kept[0], kept[1])      # (what is dropped moves on)
+
+
+def test_autograd():
+    B, L, H, d = 2, 50, 4, 32
+    q, k, v, g, beta, S, lengths = inputs(B, L, H, 2, 1, 4, d, d, F32, ragged=True)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v, g, beta, S)]
+    out, last = seq.gated_delta(*leaves, lengths)
+    dout, dS = normal(21, *out.shape), normal(22, *last.shape)
+    torch.autograd.backward((out, last), (dout, dS))
+    want = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths)
+    assert all(torch.equal(t.grad, w) for t, w in zip(leaves, want))
+    # broadcast leaves: torch adds their gradients up
+    leaf = g[:1, :1].clone().requires_grad_()
+    seq.gated_delta(q, k, v, leaf.expand(B, L, H), beta, S)[0].backward(dout)
+    want = seq.gated_delta_backward(dout, q, k, v, g[:1, :1].expand(B, L, H), beta, S)[3].sum((0, 1), keepdim=True)
+    near(leaf.grad, oracle.f64(want), 1e-5, "broadcast")
+    # not where results are given, not twice, not for one token
+    with pytest.raises(RuntimeError):
+        seq.gated_delta(*leaves, lengths, out=torch.empty_like(out))
+    with pytest.raises(RuntimeError):
+        seq.gated_delta_step(leaves[0][:, :1], k[:, :1], v[:, :1], g[:, :1], beta[:, :1], S)
+    (dq,) = torch.autograd.grad(seq.gated_delta(*leaves, lengths)[0].sum(), leaves[0], create_graph=True)
+    with pytest.raises(RuntimeError):
+        dq.sum().backward()
+    # a state that is written in place after it was kept is noticed
+    T = S.clone()
+    out, _ = seq.gated_delta(leaves[0], k, v, g, beta, T)
+    seq.gated_delta_step(q[:, :1], k[:, :1], v[:, :1], g[:, :1], beta[:, :1], T)
+    with pytest.raises(RuntimeError):
+        out.sum().backward()
+
+
+def test_refusals():
+    q, k, v, g, beta, S, _ = inputs(2, 8, 4, 2, 2, 4, 16, 16, BF16)
+    refused = [
+        lambda: seq.gated_delta(q.half(), k.half(), v.half(), g, beta),
+        lambda: seq.gated_delta(q, k.float(), v, g, beta),
+        lambda: seq.gated_delta(q, k[:, :4], v, g, beta),
+        lambda: seq.gated_delta(q[:, :, :1].expand(-1, -1, 3, -1), k, v, g, beta),
+        lambda: seq.gated_delta(q, k, v, g[:, :, :3], beta),
+        lambda: seq.gated_delta(q, k, v, g, beta.bfloat16()),
+        lambda: seq.gated_delta(q, k, v, g[:, :4], beta),
+        lambda: seq.gated_delta(q, k, v, g, beta, S[:1]),
+        lambda: seq.gated_delta(q, k, v, g, beta, S.transpose(-1, -2)),
+        lambda: seq.gated_delta(q, k, v, g, beta, S.bfloat16()),
+        lambda: seq.gated_delta(q, k, v, g, beta, lengths=torch.ones(2, device="cuda")),
+        lambda: seq.gated_delta(q, k, v, g, beta, scale=math.nan),
+        lambda: seq.gated_delta(q.cpu(), k, v, g, beta),
+        lambda: seq.gated_delta(q, k, v, g.cpu(), beta),
+        lambda: seq.gated_delta(q, k, v, g, beta, out=q),
+        lambda: seq.gated_delta(q.transpose(-1, -2), k.transpose(-1, -2), v, g, beta),
+        lambda: seq.gated_delta(q[0], k[0], v[0], g[0], beta[0]),
+        lambda: seq.gated_delta(*(torch.zeros(1, 2, 1, 130, dtype=BF16, device="cuda"),) * 3, g[:1, :2, :1], beta[:1, :2, :1]),
+        lambda: seq.gated_delta_backward(v, q, k, v, g, beta, S, S, dstate0=S),
+        lambda: seq.gated_delta_backward(v[:, :, :2], q, k, v, g, beta),
+        lambda: seq.gated_delta_backward(v, q, k, v, g, beta, dv=v),
+        lambda: seq.gated_delta_backward(v, q, k, v, g, beta, dlog_decay=beta),
+        lambda: seq.gated_delta_step(q, k, v, g, beta, S),
+    ]
+    for i, call in enumerate(refused):
+        with pytest.raises((ValueError, TypeError, seq.PerError)):
+            call()
+            pytest.fail(f"call {i} was not refused")
+    with pytest.raises(ValueError, match="active"):
+        seq.gated_delta_step(q[:, :1], k[:, :1], v[:, :1], g[:, :1], beta[:, :1], S, active=torch.ones(3, dtype=torch.int32, device="cuda"))
