@@ -24,9 +24,9 @@ template <typename T, int LANES, int N>
 struct HeldRow {
   static constexpr uint32_t W = Piece<T>::W;
   static constexpr int ALL = N * W;
-  uint32_t col[N], twice[N];
+  uint32_t col[N], twice[N], whole;   // whole: the first pieces, which all lanes have
   bool on[N];
-  __device__ __forceinline__ HeldRow(uint32_t lane, uint32_t dim) {
+  __device__ __forceinline__ HeldRow(uint32_t lane, uint32_t dim) : whole(dim / (LANES * W)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const uint32_t first = (lane + i * LANES) * W;
@@ -36,19 +36,49 @@ struct HeldRow {
     }
   }
   __device__ __forceinline__ bool counts(int i, uint32_t e) const { return e >= twice[i]; }
-  __device__ __forceinline__ void load(const T* row, float (&x)[ALL]) const {
+  // (so that comparisons are made where they are used: held over a loop they would take two scalar registers for each element)
+  __device__ __forceinline__ void again() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(twice[i]));
+  }
+  // The sum of f(i) over the elements that count.
+  template <typename F>
+  __device__ __forceinline__ float sum(F f) const {
+    float all = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const typename Piece<T>::Vec v = *reinterpret_cast<const typename Piece<T>::Loose*>(row + (on[i] ? col[i] : 0));
+      if ((uint32_t)i < whole) {
 #pragma unroll
-      for (uint32_t e = 0; e < W; ++e) x[i * W + e] = as_float(v[e]);
+        for (uint32_t e = 0; e < W; ++e) all += f(i * W + e);
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < W; ++e) all += counts(i, e) ? f(i * W + e) : 0.0f;
+      }
     }
+    return all;
   }
-  __device__ __forceinline__ void load_plain(const float* row, float (&x)[ALL], float none) const {
+  typedef typename Piece<T>::Vec Raw[N];
+  __device__ __forceinline__ void load(const T* row, Raw& v) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = *reinterpret_cast<const typename Piece<T>::Loose*>(row + (on[i] ? col[i] : 0));
+  }
+  __device__ __forceinline__ void widen(const Raw& v, float (&x)[ALL]) const {
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-      for (uint32_t e = 0; e < W; ++e) x[i * W + e] = row && on[i] ? row[col[i] + e] : none;
+      for (uint32_t e = 0; e < W; ++e) x[i * W + e] = as_float(v[i][e]);
+  }
+  __device__ __forceinline__ void load_plain(const float* row, float (&x)[ALL], float none) const {
+    typedef Piece<float>::Loose Four;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (uint32_t e = 0; e < W; e += 4) {
+        Piece<float>::Vec v = {none, none, none, none};
+        if (row) v = *reinterpret_cast<const Four*>(row + (on[i] ? col[i] : 0) + e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[i * W + e + j] = v[j];
+      }
   }
   __device__ __forceinline__ void store(T* row, const float (&x)[ALL]) const {
 #pragma unroll
@@ -62,14 +92,17 @@ struct HeldRow {
   }
 };
 
+// The sum over a wave, the same in every lane: four additions across 16 lanes, then the four of them in their order.
+__device__ __forceinline__ float wave_sum(float x) {
+  const int y = __builtin_bit_cast(int, sum16(x));
+  auto lane = [&](int i) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(y, i)); };
+  return (lane(0) + lane(16)) + (lane(32) + lane(48));
+}
 // Sums of a row's lanes, two at once: of a wave, or of the workgroup's four in their order.
 template <int LANES>
 __device__ __forceinline__ void row_sums(float* a, float* b, float (*lds)[2]) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) {
-    *a += __shfl_xor(*a, d);
-    *b += __shfl_xor(*b, d);
-  }
+  *a = wave_sum(*a);
+  *b = wave_sum(*b);
   if (LANES == 64) return;
   if ((threadIdx.x & 63) == 0) {
     lds[threadIdx.x >> 6][0] = *a;
@@ -83,25 +116,19 @@ __device__ __forceinline__ void row_sums(float* a, float* b, float (*lds)[2]) {
 // Mean and reciprocal root of the variance of a row that is held: the variance from the differences, not from squares.
 template <typename T, int LANES, int N>
 __device__ __forceinline__ void standardise(const HeldRow<T, LANES, N>& at, float (&x)[N * Piece<T>::W], const BlockArgs& a, float* r, float (*lds)[4][2]) {
-  constexpr uint32_t W = Piece<T>::W;
-  float sum = 0.0f, none = 0.0f;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (uint32_t e = 0; e < W; ++e) sum += at.counts(i, e) ? x[i * W + e] : 0.0f;
+  float sum = at.sum([&](int i) { return x[i]; }), none = 0.0f;
   row_sums<LANES>(&sum, &none, lds[0]);
   const float mean = sum / (float)a.dim;
-  float square = 0.0f;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (uint32_t e = 0; e < W; ++e) {
-      x[i * W + e] -= mean;
-      square += at.counts(i, e) ? x[i * W + e] * x[i * W + e] : 0.0f;
-    }
+  for (int i = 0; i < at.ALL; ++i) x[i] -= mean;
+  float square = at.sum([&](int i) { return x[i] * x[i]; });
   row_sums<LANES>(&square, &none, lds[1]);
   *r = 1.0f / sqrtf(square / (float)a.dim + a.eps);
 }
+
+// Which of a workgroup's rows a wave takes.
+template <int LANES>
+__device__ __forceinline__ uint32_t row_of_block() { return LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0; }
 
 // LANES 64: four rows to a workgroup.  Weights stay in registers from row to row.
 template <typename T, int LANES, int N>
@@ -109,13 +136,18 @@ __global__ __launch_bounds__(256) void k_layer_norm(BlockArgs a) {
   constexpr int ALL = N * Piece<T>::W, ROWS = 256 / LANES;
   __shared__ float lds[2][4][2];
   const uint32_t lane = threadIdx.x % LANES;
-  const HeldRow<T, LANES, N> at(lane, a.dim);
+  HeldRow<T, LANES, N> at(lane, a.dim);
   float w[ALL], b[ALL], x[ALL], r;
+  typename HeldRow<T, LANES, N>::Raw next;
+  const uint64_t rows = (uint64_t)a.B * a.L * a.H, stride = (uint64_t)gridDim.x * ROWS;
+  uint64_t row = (uint64_t)blockIdx.x * ROWS + row_of_block<LANES>();
+  if (row < rows) at.load(row_at<T>(a.x, row, a), next);
   at.load_plain(a.weight, w, 1.0f);
   at.load_plain(a.bias, b, 0.0f);
-  const uint64_t rows = (uint64_t)a.B * a.L * a.H, stride = (uint64_t)gridDim.x * ROWS;
-  for (uint64_t row = (uint64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < rows; row += stride) {
-    at.load(row_at<T>(a.x, row, a), x);
+  for (; row < rows; row += stride) {
+    at.again();
+    at.widen(next, x);
+    if (row + stride < rows) at.load(row_at<T>(a.x, row + stride, a), next);
     standardise<T, LANES, N>(at, x, a, &r, lds);
 #pragma unroll
     for (int i = 0; i < ALL; ++i) x[i] = fmaf(x[i] * r, w[i], b[i]);
@@ -126,28 +158,37 @@ __global__ __launch_bounds__(256) void k_layer_norm(BlockArgs a) {
 
 // dx = r (h - mean h - xh mean(h xh)),  h = dout w,  xh = (x - mean) r;  the workgroup's sums of dout xh and of dout are left in `partial`.
 template <typename T, int LANES, int N>
-__global__ __launch_bounds__(256) void k_layer_norm_back(BlockArgs a) {
+__global__ __launch_bounds__(256, 2) void k_layer_norm_back(BlockArgs a) {
   constexpr int W = Piece<T>::W, ALL = N * W, ROWS = 256 / LANES;
   __shared__ float lds[3][4][2];
   const uint32_t lane = threadIdx.x % LANES;
-  const HeldRow<T, LANES, N> at(lane, a.dim);
+  HeldRow<T, LANES, N> at(lane, a.dim);
   float w[ALL], dw[ALL] = {}, db[ALL] = {}, x[ALL], d[ALL], r;
-  at.load_plain(a.weight, w, 1.0f);
+  typename HeldRow<T, LANES, N>::Raw next_x, next_d;
   const uint64_t rows = (uint64_t)a.B * a.L * a.H, stride = (uint64_t)gridDim.x * ROWS;
-  for (uint64_t row = (uint64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < rows; row += stride) {
-    at.load(row_at<T>(a.x, row, a), x);
-    at.load(row_at<T>(a.more, row, a), d);
+  uint64_t row = (uint64_t)blockIdx.x * ROWS + row_of_block<LANES>();
+  if (row < rows) {
+    at.load(row_at<T>(a.x, row, a), next_x);
+    at.load(row_at<T>(a.more, row, a), next_d);
+  }
+  at.load_plain(a.weight, w, 1.0f);
+  for (; row < rows; row += stride) {
+    at.again();
+    at.widen(next_x, x);
+    at.widen(next_d, d);
+    if (row + stride < rows) {
+      at.load(row_at<T>(a.x, row + stride, a), next_x);
+      at.load(row_at<T>(a.more, row + stride, a), next_d);
+    }
     standardise<T, LANES, N>(at, x, a, &r, lds);
-    float along = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < ALL; ++i) {
       x[i] *= r;
       dw[i] = fmaf(d[i], x[i], dw[i]);
       db[i] += d[i];
       d[i] *= w[i];
-      sum += at.counts(i / W, i % W) ? d[i] : 0.0f;
-      along += at.counts(i / W, i % W) ? d[i] * x[i] : 0.0f;
     }
+    float sum = at.sum([&](int i) { return d[i]; }), along = at.sum([&](int i) { return d[i] * x[i]; });
     row_sums<LANES>(&sum, &along, lds[2]);
     sum /= (float)a.dim;
     along /= (float)a.dim;
@@ -156,15 +197,16 @@ __global__ __launch_bounds__(256) void k_layer_norm_back(BlockArgs a) {
     at.store(const_cast<T*>(row_at<T>(a.out, row, a)), x);
     if (LANES > 64) __syncthreads();
   }
-  float* const to = a.partial + (size_t)(blockIdx.x * ROWS + threadIdx.x / LANES) * 2 * a.dim;
+  // The waves' sums one after the other, lane by lane: element e of piece i of lane l at (i W + e) LANES + l, as k_norm_sums takes them.
+  extern __shared__ float sums[];
+  for (int turn = 0; turn < ROWS; ++turn) {
+    if (turn) __syncthreads();
+    if (row_of_block<LANES>() != (uint32_t)turn) continue;
+    float* const to = (turn + 1 < ROWS ? sums : a.partial + (size_t)blockIdx.x * 2 * ALL * LANES) + lane;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (!at.on[i]) continue;
-#pragma unroll
-    for (int e = 0; e < W; ++e) {
-      if (!at.counts(i, e)) continue;
-      to[at.col[i] + e] = dw[i * W + e];
-      to[a.dim + at.col[i] + e] = db[i * W + e];
+    for (int i = 0; i < ALL; ++i) {
+      to[i * LANES] = turn ? sums[i * LANES + lane] + dw[i] : dw[i];
+      to[(ALL + i) * LANES] = turn ? sums[(ALL + i) * LANES + lane] + db[i] : db[i];
     }
   }
 }
@@ -218,19 +260,41 @@ __global__ __launch_bounds__(256) void k_layer_norm_any(BlockArgs a) {
   }
 }
 
-// The gradients of weight and bias from the sums that were left, in their order: 16 columns to a workgroup, 16 rows of sums at a time.
-__global__ __launch_bounds__(256) void k_norm_sums(const float* partial, uint32_t rows, uint32_t dim, float* dweight, float* dbias) {
+// The gradients of weight and bias from the sums that were left, in their order: 16 of them to a workgroup, 16 rows of sums at a time.  A row has
+// `width` for the weight, then as many for the bias, by column (lanes 0) or by lane.
+struct NormSums {
+  const float* from;
+  float *dweight, *dbias;
+  uint32_t rows, dim, width, lanes, W;
+};
+__global__ __launch_bounds__(256) void k_norm_sums(NormSums p) {
   __shared__ float lds[16][17];
-  const uint32_t c = threadIdx.x & 15, at = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+  const uint32_t c = threadIdx.x & 15, at = threadIdx.x >> 4, place = blockIdx.x * 16 + c, row = 2 * p.width;
   float sum = 0.0f;
-  if (col < 2 * dim)
-    for (uint32_t i = at; i < rows; i += 16) sum += partial[(size_t)i * 2 * dim + col];
+  if (place < row) {
+    const float* from = p.from + place;
+    uint32_t i = at;
+    for (; i + 7 * 16 < p.rows; i += 8 * 16) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = from[(size_t)(i + 16 * e) * row];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += x[e];
+    }
+    for (; i < p.rows; i += 16) sum += from[(size_t)i * row];
+  }
   lds[at][c] = sum;
   __syncthreads();
-  if (at || col >= 2 * dim) return;
+  if (at || place >= row) return;
   for (int i = 1; i < 16; ++i) sum += lds[i][c];
-  float* const to = col < dim ? dweight : dbias;
-  if (to) to[col < dim ? col : col - dim] = sum;
+  uint32_t col = place % p.width;
+  if (p.lanes) {
+    const uint32_t k = col / p.lanes, first = (col % p.lanes + k / p.W * p.lanes) * p.W;
+    col = (first + p.W <= p.dim ? first : p.dim - p.W) + k % p.W;
+    if (first >= p.dim || col < first) return;
+  }
+  float* const to = place < p.width ? p.dweight : p.dbias;
+  if (to) to[col] = sum;
 }
 
 // Philox4x32-10: four words of a counter and a key (Salmon et al., Parallel Random Numbers: As Easy as 1, 2, 3).

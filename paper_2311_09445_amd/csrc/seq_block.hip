@@ -1,5 +1,5 @@
 // Rows of a residual block: layer norm with its gradient, and dropout.
-#include "dev_seq.h"
+#include "dev_parts.h"
 
 namespace per {
 
@@ -19,9 +19,10 @@ Shape shape_of(uint32_t dtype, uint32_t dim) {
   while (lanes * n * W < dim) n *= 2;
   return Shape{lanes, n};
 }
-constexpr uint32_t kBlocks = 2048;     // workgroups of a norm: eight to a compute unit
-constexpr uint32_t kBackBlocks = 512;   // of a gradient: each row in flight leaves a row of sums
+constexpr uint32_t kBlocks = 1024;     // workgroups of a norm: four to a compute unit
+constexpr uint32_t kBackBlocks = 512;   // of a gradient: each leaves a row of sums
 
+uint32_t sums_width(const Shape& s, uint32_t dtype, uint32_t dim) { return s.pieces ? s.lanes * s.pieces * (dtype == PER_SEQ_BF16 ? 8 : 4) : dim; }
 uint32_t rows_each(const Shape& s) { return s.pieces ? 256 / s.lanes : 1; }
 uint32_t back_blocks(const BlockArgs& a, uint32_t each) {
   const uint64_t need = (count_of(a) + each - 1) / each;
@@ -32,7 +33,7 @@ template <typename T, int LANES, int N>
 hipError_t norm_as(const BlockArgs& a, bool back, hipStream_t s) {
   constexpr uint32_t each = 256 / LANES;
   if (back) {
-    k_layer_norm_back<T, LANES, N><<<back_blocks(a, each), 256, 0, s>>>(a);
+    k_layer_norm_back<T, LANES, N><<<back_blocks(a, each), 256, LANES == 64 ? 2 * N * Piece<T>::W * 64 * sizeof(float) : 0, s>>>(a);
   } else {
     const uint64_t need = (count_of(a) + each - 1) / each;
     k_layer_norm<T, LANES, N><<<(uint32_t)(need < kBlocks ? need : kBlocks), 256, 0, s>>>(a);
@@ -81,8 +82,8 @@ hipError_t dropout(const BlockArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t norm_work_bytes(uint32_t dtype, const BlockArgs& a) {
-  const uint32_t each = rows_each(shape_of(dtype, a.dim));
-  return (size_t)back_blocks(a, each) * each * 2 * a.dim * sizeof(float);
+  const Shape shape = shape_of(dtype, a.dim);
+  return (size_t)back_blocks(a, rows_each(shape)) * 2 * sums_width(shape, dtype, a.dim) * sizeof(float);
 }
 
 hipError_t launch_layer_norm(uint32_t dtype, const BlockArgs& a, hipStream_t s) {
@@ -90,15 +91,15 @@ hipError_t launch_layer_norm(uint32_t dtype, const BlockArgs& a, hipStream_t s) 
 }
 
 hipError_t launch_layer_norm_backward(uint32_t dtype, const BlockArgs& a, hipStream_t s) {
-  uint32_t left = 0;   // rows of sums
+  const Shape shape = shape_of(dtype, a.dim);
+  NormSums p{a.partial, a.dweight, a.dbias, back_blocks(a, rows_each(shape)), a.dim, sums_width(shape, dtype, a.dim), shape.pieces ? shape.lanes : 0,
+             dtype == PER_SEQ_BF16 ? 8u : 4u};
   if (count_of(a)) {
     const hipError_t e = dtype == PER_SEQ_BF16 ? norm<bf16>(dtype, a, true, s) : norm<float>(dtype, a, true, s);
     if (e != hipSuccess) return e;
-    const uint32_t each = rows_each(shape_of(dtype, a.dim));
-    left = back_blocks(a, each) * each;
   }
   if (!a.dweight && !a.dbias) return hipSuccess;
-  k_norm_sums<<<(2 * a.dim + 15) / 16, 256, 0, s>>>(a.partial, left, a.dim, a.dweight, a.dbias);
+  k_norm_sums<<<(2 * p.width + 15) / 16, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
