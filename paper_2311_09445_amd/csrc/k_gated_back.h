@@ -31,7 +31,7 @@ constexpr int kGradParts = sizeof(T) == 2 ? 1 : 3;   // of states in the product
 template <typename T, int DK>
 __global__ __launch_bounds__(256) void k_delta_back(DeltaBack p) {
   constexpr int TX = DK / 16, KX = DK / 32, PT = kParts<T>;
-  constexpr uint32_t BUFFER = 2 * PT * Tile<DK>::SIZE;
+  constexpr uint32_t BUFFER = RunLds<T, DK, 3, false>::SIZE;
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   bf16* const lds = reinterpret_cast<bf16*>(lds_raw);
   const uint32_t slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, h = bh % p.H, b = bh / p.H;
@@ -68,7 +68,9 @@ __global__ __launch_bounds__(256) void k_delta_back(DeltaBack p) {
     }
     if (works) {
       RecordRows<3> rec;
-      rec.load(&records[c].of, records[c].solve_t, records[c].pairs_t, lane, g);
+      RecordNumbers num;
+      rec.load(&records[c].solve_t[0][0][0], &records[c].pairs_t[0][0][0], lane);
+      num.load(&records[c].of, m, g);
       f32x4 v[2], d[2], y[2], w[2] = {};
       load_column<T>(p.v, v0, first, valid, on, col, g, v);
       load_column<T>(p.dout, d0, first, valid, on, col, g, d);
@@ -88,12 +90,12 @@ __global__ __launch_bounds__(256) void k_delta_back(DeltaBack p) {
       const Operand<T> dp = operand_of<T>(d);
       f32x4 du[2], dz[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) w[i] = mma(rec.pairs[i], dp.v, rec.left[i] * w[i]);
+      for (int i = 0; i < 2; ++i) w[i] = mma(rec.pairs[i], dp.v, num.left[i] * w[i]);
       const Parts<3> wp = Parts<3>::of(w[0], w[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         du[i] = mma(rec.solve[i], wp.v, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-        dz[i] = rec.beta[i] * du[i];
+        dz[i] = num.beta[i] * du[i];
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -111,8 +113,8 @@ __global__ __launch_bounds__(256) void k_delta_back(DeltaBack p) {
       f32x4 into[2], outof[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        into[i] = p.scale * rec.gamma[i] * d[i];
-        outof[i] = -rec.gamma[i] * dz[i];
+        into[i] = p.scale * num.gamma[i] * d[i];
+        outof[i] = -num.gamma[i] * dz[i];
       }
       const Parts<3> ip = Parts<3>::of(into[0], into[1]), op = Parts<3>::of(outof[0], outof[1]);
       float border = 0.0f;
@@ -120,8 +122,7 @@ __global__ __launch_bounds__(256) void k_delta_back(DeltaBack p) {
       for (int k = 0; k < KX; ++k) {
 #pragma unroll
         for (int a = 2 * k; a < 2 * k + 2; ++a) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[a][e] = kept(s[a][e], rec.keep);
+          s[a] = num.keep(s[a]);
           auto column = [&](uint32_t i) { return state_row(a, i); };
           s[a] = mma(Operand<T>::template across<DK>(Q, column, m, g).v, ip.v, s[a]);
           s[a] = mma(Operand<T>::template across<DK>(K, column, m, g).v, op.v, s[a]);

@@ -19,7 +19,7 @@ struct Gates {
 struct DeltaRecord {
   bf16x8 solve[3][2][64], pairs[3][2][64];
   float gamma[32], left[32], beta[32];   // e^G, e^(G at the end - G), strengths
-  Keep keep;
+  float kept[2];                         // what is left of a state over the chunk, as a number and what rounding it left
   float pad[30];
 };
 struct DeltaRecordBack {
@@ -147,7 +147,11 @@ __global__ __launch_bounds__(256) void k_delta_pairs(DeltaPairs p) {
     record->left[lane] = expf((float)(total - sum));
     record->beta[lane] = strength;
   }
-  if (lane == 0) record->keep = keeps((float)total);
+  if (lane == 0) {
+    const double all = exp(total);
+    record->kept[0] = (float)all;
+    record->kept[1] = (float)(all - (double)(float)all);
+  }
 #pragma unroll
   for (int x = 0; x < 3; ++x) {
     const uint32_t row = 16 * (x > 0) + 4 * g, col = 16 * (x > 1) + m;

@@ -37,25 +37,87 @@ __device__ __forceinline__ size_t state_at(uint32_t bh, uint32_t chunks, uint32_
   return ((size_t)bh * chunks + c) * parts * ((dv + 31) / 32) * Tile<DK>::SIZE;
 }
 
+// What a pass takes of a record: rows of products, and numbers for the tokens 16 i + 4 g + r (and 16 i + m).
 template <int N>
-struct RecordRows {   // what a pass takes of a record, in registers
+struct RecordRows {
   bf16x8 solve[2][3], pairs[2][N];
-  f32x4 gamma[2], left[2], beta[2];
-  Keep keep;
-  __device__ __forceinline__ void load(const DeltaRecord* r, const bf16x8 (&s)[3][2][64], const bf16x8 (&p)[3][2][64], uint32_t lane, uint32_t g) {
+  __device__ __forceinline__ void load(const bf16x8* solves, const bf16x8* pairings, uint32_t lane) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int t = 0; t < 3; ++t) solve[i][t] = s[t][i][lane];
+      for (int t = 0; t < 3; ++t) solve[i][t] = solves[(2 * t + i) * 64 + lane];
 #pragma unroll
-      for (int t = 0; t < N; ++t) pairs[i][t] = p[t][i][lane];
+      for (int t = 0; t < N; ++t) pairs[i][t] = pairings[(2 * t + i) * 64 + lane];
+    }
+  }
+};
+struct RecordNumbers {
+  f32x4 gamma[2], left[2], beta[2];
+  float gamma_m[2], kept[2];
+  __device__ __forceinline__ void load(const DeltaRecord* r, uint32_t m, uint32_t g) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
       gamma[i] = *reinterpret_cast<const f32x4*>(r->gamma + 16 * i + 4 * g);
       left[i] = *reinterpret_cast<const f32x4*>(r->left + 16 * i + 4 * g);
       beta[i] = *reinterpret_cast<const f32x4*>(r->beta + 16 * i + 4 * g);
+      gamma_m[i] = r->gamma[16 * i + m];
+      kept[i] = r->kept[i];
     }
-    keep = r->keep;
+  }
+  // They are there: the compiler waits for its loads here, not where they are used, behind loads to LDS that it does not know of.
+  __device__ __forceinline__ void there() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(gamma[i]), "+v"(left[i]), "+v"(beta[i]), "+v"(gamma_m[i]), "+v"(kept[i]));
+  }
+  // What is left of a state: one rounding, of the sum (a rounded decay alone would be off by the same 2^-25 in each chunk).
+  __device__ __forceinline__ f32x4 keep(f32x4 s) const {
+    f32x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(s[e], kept[0], s[e] * kept[1]);
+    return o;
   }
 };
+
+// Rows of D columns straight into a tile in LDS, by four waves: each instruction of a wave fills 1 KiB, 64 pieces, and asks memory for those that
+// belong there.  Pieces behind the width are never asked for (they are cleared once); rows behind the last valid one are asked for as that
+// one, and cleared when they are there.
+template <int D>
+struct DirectRows {
+  static constexpr uint32_t N = Tile<D>::SIZE / 512 / 4;   // of a wave
+  uint32_t offset[N], row[N];
+  bool on[N];
+  uint32_t bytes;
+  __device__ __forceinline__ void set(const SeqRows& r, uint32_t width, uint32_t wave, uint32_t lane) {
+    bytes = (uint32_t)r.token * 2;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) {
+      const uint32_t place = (wave + 4 * i) * 64 + lane;
+      row[i] = place / Tile<D>::PIECES;
+      const uint32_t piece = place % Tile<D>::PIECES ^ Tile<D>::turn(row[i]);
+      on[i] = piece * 8 < width;
+      offset[i] = row[i] * bytes + piece * 16;
+    }
+  }
+  // n: rows that there are, of 32
+  __device__ __forceinline__ void ask(uint32_t to, const uint8_t* base, uint32_t wave, uint32_t n) const {
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) {
+      const uint32_t back = row[i] < n ? 0 : row[i] - (n - 1);
+      if (on[i]) load_to_lds(to + (wave + 4 * i) * 1024, base, offset[i] - back * bytes);
+    }
+  }
+  __device__ __forceinline__ static void clear(bf16* tile, uint32_t n, uint32_t thread) {
+    const bf16x8 zero = {};
+    for (uint32_t i = n * Tile<D>::PIECES + thread; i < Tile<D>::SIZE / 8; i += 256) *reinterpret_cast<bf16x8*>(tile + 8 * i) = zero;
+  }
+};
+// The first n KiB of a record's rows of products.
+__device__ __forceinline__ void ask_rows(uint32_t to, const void* from, uint32_t n, uint32_t wave, uint32_t lane) {
+  for (uint32_t i = wave; i < n; i += 4) load_to_lds(to + i * 1024, static_cast<const uint8_t*>(from) + i * 1024, lane * 16);
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
+}
 
 struct Halves { bf16x8 v[2]; };
 __device__ __forceinline__ Halves halves_of(f32x4 a, f32x4 b) {
@@ -131,6 +193,29 @@ __device__ __forceinline__ void store_four(T* row, bool wide, uint32_t col, uint
   }
 }
 
+// The same as the row has them (a conversion would be waited for).
+template <typename T>
+struct Four { T v[4]; };
+template <typename T>
+__device__ __forceinline__ void ask_four(const T* row, bool wide, uint32_t col, uint32_t width, Four<T>* o) {
+  typedef T Vec __attribute__((ext_vector_type(4)));
+  if (wide && width % 4 == 0) {
+    const Vec v = *reinterpret_cast<const Vec*>(row + (col < width ? col : 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o->v[i] = v[i];
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) o->v[i] = row[col + i < width ? col + i : 0];
+  }
+}
+template <typename T>
+__device__ __forceinline__ f32x4 four_of(const Four<T>& f, bool on, uint32_t col, uint32_t width) {
+  f32x4 o;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) o[i] = on && col + i < width ? as_float(f.v[i]) : 0.0f;
+  return o;
+}
+
 // Rows of queries and keys on their way to LDS.
 template <typename T, int DK>
 struct TwoRows {
@@ -160,23 +245,32 @@ struct TwoRows {
   }
 };
 
-template <typename T, int DK>
-constexpr uint32_t run_lds() { return 2 * 2 * kParts<T> * Tile<DK>::SIZE * sizeof(bf16); }
+// LDS of a chunk: rows of queries and keys, and where they come straight from memory those of 64 values and the record's products too (twice 32 KiB:
+// as far as such loads reach).
+template <typename T, int DK, int NP, bool DIRECT_ROWS>
+struct RunLds {
+  static constexpr uint32_t Q = 0, K = kParts<T> * Tile<DK>::SIZE, V = 2 * K, SOLVE = V + (DIRECT_ROWS ? Tile<64>::SIZE : 0),
+                            PAIRS = SOLVE + (DIRECT_ROWS ? 3 * 1024 : 0), SIZE = PAIRS + (DIRECT_ROWS ? NP * 1024 : 0), BYTES = 2 * SIZE * sizeof(bf16);
+};
+template <typename T, DeltaMode MODE>
+constexpr int kPairParts = sizeof(T) == 2 && MODE == FORWARD ? 2 : 3;
 
-template <typename T, int DK, DeltaMode MODE>
-__global__ __launch_bounds__(256) void k_delta_run(DeltaRun p) {
-  constexpr int TX = DK / 16, KX = DK / 32, PT = kParts<T>, LESS = sizeof(T) == 2 && MODE == FORWARD ? 1 : 2, NP = LESS + 1;
-  constexpr uint32_t BUFFER = 2 * PT * Tile<DK>::SIZE;
+template <typename T, int DK, DeltaMode MODE, bool DIRECT_ROWS>
+__global__ __launch_bounds__(256, 1) void k_delta_run(DeltaRun p) {
+  constexpr int TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = NP - 1;
+  typedef RunLds<T, DK, NP, DIRECT_ROWS> Lds;
+  static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   bf16* const lds = reinterpret_cast<bf16*>(lds_raw);
   const uint32_t slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, h = bh % p.H, b = bh / p.H;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  const uint32_t L = p.L, dk = p.dk, dv = p.dv, col0 = 64 * slice + 16 * wave, col = col0 + m;
-  const bool on = col < dv, works = col0 < (dv + 31) / 32 * 32;
+  const uint32_t L = p.L, dk = p.dk, dv = p.dv, blocks = (dv + 31) / 32, col0 = 64 * slice + 16 * wave, col = col0 + m;
+  const bool on = col < dv, works = col0 < blocks * 32;
   const uint32_t valid = valid_tokens(p.lengths, b, L), chunks = (valid + kChunk - 1) / kChunk;
   typedef typename RecordOf<MODE == KEEPING>::type Record;
   const Record* const records = static_cast<const Record*>(p.records) + (size_t)bh * p.chunks;
   const bool pieces = p.q.near && p.k.near && dk >= 16 / sizeof(T);
+  auto record = [&](uint32_t c) { return reinterpret_cast<const DeltaRecord*>(records + c); };
 
   f32x4 s[TX];
 #pragma unroll
@@ -188,102 +282,161 @@ __global__ __launch_bounds__(256) void k_delta_run(DeltaRun p) {
     }
   const T *const q0 = row_of<T>(p.q, b, 0, h), *const k0 = row_of<T>(p.k, b, 0, h), *const v0 = row_of<T>(p.v, b, 0, h);
   TwoRows<T, DK> rows;
-  RecordRows<NP> rec, next;
-  f32x4 v[2], next_v[2];
-  auto load_record = [&](uint32_t c, RecordRows<NP>* to) {
-    const DeltaRecord* r = reinterpret_cast<const DeltaRecord*>(records + c);
-    to->load(r, r->solve, r->pairs, lane, g);
+  DirectRows<DK> direct_q, direct_k;
+  DirectRows<64> direct_v;
+  RecordRows<NP> next;
+  RecordNumbers num, next_num;
+  f32x4 next_v[2];
+  Four<T> next_d[2], now_d[2];
+  const uint32_t lds0 = lds_address(lds);
+  auto fetch = [&](uint32_t c) {   // chunk c, to LDS or (rows by way of registers: the one behind it) to registers
+    if constexpr (DIRECT_ROWS) {
+      const uint32_t n = valid - c * kChunk, to = lds0 + (c & 1) * Lds::SIZE * 2;
+      auto rows_at = [&](const T* head, const SeqRows& r) { return reinterpret_cast<const uint8_t*>(head) + (int64_t)c * kChunk * r.token * 2; };
+      direct_q.ask(to + Lds::Q * 2, rows_at(q0, p.q), wave, n);
+      direct_k.ask(to + Lds::K * 2, rows_at(k0, p.k), wave, n);
+      direct_v.ask(to + Lds::V * 2, rows_at(v0 + 64 * slice, p.v), wave, n);
+      ask_rows(to + Lds::SOLVE * 2, record(c)->solve, 6, wave, lane);
+      ask_rows(to + Lds::PAIRS * 2, record(c)->pairs, 2 * NP, wave, lane);
+    } else {
+      rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
+      if (c + 1 < chunks) rows.load(p.q, p.k, q0, k0, (c + 1) * kChunk, valid, dk, pieces);
+      next.load(&record(c)->solve[0][0][0], &record(c)->pairs[0][0][0], lane);
+      load_column<T>(p.v, v0, c * kChunk, valid, on, col, g, next_v);
+    }
+    if constexpr (MODE == KEEPING) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t t = c * kChunk + 16 * i + m;
+        ask_four<T>(row_of<T>(p.dout, b, t < valid ? t : valid - 1, h), p.dout.wide, col0 + 4 * g, dv, &next_d[i]);
+      }
+    }
+    next_num.load(record(c), m, g);
   };
-  if (chunks) {
+  if constexpr (DIRECT_ROWS) {
+    direct_q.set(p.q, dk, wave, lane);
+    direct_k.set(p.k, dk, wave, lane);
+    direct_v.set(p.v, dv - 64 * slice, wave, lane);
+    if (dk < DK || dv - 64 * slice < 64) {
+      for (uint32_t i = 0; i < 2; ++i) {
+        DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::Q, 0, threadIdx.x);
+        DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::K, 0, threadIdx.x);
+        DirectRows<64>::clear(lds + i * Lds::SIZE + Lds::V, 0, threadIdx.x);
+      }
+      __syncthreads();
+    }
+  } else if (chunks) {
     rows.load(p.q, p.k, q0, k0, 0, valid, dk, pieces);
-    load_record(0, &next);
-    load_column<T>(p.v, v0, 0, valid, on, col, g, next_v);
-    rows.store(lds, valid, dk, pieces);
-    if (chunks > 1) rows.load(p.q, p.k, q0, k0, kChunk, valid, dk, pieces);
-    __syncthreads();
   }
+  if (chunks) fetch(0);
+  f32x4 o[2] = {}, y[2] = {};
+  // What chunk c leaves in memory is stored behind the next barrier: stores are older then than the loads that are waited for.
+  auto flush = [&](uint32_t c) {
+    if (!works) return;
+    const uint32_t first = c * kChunk;
+    if constexpr (MODE == KEEPING) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float* to = p.y + ((size_t)bh * p.chunks * kChunk + first + 16 * i + 4 * g) * (blocks * 32) + col;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[e * blocks * 32] = y[i][e];
+        const uint32_t t = first + 16 * i + m;
+        if (g == 0) p.along[((size_t)bh * (blocks * 2) + col0 / 16) * p.chunks * kChunk + t] = o[i][0];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t t = first + 16 * i + m;
+        if (t < L) store_four<T>(row_to<T>(p.out, b, t, h), p.out.wide, col0 + 4 * g, dv, t < valid ? o[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+      }
+    }
+  };
   for (uint32_t c = 0; c < chunks; ++c) {
     const uint32_t first = c * kChunk;
-    bf16 *const Q = lds + (c & 1) * BUFFER, *const K = Q + PT * Tile<DK>::SIZE;
-    rec = next;
-    v[0] = next_v[0];
-    v[1] = next_v[1];
-    if (c + 1 < chunks) {
-      rows.store(lds + ((c + 1) & 1) * BUFFER, valid - first - kChunk, dk, pieces);
-      if (c + 2 < chunks) rows.load(p.q, p.k, q0, k0, first + 2 * kChunk, valid, dk, pieces);
-      load_record(c + 1, &next);
-      load_column<T>(p.v, v0, first + kChunk, valid, on, col, g, next_v);
+    bf16 *const buffer = lds + (c & 1) * Lds::SIZE, *const Q = buffer + Lds::Q, *const K = buffer + Lds::K;
+    if constexpr (DIRECT_ROWS) {
+      arrive<0>();
+      if (valid - first < kChunk) {
+        DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
+        DirectRows<DK>::clear(K, valid - first, threadIdx.x);
+        DirectRows<64>::clear(buffer + Lds::V, valid - first, threadIdx.x);
+        __syncthreads();
+      }
+    } else {
+      __syncthreads();
     }
-    if (works) {
-      f32x4 x[2] = {}, o[2] = {};
+    next_num.there();
+    num = next_num;
+    RecordRows<NP> rec = next;
+    f32x4 v[2] = {next_v[0], next_v[1]};
+    if (c) flush(c - 1);
+    if constexpr (MODE == KEEPING) {
+      now_d[0] = next_d[0];
+      now_d[1] = next_d[1];
+      if (works) {
 #pragma unroll
-      for (int k = 0; k < KX; ++k) {
-        const Parts<3> sp = Parts<3>::of(s[2 * k], s[2 * k + 1]);
-        if constexpr (MODE == KEEPING) {
+        for (int k = 0; k < KX; ++k) {
           bf16* to = p.states + state_at<DK>(bh, p.chunks, c, dv, kStateParts<T>) + (size_t)(col0 / 32) * Tile<DK>::SIZE + Tile<DK>::at(col0 % 32 + m, 4 * k + g);
           if constexpr (sizeof(T) == 2) {
             const Halves both = halves_of(s[2 * k], s[2 * k + 1]);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * ((dv + 31) / 32) * Tile<DK>::SIZE) = both.v[t];
+            for (int t = 0; t < 2; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * blocks * Tile<DK>::SIZE) = both.v[t];
           } else {
+            const Parts<3> sp = Parts<3>::of(s[2 * k], s[2 * k + 1]);
 #pragma unroll
-            for (int t = 0; t < 3; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * ((dv + 31) / 32) * Tile<DK>::SIZE) = sp.v[t];
+            for (int t = 0; t < 3; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * blocks * Tile<DK>::SIZE) = sp.v[t];
           }
         }
+      }
+    }
+    if (c + 1 < chunks) fetch(c + 1);
+    if (works) {
+      f32x4 x[2] = {};
+      o[0] = o[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < KX; ++k) {
+        const Parts<3> sp = Parts<3>::of(s[2 * k], s[2 * k + 1]);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           x[i] = mma(Operand<T>::template along<DK>(K, 16 * i + m, k, g).v, sp.v, x[i]);
           o[i] = mma<LESS>(sp.v, Operand<T>::template along<DK>(Q, 16 * i + m, k, g).v, o[i]);
         }
       }
-      const Parts<3> z = Parts<3>::of(v[0] - rec.gamma[0] * x[0], v[1] - rec.gamma[1] * x[1]);
-      f32x4 y[2], u[2];
+      if constexpr (DIRECT_ROWS) {
+        rec.load(reinterpret_cast<const bf16x8*>(buffer + Lds::SOLVE), reinterpret_cast<const bf16x8*>(buffer + Lds::PAIRS), lane);
+        Operand<bf16>::across<64>(buffer + Lds::V, [&](uint32_t i) { return 16 * wave + i; }, m, g).widen(&v[0], &v[1]);
+      }
+      const Parts<3> z = Parts<3>::of(v[0] - num.gamma[0] * x[0], v[1] - num.gamma[1] * x[1]);
+      f32x4 u[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         y[i] = mma(rec.solve[i], z.v, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-        u[i] = rec.beta[i] * y[i];
+        u[i] = num.beta[i] * y[i];
       }
+      const Parts<3> w = Parts<3>::of(num.left[0] * u[0], num.left[1] * u[1]);
       const Parts<NP> up = Parts<NP>::of(u[0], u[1]);
-      const DeltaRecord* r = reinterpret_cast<const DeltaRecord*>(records + c);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        o[i] *= p.scale * r->gamma[16 * i + m];
+        o[i] *= p.scale * num.gamma_m[i];
         o[i] = mma<LESS>(up.v, rec.pairs[i], o[i]);
       }
       if constexpr (MODE == KEEPING) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float* to = p.y + ((size_t)bh * p.chunks * kChunk + first + 16 * i + 4 * g) * ((dv + 31) / 32 * 32) + col;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) to[(size_t)e * ((dv + 31) / 32 * 32)] = y[i][e];
-          const uint32_t t = first + 16 * i + m;
+          const f32x4 d = four_of<T>(now_d[i], first + 16 * i + m < valid, col0 + 4 * g, dv);
           float dot = 0.0f;
-          if (t < valid) {
-            const f32x4 d = load_four<T>(row_of<T>(p.dout, b, t, h), p.dout.wide, col0 + 4 * g, dv);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) dot = fmaf(d[e], o[i][e], dot);
-          }
+          for (int e = 0; e < 4; ++e) dot = fmaf(d[e], o[i][e], dot);
           dot += __shfl_xor(dot, 16);
-          dot += __shfl_xor(dot, 32);
-          if (g == 0) p.along[((size_t)bh * ((dv + 31) / 32 * 2) + col0 / 16) * p.chunks * kChunk + t] = dot;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t t = first + 16 * i + m;
-          if (t < L) store_four<T>(row_to<T>(p.out, b, t, h), p.out.wide, col0 + 4 * g, dv, t < valid ? o[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+          o[i][0] = dot + __shfl_xor(dot, 32);
         }
       }
-      const Parts<3> w = Parts<3>::of(rec.left[0] * u[0], rec.left[1] * u[1]);
 #pragma unroll
-      for (int a = 0; a < TX; ++a) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[a][e] = kept(s[a][e], rec.keep);
-        s[a] = mma(Operand<T>::template across<DK>(K, [&](uint32_t i) { return state_row(a, i); }, m, g).v, w.v, s[a]);
-      }
+      for (int a = 0; a < TX; ++a)
+        s[a] = mma(Operand<T>::template across<DK>(K, [&](uint32_t i) { return state_row(a, i); }, m, g).v, w.v, num.keep(s[a]));
     }
-    __syncthreads();
   }
+  if (chunks) flush(chunks - 1);
   if (MODE == FORWARD && works)
     for (uint32_t t = chunks * kChunk + m; t < L; t += 16) store_four<T>(row_to<T>(p.out, b, t, h), p.out.wide, col0 + 4 * g, dv, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
   if (p.to && on)

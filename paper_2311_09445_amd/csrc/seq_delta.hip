@@ -69,15 +69,21 @@ hipError_t launch(void (*kernel)(Args), std::atomic<uint64_t>* granted, uint32_t
   kernel<<<grid, 256, lds, s>>>(args);
   return hipGetLastError();
 }
+// In bfloat16 straight into LDS where rows are made up of pieces of 16 bytes.
 template <typename T, int DK, DeltaMode MODE>
 hipError_t launch_run(const DeltaRun& p, uint32_t bh, hipStream_t s) {
-  static std::atomic<uint64_t> granted{0};
-  return launch(k_delta_run<T, DK, MODE>, &granted, bh * p.slices, run_lds<T, DK>(), p, s);
+  static std::atomic<uint64_t> granted[2] = {};
+  constexpr int NP = kPairParts<T, MODE>;
+  if constexpr (sizeof(T) == 2) {
+    if (p.q.wide && p.k.wide && p.v.wide && p.dk % 8 == 0 && p.dv % 8 == 0)
+      return launch(k_delta_run<T, DK, MODE, true>, &granted[1], bh * p.slices, RunLds<T, DK, NP, true>::BYTES, p, s);
+  }
+  return launch(k_delta_run<T, DK, MODE, false>, &granted[0], bh * p.slices, RunLds<T, DK, NP, false>::BYTES, p, s);
 }
 template <typename T, int DK>
 hipError_t launch_back(const DeltaBack& p, uint32_t bh, hipStream_t s) {
   static std::atomic<uint64_t> granted{0};
-  return launch(k_delta_back<T, DK>, &granted, bh * p.slices, run_lds<T, DK>(), p, s);
+  return launch(k_delta_back<T, DK>, &granted, bh * p.slices, RunLds<T, DK, 3, false>::BYTES, p, s);
 }
 template <typename T, int DK>
 hipError_t launch_grads(const DeltaGrads& p, uint32_t bh, hipStream_t s) {
