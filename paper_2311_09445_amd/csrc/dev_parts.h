@@ -10,20 +10,22 @@ template <int N>
 struct Parts {
   bf16x8 v[N];
   __device__ __forceinline__ static Parts of(f32x4 a, f32x4 b) {
+    typedef float Two __attribute__((ext_vector_type(2)));
+    typedef bf16 Rounded __attribute__((ext_vector_type(2)));
+    Two x[4] = {{a[0], a[1]}, {a[2], a[3]}, {b[0], b[1]}, {b[2], b[3]}};
     Parts o;
 #pragma unroll
     for (int t = 0; t < N; ++t) {
+      u32x4 packed;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        o.v[t][i] = (bf16)a[i];
-        o.v[t][i + 4] = (bf16)b[i];
-      }
-      if (t + 1 < N)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          a[i] -= (float)o.v[t][i];
-          b[i] -= (float)o.v[t][i + 4];
+        packed[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x[i], Rounded));
+        if (t + 1 < N) {
+          x[i][0] -= __builtin_bit_cast(float, packed[i] << 16);
+          x[i][1] -= __builtin_bit_cast(float, packed[i] & 0xFFFF0000u);
         }
+      }
+      o.v[t] = __builtin_bit_cast(bf16x8, packed);
     }
     return o;
   }
@@ -38,6 +40,18 @@ __device__ __forceinline__ f32x4 mma(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB
     for (int i = 0; i < NA; ++i)
       if (s - i >= 0 && s - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], c, 0, 0, 0);
   return c;
+}
+
+// c[m] += a(m) b(m) for M products at once, in turn: an instruction that takes the result of the one before it waits for all of its passes.
+template <int M, int LEAST, int NA, int NB, typename A, typename B>
+__device__ __forceinline__ void mma_turns(A a, B b, f32x4 (&c)[M]) {
+#pragma unroll
+  for (int s = LEAST; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+      if (s - i >= 0 && s - i < NB)
+#pragma unroll
+        for (int m = 0; m < M; ++m) c[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a(m)[i], b(m)[s - i], c[m], 0, 0, 0);
 }
 
 // LDS of a wave's own: written by some lanes, read by others behind this.

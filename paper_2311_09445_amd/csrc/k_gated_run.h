@@ -256,8 +256,8 @@ template <typename T, DeltaMode MODE>
 constexpr int kPairParts = sizeof(T) == 2 && MODE == FORWARD ? 2 : 3;
 
 template <typename T, int DK, DeltaMode MODE, bool DIRECT_ROWS>
-__global__ __launch_bounds__(256, 1) void k_delta_run(DeltaRun p) {
-  constexpr int TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = NP - 1;
+__global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ? 2 : 1) void k_delta_run(DeltaRun p) {
+  constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = NP - 1;
   typedef RunLds<T, DK, NP, DIRECT_ROWS> Lds;
   static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
@@ -343,6 +343,11 @@ __global__ __launch_bounds__(256, 1) void k_delta_run(DeltaRun p) {
         const uint32_t t = first + 16 * i + m;
         if (g == 0) p.along[((size_t)bh * (blocks * 2) + col0 / 16) * p.chunks * kChunk + t] = o[i][0];
       }
+    } else if (DIRECT_ROWS && p.out.wide && valid - first >= kChunk) {
+      if (col0 + 4 * g < dv) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) store_four<T>(row_to<T>(p.out, b, first, h) + (int64_t)(16 * i + m) * p.out.token, true, col0 + 4 * g, ~0u, o[i]);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -391,34 +396,52 @@ __global__ __launch_bounds__(256, 1) void k_delta_run(DeltaRun p) {
     }
     if (c + 1 < chunks) fetch(c + 1);
     if (works) {
-      f32x4 x[2] = {};
-      o[0] = o[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      f32x4 x4[4] = {}, o4[4] = {};   // (of even and odd k)
+      Parts<3> sp[KX];
 #pragma unroll
-      for (int k = 0; k < KX; ++k) {
-        const Parts<3> sp = Parts<3>::of(s[2 * k], s[2 * k + 1]);
+      for (int k = 0; k < KX; k += 2) {
+        Operand<T> rows_k[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          x[i] = mma(Operand<T>::template along<DK>(K, 16 * i + m, k, g).v, sp.v, x[i]);
-          o[i] = mma<LESS>(sp.v, Operand<T>::template along<DK>(Q, 16 * i + m, k, g).v, o[i]);
-        }
+        for (int j = 0; j < 4; ++j) rows_k[j] = Operand<T>::template along<DK>(K, 16 * (j & 1) + m, k + j / 2, g);
+        sp[k] = Parts<3>::of(s[2 * k], s[2 * k + 1]);
+        sp[k + 1] = Parts<3>::of(s[2 * k + 2], s[2 * k + 3]);
+        mma_turns<4, 2, PT, 3>([&](int j) -> const bf16x8 (&)[PT] { return rows_k[j].v; }, [&](int j) -> const bf16x8 (&)[3] { return sp[k + j / 2].v; }, x4);
       }
       if constexpr (DIRECT_ROWS) {
         rec.load(reinterpret_cast<const bf16x8*>(buffer + Lds::SOLVE), reinterpret_cast<const bf16x8*>(buffer + Lds::PAIRS), lane);
         Operand<bf16>::across<64>(buffer + Lds::V, [&](uint32_t i) { return 16 * wave + i; }, m, g).widen(&v[0], &v[1]);
       }
-      const Parts<3> z = Parts<3>::of(v[0] - num.gamma[0] * x[0], v[1] - num.gamma[1] * x[1]);
+      const Parts<3> z = Parts<3>::of(v[0] - num.gamma[0] * (x4[0] + x4[2]), v[1] - num.gamma[1] * (x4[1] + x4[3]));
       f32x4 u[2];
+      y[0] = y[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      mma_turns<2, 2, 3, 3>([&](int i) -> const bf16x8 (&)[3] { return rec.solve[i]; }, [&](int) -> const bf16x8 (&)[3] { return z.v; }, y);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        y[i] = mma(rec.solve[i], z.v, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-        u[i] = num.beta[i] * y[i];
+      for (int k = 0; k < KX; k += 2) {
+        Operand<T> rows_q[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rows_q[j] = Operand<T>::template along<DK>(Q, 16 * (j & 1) + m, k + j / 2, g);
+        mma_turns<4, LESS, 3, PT>([&](int j) -> const bf16x8 (&)[3] { return sp[k + j / 2].v; }, [&](int j) -> const bf16x8 (&)[PT] { return rows_q[j].v; }, o4);
       }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) u[i] = num.beta[i] * y[i];
       const Parts<3> w = Parts<3>::of(num.left[0] * u[0], num.left[1] * u[1]);
       const Parts<NP> up = Parts<NP>::of(u[0], u[1]);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        o[i] *= p.scale * num.gamma_m[i];
-        o[i] = mma<LESS>(up.v, rec.pairs[i], o[i]);
+      for (int i = 0; i < 2; ++i) o[i] = p.scale * num.gamma_m[i] * (o4[i] + o4[i + 2]);
+      mma_turns<2, LESS, NP, NP>([&](int) -> const bf16x8 (&)[NP] { return up.v; }, [&](int i) -> const bf16x8 (&)[NP] { return rec.pairs[i]; }, o);
+      constexpr int TURN = PT == 1 ? TX : 4;
+#pragma unroll
+      for (int a0 = 0; a0 < TX; a0 += TURN) {
+        Operand<T> cols_k[TURN];
+        f32x4 part[TURN];
+#pragma unroll
+        for (int a = 0; a < TURN; ++a) {
+          cols_k[a] = Operand<T>::template across<DK>(K, [&](uint32_t i) { return state_row(a0 + a, i); }, m, g);
+          part[a] = num.keep(s[a0 + a]);
+        }
+        mma_turns<TURN, 2, PT, 3>([&](int a) -> const bf16x8 (&)[PT] { return cols_k[a].v; }, [&](int) -> const bf16x8 (&)[3] { return w.v; }, part);
+#pragma unroll
+        for (int a = 0; a < TURN; ++a) s[a0 + a] = part[a];
       }
       if constexpr (MODE == KEEPING) {
 #pragma unroll
@@ -431,9 +454,6 @@ __global__ __launch_bounds__(256, 1) void k_delta_run(DeltaRun p) {
           o[i][0] = dot + __shfl_xor(dot, 32);
         }
       }
-#pragma unroll
-      for (int a = 0; a < TX; ++a)
-        s[a] = mma(Operand<T>::template across<DK>(K, [&](uint32_t i) { return state_row(a, i); }, m, g).v, w.v, num.keep(s[a]));
     }
   }
   if (chunks) flush(chunks - 1);
