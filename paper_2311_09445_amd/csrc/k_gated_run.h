@@ -15,15 +15,17 @@ struct DeltaRun {
   const int32_t* lengths;
   const float* in;
   float* to;
-  int64_t in_batch, in_head, to_batch, to_head;
-  uint32_t L, H, dk, dv, chunks, slices;
+  int64_t in_batch, in_head, in_segment, to_batch, to_head;
+  uint32_t L, H, dk, dv, chunks, slices, segments, segment, run;   // segment: chunks of one; run: segments that are taken
   float scale;
+  float* carried;                // [sequence, head][segment]: what a segment adds [dk][dv], what it makes of a state [dk][dk]
   // kept for a gradient: the states before the chunks, Y, rows of out . dout
   bf16* states;
   float *y, *along;
 };
 
-enum DeltaMode { FORWARD, KEEPING };
+// CARRYING: no outputs; what a segment adds to a state, and (in slices of their own) what it makes of one: its product with the state before it.
+enum DeltaMode { FORWARD, KEEPING, CARRYING };
 
 // Planes of 16 bits that states are kept in for a gradient: where rows are bfloat16 the rounded state, which the products for bfloat16 gradients
 // take, and the lower half of the sum that rounded it, so that both together are the 32 bits (two rounded parts held 17, and the decays'
@@ -253,20 +255,24 @@ struct RunLds {
                             PAIRS = SOLVE + (DIRECT_ROWS ? 3 * 1024 : 0), SIZE = PAIRS + (DIRECT_ROWS ? NP * 1024 : 0), BYTES = 2 * SIZE * sizeof(bf16);
 };
 template <typename T, DeltaMode MODE>
-constexpr int kPairParts = sizeof(T) == 2 && MODE == FORWARD ? 2 : 3;
+constexpr int kPairParts = MODE == CARRYING ? 1 : sizeof(T) == 2 && MODE == FORWARD ? 2 : 3;
 
 template <typename T, int DK, DeltaMode MODE, bool DIRECT_ROWS>
-__global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ? 2 : 1) void k_delta_run(DeltaRun p) {
+__global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ? 2 : 1) void k_delta_run(DeltaRun p) {
   constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = NP - 1;
   typedef RunLds<T, DK, NP, DIRECT_ROWS> Lds;
   static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   bf16* const lds = reinterpret_cast<bf16*>(lds_raw);
-  const uint32_t slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, h = bh % p.H, b = bh / p.H;
+  const uint32_t dk = p.dk, all_slices = MODE == CARRYING ? p.slices + (dk + 63) / 64 : p.slices;
+  const uint32_t item = blockIdx.x / all_slices, slice_of_all = blockIdx.x % all_slices, seg = item % p.run, bh = item / p.run, h = bh % p.H, b = bh / p.H;
+  const bool product = MODE == CARRYING && slice_of_all >= p.slices;
+  const uint32_t slice = product ? slice_of_all - p.slices : slice_of_all;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  const uint32_t L = p.L, dk = p.dk, dv = p.dv, blocks = (dv + 31) / 32, col0 = 64 * slice + 16 * wave, col = col0 + m;
-  const bool on = col < dv, works = col0 < blocks * 32;
-  const uint32_t valid = valid_tokens(p.lengths, b, L), chunks = (valid + kChunk - 1) / kChunk;
+  const uint32_t L = p.L, dv = product ? dk : p.dv, blocks = (dv + 31) / 32, col0 = 64 * slice + 16 * wave, col = col0 + m;
+  const bool on = col < dv, works = col0 < blocks * 32, takes = on && !product;   // takes: values
+  const uint32_t valid = valid_tokens(p.lengths, b, L), all_chunks = (valid + kChunk - 1) / kChunk;
+  const uint32_t chunk0 = seg * p.segment, chunks = all_chunks < chunk0 ? chunk0 : all_chunks - chunk0 < p.segment ? all_chunks : chunk0 + p.segment;   // its end
   typedef typename RecordOf<MODE == KEEPING>::type Record;
   const Record* const records = static_cast<const Record*>(p.records) + (size_t)bh * p.chunks;
   const bool pieces = p.q.near && p.k.near && dk >= 16 / sizeof(T);
@@ -278,7 +284,8 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const uint32_t row = state_row(a, 4 * g + r);
-      s[a][r] = p.in && on && row < dk ? p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + (size_t)row * dv + col] : 0.0f;
+      if (MODE == CARRYING) s[a][r] = product && row == col && on ? 1.0f : 0.0f;
+      else s[a][r] = p.in && on && row < dk ? p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + seg * p.in_segment + (size_t)row * dv + col] : 0.0f;
     }
   const T *const q0 = row_of<T>(p.q, b, 0, h), *const k0 = row_of<T>(p.k, b, 0, h), *const v0 = row_of<T>(p.v, b, 0, h);
   TwoRows<T, DK> rows;
@@ -293,16 +300,16 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
     if constexpr (DIRECT_ROWS) {
       const uint32_t n = valid - c * kChunk, to = lds0 + (c & 1) * Lds::SIZE * 2;
       auto rows_at = [&](const T* head, const SeqRows& r) { return reinterpret_cast<const uint8_t*>(head) + (int64_t)c * kChunk * r.token * 2; };
-      direct_q.ask(to + Lds::Q * 2, rows_at(q0, p.q), wave, n);
+      if (MODE != CARRYING) direct_q.ask(to + Lds::Q * 2, rows_at(q0, p.q), wave, n);
       direct_k.ask(to + Lds::K * 2, rows_at(k0, p.k), wave, n);
-      direct_v.ask(to + Lds::V * 2, rows_at(v0 + 64 * slice, p.v), wave, n);
+      if (!product) direct_v.ask(to + Lds::V * 2, rows_at(v0 + 64 * slice, p.v), wave, n);
       ask_rows(to + Lds::SOLVE * 2, record(c)->solve, 6, wave, lane);
-      ask_rows(to + Lds::PAIRS * 2, record(c)->pairs, 2 * NP, wave, lane);
+      if (MODE != CARRYING) ask_rows(to + Lds::PAIRS * 2, record(c)->pairs, 2 * NP, wave, lane);
     } else {
       rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
       if (c + 1 < chunks) rows.load(p.q, p.k, q0, k0, (c + 1) * kChunk, valid, dk, pieces);
       next.load(&record(c)->solve[0][0][0], &record(c)->pairs[0][0][0], lane);
-      load_column<T>(p.v, v0, c * kChunk, valid, on, col, g, next_v);
+      load_column<T>(p.v, v0, c * kChunk, valid, takes, col, g, next_v);
     }
     if constexpr (MODE == KEEPING) {
 #pragma unroll
@@ -316,8 +323,8 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
   if constexpr (DIRECT_ROWS) {
     direct_q.set(p.q, dk, wave, lane);
     direct_k.set(p.k, dk, wave, lane);
-    direct_v.set(p.v, dv - 64 * slice, wave, lane);
-    if (dk < DK || dv - 64 * slice < 64) {
+    direct_v.set(p.v, product ? 0 : dv - 64 * slice, wave, lane);
+    if (dk < DK || dv - 64 * slice < 64 || product) {
       for (uint32_t i = 0; i < 2; ++i) {
         DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::Q, 0, threadIdx.x);
         DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::K, 0, threadIdx.x);
@@ -325,14 +332,14 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
       }
       __syncthreads();
     }
-  } else if (chunks) {
-    rows.load(p.q, p.k, q0, k0, 0, valid, dk, pieces);
+  } else if (chunk0 < chunks) {
+    rows.load(p.q, p.k, q0, k0, chunk0 * kChunk, valid, dk, pieces);
   }
-  if (chunks) fetch(0);
+  if (chunk0 < chunks) fetch(chunk0);
   f32x4 o[2] = {}, y[2] = {};
   // What chunk c leaves in memory is stored behind the next barrier: stores are older then than the loads that are waited for.
   auto flush = [&](uint32_t c) {
-    if (!works) return;
+    if (!works || MODE == CARRYING) return;
     const uint32_t first = c * kChunk;
     if constexpr (MODE == KEEPING) {
 #pragma unroll
@@ -356,7 +363,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
       }
     }
   };
-  for (uint32_t c = 0; c < chunks; ++c) {
+  for (uint32_t c = chunk0; c < chunks; ++c) {
     const uint32_t first = c * kChunk;
     bf16 *const buffer = lds + (c & 1) * Lds::SIZE, *const Q = buffer + Lds::Q, *const K = buffer + Lds::K;
     if constexpr (DIRECT_ROWS) {
@@ -374,7 +381,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
     num = next_num;
     RecordRows<NP> rec = next;
     f32x4 v[2] = {next_v[0], next_v[1]};
-    if (c) flush(c - 1);
+    if (c > chunk0) flush(c - 1);
     if constexpr (MODE == KEEPING) {
       now_d[0] = next_d[0];
       now_d[1] = next_d[1];
@@ -415,6 +422,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
       f32x4 u[2];
       y[0] = y[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       mma_turns<2, 2, 3, 3>([&](int i) -> const bf16x8 (&)[3] { return rec.solve[i]; }, [&](int) -> const bf16x8 (&)[3] { return z.v; }, y);
+      if constexpr (MODE != CARRYING)
 #pragma unroll
       for (int k = 0; k < KX; k += 2) {
         Operand<T> rows_q[4];
@@ -428,7 +436,8 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
       const Parts<NP> up = Parts<NP>::of(u[0], u[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) o[i] = p.scale * num.gamma_m[i] * (o4[i] + o4[i + 2]);
-      mma_turns<2, LESS, NP, NP>([&](int) -> const bf16x8 (&)[NP] { return up.v; }, [&](int i) -> const bf16x8 (&)[NP] { return rec.pairs[i]; }, o);
+      if constexpr (MODE != CARRYING)
+        mma_turns<2, LESS, NP, NP>([&](int) -> const bf16x8 (&)[NP] { return up.v; }, [&](int i) -> const bf16x8 (&)[NP] { return rec.pairs[i]; }, o);
       constexpr int TURN = PT == 1 ? TX : 4;
 #pragma unroll
       for (int a0 = 0; a0 < TX; a0 += TURN) {
@@ -456,15 +465,113 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE == FORWARD || DK == 64) ?
       }
     }
   }
-  if (chunks) flush(chunks - 1);
-  if (MODE == FORWARD && works)
-    for (uint32_t t = chunks * kChunk + m; t < L; t += 16) store_four<T>(row_to<T>(p.out, b, t, h), p.out.wide, col0 + 4 * g, dv, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-  if (p.to && on)
+  if (chunk0 < chunks) flush(chunks - 1);
+  if (MODE == FORWARD && works) {
+    const uint32_t end = p.segment < (L - chunk0 * kChunk + kChunk - 1) / kChunk ? (chunk0 + p.segment) * kChunk : L;
+    for (uint32_t t = chunks * kChunk + m; t < end; t += 16) store_four<T>(row_to<T>(p.out, b, t, h), p.out.wide, col0 + 4 * g, dv, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+  }
+  float* to = seg + 1 == p.segments && p.to ? p.to + (int64_t)b * p.to_batch + (int64_t)h * p.to_head : nullptr;
+  if (MODE == CARRYING) to = p.carried + ((size_t)bh * p.segments + seg) * dk * (p.dv + dk) + (product ? dk * p.dv : 0);
+  if (to && on)
 #pragma unroll
     for (int a = 0; a < TX; ++a)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const uint32_t row = state_row(a, 4 * g + r);
-        if (row < dk) p.to[(int64_t)b * p.to_batch + (int64_t)h * p.to_head + (size_t)row * dv + col] = s[a][r];
+        if (row < dk) to[(size_t)row * dv + col] = s[a][r];
       }
+}
+
+// The states that segments start from, one behind the other: S <- P S + B, with what each segment carries; S takes the place of B.  BACK: of
+// the gradients behind the segments, R <- P^T R + C.  A workgroup takes 64 columns, a wave 16 rows of them; the rows' parts meet in LDS, where
+// they lie as operands, and the next segment's product is under way meanwhile.  (A wave for 16 columns and all rows took 45 us for a
+// segment: it takes all of P apart by itself.)
+struct DeltaJoin {
+  float* carried;            // [sequence, head][segment]: B or C, rows of dv
+  const float* products;     // P, rows of dk
+  const float* in;
+  int64_t in_batch, in_head;
+  size_t stride, product_stride;
+  uint32_t H, dk, dv, slices, segments;
+};
+template <int DK, bool BACK>
+__global__ __launch_bounds__(4 * DK) void k_delta_join(DeltaJoin p) {
+  constexpr int KX = DK / 32;
+  __shared__ __attribute__((aligned(16))) bf16x8 lds[3][KX][4][64];
+  const uint32_t slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, h = bh % p.H, b = bh / p.H;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const uint32_t dk = p.dk, dv = p.dv, row = state_row(wave, 4 * g), of_m = state_row(wave, m);
+  uint32_t at[4][4];   // of the wave's elements
+  bool on[4][4];
+  f32x4 s[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (uint32_t r = 0; r < 4; ++r) {
+      const uint32_t col = 64 * slice + 16 * c + m;
+      on[c][r] = col < dv && row + r < dk;
+      at[c][r] = on[c][r] ? (row + r) * dv + col : 0;
+      s[c][r] = p.in && on[c][r] ? p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + at[c][r]] : 0.0f;
+    }
+  f32x4 product[KX][2], add[4];
+  auto load = [&](uint32_t i) {
+    const uint32_t seg = BACK ? p.segments - 1 - i : i;
+    const float* const from = p.carried + ((size_t)bh * p.segments + seg) * p.stride;
+    const float* const P = p.products + ((size_t)bh * p.segments + seg) * p.product_stride;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) add[c][r] = from[at[c][r]];
+    if (i + 1 == p.segments) return;   // (the last one's product leads nowhere)
+#pragma unroll
+    for (int k = 0; k < KX; ++k)
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) {
+        const uint32_t place = 32 * k + 8 * g + e, x = of_m < dk && place < dk ? (BACK ? place * dk + of_m : of_m * dk + place) : 0;
+        product[k][e / 4][e % 4] = P[x];
+      }
+  };
+  load(0);
+  for (uint32_t i = 0; i < p.segments; ++i) {
+    const uint32_t seg = BACK ? p.segments - 1 - i : i;
+    float* const to = p.carried + ((size_t)bh * p.segments + seg) * p.stride;
+    f32x4 acc[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        acc[c][r] = on[c][r] ? add[c][r] : 0.0f;
+        if (on[c][r]) to[at[c][r]] = s[c][r];
+      }
+    if (i + 1 == p.segments) break;
+    Parts<3> P[KX];
+#pragma unroll
+    for (int k = 0; k < KX; ++k) {
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if (of_m >= dk || 32 * k + 8 * g + e >= dk) product[k][e / 4][e % 4] = 0.0f;
+      P[k] = Parts<3>::of(product[k][0], product[k][1]);
+    }
+    load(i + 1);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const Parts<3> x = Parts<3>::of(s[c], s[c]);
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        reinterpret_cast<bf16x4*>(&lds[t][wave / 2][c][lane])[wave & 1] = __builtin_shufflevector(x.v[t], x.v[t], 0, 1, 2, 3);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < KX; ++k) {
+      bf16x8 x[4][3];
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int t = 0; t < 3; ++t) x[c][t] = lds[t][k][c][lane];
+      mma_turns<4, 2, 3, 3>([&](int) -> const bf16x8 (&)[3] { return P[k].v; }, [&](int c) -> const bf16x8 (&)[3] { return x[c]; }, acc);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) s[c] = acc[c];
+    __syncthreads();
+  }
 }

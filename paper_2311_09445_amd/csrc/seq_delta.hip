@@ -5,6 +5,7 @@
 // Sequences are taken in chunks of 32 tokens (k_gated_pairs.h: what a chunk's tokens make of each other, all chunks at once; k_gated_run.h: the
 // states one chunk behind the other; k_gated_back.h: the gradient, against time and then all chunks at once), single tokens in k_gated_step.h.
 #include <atomic>
+#include <stdlib.h>
 
 #include "dev_parts.h"
 
@@ -22,6 +23,21 @@ Gates gates(const per_seq_gates& g) { return Gates{g.d, g.batch, g.token, g.head
 uint32_t chunks_of(uint32_t L) { return (L + kChunk - 1) / kChunk; }
 // (256 divides every chunk's part of a workspace, so that the parts stay aligned)
 uint32_t padded(uint32_t dk) { return dk <= 64 ? 64 : 128; }
+
+// How a sequence is cut: in segments of whole chunks, each from the state that those before it bring.
+struct Cut { uint32_t segments, segment; };
+Cut cut(const DeltaSizes& a, bool backward) {
+  const uint32_t chunks = chunks_of(a.L);
+  static const int force = getenv("PER_CUT") ? atoi(getenv("PER_CUT")) : 0;
+  uint32_t s = force ? force : 1;
+  if (s > chunks) s = chunks ? chunks : 1;
+  const uint32_t segment = chunks ? (chunks + s - 1) / s : 1;
+  return Cut{chunks ? (chunks + segment - 1) / segment : 1, segment};
+}
+size_t carried_floats(const DeltaSizes& a) { return (size_t)a.dk * (a.dk + a.dv); }   // of a segment
+size_t carried_bytes(const DeltaSizes& a, const Cut& c) { return c.segments < 2 ? 0 : align256((size_t)a.B * a.H * c.segments * carried_floats(a) * sizeof(float)); }
+
+size_t record_bytes(const DeltaSizes& a) { return (size_t)a.B * a.H * chunks_of(a.L) * sizeof(DeltaRecord); }
 
 // Where a gradient's intermediate results lie in the workspace.
 struct BackWork {
@@ -74,11 +90,12 @@ template <typename T, int DK, DeltaMode MODE>
 hipError_t launch_run(const DeltaRun& p, uint32_t bh, hipStream_t s) {
   static std::atomic<uint64_t> granted[2] = {};
   constexpr int NP = kPairParts<T, MODE>;
+  const uint32_t grid = bh * p.run * (p.slices + (MODE == CARRYING ? (p.dk + 63) / 64 : 0));
   if constexpr (sizeof(T) == 2) {
     if (p.q.wide && p.k.wide && p.v.wide && p.dk % 8 == 0 && p.dv % 8 == 0)
-      return launch(k_delta_run<T, DK, MODE, true>, &granted[1], bh * p.slices, RunLds<T, DK, NP, true>::BYTES, p, s);
+      return launch(k_delta_run<T, DK, MODE, true>, &granted[1], grid, RunLds<T, DK, NP, true>::BYTES, p, s);
   }
-  return launch(k_delta_run<T, DK, MODE, false>, &granted[0], bh * p.slices, RunLds<T, DK, NP, false>::BYTES, p, s);
+  return launch(k_delta_run<T, DK, MODE, false>, &granted[0], grid, RunLds<T, DK, NP, false>::BYTES, p, s);
 }
 template <typename T, int DK>
 hipError_t launch_back(const DeltaBack& p, uint32_t bh, hipStream_t s) {
@@ -115,15 +132,41 @@ DeltaRun make_run(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows
   p.chunks = chunks_of(a.L);
   p.slices = (a.dv + 63) / 64;
   p.scale = a.scale;
+  p.segments = p.segment = p.run = 1;
+  if (p.chunks) p.segment = p.chunks;
   return p;
+}
+// The states that segments start from: what each carries (all but the last; with `all`, the last's product too), then one behind the other.
+template <typename T, int DK>
+hipError_t launch_carry(DeltaRun* p, const DeltaSizes& a, const Cut& c, const per_seq_states* state, float* carried, bool all, hipStream_t s) {
+  p->segments = p->run = c.segments;
+  p->segment = c.segment;
+  if (c.segments < 2) return hipSuccess;
+  p->carried = carried;
+  p->run = all ? c.segments : c.segments - 1;
+  hipError_t e = launch_run<T, DK, CARRYING>(*p, a.B * a.H, s);
+  if (e != hipSuccess) return e;
+  const size_t each = carried_floats(a);
+  DeltaJoin j{carried, carried + (size_t)a.dk * a.dv, nullptr, 0, 0, each, each, a.H, a.dk, a.dv, p->slices, c.segments};
+  if (state) { j.in = state->d; j.in_batch = state->batch; j.in_head = state->head; }
+  k_delta_join<DK, false><<<a.B * a.H * p->slices, 4 * DK, 0, s>>>(j);
+  e = hipGetLastError();
+  p->run = c.segments;
+  p->in = carried;
+  p->in_segment = (int64_t)each;
+  p->in_head = p->in_segment * c.segments;
+  p->in_batch = p->in_head * a.H;
+  return e;
 }
 
 template <typename T, int DK>
 hipError_t forward(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state,
                    const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
-  const hipError_t e = launch_pairs<T, DK, false>(a, q, k, work, s);
+  hipError_t e = launch_pairs<T, DK, false>(a, q, k, work, s);
   if (e != hipSuccess) return e;
   DeltaRun p = make_run(a, q, k, v, state, work);
+  e = launch_carry<T, DK>(&p, a, cut(a, false), state, reinterpret_cast<float*>(static_cast<uint8_t*>(work) + record_bytes(a)), false, s);
+  if (e != hipSuccess) return e;
   p.out = rows(out, a.dtype, 1);
   if (out_state) { p.to = out_state->d; p.to_batch = out_state->batch; p.to_head = out_state->head; }
   return launch_run<T, DK, FORWARD>(p, a.B * a.H, s);
@@ -241,7 +284,7 @@ hipError_t step(DeltaStep p, uint32_t rows, hipStream_t s) {
 
 size_t delta_work_bytes(const DeltaSizes& a, bool backward) {
   if (!a.B || !a.H || !a.L) return 0;
-  return backward ? back_work(a).bytes : (size_t)a.B * a.H * chunks_of(a.L) * sizeof(DeltaRecord);
+  return backward ? back_work(a).bytes : record_bytes(a) + carried_bytes(a, cut(a, false));
 }
 
 hipError_t launch_delta(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state,
