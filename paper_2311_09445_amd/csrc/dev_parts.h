@@ -68,4 +68,19 @@ __device__ __forceinline__ float sum16(float x) {
   return x;
 }
 
+// Sums over the 16 lanes that share a lane's g, of 16 values at once: value m in lane m.  Halves of the values and of the lanes meet.
+__device__ __forceinline__ float sums16(float (&v)[16], uint32_t m) {
+#define PER_MEET(n, ctrl, upper)                                                                                                    \
+  _Pragma("unroll") for (int i = 0; i < n; ++i) {                                                                                   \
+    const float keep = (upper) ? v[i + n] : v[i], give = (upper) ? v[i] : v[i + n];                                                 \
+    v[i] = keep + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, give), ctrl, 0xF, 0xF, false));  \
+  }
+  PER_MEET(8, 0x140, m & 8)   // the row turned around
+  PER_MEET(4, 0x141, m & 4)   // the half row
+  PER_MEET(2, 0x4E, m & 2)
+  PER_MEET(1, 0xB1, m & 1)
+#undef PER_MEET
+  return v[0];
+}
+
 }  // namespace per

@@ -10,15 +10,16 @@
 // <R, S>; from one token to the next it falls by out . dO - dZ . V, which is added up within a chunk only.
 
 struct DeltaBack {
-  SeqRows q, k, v, dout, dv;
+  SeqRows q, k, v, dout;
   const void* records;
   const int32_t* lengths;
   const float* in;
   float* to;
-  int64_t in_batch, in_head, to_batch, to_head;
-  uint32_t L, H, dk, dvw, chunks, slices;
+  int64_t in_batch, in_head, in_segment, to_batch, to_head;
+  uint32_t L, H, dk, dv, chunks, slices, segments, segment;   // segment: chunks of one
+  uint32_t first_segment, run;   // the segments that are taken
   float scale;
-  uint32_t direct;               // dV goes to its rows (no heads share them)
+  float* carried;                // [sequence, head][segment][dk][dv]: what a segment adds to the gradient of the state before it
   const bf16* states;
   const float* y;
   bf16* dstates;                 // the gradients of the states behind the chunks
@@ -28,17 +29,26 @@ struct DeltaBack {
 template <typename T>
 constexpr int kGradParts = sizeof(T) == 2 ? 1 : 3;   // of states in the products for rows
 
-template <typename T, int DK>
-__global__ __launch_bounds__(256) void k_delta_back(DeltaBack p) {
-  constexpr int TX = DK / 16, KX = DK / 32, PT = kParts<T>;
-  constexpr uint32_t BUFFER = RunLds<T, DK, 3, false>::SIZE;
+template <typename T, int DK, bool DIRECT_ROWS>
+struct BackLds {
+  static constexpr uint32_t Q = 0, K = kParts<T> * Tile<DK>::SIZE, V = 2 * K, D = V + (DIRECT_ROWS ? Tile<64>::SIZE : 0),
+                            SOLVE = D + (DIRECT_ROWS ? Tile<64>::SIZE : 0), SIZE = SOLVE + (DIRECT_ROWS ? 3 * 1024 : 0), BYTES = 2 * SIZE * sizeof(bf16);
+};
+
+// CARRY: only what a segment adds.
+template <typename T, int DK, bool CARRY, bool DIRECT_ROWS>
+__global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
+  constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, TURN = PT == 1 ? TX : 4;
+  typedef BackLds<T, DK, DIRECT_ROWS> Lds;
+  static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   bf16* const lds = reinterpret_cast<bf16*>(lds_raw);
-  const uint32_t slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, h = bh % p.H, b = bh / p.H;
+  const uint32_t slice = blockIdx.x % p.slices, item = blockIdx.x / p.slices, seg = p.first_segment + item % p.run, bh = item / p.run, h = bh % p.H, b = bh / p.H;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  const uint32_t L = p.L, dk = p.dk, dv = p.dvw, blocks = (dv + 31) / 32, col0 = 64 * slice + 16 * wave, col = col0 + m;
+  const uint32_t L = p.L, dk = p.dk, dv = p.dv, blocks = (dv + 31) / 32, col0 = 64 * slice + 16 * wave, col = col0 + m;
   const bool on = col < dv, works = col0 < blocks * 32;
-  const uint32_t valid = valid_tokens(p.lengths, b, L), chunks = (valid + kChunk - 1) / kChunk, width = blocks * 32;
+  const uint32_t valid = __builtin_amdgcn_readfirstlane(valid_tokens(p.lengths, b, L)), all_chunks = (valid + kChunk - 1) / kChunk, width = blocks * 32;
+  const uint32_t chunk0 = seg * p.segment, chunks = all_chunks < chunk0 ? chunk0 : all_chunks - chunk0 < p.segment ? all_chunks : chunk0 + p.segment;   // its end
   const DeltaRecordBack* const records = static_cast<const DeltaRecordBack*>(p.records) + (size_t)bh * p.chunks;
   const bool pieces = p.q.near && p.k.near && dk >= 16 / sizeof(T);
   const size_t row0 = (size_t)bh * p.chunks * kChunk, part0 = ((size_t)bh * (blocks * 2) + col0 / 16) * p.chunks;
@@ -49,132 +59,223 @@ __global__ __launch_bounds__(256) void k_delta_back(DeltaBack p) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const uint32_t row = state_row(a, 4 * g + r);
-      s[a][r] = p.in && on && row < dk ? p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + (size_t)row * dv + col] : 0.0f;
+      s[a][r] = !CARRY && p.in && on && row < dk ? p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + seg * p.in_segment + (size_t)row * dv + col] : 0.0f;
     }
   const T *const q0 = row_of<T>(p.q, b, 0, h), *const k0 = row_of<T>(p.k, b, 0, h), *const v0 = row_of<T>(p.v, b, 0, h), *const d0 = row_of<T>(p.dout, b, 0, h);
   TwoRows<T, DK> rows;
-  if (chunks) {
-    rows.load(p.q, p.k, q0, k0, (chunks - 1) * kChunk, valid, dk, pieces);
-    rows.store(lds + ((chunks - 1) & 1) * BUFFER, valid - (chunks - 1) * kChunk, dk, pieces);
-    if (chunks > 1) rows.load(p.q, p.k, q0, k0, (chunks - 2) * kChunk, valid, dk, pieces);
-    __syncthreads();
-  }
-  for (uint32_t left_chunks = chunks; left_chunks; --left_chunks) {
-    const uint32_t c = left_chunks - 1, first = c * kChunk;
-    bf16 *const Q = lds + (c & 1) * BUFFER, *const K = Q + PT * Tile<DK>::SIZE;
-    if (c) {
-      rows.store(lds + ((c - 1) & 1) * BUFFER, kChunk, dk, pieces);
-      if (c > 1) rows.load(p.q, p.k, q0, k0, first - 2 * kChunk, valid, dk, pieces);
+  DirectRows<DK> direct_q, direct_k;
+  DirectRows<64> direct_v, direct_d;
+  struct Next {
+    bf16x8 pairs[3][2], solve[3][2];
+    f32x4 y[2], v[2], d[2];
+  } next, now;
+  RecordNumbers num, next_num;
+  const uint32_t lds0 = lds_address(lds);
+  auto fetch = [&](uint32_t c) {
+    const DeltaRecordBack* const record = records + c;
+    if constexpr (DIRECT_ROWS) {
+      const uint32_t n = valid - c * kChunk, to = lds0 + (c & 1) * Lds::SIZE * 2;
+      auto rows_at = [&](const T* head, const SeqRows& r) { return reinterpret_cast<const uint8_t*>(head) + (int64_t)c * kChunk * r.token * 2; };
+      direct_q.ask(to + Lds::Q * 2, rows_at(q0, p.q), wave, n);
+      direct_k.ask(to + Lds::K * 2, rows_at(k0, p.k), wave, n);
+      if (!CARRY) direct_v.ask(to + Lds::V * 2, rows_at(v0 + 64 * slice, p.v), wave, n);
+      direct_d.ask(to + Lds::D * 2, rows_at(d0 + 64 * slice, p.dout), wave, n);
+      ask_rows(to + Lds::SOLVE * 2, record->solve_t, 6, wave, lane);
+    } else {
+      rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
+      if (c > chunk0) rows.load(p.q, p.k, q0, k0, (c - 1) * kChunk, valid, dk, pieces);
+      if (!CARRY) load_column<T>(p.v, v0, c * kChunk, valid, on, col, g, next.v);
+      load_column<T>(p.dout, d0, c * kChunk, valid, on, col, g, next.d);
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) next.solve[t][i] = record->solve_t[t][i][lane];
     }
-    if (works) {
-      RecordRows<3> rec;
-      RecordNumbers num;
-      rec.load(&records[c].solve_t[0][0][0], &records[c].pairs_t[0][0][0], lane);
-      num.load(&records[c].of, m, g);
-      f32x4 v[2], d[2], y[2], w[2] = {};
-      load_column<T>(p.v, v0, first, valid, on, col, g, v);
-      load_column<T>(p.dout, d0, first, valid, on, col, g, d);
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) next.pairs[t][i] = record->pairs_t[t][i][lane];
+    if (!CARRY && works)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y[i][r] = p.y[(row0 + first + 16 * i + 4 * g + r) * width + col];
+        for (int r = 0; r < 4; ++r) next.y[i][r] = p.y[(row0 + c * kChunk + 16 * i + 4 * g + r) * width + col];
+    next_num.load(&record->of, m, g);
+  };
+  if constexpr (DIRECT_ROWS) {
+    direct_q.set(p.q, dk, wave, lane);
+    direct_k.set(p.k, dk, wave, lane);
+    direct_v.set(p.v, dv - 64 * slice, wave, lane);
+    direct_d.set(p.dout, dv - 64 * slice, wave, lane);
+    if (dk < DK || dv - 64 * slice < 64) {
+      for (uint32_t i = 0; i < 2; ++i) {
+        DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::Q, 0, threadIdx.x);
+        DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::K, 0, threadIdx.x);
+        DirectRows<64>::clear(lds + i * Lds::SIZE + Lds::V, 0, threadIdx.x);
+        DirectRows<64>::clear(lds + i * Lds::SIZE + Lds::D, 0, threadIdx.x);
+      }
+      __syncthreads();
+    }
+  } else if (chunk0 < chunks) {
+    rows.load(p.q, p.k, q0, k0, (chunks - 1) * kChunk, valid, dk, pieces);
+  }
+  if (chunk0 < chunks) fetch(chunks - 1);
+  f32x4 dz[2] = {};
+  float sums = 0.0f, border = 0.0f;
+  auto flush = [&](uint32_t c) {   // (behind the next barrier, as over time)
+    if (CARRY || !works) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p.dz[(row0 + c * kChunk + 16 * i + 4 * g + r) * width + col] = dz[i][r];
+    (m & 8 ? p.strength : p.along)[part0 * kChunk + c * kChunk + 4 * (m & 4) + 4 * g + (m & 3)] = sums;
+    if (lane == 0) p.border[part0 + c] = border;
+  };
+  for (uint32_t end = chunks; end > chunk0; --end) {
+    const uint32_t c = end - 1, first = c * kChunk;
+    bf16 *const buffer = lds + (c & 1) * Lds::SIZE, *const Q = buffer + Lds::Q, *const K = buffer + Lds::K;
+    if constexpr (DIRECT_ROWS) {
+      arrive<0>();
+      if (valid - first < kChunk) {
+        DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
+        DirectRows<DK>::clear(K, valid - first, threadIdx.x);
+        DirectRows<64>::clear(buffer + Lds::V, valid - first, threadIdx.x);
+        DirectRows<64>::clear(buffer + Lds::D, valid - first, threadIdx.x);
+        __syncthreads();
+      }
+    } else {
+      __syncthreads();
+    }
+    next_num.there();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (!CARRY) asm volatile("" : "+v"(next.y[i]));
+#pragma unroll
+      for (int t = 0; t < 3; ++t) asm volatile("" : "+v"(next.pairs[t][i]));
+    }
+    num = next_num;
+    now = next;
+    if (end < chunks) flush(c + 1);
+    bf16x8 before[KX][kStateParts<T>];
+    if (!CARRY && works) {
 #pragma unroll
       for (int k = 0; k < KX; ++k) {
-        const Parts<3> sp = Parts<3>::of(s[2 * k], s[2 * k + 1]);
-        bf16* to = p.dstates + state_at<DK>(bh, p.chunks, c, dv, kGradParts<T>) + (size_t)(col0 / 32) * Tile<DK>::SIZE + Tile<DK>::at(col0 % 32 + m, 4 * k + g);
+        const size_t at = (size_t)(col0 / 32) * Tile<DK>::SIZE + Tile<DK>::at(col0 % 32 + m, 4 * k + g);
+        bf16* to = p.dstates + state_at<DK>(bh, p.chunks, c, dv, kGradParts<T>) + at;
+        const Parts<kGradParts<T>> parts = Parts<kGradParts<T>>::of(s[2 * k], s[2 * k + 1]);
 #pragma unroll
-        for (int t = 0; t < kGradParts<T>; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * blocks * Tile<DK>::SIZE) = sp.v[t];
+        for (int t = 0; t < kGradParts<T>; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * blocks * Tile<DK>::SIZE) = parts.v[t];
+        const bf16* from = p.states + state_at<DK>(bh, p.chunks, c, dv, kStateParts<T>) + at;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) w[i] = mma(Operand<T>::template along<DK>(K, 16 * i + m, k, g).v, sp.v, w[i]);
+        for (int t = 0; t < kStateParts<T>; ++t) before[k][t] = *reinterpret_cast<const bf16x8*>(from + (size_t)t * blocks * Tile<DK>::SIZE);
+      }
+    }
+    if (c > chunk0) fetch(c - 1);
+    if (works) {
+      f32x4 w4[4] = {};   // (of even and odd k)
+#pragma unroll
+      for (int k = 0; k < KX; k += 2) {
+        Operand<T> rows_k[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rows_k[j] = Operand<T>::template along<DK>(K, 16 * (j & 1) + m, k + j / 2, g);
+        const Parts<3> sp[2] = {Parts<3>::of(s[2 * k], s[2 * k + 1]), Parts<3>::of(s[2 * k + 2], s[2 * k + 3])};
+        mma_turns<4, 2, PT, 3>([&](int j) -> const bf16x8 (&)[PT] { return rows_k[j].v; }, [&](int j) -> const bf16x8 (&)[3] { return sp[j / 2].v; }, w4);
+      }
+      f32x4 v[2] = {now.v[0], now.v[1]}, d[2] = {now.d[0], now.d[1]};
+      bf16x8 solve[2][3], pairs[2][3];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+          solve[i][t] = DIRECT_ROWS ? reinterpret_cast<const bf16x8*>(buffer + Lds::SOLVE)[(2 * t + i) * 64 + lane] : now.solve[t][i];
+          pairs[i][t] = now.pairs[t][i];
+        }
+      if constexpr (DIRECT_ROWS) {
+        auto column = [&](uint32_t i) { return 16 * wave + i; };
+        Operand<bf16>::across<64>(buffer + Lds::D, column, m, g).widen(&d[0], &d[1]);
+        if (!CARRY) Operand<bf16>::across<64>(buffer + Lds::V, column, m, g).widen(&v[0], &v[1]);
       }
       const Operand<T> dp = operand_of<T>(d);
-      f32x4 du[2], dz[2];
+      f32x4 w[2], du[2] = {};
 #pragma unroll
-      for (int i = 0; i < 2; ++i) w[i] = mma(rec.pairs[i], dp.v, num.left[i] * w[i]);
+      for (int i = 0; i < 2; ++i) w[i] = num.left[i] * (w4[i] + w4[i + 2]);
+      mma_turns<2, 2, 3, PT>([&](int i) -> const bf16x8 (&)[3] { return pairs[i]; }, [&](int) -> const bf16x8 (&)[PT] { return dp.v; }, w);
       const Parts<3> wp = Parts<3>::of(w[0], w[1]);
+      mma_turns<2, 2, 3, 3>([&](int i) -> const bf16x8 (&)[3] { return solve[i]; }, [&](int) -> const bf16x8 (&)[3] { return wp.v; }, du);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        du[i] = mma(rec.solve[i], wp.v, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-        dz[i] = num.beta[i] * du[i];
+      for (int i = 0; i < 2; ++i) dz[i] = num.beta[i] * du[i];
+      const Parts<3> ip = Parts<3>::of(p.scale * num.gamma[0] * d[0], p.scale * num.gamma[1] * d[1]), op = Parts<3>::of(-num.gamma[0] * dz[0], -num.gamma[1] * dz[1]);
+#pragma unroll
+      for (int a0 = 0; a0 < TX; a0 += TURN) {
+        Operand<T> cols[TURN];
+        f32x4 part[TURN];
+#pragma unroll
+        for (int a = 0; a < TURN; ++a) {
+          cols[a] = Operand<T>::template across<DK>(Q, [&](uint32_t i) { return state_row(a0 + a, i); }, m, g);
+          part[a] = num.keep(s[a0 + a]);
+        }
+        mma_turns<TURN, 2, PT, 3>([&](int a) -> const bf16x8 (&)[PT] { return cols[a].v; }, [&](int) -> const bf16x8 (&)[3] { return ip.v; }, part);
+#pragma unroll
+        for (int a = 0; a < TURN; ++a) cols[a] = Operand<T>::template across<DK>(K, [&](uint32_t i) { return state_row(a0 + a, i); }, m, g);
+        mma_turns<TURN, 2, PT, 3>([&](int a) -> const bf16x8 (&)[PT] { return cols[a].v; }, [&](int) -> const bf16x8 (&)[3] { return op.v; }, part);
+#pragma unroll
+        for (int a = 0; a < TURN; ++a) s[a0 + a] = part[a];
       }
+      if constexpr (!CARRY) {
+        float products[16];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 8; ++i) {
+          products[i] = dz[i / 4][i % 4] * v[i / 4][i % 4];
+          products[i + 8] = now.y[i / 4][i % 4] * du[i / 4][i % 4];
+        }
+        sums = sums16(products, m);
+        border = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const uint32_t t = first + 16 * i + 4 * g + r;
-          p.dz[(row0 + t) * width + col] = dz[i][r];
-          if (p.direct && on && t < L) row_to<T>(p.dv, b, t, h)[col] = (T)(t < valid ? dz[i][r] : 0.0f);
-          const float along = sum16(dz[i][r] * v[i][r]), strength = sum16(y[i][r] * du[i][r]);
-          if (m == 0) {
-            p.along[part0 * kChunk + t] -= along;
-            p.strength[part0 * kChunk + t] = strength;
+        for (int k = 0; k < KX; ++k) {
+          f32x4 x[2] = {};
+          if constexpr (sizeof(T) == 2) {
+            of_halves(before[k], &x[0], &x[1]);
+          } else {
+#pragma unroll
+            for (int t = 2; t >= 0; --t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                x[0][e] += (float)before[k][t][e];
+                x[1][e] += (float)before[k][t][e + 4];
+              }
           }
-        }
-      f32x4 into[2], outof[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        into[i] = p.scale * num.gamma[i] * d[i];
-        outof[i] = -num.gamma[i] * dz[i];
+          for (int e = 0; e < 4; ++e) border = fmaf(x[0][e], s[2 * k][e], fmaf(x[1][e], s[2 * k + 1][e], border));
+        }
+        border = sum16(border);
+        border += __shfl_xor(border, 16);
+        border += __shfl_xor(border, 32);
       }
-      const Parts<3> ip = Parts<3>::of(into[0], into[1]), op = Parts<3>::of(outof[0], outof[1]);
-      float border = 0.0f;
-#pragma unroll
-      for (int k = 0; k < KX; ++k) {
-#pragma unroll
-        for (int a = 2 * k; a < 2 * k + 2; ++a) {
-          s[a] = num.keep(s[a]);
-          auto column = [&](uint32_t i) { return state_row(a, i); };
-          s[a] = mma(Operand<T>::template across<DK>(Q, column, m, g).v, ip.v, s[a]);
-          s[a] = mma(Operand<T>::template across<DK>(K, column, m, g).v, op.v, s[a]);
-        }
-        const bf16* from = p.states + state_at<DK>(bh, p.chunks, c, dv, kStateParts<T>) + (size_t)(col0 / 32) * Tile<DK>::SIZE + Tile<DK>::at(col0 % 32 + m, 4 * k + g);
-        f32x4 before[2] = {};
-        bf16x8 x[kStateParts<T>];
-#pragma unroll
-        for (int t = 0; t < kStateParts<T>; ++t) x[t] = *reinterpret_cast<const bf16x8*>(from + (size_t)t * blocks * Tile<DK>::SIZE);
-        if constexpr (sizeof(T) == 2) {
-          of_halves(x, &before[0], &before[1]);
-        } else {
-#pragma unroll
-          for (int t = 2; t >= 0; --t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              before[0][e] += (float)x[t][e];
-              before[1][e] += (float)x[t][e + 4];
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) border = fmaf(before[0][e], s[2 * k][e], fmaf(before[1][e], s[2 * k + 1][e], border));
-      }
-      border = sum16(border);
-      border += __shfl_xor(border, 16);
-      border += __shfl_xor(border, 32);
-      if (lane == 0) p.border[part0 + c] = border;
     }
-    __syncthreads();
   }
-  if (p.direct && works)
-    for (uint32_t t = chunks * kChunk + m; t < L; t += 16) store_four<T>(row_to<T>(p.dv, b, t, h), p.dv.wide, col0 + 4 * g, dv, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-  if (p.to && on)
+  if (chunk0 < chunks) flush(chunk0);
+  float* to = seg == 0 && p.to ? p.to + (int64_t)b * p.to_batch + (int64_t)h * p.to_head : nullptr;
+  if (CARRY) to = p.carried + ((size_t)bh * p.segments + seg) * dk * dv;
+  if (to && on)
 #pragma unroll
     for (int a = 0; a < TX; ++a)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const uint32_t row = state_row(a, 4 * g + r);
-        if (row < dk) p.to[(int64_t)b * p.to_batch + (int64_t)h * p.to_head + (size_t)row * dv + col] = s[a][r];
+        if (row < dk) to[(size_t)row * dv + col] = s[a][r];
       }
 }
 
 struct DeltaGrads {
-  SeqRows q, k, dout, dq, dk;
+  SeqRows q, k, dout, dq, dk, dvr;
   Gates log_decay, beta, dlog_decay, dbeta;
   const int32_t* lengths;
   uint32_t L, H, dkw, dv, chunks;
   float scale;
-  uint32_t direct_q, direct_k;   // to their rows; else to fold_q, fold_k, [sequence and head][token][dk] in fp32
+  uint32_t direct_q, direct_k, direct_v;   // to their rows; else to fold_q, fold_k, [sequence and head][token][dk] in fp32, and left in dz
   float *fold_q, *fold_k;
   const bf16 *states, *dstates;
-  const float *y, *dz, *along, *strength, *border;
+  const float *y, *dz, *read, *along, *strength, *border;   // read, along: rows of out . dout, of dZ . V
 };
 
 template <typename T, int DK>
@@ -217,6 +318,8 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
       if (p.direct_q) store_four<T>(row_to<T>(p.dq, b, t, h), p.dq.wide, col, dk, zero);
       if (p.direct_k) store_four<T>(row_to<T>(p.dk, b, t, h), p.dk.wide, col, dk, zero);
     }
+    for (uint32_t i = threadIdx.x; p.direct_v && i < end * ((dv + 3) / 4); i += 256)
+      store_four<T>(row_to<T>(p.dvr, b, first + i / ((dv + 3) / 4), h), p.dvr.wide, i % ((dv + 3) / 4) * 4, dv, zero);
     if (threadIdx.x < end) {
       *to_gate(p.dlog_decay, first + threadIdx.x) = 0.0f;
       *to_gate(p.dbeta, first + threadIdx.x) = 0.0f;
@@ -247,7 +350,7 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
     for (uint32_t i = 0; i < parts; ++i) {
       const size_t at = (size_t)bh * parts + i;
       strength += p.strength[at * p.chunks * kChunk + first + column];
-      along += p.along[at * p.chunks * kChunk + first + column];
+      along += p.read[at * p.chunks * kChunk + first + column] - p.along[at * p.chunks * kChunk + first + column];
       border += p.border[at * p.chunks + chunk];
     }
     float before = along;
@@ -284,6 +387,11 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
       const f32x4 z0 = *reinterpret_cast<const f32x4*>(zr), z1 = *reinterpret_cast<const f32x4*>(zr + 16);
       const f32x4 u0 = beta[t] * *reinterpret_cast<const f32x4*>(yr), u1 = beta[t] * *reinterpret_cast<const f32x4*>(yr + 16);
       z[i] = Parts<PU>::of(z0, z1);
+      if (p.direct_v && wave == (block & 3) && t < end) {
+        T* const to = row_to<T>(p.dvr, b, first + t, h);
+        store_four<T>(to, p.dvr.wide, 32 * block + 4 * g, dv, t < n ? z0 : zero);
+        store_four<T>(to, p.dvr.wide, 32 * block + 16 + 4 * g, dv, t < n ? z1 : zero);
+      }
       u[i] = Parts<PU>::of(u0, u1);
       zs[i] = Parts<PU>::of(-gamma[t] * z0, -gamma[t] * z1);
       ul[i] = Parts<PU>::of(left[t] * u0, left[t] * u1);

@@ -12,6 +12,7 @@
 struct DeltaRun {
   SeqRows q, k, v, out, dout;
   const void* records;
+  uint32_t record_bytes;
   const int32_t* lengths;
   const float* in;
   float* to;
@@ -271,12 +272,11 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const uint32_t L = p.L, dv = product ? dk : p.dv, blocks = (dv + 31) / 32, col0 = 64 * slice + 16 * wave, col = col0 + m;
   const bool on = col < dv, works = col0 < blocks * 32, takes = on && !product;   // takes: values
-  const uint32_t valid = valid_tokens(p.lengths, b, L), all_chunks = (valid + kChunk - 1) / kChunk;
+  const uint32_t valid = __builtin_amdgcn_readfirstlane(valid_tokens(p.lengths, b, L)), all_chunks = (valid + kChunk - 1) / kChunk;
   const uint32_t chunk0 = seg * p.segment, chunks = all_chunks < chunk0 ? chunk0 : all_chunks - chunk0 < p.segment ? all_chunks : chunk0 + p.segment;   // its end
-  typedef typename RecordOf<MODE == KEEPING>::type Record;
-  const Record* const records = static_cast<const Record*>(p.records) + (size_t)bh * p.chunks;
+  const uint8_t* const records = static_cast<const uint8_t*>(p.records) + (size_t)bh * p.chunks * p.record_bytes;
   const bool pieces = p.q.near && p.k.near && dk >= 16 / sizeof(T);
-  auto record = [&](uint32_t c) { return reinterpret_cast<const DeltaRecord*>(records + c); };
+  auto record = [&](uint32_t c) { return reinterpret_cast<const DeltaRecord*>(records + (size_t)c * p.record_bytes); };
 
   f32x4 s[TX];
 #pragma unroll

@@ -41,7 +41,7 @@ size_t record_bytes(const DeltaSizes& a) { return (size_t)a.B * a.H * chunks_of(
 
 // Where a gradient's intermediate results lie in the workspace.
 struct BackWork {
-  size_t records, states, dstates, y, dz, along, strength, border, fold_q, fold_k, bytes;
+  size_t records, states, dstates, y, dz, read, along, strength, border, fold_q, fold_k, carried, carried_back, bytes;
 };
 BackWork back_work(const DeltaSizes& a) {
   const uint64_t bh = (uint64_t)a.B * a.H, chunks = bh * chunks_of(a.L), tokens = chunks * kChunk;
@@ -59,11 +59,15 @@ BackWork back_work(const DeltaSizes& a) {
   w.dstates = take(chunks * state * (e ? 1 : 3));
   w.y = take(tokens * blocks * 32 * sizeof(float));
   w.dz = take(tokens * blocks * 32 * sizeof(float));
+  w.read = take(tokens * parts * sizeof(float));
   w.along = take(tokens * parts * sizeof(float));
   w.strength = take(tokens * parts * sizeof(float));
   w.border = take(chunks * parts * sizeof(float));
   w.fold_q = take(a.Q == a.H ? 0 : tokens * a.dk * sizeof(float));
   w.fold_k = take(a.K == a.H ? 0 : tokens * a.dk * sizeof(float));
+  const Cut c = cut(a, true);
+  w.carried = take(carried_bytes(a, c));
+  w.carried_back = take(c.segments < 2 ? 0 : bh * c.segments * a.dk * a.dv * sizeof(float));
   w.bytes = at;
   return w;
 }
@@ -97,10 +101,15 @@ hipError_t launch_run(const DeltaRun& p, uint32_t bh, hipStream_t s) {
   }
   return launch(k_delta_run<T, DK, MODE, false>, &granted[0], grid, RunLds<T, DK, NP, false>::BYTES, p, s);
 }
-template <typename T, int DK>
+template <typename T, int DK, bool CARRY>
 hipError_t launch_back(const DeltaBack& p, uint32_t bh, hipStream_t s) {
-  static std::atomic<uint64_t> granted{0};
-  return launch(k_delta_back<T, DK>, &granted, bh * p.slices, RunLds<T, DK, 3, false>::BYTES, p, s);
+  static std::atomic<uint64_t> granted[2] = {};
+  const uint32_t grid = bh * p.run * p.slices;
+  if constexpr (sizeof(T) == 2) {
+    if (p.q.wide && p.k.wide && p.v.wide && p.dout.wide && p.dk % 8 == 0 && p.dv % 8 == 0)
+      return launch(k_delta_back<T, DK, CARRY, true>, &granted[1], grid, BackLds<T, DK, true>::BYTES, p, s);
+  }
+  return launch(k_delta_back<T, DK, CARRY, false>, &granted[0], grid, BackLds<T, DK, false>::BYTES, p, s);
 }
 template <typename T, int DK>
 hipError_t launch_grads(const DeltaGrads& p, uint32_t bh, hipStream_t s) {
@@ -117,12 +126,14 @@ hipError_t launch_pairs(const DeltaSizes& a, const per_seq_rows& q, const per_se
   return hipGetLastError();
 }
 
-DeltaRun make_run(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state, const void* records) {
+DeltaRun make_run(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state, const void* records,
+                  size_t record) {
   DeltaRun p{};
   p.q = rows(q, a.dtype, a.H / a.Q);
   p.k = rows(k, a.dtype, a.H / a.K);
   p.v = rows(v, a.dtype, a.H / a.V);
   p.records = records;
+  p.record_bytes = (uint32_t)record;
   p.lengths = a.lengths;
   if (state) { p.in = state->d; p.in_batch = state->batch; p.in_head = state->head; }
   p.L = a.L;
@@ -164,7 +175,7 @@ hipError_t forward(const DeltaSizes& a, const per_seq_rows& q, const per_seq_row
                    const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
   hipError_t e = launch_pairs<T, DK, false>(a, q, k, work, s);
   if (e != hipSuccess) return e;
-  DeltaRun p = make_run(a, q, k, v, state, work);
+  DeltaRun p = make_run(a, q, k, v, state, work, sizeof(DeltaRecord));
   e = launch_carry<T, DK>(&p, a, cut(a, false), state, reinterpret_cast<float*>(static_cast<uint8_t*>(work) + record_bytes(a)), false, s);
   if (e != hipSuccess) return e;
   p.out = rows(out, a.dtype, 1);
@@ -193,39 +204,59 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   const uint32_t bh = a.B * a.H;
   hipError_t e = launch_pairs<T, DK, true>(a, q, k, at + w.records, s);
   if (e != hipSuccess) return e;
-  DeltaRun run = make_run(a, q, k, v, state, at + w.records);
+  DeltaRun run = make_run(a, q, k, v, state, at + w.records, sizeof(DeltaRecordBack));
   run.dout = rows(dout, a.dtype, 1);
   run.states = reinterpret_cast<bf16*>(at + w.states);
   run.y = floats(w.y);
-  run.along = floats(w.along);
-  if (run.chunks) e = launch_run<T, DK, KEEPING>(run, bh, s);
+  run.along = floats(w.read);
+  const Cut c = cut(a, true);
+  e = launch_carry<T, DK>(&run, a, c, state, floats(w.carried), true, s);
+  if (e == hipSuccess && run.chunks) e = launch_run<T, DK, KEEPING>(run, bh, s);
   if (e != hipSuccess) return e;
   DeltaBack b{};
   b.q = run.q;
   b.k = run.k;
   b.v = run.v;
   b.dout = run.dout;
-  b.dv = rows(dv, a.dtype, 1);
   b.records = run.records;
   b.lengths = a.lengths;
   if (dstate) { b.in = dstate->d; b.in_batch = dstate->batch; b.in_head = dstate->head; }
-  if (dstate0) { b.to = dstate0->d; b.to_batch = dstate0->batch; b.to_head = dstate0->head; }
   b.L = a.L;
   b.H = a.H;
   b.dk = a.dk;
-  b.dvw = a.dv;
+  b.dv = a.dv;
   b.chunks = run.chunks;
   b.slices = run.slices;
+  b.segments = c.segments;
+  b.segment = c.segment;
   b.scale = a.scale;
-  b.direct = a.V == a.H;
   b.states = run.states;
   b.y = run.y;
   b.dstates = reinterpret_cast<bf16*>(at + w.dstates);
   b.dz = floats(w.dz);
-  b.along = run.along;
+  b.along = floats(w.along);
   b.strength = floats(w.strength);
   b.border = floats(w.border);
-  e = launch_back<T, DK>(b, bh, s);
+  if (c.segments > 1) {   // what each segment but the first adds, then the gradients behind the segments
+    b.carried = floats(w.carried_back);
+    b.first_segment = 1;
+    b.run = c.segments - 1;
+    e = launch_back<T, DK, true>(b, bh, s);
+    if (e != hipSuccess) return e;
+    const size_t each = (size_t)a.dk * a.dv;
+    const DeltaJoin j{b.carried, floats(w.carried) + each, b.in, b.in_batch, b.in_head, each, carried_floats(a), a.H, a.dk, a.dv, b.slices, c.segments};
+    k_delta_join<DK, true><<<bh * b.slices, 4 * DK, 0, s>>>(j);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    b.in = b.carried;
+    b.in_segment = (int64_t)each;
+    b.in_head = b.in_segment * c.segments;
+    b.in_batch = b.in_head * a.H;
+  }
+  b.first_segment = 0;
+  b.run = c.segments;
+  if (dstate0) { b.to = dstate0->d; b.to_batch = dstate0->batch; b.to_head = dstate0->head; }
+  e = launch_back<T, DK, false>(b, bh, s);
   if (e != hipSuccess || !run.chunks) return e;
   DeltaGrads g{};
   g.q = run.q;
@@ -233,6 +264,7 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   g.dout = run.dout;
   g.dq = rows(dq, a.dtype, 1);
   g.dk = rows(dk, a.dtype, 1);
+  g.dvr = rows(dv, a.dtype, 1);
   g.log_decay = gates(a.log_decay);
   g.beta = gates(a.beta);
   g.dlog_decay = gates(dlog_decay);
@@ -246,19 +278,21 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   g.scale = a.scale;
   g.direct_q = a.Q == a.H;
   g.direct_k = a.K == a.H;
+  g.direct_v = a.V == a.H;
   g.fold_q = floats(w.fold_q);
   g.fold_k = floats(w.fold_k);
   g.states = run.states;
   g.dstates = b.dstates;
   g.y = run.y;
   g.dz = b.dz;
-  g.along = run.along;
+  g.read = run.along;
+  g.along = b.along;
   g.strength = b.strength;
   g.border = b.border;
   e = launch_grads<T, DK>(g, bh, s);
   if (e == hipSuccess && !g.direct_q) e = fold<T>(a, g.fold_q, dq, a.Q, a.dk, a.dk, s);
   if (e == hipSuccess && !g.direct_k) e = fold<T>(a, g.fold_k, dk, a.K, a.dk, a.dk, s);
-  if (e == hipSuccess && !b.direct) e = fold<T>(a, b.dz, dv, a.V, a.dv, (a.dv + 31) / 32 * 32, s);
+  if (e == hipSuccess && !g.direct_v) e = fold<T>(a, b.dz, dv, a.V, a.dv, (a.dv + 31) / 32 * 32, s);
   return e;
 }
 
