@@ -20,9 +20,9 @@ struct DeltaBack {
   uint32_t first_segment, run;   // the segments that are taken
   float scale;
   float* carried;                // [sequence, head][segment][dk][dv]: what a segment adds to the gradient of the state before it
-  const bf16* states;
+  const bf16x8 *states, *lower;
   const float* y;
-  bf16* dstates;                 // the gradients of the states behind the chunks
+  bf16x8* dstates;                 // the gradients of the states behind the chunks
   float *dz, *along, *strength, *border;
 };
 
@@ -135,7 +135,9 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
     const uint32_t c = end - 1, first = c * kChunk;
     bf16 *const buffer = lds + (c & 1) * Lds::SIZE, *const Q = buffer + Lds::Q, *const K = buffer + Lds::K;
     if constexpr (DIRECT_ROWS) {
-      arrive<0>();
+      // (what is stored behind the loads: the gradient's plane, and from the second chunk dZ)
+      if (!CARRY && works && end + 1 < chunks) arrive<KX + 8>();
+      else arrive<0>();
       if (valid - first < kChunk) {
         DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
         DirectRows<DK>::clear(K, valid - first, threadIdx.x);
@@ -155,22 +157,28 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
     }
     num = next_num;
     now = next;
+    // (before a chunk at a border: the state's two halves, or its parts)
+    constexpr int HALVES = sizeof(T) == 2 ? 2 : 3;
+    const bool bordered = !CARRY && c % kBorder == 0;
+    bf16x8 before[KX][HALVES];
+    if (bordered && works) {
+#pragma unroll
+      for (int k = 0; k < KX; ++k)
+#pragma unroll
+        for (int t = 0; t < HALVES; ++t)
+          before[k][t] = sizeof(T) == 2 && t == 1 ? p.lower[state_at<DK>(bh, (p.chunks + kBorder - 1) / kBorder, c / kBorder, blocks, 1, 0, col0 / 16) + k * 64 + lane]
+                                                  : p.states[state_at<DK>(bh, p.chunks, c, blocks, kStateParts<T>, t, col0 / 16) + k * 64 + lane];
+    }
+    if (c > chunk0) fetch(c - 1);
     if (end < chunks) flush(c + 1);
-    bf16x8 before[KX][kStateParts<T>];
     if (!CARRY && works) {
 #pragma unroll
       for (int k = 0; k < KX; ++k) {
-        const size_t at = (size_t)(col0 / 32) * Tile<DK>::SIZE + Tile<DK>::at(col0 % 32 + m, 4 * k + g);
-        bf16* to = p.dstates + state_at<DK>(bh, p.chunks, c, dv, kGradParts<T>) + at;
         const Parts<kGradParts<T>> parts = Parts<kGradParts<T>>::of(s[2 * k], s[2 * k + 1]);
 #pragma unroll
-        for (int t = 0; t < kGradParts<T>; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * blocks * Tile<DK>::SIZE) = parts.v[t];
-        const bf16* from = p.states + state_at<DK>(bh, p.chunks, c, dv, kStateParts<T>) + at;
-#pragma unroll
-        for (int t = 0; t < kStateParts<T>; ++t) before[k][t] = *reinterpret_cast<const bf16x8*>(from + (size_t)t * blocks * Tile<DK>::SIZE);
+        for (int t = 0; t < kGradParts<T>; ++t) p.dstates[state_at<DK>(bh, p.chunks, c, blocks, kGradParts<T>, t, col0 / 16) + k * 64 + lane] = parts.v[t];
       }
     }
-    if (c > chunk0) fetch(c - 1);
     if (works) {
       f32x4 w4[4] = {};   // (of even and odd k)
 #pragma unroll
@@ -230,26 +238,28 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
         }
         sums = sums16(products, m);
         border = 0.0f;
+        if (bordered) {
 #pragma unroll
-        for (int k = 0; k < KX; ++k) {
-          f32x4 x[2] = {};
-          if constexpr (sizeof(T) == 2) {
-            of_halves(before[k], &x[0], &x[1]);
-          } else {
+          for (int k = 0; k < KX; ++k) {
+            f32x4 x[2] = {};
+            if constexpr (sizeof(T) == 2) {
+              of_halves(before[k], &x[0], &x[1]);
+            } else {
 #pragma unroll
-            for (int t = 2; t >= 0; --t)
+              for (int t = 2; t >= 0; --t)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                x[0][e] += (float)before[k][t][e];
-                x[1][e] += (float)before[k][t][e + 4];
-              }
+                for (int e = 0; e < 4; ++e) {
+                  x[0][e] += (float)before[k][t][e];
+                  x[1][e] += (float)before[k][t][e + 4];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) border = fmaf(x[0][e], s[2 * k][e], fmaf(x[1][e], s[2 * k + 1][e], border));
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) border = fmaf(x[0][e], s[2 * k][e], fmaf(x[1][e], s[2 * k + 1][e], border));
+          border = sum16(border);
+          border += __shfl_xor(border, 16);
+          border += __shfl_xor(border, 32);
         }
-        border = sum16(border);
-        border += __shfl_xor(border, 16);
-        border += __shfl_xor(border, 32);
       }
     }
   }
@@ -274,23 +284,12 @@ struct DeltaGrads {
   float scale;
   uint32_t direct_q, direct_k, direct_v;   // to their rows; else to fold_q, fold_k, [sequence and head][token][dk] in fp32, and left in dz
   float *fold_q, *fold_k;
-  const bf16 *states, *dstates;
+  const bf16x8 *states, *dstates;
   const float *y, *dz, *read, *along, *strength, *border;   // read, along: rows of out . dout, of dZ . V
 };
 
 template <typename T, int DK>
 constexpr uint32_t grads_lds() { return (2 * kParts<T> + 2 * kGradParts<T>) * Tile<DK>::SIZE * sizeof(bf16) + 2 * 32 * kPairRow * sizeof(float); }
-
-// Places {4 g .., 16 + 4 g ..} of a row's 32 from column `col`.
-template <typename T>
-__device__ __forceinline__ Operand<T> row_places(const T* row, bool on, bool wide, uint32_t col, uint32_t g, uint32_t width) {
-  f32x4 a = {}, c = {};
-  if (on) {
-    a = load_four<T>(row, wide, col + 4 * g, width);
-    c = load_four<T>(row, wide, col + 16 + 4 * g, width);
-  }
-  return Operand<T>::of(a, c);
-}
 
 // A workgroup takes a chunk; its waves share the chunk's columns of dk, and the four 16 x 16 tiles of its pairs.
 template <typename T, int DK>
@@ -346,13 +345,33 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
     }
   } else if (wave == 1) {
     const uint32_t column = lane & 31;
-    float strength = 0.0f, along = 0.0f, border = 0.0f;
-    for (uint32_t i = 0; i < parts; ++i) {
-      const size_t at = (size_t)bh * parts + i;
-      strength += p.strength[at * p.chunks * kChunk + first + column];
-      along += p.read[at * p.chunks * kChunk + first + column] - p.along[at * p.chunks * kChunk + first + column];
-      border += p.border[at * p.chunks + chunk];
+    // The decays' gradient falls from token to token by what is read along dout less what is written along V, from the last border on.
+    // (All of it is loaded at once: a loop that adds as it loads takes a memory's latency for each of up to eight slices.)
+    const uint32_t since = chunk % kBorder;
+    float strengths[8], borders[8], falls[kBorder][8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const size_t at = (size_t)bh * parts + (i < parts ? i : parts - 1);
+      strengths[i] = p.strength[at * p.chunks * kChunk + first + column];
+      borders[i] = p.border[at * p.chunks + chunk - since];
+#pragma unroll
+      for (uint32_t j = 0; j < kBorder; ++j) {
+        const size_t row = at * p.chunks * kChunk + first + column - (j <= since ? j : 0) * kChunk;
+        falls[j][i] = p.read[row] - p.along[row];
+      }
     }
+    float strength = 0.0f, along = 0.0f, border = 0.0f, earlier = 0.0f;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      if (i >= parts) break;
+      strength += strengths[i];
+      border += borders[i];
+      along += falls[0][i];
+#pragma unroll
+      for (uint32_t j = 1; j < kBorder; ++j) earlier += j <= since ? falls[j][i] : 0.0f;
+    }
+    earlier = sum16(earlier);
+    border -= earlier + __shfl_xor(earlier, 16);   // (both halves of the wave have the 32 tokens)
     float before = along;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -366,35 +385,62 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
     }
   }
   __syncthreads();
-  f32x4 aq[2][NC] = {}, ak[2][NC] = {}, dm = zero, dn = zero;
+  // of queries; of keys by the state, and by its gradient, whose rows are scaled at the end
+  f32x4 aq[2][NC] = {}, as[2][NC] = {}, ar[2][NC] = {}, dm = zero, dn = zero;
   const uint32_t ti = wave >> 1, tj = wave & 1;
-  const size_t from_s = state_at<DK>(bh, p.chunks, chunk, dv, kStateParts<T>), from_r = state_at<DK>(bh, p.chunks, chunk, dv, PS);
+  constexpr uint32_t HELD = 2 * (DK / 32) * 64 / 256;   // pieces of a thread in 32 columns of a plane
+  struct Next {
+    bf16x8 s[PS][HELD], r[PS][HELD];
+    Four<T> d[2][2];
+    f32x4 z[2][2], y[2][2];
+  } next, now;
+  auto ask = [&](uint32_t block) {
+#pragma unroll
+    for (int t = 0; t < PS; ++t)
+#pragma unroll
+      for (uint32_t i = 0; i < HELD; ++i) {
+        next.s[t][i] = p.states[state_at<DK>(bh, p.chunks, chunk, blocks, kStateParts<T>, t, 2 * block) + threadIdx.x + 256 * i];
+        next.r[t][i] = p.dstates[state_at<DK>(bh, p.chunks, chunk, blocks, PS, t, 2 * block) + threadIdx.x + 256 * i];
+      }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t t = 16 * i + m;
+      const T* row = row_of<T>(p.dout, b, t < n ? first + t : first, h);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t col = 32 * block + 16 * e + 4 * g;
+        ask_four<T>(row, p.dout.wide, col, dv, &next.d[i][e]);
+        next.z[i][e] = *reinterpret_cast<const f32x4*>(p.dz + (row0 + t) * width + col);
+        next.y[i][e] = *reinterpret_cast<const f32x4*>(p.y + (row0 + t) * width + col);
+      }
+    }
+  };
+  ask(0);
   for (uint32_t block = 0; block < blocks; ++block) {
     if (block) __syncthreads();
 #pragma unroll
     for (int t = 0; t < PS; ++t)
-      for (uint32_t i = threadIdx.x; i < Tile<DK>::SIZE / 8; i += 256) {
-        *reinterpret_cast<bf16x8*>(S + t * Tile<DK>::SIZE + 8 * i) = *reinterpret_cast<const bf16x8*>(p.states + from_s + ((size_t)t * blocks + block) * Tile<DK>::SIZE + 8 * i);
-        *reinterpret_cast<bf16x8*>(R + t * Tile<DK>::SIZE + 8 * i) = *reinterpret_cast<const bf16x8*>(p.dstates + from_r + ((size_t)t * blocks + block) * Tile<DK>::SIZE + 8 * i);
+#pragma unroll
+      for (uint32_t i = 0; i < HELD; ++i) {   // lane 16 g + m of tile and k: column 16 tile + m, places 32 k + 8 g ..
+        const uint32_t at = threadIdx.x + 256 * i, place = Tile<DK>::at(16 * (at / (64 * (DK / 32))) + (at & 15), 4 * (at / 64 % (DK / 32)) + (at >> 4 & 3));
+        *reinterpret_cast<bf16x8*>(S + t * Tile<DK>::SIZE + place) = next.s[t][i];
+        *reinterpret_cast<bf16x8*>(R + t * Tile<DK>::SIZE + place) = next.r[t][i];
       }
+    now = next;
+    if (block + 1 < blocks) ask(block + 1);
     Operand<T> d[2];
-    Parts<PU> z[2], zs[2], u[2], ul[2];
+    Parts<PU> z[2], u[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t t = 16 * i + m;
-      d[i] = row_places<T>(row_of<T>(p.dout, b, t < n ? first + t : first, h), t < n, p.dout.wide, 32 * block, g, dv);
-      const float *zr = p.dz + (row0 + t) * width + 32 * block + 4 * g, *yr = p.y + (row0 + t) * width + 32 * block + 4 * g;
-      const f32x4 z0 = *reinterpret_cast<const f32x4*>(zr), z1 = *reinterpret_cast<const f32x4*>(zr + 16);
-      const f32x4 u0 = beta[t] * *reinterpret_cast<const f32x4*>(yr), u1 = beta[t] * *reinterpret_cast<const f32x4*>(yr + 16);
-      z[i] = Parts<PU>::of(z0, z1);
+      d[i] = Operand<T>::of(four_of<T>(now.d[i][0], t < n, 32 * block + 4 * g, dv), four_of<T>(now.d[i][1], t < n, 32 * block + 16 + 4 * g, dv));
+      z[i] = Parts<PU>::of(now.z[i][0], now.z[i][1]);
+      u[i] = Parts<PU>::of(beta[t] * now.y[i][0], beta[t] * now.y[i][1]);
       if (p.direct_v && wave == (block & 3) && t < end) {
         T* const to = row_to<T>(p.dvr, b, first + t, h);
-        store_four<T>(to, p.dvr.wide, 32 * block + 4 * g, dv, t < n ? z0 : zero);
-        store_four<T>(to, p.dvr.wide, 32 * block + 16 + 4 * g, dv, t < n ? z1 : zero);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) store_four<T>(to, p.dvr.wide, 32 * block + 16 * e + 4 * g, dv, t < n ? now.z[i][e] : zero);
       }
-      u[i] = Parts<PU>::of(u0, u1);
-      zs[i] = Parts<PU>::of(-gamma[t] * z0, -gamma[t] * z1);
-      ul[i] = Parts<PU>::of(left[t] * u0, left[t] * u1);
     }
     if (tj <= ti) {
       dm = mma<LESS>(ti ? d[1].v : d[0].v, tj ? u[1].v : u[0].v, dm);
@@ -413,8 +459,8 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         aq[i][a] = mma<LESS>(s, d[i].v, aq[i][a]);
-        ak[i][a] = mma<LESS>(s, zs[i].v, ak[i][a]);
-        ak[i][a] = mma<LESS>(r, ul[i].v, ak[i][a]);
+        as[i][a] = mma<LESS>(s, z[i].v, as[i][a]);
+        ar[i][a] = mma<LESS>(r, u[i].v, ar[i][a]);
       }
     }
   }
@@ -451,16 +497,16 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t t = 16 * i + m, col = 16 * tile + 4 * g;
-      aq[i][a] *= p.scale * gamma[t];
-      aq[i][a] = mma<LESS>(k.v, rows_m[i].v, aq[i][a]);
-      ak[i][a] = mma<LESS>(q.v, cols_m[i].v, ak[i][a]);
-      ak[i][a] = mma<LESS>(k.v, both_n[i].v, ak[i][a]);
+      f32x4 oq = p.scale * gamma[t] * aq[i][a], ok = left[t] * ar[i][a] - gamma[t] * as[i][a];
+      oq = mma<LESS>(k.v, rows_m[i].v, oq);
+      ok = mma<LESS>(q.v, cols_m[i].v, ok);
+      ok = mma<LESS>(k.v, both_n[i].v, ok);
       if (t >= end) continue;
-      if (t >= n) aq[i][a] = ak[i][a] = zero;
-      if (p.direct_q) store_four<T>(row_to<T>(p.dq, b, first + t, h), p.dq.wide, col, dk, aq[i][a]);
-      else store_four<float>(p.fold_q + (row0 + t) * dk, dk % 4 == 0, col, dk, aq[i][a]);
-      if (p.direct_k) store_four<T>(row_to<T>(p.dk, b, first + t, h), p.dk.wide, col, dk, ak[i][a]);
-      else store_four<float>(p.fold_k + (row0 + t) * dk, dk % 4 == 0, col, dk, ak[i][a]);
+      if (t >= n) oq = ok = zero;
+      if (p.direct_q) store_four<T>(row_to<T>(p.dq, b, first + t, h), p.dq.wide, col, dk, oq);
+      else store_four<float>(p.fold_q + (row0 + t) * dk, dk % 4 == 0, col, dk, oq);
+      if (p.direct_k) store_four<T>(row_to<T>(p.dk, b, first + t, h), p.dk.wide, col, dk, ok);
+      else store_four<float>(p.fold_k + (row0 + t) * dk, dk % 4 == 0, col, dk, ok);
     }
   }
 }

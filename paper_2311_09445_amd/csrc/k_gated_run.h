@@ -21,23 +21,27 @@ struct DeltaRun {
   float scale;
   float* carried;                // [sequence, head][segment]: what a segment adds [dk][dv], what it makes of a state [dk][dk]
   // kept for a gradient: the states before the chunks, Y, rows of out . dout
-  bf16* states;
+  bf16x8 *states, *lower;
   float *y, *along;
 };
 
 // CARRYING: no outputs; what a segment adds to a state, and (in slices of their own) what it makes of one: its product with the state before it.
 enum DeltaMode { FORWARD, KEEPING, CARRYING };
 
-// Planes of 16 bits that states are kept in for a gradient: where rows are bfloat16 the rounded state, which the products for bfloat16 gradients
-// take, and the lower half of the sum that rounded it, so that both together are the 32 bits (two rounded parts held 17, and the decays'
-// gradient was off by 2e-6 of itself); else the three parts that an operand takes.
+// Planes of 16 bits that the states before the chunks are kept in for a gradient: where rows are bfloat16 the rounded state, which the products for
+// bfloat16 gradients take, else the three parts that an operand takes.  Before every kBorder-th chunk the gradient of a decay is the whole
+// state's product with its gradient; there the lower half of the sum that rounded it is kept too, so that both together are the 32 bits.
+// (From state to state the gradient is carried on by rows' products, which are off by 2^-24 of themselves; over four chunks that stays below 1e-6.)
 template <typename T>
-constexpr int kStateParts = sizeof(T) == 2 ? 2 : 3;
+constexpr int kStateParts = sizeof(T) == 2 ? 1 : 3;
+constexpr uint32_t kBorder = 4;
 
-// Where the states kept for chunk c of a sequence and head start: [part][32 columns of dv][Tile of dk], columns as rows.
+// Where plane `part` of the states kept for chunk c of a sequence and head lies: [part][16 columns of dv][32 places of dk][lane], eight places a lane
+// as registers hold them, so that a wave's instruction writes and reads 1 KiB in a row.  (As tiles of columns, pieces of 16 bytes in lines of
+// their own, the pass that keeps them took 6.5 us for a chunk of 128 x 128, and the one that reads them 6.)
 template <int DK>
-__device__ __forceinline__ size_t state_at(uint32_t bh, uint32_t chunks, uint32_t c, uint32_t dv, uint32_t parts) {
-  return ((size_t)bh * chunks + c) * parts * ((dv + 31) / 32) * Tile<DK>::SIZE;
+__device__ __forceinline__ size_t state_at(uint32_t bh, uint32_t chunks, uint32_t c, uint32_t blocks, uint32_t parts, uint32_t part, uint32_t tile) {
+  return ((((size_t)bh * chunks + c) * parts + part) * blocks * 2 + tile) * (DK / 32) * 64;
 }
 
 // What a pass takes of a record: rows of products, and numbers for the tokens 16 i + 4 g + r (and 16 i + m).
@@ -367,7 +371,9 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
     const uint32_t first = c * kChunk;
     bf16 *const buffer = lds + (c & 1) * Lds::SIZE, *const Q = buffer + Lds::Q, *const K = buffer + Lds::K;
     if constexpr (DIRECT_ROWS) {
-      arrive<0>();
+      // (what a pass that keeps states stores behind the loads: the state's plane, and from the second chunk Y)
+      if (MODE == KEEPING && works && c > chunk0 + 1) arrive<KX + 8>();
+      else arrive<0>();
       if (valid - first < kChunk) {
         DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
         DirectRows<DK>::clear(K, valid - first, threadIdx.x);
@@ -381,27 +387,30 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
     num = next_num;
     RecordRows<NP> rec = next;
     f32x4 v[2] = {next_v[0], next_v[1]};
-    if (c > chunk0) flush(c - 1);
     if constexpr (MODE == KEEPING) {
       now_d[0] = next_d[0];
       now_d[1] = next_d[1];
+    }
+    if (MODE != KEEPING && c > chunk0) flush(c - 1);
+    if (c + 1 < chunks) fetch(c + 1);
+    if constexpr (MODE == KEEPING) {   // (behind the loads: the next barrier does not wait for these)
+      if (c > chunk0) flush(c - 1);
       if (works) {
 #pragma unroll
         for (int k = 0; k < KX; ++k) {
-          bf16* to = p.states + state_at<DK>(bh, p.chunks, c, dv, kStateParts<T>) + (size_t)(col0 / 32) * Tile<DK>::SIZE + Tile<DK>::at(col0 % 32 + m, 4 * k + g);
-          if constexpr (sizeof(T) == 2) {
+          auto to = [&](int t) { return p.states + state_at<DK>(bh, p.chunks, c, blocks, kStateParts<T>, t, col0 / 16) + k * 64 + lane; };
+          if (sizeof(T) == 2 && c % kBorder == 0) {
             const Halves both = halves_of(s[2 * k], s[2 * k + 1]);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * blocks * Tile<DK>::SIZE) = both.v[t];
+            *to(0) = both.v[0];
+            p.lower[state_at<DK>(bh, (p.chunks + kBorder - 1) / kBorder, c / kBorder, blocks, 1, 0, col0 / 16) + k * 64 + lane] = both.v[1];
           } else {
-            const Parts<3> sp = Parts<3>::of(s[2 * k], s[2 * k + 1]);
+            const Parts<kStateParts<T>> parts = Parts<kStateParts<T>>::of(s[2 * k], s[2 * k + 1]);
 #pragma unroll
-            for (int t = 0; t < 3; ++t) *reinterpret_cast<bf16x8*>(to + (size_t)t * blocks * Tile<DK>::SIZE) = sp.v[t];
+            for (int t = 0; t < kStateParts<T>; ++t) *to(t) = parts.v[t];
           }
         }
       }
     }
-    if (c + 1 < chunks) fetch(c + 1);
     if (works) {
       f32x4 x4[4] = {}, o4[4] = {};   // (of even and odd k)
       Parts<3> sp[KX];

@@ -41,7 +41,7 @@ size_t record_bytes(const DeltaSizes& a) { return (size_t)a.B * a.H * chunks_of(
 
 // Where a gradient's intermediate results lie in the workspace.
 struct BackWork {
-  size_t records, states, dstates, y, dz, read, along, strength, border, fold_q, fold_k, carried, carried_back, bytes;
+  size_t records, states, lower, dstates, y, dz, read, along, strength, border, fold_q, fold_k, carried, carried_back, bytes;
 };
 BackWork back_work(const DeltaSizes& a) {
   const uint64_t bh = (uint64_t)a.B * a.H, chunks = bh * chunks_of(a.L), tokens = chunks * kChunk;
@@ -55,7 +55,8 @@ BackWork back_work(const DeltaSizes& a) {
   };
   const uint64_t state = blocks * 32 * padded(a.dk) * sizeof(bf16);
   w.records = take(chunks * sizeof(DeltaRecordBack));
-  w.states = take(chunks * state * (e ? 2 : 3));
+  w.states = take(chunks * state * (e ? 1 : 3));
+  w.lower = take(e ? bh * ((chunks_of(a.L) + kBorder - 1) / kBorder) * state : 0);
   w.dstates = take(chunks * state * (e ? 1 : 3));
   w.y = take(tokens * blocks * 32 * sizeof(float));
   w.dz = take(tokens * blocks * 32 * sizeof(float));
@@ -206,7 +207,8 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   if (e != hipSuccess) return e;
   DeltaRun run = make_run(a, q, k, v, state, at + w.records, sizeof(DeltaRecordBack));
   run.dout = rows(dout, a.dtype, 1);
-  run.states = reinterpret_cast<bf16*>(at + w.states);
+  run.states = reinterpret_cast<bf16x8*>(at + w.states);
+  run.lower = reinterpret_cast<bf16x8*>(at + w.lower);
   run.y = floats(w.y);
   run.along = floats(w.read);
   const Cut c = cut(a, true);
@@ -231,8 +233,9 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   b.segment = c.segment;
   b.scale = a.scale;
   b.states = run.states;
+  b.lower = run.lower;
   b.y = run.y;
-  b.dstates = reinterpret_cast<bf16*>(at + w.dstates);
+  b.dstates = reinterpret_cast<bf16x8*>(at + w.dstates);
   b.dz = floats(w.dz);
   b.along = floats(w.along);
   b.strength = floats(w.strength);
