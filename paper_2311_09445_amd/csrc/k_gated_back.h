@@ -67,7 +67,8 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
   DirectRows<64> direct_v, direct_d;
   struct Next {
     bf16x8 pairs[3][2], solve[3][2];
-    f32x4 y[2], v[2], d[2];
+    f32x4 y[2];
+    Column<T> v, d;
   } next, now;
   RecordNumbers num, next_num;
   const uint32_t lds0 = lds_address(lds);
@@ -84,8 +85,8 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
     } else {
       rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
       if (c > chunk0) rows.load(p.q, p.k, q0, k0, (c - 1) * kChunk, valid, dk, pieces);
-      if (!CARRY) load_column<T>(p.v, v0, c * kChunk, valid, on, col, g, next.v);
-      load_column<T>(p.dout, d0, c * kChunk, valid, on, col, g, next.d);
+      if (!CARRY) next.v.ask(p.v, v0, c * kChunk, valid, on, col, g);
+      next.d.ask(p.dout, d0, c * kChunk, valid, on, col, g);
 #pragma unroll
       for (int t = 0; t < 3; ++t)
 #pragma unroll
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
         const Parts<3> sp[2] = {Parts<3>::of(s[2 * k], s[2 * k + 1]), Parts<3>::of(s[2 * k + 2], s[2 * k + 3])};
         mma_turns<4, 2, PT, 3>([&](int j) -> const bf16x8 (&)[PT] { return rows_k[j].v; }, [&](int j) -> const bf16x8 (&)[3] { return sp[j / 2].v; }, w4);
       }
-      f32x4 v[2] = {now.v[0], now.v[1]}, d[2] = {now.d[0], now.d[1]};
+      f32x4 v[2], d[2];
       bf16x8 solve[2][3], pairs[2][3];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -202,6 +203,9 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
         auto column = [&](uint32_t i) { return 16 * wave + i; };
         Operand<bf16>::across<64>(buffer + Lds::D, column, m, g).widen(&d[0], &d[1]);
         if (!CARRY) Operand<bf16>::across<64>(buffer + Lds::V, column, m, g).widen(&v[0], &v[1]);
+      } else {
+        now.d.widen(first, valid, on, g, d);
+        if (!CARRY) now.v.widen(first, valid, on, g, v);
       }
       const Operand<T> dp = operand_of<T>(d);
       f32x4 w[2], du[2] = {};

@@ -154,18 +154,27 @@ __device__ __forceinline__ void of_halves(const bf16x8 (&h)[2], f32x4* a, f32x4*
     }
 }
 
-// Rows 16 i + 4 g + r of a chunk, column col, as fp32.
+// Rows 16 i + 4 g + r of a chunk, column col, as the rows have them (a conversion, or clearing one, would be waited for where it is asked for),
+// and as fp32.
 template <typename T>
-__device__ __forceinline__ void load_column(const SeqRows& rows, const T* head, uint32_t first, uint32_t valid, bool on, uint32_t col, uint32_t g, f32x4 (&v)[2]) {
+struct Column {
+  T v[2][4];
+  __device__ __forceinline__ void ask(const SeqRows& rows, const T* head, uint32_t first, uint32_t valid, bool on, uint32_t col, uint32_t g) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const uint32_t t = first + 16 * i + 4 * g + r;
-      const T x = head[(int64_t)(t < valid ? t : valid - 1) * rows.token + (on ? col : 0)];
-      v[i][r] = on && t < valid ? as_float(x) : 0.0f;
-    }
-}
+      for (int r = 0; r < 4; ++r) {
+        const uint32_t t = first + 16 * i + 4 * g + r;
+        v[i][r] = head[(int64_t)(t < valid ? t : valid - 1) * rows.token + (on ? col : 0)];
+      }
+  }
+  __device__ __forceinline__ void widen(uint32_t first, uint32_t valid, bool on, uint32_t g, f32x4 (&x)[2]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[i][r] = on && first + 16 * i + 4 * g + r < valid ? as_float(v[i][r]) : 0.0f;
+  }
+};
 template <typename T>
 __device__ __forceinline__ Operand<T> operand_of(const f32x4 (&v)[2]) { return Operand<T>::of(v[0], v[1]); }
 
@@ -200,16 +209,16 @@ __device__ __forceinline__ void store_four(T* row, bool wide, uint32_t col, uint
   }
 }
 
-// The same as the row has them (a conversion would be waited for).
+// The same as the row has them.
 template <typename T>
-struct Four { T v[4]; };
+struct Four {
+  typedef T Vec __attribute__((ext_vector_type(4)));
+  Vec v;
+};
 template <typename T>
 __device__ __forceinline__ void ask_four(const T* row, bool wide, uint32_t col, uint32_t width, Four<T>* o) {
-  typedef T Vec __attribute__((ext_vector_type(4)));
   if (wide && width % 4 == 0) {
-    const Vec v = *reinterpret_cast<const Vec*>(row + (col < width ? col : 0));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o->v[i] = v[i];
+    o->v = *reinterpret_cast<const typename Four<T>::Vec*>(row + (col < width ? col : 0));
   } else {
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) o->v[i] = row[col + i < width ? col + i : 0];
@@ -297,7 +306,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
   DirectRows<64> direct_v;
   RecordRows<NP> next;
   RecordNumbers num, next_num;
-  f32x4 next_v[2];
+  Column<T> next_v, now_v;
   Four<T> next_d[2], now_d[2];
   const uint32_t lds0 = lds_address(lds);
   auto fetch = [&](uint32_t c) {   // chunk c, to LDS or (rows by way of registers: the one behind it) to registers
@@ -313,7 +322,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
       rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
       if (c + 1 < chunks) rows.load(p.q, p.k, q0, k0, (c + 1) * kChunk, valid, dk, pieces);
       next.load(&record(c)->solve[0][0][0], &record(c)->pairs[0][0][0], lane);
-      load_column<T>(p.v, v0, c * kChunk, valid, takes, col, g, next_v);
+      next_v.ask(p.v, v0, c * kChunk, valid, takes, col, g);
     }
     if constexpr (MODE == KEEPING) {
 #pragma unroll
@@ -386,7 +395,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
     next_num.there();
     num = next_num;
     RecordRows<NP> rec = next;
-    f32x4 v[2] = {next_v[0], next_v[1]};
+    now_v = next_v;
     if constexpr (MODE == KEEPING) {
       now_d[0] = next_d[0];
       now_d[1] = next_d[1];
@@ -423,10 +432,12 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
         sp[k + 1] = Parts<3>::of(s[2 * k + 2], s[2 * k + 3]);
         mma_turns<4, 2, PT, 3>([&](int j) -> const bf16x8 (&)[PT] { return rows_k[j].v; }, [&](int j) -> const bf16x8 (&)[3] { return sp[k + j / 2].v; }, x4);
       }
+      f32x4 v[2];
       if constexpr (DIRECT_ROWS) {
         rec.load(reinterpret_cast<const bf16x8*>(buffer + Lds::SOLVE), reinterpret_cast<const bf16x8*>(buffer + Lds::PAIRS), lane);
         Operand<bf16>::across<64>(buffer + Lds::V, [&](uint32_t i) { return 16 * wave + i; }, m, g).widen(&v[0], &v[1]);
       }
+      else now_v.widen(first, valid, takes, g, v);
       const Parts<3> z = Parts<3>::of(v[0] - num.gamma[0] * (x4[0] + x4[2]), v[1] - num.gamma[1] * (x4[1] + x4[3]));
       f32x4 u[2];
       y[0] = y[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
