@@ -37,7 +37,7 @@ struct BackLds {
 
 // CARRY: only what a segment adds.
 template <typename T, int DK, bool CARRY, bool DIRECT_ROWS>
-__global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
+__global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) void k_delta_back(DeltaBack p) {
   constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, TURN = PT == 1 ? TX : 4;
   typedef BackLds<T, DK, DIRECT_ROWS> Lds;
   static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
@@ -65,6 +65,7 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
   TwoRows<T, DK> rows;
   DirectRows<DK> direct_q, direct_k;
   DirectRows<64> direct_v, direct_d;
+  Walk walk_q, walk_k, walk_v, walk_d;
   struct Next {
     bf16x8 pairs[3][2], solve[3][2];
     f32x4 y[2];
@@ -76,12 +77,11 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
     const DeltaRecordBack* const record = records + c;
     if constexpr (DIRECT_ROWS) {
       const uint32_t n = valid - c * kChunk, to = lds0 + (c & 1) * Lds::SIZE * 2;
-      auto rows_at = [&](const T* head, const SeqRows& r) { return reinterpret_cast<const uint8_t*>(head) + (int64_t)c * kChunk * r.token * 2; };
-      direct_q.ask(to + Lds::Q * 2, rows_at(q0, p.q), wave, n);
-      direct_k.ask(to + Lds::K * 2, rows_at(k0, p.k), wave, n);
-      if (!CARRY) direct_v.ask(to + Lds::V * 2, rows_at(v0 + 64 * slice, p.v), wave, n);
-      direct_d.ask(to + Lds::D * 2, rows_at(d0 + 64 * slice, p.dout), wave, n);
-      ask_rows(to + Lds::SOLVE * 2, record->solve_t, 6, wave, lane);
+      direct_q.ask(to + Lds::Q * 2, walk_q.next(), wave, n);
+      direct_k.ask(to + Lds::K * 2, walk_k.next(), wave, n);
+      if (!CARRY) direct_v.ask(to + Lds::V * 2, walk_v.next(), wave, n);
+      direct_d.ask(to + Lds::D * 2, walk_d.next(), wave, n);
+      ask_rows<6>(to + Lds::SOLVE * 2, record->solve_t, wave, lane);
     } else {
       rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
       if (c > chunk0) rows.load(p.q, p.k, q0, k0, (c - 1) * kChunk, valid, dk, pieces);
@@ -104,6 +104,11 @@ __global__ __launch_bounds__(256, 1) void k_delta_back(DeltaBack p) {
     next_num.load(&record->of, m, g);
   };
   if constexpr (DIRECT_ROWS) {
+    const uint32_t last = chunks > chunk0 ? chunks - 1 : chunk0;
+    walk_q.set(p.q, q0, last, true);
+    walk_k.set(p.k, k0, last, true);
+    walk_v.set(p.v, v0 + 64 * slice, last, true);
+    walk_d.set(p.dout, d0 + 64 * slice, last, true);
     direct_q.set(p.q, dk, wave, lane);
     direct_k.set(p.k, dk, wave, lane);
     direct_v.set(p.v, dv - 64 * slice, wave, lane);

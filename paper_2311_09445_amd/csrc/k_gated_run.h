@@ -107,6 +107,12 @@ struct DirectRows {
   }
   // n: rows that there are, of 32
   __device__ __forceinline__ void ask(uint32_t to, const uint8_t* base, uint32_t wave, uint32_t n) const {
+    if (n >= kChunk) {
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i)
+        if (on[i]) load_to_lds(to + (wave + 4 * i) * 1024, base, offset[i]);
+      return;
+    }
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i) {
       const uint32_t back = row[i] < n ? 0 : row[i] - (n - 1);
@@ -119,9 +125,27 @@ struct DirectRows {
   }
 };
 // The first n KiB of a record's rows of products.
-__device__ __forceinline__ void ask_rows(uint32_t to, const void* from, uint32_t n, uint32_t wave, uint32_t lane) {
-  for (uint32_t i = wave; i < n; i += 4) load_to_lds(to + i * 1024, static_cast<const uint8_t*>(from) + i * 1024, lane * 16);
+template <uint32_t N>
+__device__ __forceinline__ void ask_rows(uint32_t to, const void* from, uint32_t wave, uint32_t lane) {
+#pragma unroll
+  for (uint32_t i = 0; i < N; i += 4)   // (the last wave's twice where four waves do not share N)
+    load_to_lds(to + (i + wave < N ? i + wave : N - 1) * 1024, static_cast<const uint8_t*>(from), (i + wave < N ? i + wave : N - 1) * 1024 + lane * 16);
 }
+// Rows of a head from chunk to chunk.
+struct Walk {
+  const uint8_t* at;
+  int64_t step;
+  __device__ __forceinline__ void set(const SeqRows& r, const void* head, uint32_t chunk, bool back) {
+    const int64_t bytes = (int64_t)kChunk * r.token * 2;
+    at = static_cast<const uint8_t*>(head) + chunk * bytes;
+    step = back ? -bytes : bytes;
+  }
+  __device__ __forceinline__ const uint8_t* next() {
+    const uint8_t* here = at;
+    at += step;
+    return here;
+  }
+};
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
 }
@@ -272,7 +296,7 @@ template <typename T, DeltaMode MODE>
 constexpr int kPairParts = MODE == CARRYING ? 1 : sizeof(T) == 2 && MODE == FORWARD ? 2 : 3;
 
 template <typename T, int DK, DeltaMode MODE, bool DIRECT_ROWS>
-__global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ? 2 : 1) void k_delta_run(DeltaRun p) {
+__global__ __launch_bounds__(256, DIRECT_ROWS ? 2 : 1) void k_delta_run(DeltaRun p) {
   constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = NP - 1;
   typedef RunLds<T, DK, NP, DIRECT_ROWS> Lds;
   static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
@@ -304,6 +328,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
   TwoRows<T, DK> rows;
   DirectRows<DK> direct_q, direct_k;
   DirectRows<64> direct_v;
+  Walk walk_q, walk_k, walk_v, walk_out;
   RecordRows<NP> next;
   RecordNumbers num, next_num;
   Column<T> next_v, now_v;
@@ -312,12 +337,11 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
   auto fetch = [&](uint32_t c) {   // chunk c, to LDS or (rows by way of registers: the one behind it) to registers
     if constexpr (DIRECT_ROWS) {
       const uint32_t n = valid - c * kChunk, to = lds0 + (c & 1) * Lds::SIZE * 2;
-      auto rows_at = [&](const T* head, const SeqRows& r) { return reinterpret_cast<const uint8_t*>(head) + (int64_t)c * kChunk * r.token * 2; };
-      if (MODE != CARRYING) direct_q.ask(to + Lds::Q * 2, rows_at(q0, p.q), wave, n);
-      direct_k.ask(to + Lds::K * 2, rows_at(k0, p.k), wave, n);
-      if (!product) direct_v.ask(to + Lds::V * 2, rows_at(v0 + 64 * slice, p.v), wave, n);
-      ask_rows(to + Lds::SOLVE * 2, record(c)->solve, 6, wave, lane);
-      if (MODE != CARRYING) ask_rows(to + Lds::PAIRS * 2, record(c)->pairs, 2 * NP, wave, lane);
+      if (MODE != CARRYING) direct_q.ask(to + Lds::Q * 2, walk_q.next(), wave, n);
+      direct_k.ask(to + Lds::K * 2, walk_k.next(), wave, n);
+      if (!product) direct_v.ask(to + Lds::V * 2, walk_v.next(), wave, n);
+      ask_rows<6>(to + Lds::SOLVE * 2, record(c)->solve, wave, lane);
+      if (MODE != CARRYING) ask_rows<2 * NP>(to + Lds::PAIRS * 2, record(c)->pairs, wave, lane);
     } else {
       rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
       if (c + 1 < chunks) rows.load(p.q, p.k, q0, k0, (c + 1) * kChunk, valid, dk, pieces);
@@ -334,6 +358,10 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
     next_num.load(record(c), m, g);
   };
   if constexpr (DIRECT_ROWS) {
+    walk_q.set(p.q, q0, chunk0, false);
+    walk_k.set(p.k, k0, chunk0, false);
+    walk_v.set(p.v, v0 + 64 * slice, chunk0, false);
+    if (MODE == FORWARD) walk_out.set(p.out, row_to<T>(p.out, b, 0, h) + 64 * slice, chunk0, false);
     direct_q.set(p.q, dk, wave, lane);
     direct_k.set(p.k, dk, wave, lane);
     direct_v.set(p.v, product ? 0 : dv - 64 * slice, wave, lane);
@@ -350,6 +378,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
   }
   if (chunk0 < chunks) fetch(chunk0);
   f32x4 o[2] = {}, y[2] = {};
+  const uint32_t out_at[2] = {m * (uint32_t)p.out.token * 2 + (16 * wave + 4 * g) * 2, (16 + m) * (uint32_t)p.out.token * 2 + (16 * wave + 4 * g) * 2};
   // What chunk c leaves in memory is stored behind the next barrier: stores are older then than the loads that are waited for.
   auto flush = [&](uint32_t c) {
     if (!works || MODE == CARRYING) return;
@@ -364,9 +393,10 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (MODE != KEEPING || DK == 64) ?
         if (g == 0) p.along[((size_t)bh * (blocks * 2) + col0 / 16) * p.chunks * kChunk + t] = o[i][0];
       }
     } else if (DIRECT_ROWS && p.out.wide && valid - first >= kChunk) {
+      uint8_t* const to = const_cast<uint8_t*>(walk_out.next());
       if (col0 + 4 * g < dv) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) store_four<T>(row_to<T>(p.out, b, first, h) + (int64_t)(16 * i + m) * p.out.token, true, col0 + 4 * g, ~0u, o[i]);
+        for (int i = 0; i < 2; ++i) store_four<T>(reinterpret_cast<T*>(to + out_at[i]), true, 0, ~0u, o[i]);
       }
     } else {
 #pragma unroll
