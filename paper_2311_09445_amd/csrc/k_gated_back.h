@@ -287,22 +287,47 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
 
 struct DeltaGrads {
   SeqRows q, k, dout, dq, dk, dvr;
-  Gates log_decay, beta, dlog_decay, dbeta;
+  Gates log_decay, beta;
   const int32_t* lengths;
   uint32_t L, H, dkw, dv, chunks;
   float scale;
   uint32_t direct_q, direct_k, direct_v;   // to their rows; else to fold_q, fold_k, [sequence and head][token][dk] in fp32, and left in dz
   float *fold_q, *fold_k;
   const bf16x8 *states, *dstates;
-  const float *y, *dz, *read, *along, *strength, *border;   // read, along: rows of out . dout, of dZ . V
+  const float *y, *dz;
 };
+struct DeltaGates {
+  Gates dlog_decay, dbeta;
+  const int32_t* lengths;
+  uint32_t L, H, chunks, parts;   // parts: slices of 16 columns, which sums come in
+  const float *read, *along, *strength, *border;   // read, along: rows of out . dout, of dZ . V
+};
+// Eight neighbours of a row.
+template <typename T>
+__device__ __forceinline__ void store_eight(T* row, bool wide, uint32_t col, uint32_t width, f32x4 a, f32x4 c) {
+  typedef T Vec __attribute__((ext_vector_type(8)));
+  if (sizeof(T) == 2 && wide && col + 8 <= width) {
+    Vec o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[i] = (T)a[i];
+      o[i + 4] = (T)c[i];
+    }
+    *reinterpret_cast<Vec*>(row + col) = o;
+  } else {
+    store_four<T>(row, wide, col, width, a);
+    store_four<T>(row, wide, col + 4, width, c);
+  }
+}
 
 template <typename T, int DK>
 constexpr uint32_t grads_lds() { return (2 * kParts<T> + 2 * kGradParts<T>) * Tile<DK>::SIZE * sizeof(bf16) + 2 * 32 * kPairRow * sizeof(float); }
 
-// A workgroup takes a chunk; its waves share the chunk's columns of dk, and the four 16 x 16 tiles of its pairs.
+// A workgroup takes a chunk; its waves share the chunk's columns of dk, and the four 16 x 16 tiles of its pairs.  Everything that comes from memory is
+// asked for before anything is waited for.  Columns of dv go to LDS mixed, column 8 g + 4 s + e of a block to row 16 s + 4 g + e, and so are rows of
+// results, so that what a lane reads and writes of a token are eight elements in a row.
 template <typename T, int DK>
-__global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_delta_grads(DeltaGrads p) {
   constexpr int NC = DK / 64, PT = kParts<T>, PS = kGradParts<T>, PU = sizeof(T) == 2 ? 2 : 3, LESS = PU - 1;
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   bf16* const Q = reinterpret_cast<bf16*>(lds_raw);
@@ -315,10 +340,9 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
   __shared__ __attribute__((aligned(16))) float gamma[32], left[32], beta[32];
   const uint32_t chunk = blockIdx.x % p.chunks, bh = blockIdx.x / p.chunks, h = bh % p.H, b = bh / p.H;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  const uint32_t L = p.L, dk = p.dkw, dv = p.dv, blocks = (dv + 31) / 32, width = blocks * 32, parts = blocks * 2;
-  const uint32_t valid = valid_tokens(p.lengths, b, L), first = chunk * kChunk, end = L - first < kChunk ? L - first : kChunk;
+  const uint32_t L = p.L, dk = p.dkw, dv = p.dv, blocks = (dv + 31) / 32, width = blocks * 32;
+  const uint32_t valid = __builtin_amdgcn_readfirstlane(valid_tokens(p.lengths, b, L)), first = chunk * kChunk, end = L - first < kChunk ? L - first : kChunk;
   const size_t row0 = (size_t)bh * p.chunks * kChunk + first;
-  auto to_gate = [&](const Gates& x, uint32_t t) { return const_cast<float*>(x.d) + (int64_t)b * x.batch + (int64_t)t * x.token + (int64_t)h * x.head; };
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   if (first >= valid) {
     for (uint32_t i = threadIdx.x; i < end * ((dk + 3) / 4); i += 256) {
@@ -328,88 +352,20 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
     }
     for (uint32_t i = threadIdx.x; p.direct_v && i < end * ((dv + 3) / 4); i += 256)
       store_four<T>(row_to<T>(p.dvr, b, first + i / ((dv + 3) / 4), h), p.dvr.wide, i % ((dv + 3) / 4) * 4, dv, zero);
-    if (threadIdx.x < end) {
-      *to_gate(p.dlog_decay, first + threadIdx.x) = 0.0f;
-      *to_gate(p.dbeta, first + threadIdx.x) = 0.0f;
-    }
     return;
   }
   const uint32_t n = valid - first;   // (and more)
-  {
-    TwoRows<T, DK> rows;
-    const bool pieces = p.q.near && p.k.near && dk >= 16 / sizeof(T);
-    rows.load(p.q, p.k, row_of<T>(p.q, b, 0, h), row_of<T>(p.k, b, 0, h), first, valid, dk, pieces);
-    rows.store(Q, n, dk, pieces);
-  }
-  if (wave == 0) {
-    const uint32_t column = lane & 31;
-    const bool here = column < n;
-    const double sum = decay_sums(p.log_decay, b, h, here ? first + column : first, here, lane);
-    const double total = __shfl(sum, 31);
-    if (lane < 32) {
-      G[lane] = sum;
-      gamma[lane] = expf((float)sum);
-      left[lane] = expf((float)(total - sum));
-      beta[lane] = here ? p.beta.at(b, first + lane, h) : 0.0f;
-    }
-  } else if (wave == 1) {
-    const uint32_t column = lane & 31;
-    // The decays' gradient falls from token to token by what is read along dout less what is written along V, from the last border on.
-    // (All of it is loaded at once: a loop that adds as it loads takes a memory's latency for each of up to eight slices.)
-    const uint32_t since = chunk % kBorder;
-    float strengths[8], borders[8], falls[kBorder][8];
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      const size_t at = (size_t)bh * parts + (i < parts ? i : parts - 1);
-      strengths[i] = p.strength[at * p.chunks * kChunk + first + column];
-      borders[i] = p.border[at * p.chunks + chunk - since];
-#pragma unroll
-      for (uint32_t j = 0; j < kBorder; ++j) {
-        const size_t row = at * p.chunks * kChunk + first + column - (j <= since ? j : 0) * kChunk;
-        falls[j][i] = p.read[row] - p.along[row];
-      }
-    }
-    float strength = 0.0f, along = 0.0f, border = 0.0f, earlier = 0.0f;
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      if (i >= parts) break;
-      strength += strengths[i];
-      border += borders[i];
-      along += falls[0][i];
-#pragma unroll
-      for (uint32_t j = 1; j < kBorder; ++j) earlier += j <= since ? falls[j][i] : 0.0f;
-    }
-    earlier = sum16(earlier);
-    border -= earlier + __shfl_xor(earlier, 16);   // (both halves of the wave have the 32 tokens)
-    float before = along;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const float x = __shfl_up(before, d);
-      if (column >= (uint32_t)d) before += x;
-    }
-    before = __shfl_up(before, 1);
-    if (lane < end) {
-      *to_gate(p.dlog_decay, first + lane) = lane >= n ? 0.0f : lane ? border - before : border;
-      *to_gate(p.dbeta, first + lane) = lane < n ? strength : 0.0f;
-    }
-  }
-  __syncthreads();
-  // of queries; of keys by the state, and by its gradient, whose rows are scaled at the end
-  f32x4 aq[2][NC] = {}, as[2][NC] = {}, ar[2][NC] = {}, dm = zero, dn = zero;
-  const uint32_t ti = wave >> 1, tj = wave & 1;
   constexpr uint32_t HELD = 2 * (DK / 32) * 64 / 256;   // pieces of a thread in 32 columns of a plane
-  struct Next {
-    bf16x8 s[PS][HELD], r[PS][HELD];
-    Four<T> d[2][2];
-    f32x4 z[2][2], y[2][2];
-  } next, now;
+  bf16x8 next_s[PS][HELD], next_r[PS][HELD];
+  Four<T> next_d[2][2];
+  f32x4 next_z[2][2], next_y[2][2];
   auto ask = [&](uint32_t block) {
 #pragma unroll
     for (int t = 0; t < PS; ++t)
 #pragma unroll
       for (uint32_t i = 0; i < HELD; ++i) {
-        next.s[t][i] = p.states[state_at<DK>(bh, p.chunks, chunk, blocks, kStateParts<T>, t, 2 * block) + threadIdx.x + 256 * i];
-        next.r[t][i] = p.dstates[state_at<DK>(bh, p.chunks, chunk, blocks, PS, t, 2 * block) + threadIdx.x + 256 * i];
+        next_s[t][i] = p.states[state_at<DK>(bh, p.chunks, chunk, blocks, kStateParts<T>, t, 2 * block) + threadIdx.x + 256 * i];
+        next_r[t][i] = p.dstates[state_at<DK>(bh, p.chunks, chunk, blocks, PS, t, 2 * block) + threadIdx.x + 256 * i];
       }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -417,53 +373,72 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
       const T* row = row_of<T>(p.dout, b, t < n ? first + t : first, h);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t col = 32 * block + 16 * e + 4 * g;
-        ask_four<T>(row, p.dout.wide, col, dv, &next.d[i][e]);
-        next.z[i][e] = *reinterpret_cast<const f32x4*>(p.dz + (row0 + t) * width + col);
-        next.y[i][e] = *reinterpret_cast<const f32x4*>(p.y + (row0 + t) * width + col);
+        const uint32_t col = 32 * block + 8 * g + 4 * e;
+        ask_four<T>(row, p.dout.wide, col, dv, &next_d[i][e]);
+        next_z[i][e] = *reinterpret_cast<const f32x4*>(p.dz + (row0 + t) * width + col);
+        next_y[i][e] = *reinterpret_cast<const f32x4*>(p.y + (row0 + t) * width + col);
       }
     }
   };
+  TwoRows<T, DK> rows;
+  const bool pieces = p.q.near && p.k.near && dk >= 16 / sizeof(T);
+  rows.load(p.q, p.k, row_of<T>(p.q, b, 0, h), row_of<T>(p.k, b, 0, h), first, valid, dk, pieces);
   ask(0);
+  if (wave == 0) {
+    const uint32_t column = lane & 31;
+    const bool here = column < n;
+    const float strength = here ? p.beta.at(b, first + column, h) : 0.0f;
+    const double sum = decay_sums(p.log_decay, b, h, here ? first + column : first, here, lane);
+    const double total = __shfl(sum, 31);
+    if (lane < 32) {
+      G[lane] = sum;
+      gamma[lane] = expf((float)sum);
+      left[lane] = expf((float)(total - sum));
+      beta[lane] = strength;
+    }
+  }
+  rows.store(Q, n, dk, pieces);
+  // of queries; of keys by the state, and by its gradient, whose rows are scaled at the end
+  f32x4 aq[2][NC] = {}, as[2][NC] = {}, ar[2][NC] = {}, dm = zero, dn = zero;
+  const uint32_t ti = wave >> 1, tj = wave & 1;
+  auto column = [&](uint32_t a, uint32_t i) { return NC == 2 ? 32 * wave + 8 * (i >> 2) + 4 * a + (i & 3) : 16 * wave + i; };   // of the wave's
   for (uint32_t block = 0; block < blocks; ++block) {
     if (block) __syncthreads();
 #pragma unroll
     for (int t = 0; t < PS; ++t)
 #pragma unroll
       for (uint32_t i = 0; i < HELD; ++i) {   // lane 16 g + m of tile and k: column 16 tile + m, places 32 k + 8 g ..
-        const uint32_t at = threadIdx.x + 256 * i, place = Tile<DK>::at(16 * (at / (64 * (DK / 32))) + (at & 15), 4 * (at / 64 % (DK / 32)) + (at >> 4 & 3));
-        *reinterpret_cast<bf16x8*>(S + t * Tile<DK>::SIZE + place) = next.s[t][i];
-        *reinterpret_cast<bf16x8*>(R + t * Tile<DK>::SIZE + place) = next.r[t][i];
+        const uint32_t at = threadIdx.x + 256 * i, c = 16 * (at / (64 * (DK / 32))) + (at & 15);
+        const uint32_t place = Tile<DK>::at(16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3), 4 * (at / 64 % (DK / 32)) + (at >> 4 & 3));
+        *reinterpret_cast<bf16x8*>(S + t * Tile<DK>::SIZE + place) = next_s[t][i];
+        *reinterpret_cast<bf16x8*>(R + t * Tile<DK>::SIZE + place) = next_r[t][i];
       }
-    now = next;
-    if (block + 1 < blocks) ask(block + 1);
+    __syncthreads();
     Operand<T> d[2];
     Parts<PU> z[2], u[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t t = 16 * i + m;
-      d[i] = Operand<T>::of(four_of<T>(now.d[i][0], t < n, 32 * block + 4 * g, dv), four_of<T>(now.d[i][1], t < n, 32 * block + 16 + 4 * g, dv));
-      z[i] = Parts<PU>::of(now.z[i][0], now.z[i][1]);
-      u[i] = Parts<PU>::of(beta[t] * now.y[i][0], beta[t] * now.y[i][1]);
+      d[i] = Operand<T>::of(four_of<T>(next_d[i][0], t < n, 32 * block + 8 * g, dv), four_of<T>(next_d[i][1], t < n, 32 * block + 8 * g + 4, dv));
+      z[i] = Parts<PU>::of(next_z[i][0], next_z[i][1]);
+      u[i] = Parts<PU>::of(beta[t] * next_y[i][0], beta[t] * next_y[i][1]);
       if (p.direct_v && wave == (block & 3) && t < end) {
         T* const to = row_to<T>(p.dvr, b, first + t, h);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) store_four<T>(to, p.dvr.wide, 32 * block + 16 * e + 4 * g, dv, t < n ? now.z[i][e] : zero);
+        store_eight<T>(to, p.dvr.wide, 32 * block + 8 * g, dv, t < n ? next_z[i][0] : zero, t < n ? next_z[i][1] : zero);
       }
     }
+    if (block + 1 < blocks) ask(block + 1);
     if (tj <= ti) {
       dm = mma<LESS>(ti ? d[1].v : d[0].v, tj ? u[1].v : u[0].v, dm);
       dn = mma<LESS>(ti ? z[1].v : z[0].v, tj ? u[1].v : u[0].v, dn);
     }
-    __syncthreads();
 #pragma unroll
     for (int a = 0; a < NC; ++a) {
-      auto column = [&](uint32_t i) { return 16 * (wave * NC + a) + i; };
       bf16x8 s[PS], r[PS];
 #pragma unroll
       for (int t = 0; t < PS; ++t) {
-        s[t] = Operand<bf16>::template across<DK>(S + t * Tile<DK>::SIZE, column, m, g).v[0];
-        r[t] = Operand<bf16>::template across<DK>(R + t * Tile<DK>::SIZE, column, m, g).v[0];
+        s[t] = Operand<bf16>::template across<DK>(S + t * Tile<DK>::SIZE, [&](uint32_t i) { return column(a, i); }, m, g).v[0];
+        r[t] = Operand<bf16>::template across<DK>(R + t * Tile<DK>::SIZE, [&](uint32_t i) { return column(a, i); }, m, g).v[0];
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -481,43 +456,89 @@ __global__ __launch_bounds__(256) void k_delta_grads(DeltaGrads p) {
     dN[i * kPairRow + j] = i > j ? -x * dn[e] : 0.0f;
   }
   __syncthreads();
-  Parts<PU> rows_m[2], cols_m[2], both_n[2];
+  Operand<T> qs[NC], ks[NC];
+#pragma unroll
+  for (int a = 0; a < NC; ++a) {
+    qs[a] = Operand<T>::template across<DK>(Q, [&](uint32_t i) { return column(a, i); }, m, g);
+    ks[a] = Operand<T>::template across<DK>(K, [&](uint32_t i) { return column(a, i); }, m, g);
+  }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const uint32_t t = 16 * i + m;
-    f32x4 a, c, e, f;
-    const f32x4 na = *reinterpret_cast<const f32x4*>(dN + t * kPairRow + 4 * g), nc = *reinterpret_cast<const f32x4*>(dN + t * kPairRow + 16 + 4 * g);
+    f32x4 x, y, na, nc;
+    const float *rm = dM + t * kPairRow + 4 * g, *rn = dN + t * kPairRow + 4 * g, *cm = dM + 4 * g * kPairRow + t, *cn = dN + 4 * g * kPairRow + t;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      a[r] = dM[(4 * g + r) * kPairRow + t];
-      c[r] = dM[(16 + 4 * g + r) * kPairRow + t];
-      e[r] = dN[(4 * g + r) * kPairRow + t];
-      f[r] = dN[(16 + 4 * g + r) * kPairRow + t];
+      x[r] = cm[r * kPairRow];
+      y[r] = cm[(16 + r) * kPairRow];
+      na[r] = rn[r] + cn[r * kPairRow];
+      nc[r] = rn[16 + r] + cn[(16 + r) * kPairRow];
     }
-    rows_m[i] = Parts<PU>::of(*reinterpret_cast<const f32x4*>(dM + t * kPairRow + 4 * g), *reinterpret_cast<const f32x4*>(dM + t * kPairRow + 16 + 4 * g));
-    cols_m[i] = Parts<PU>::of(a, c);
-    both_n[i] = Parts<PU>::of(na + e, nc + f);
-  }
+    const Parts<PU> rows_m = Parts<PU>::of(*reinterpret_cast<const f32x4*>(rm), *reinterpret_cast<const f32x4*>(rm + 16));
+    const Parts<PU> cols_m = Parts<PU>::of(x, y), both_n = Parts<PU>::of(na, nc);
+    f32x4 oq[2], ok[2];
 #pragma unroll
-  for (int a = 0; a < NC; ++a) {
-    const uint32_t tile = wave * NC + a;
-    auto column = [&](uint32_t i) { return 16 * tile + i; };
-    const Operand<T> q = Operand<T>::template across<DK>(Q, column, m, g), k = Operand<T>::template across<DK>(K, column, m, g);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t t = 16 * i + m, col = 16 * tile + 4 * g;
-      f32x4 oq = p.scale * gamma[t] * aq[i][a], ok = left[t] * ar[i][a] - gamma[t] * as[i][a];
-      oq = mma<LESS>(k.v, rows_m[i].v, oq);
-      ok = mma<LESS>(q.v, cols_m[i].v, ok);
-      ok = mma<LESS>(k.v, both_n[i].v, ok);
-      if (t >= end) continue;
-      if (t >= n) oq = ok = zero;
-      if (p.direct_q) store_four<T>(row_to<T>(p.dq, b, first + t, h), p.dq.wide, col, dk, oq);
-      else store_four<float>(p.fold_q + (row0 + t) * dk, dk % 4 == 0, col, dk, oq);
-      if (p.direct_k) store_four<T>(row_to<T>(p.dk, b, first + t, h), p.dk.wide, col, dk, ok);
-      else store_four<float>(p.fold_k + (row0 + t) * dk, dk % 4 == 0, col, dk, ok);
+    for (int a = 0; a < NC; ++a) {
+      oq[a] = mma<LESS>(ks[a].v, rows_m.v, p.scale * gamma[t] * aq[i][a]);
+      ok[a] = mma<LESS>(qs[a].v, cols_m.v, left[t] * ar[i][a] - gamma[t] * as[i][a]);
+      ok[a] = mma<LESS>(ks[a].v, both_n.v, ok[a]);
+      if (t >= n) oq[a] = ok[a] = zero;
     }
+    if (t >= end) continue;
+    auto put = [&](const SeqRows& to, bool direct, float* fold, const f32x4 (&o)[2]) {
+      T* const row = direct ? row_to<T>(to, b, first + t, h) : nullptr;
+      float* const apart = fold + (row0 + t) * dk;
+      if constexpr (NC == 2) {
+        if (direct) store_eight<T>(row, to.wide, 32 * wave + 8 * g, dk, o[0], o[1]);
+        else store_eight<float>(apart, dk % 4 == 0, 32 * wave + 8 * g, dk, o[0], o[1]);
+      } else {
+        if (direct) store_four<T>(row, to.wide, 16 * wave + 4 * g, dk, o[0]);
+        else store_four<float>(apart, dk % 4 == 0, 16 * wave + 4 * g, dk, o[0]);
+      }
+    };
+    put(p.dq, p.direct_q, p.fold_q, oq);
+    put(p.dk, p.direct_k, p.fold_k, ok);
   }
+}
+
+// The gates' gradients: a thread takes a token, a workgroup the kBorder chunks behind a border.  The decays' falls from token to token by what is
+// read along dout less what is written along V.
+__global__ __launch_bounds__(kBorder * kChunk) void k_delta_gates(DeltaGates p) {
+  __shared__ float upto;
+  const uint32_t groups = (p.chunks + kBorder - 1) / kBorder, group = blockIdx.x % groups, bh = blockIdx.x / groups, h = bh % p.H, b = bh / p.H;
+  const uint32_t t = group * kBorder * kChunk + threadIdx.x, valid = valid_tokens(p.lengths, b, p.L), tokens = p.chunks * kChunk;
+  float strengths[8], falls[8], borders[8];
+  const uint32_t from = t < valid ? t : 0;
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i) {   // (all at once: a loop that adds as it loads takes a memory's latency for each)
+    const size_t at = (size_t)bh * p.parts + (i < p.parts ? i : p.parts - 1);
+    strengths[i] = p.strength[at * tokens + from];
+    falls[i] = p.read[at * tokens + from] - p.along[at * tokens + from];
+    borders[i] = p.border[at * p.chunks + group * kBorder];
+  }
+  float strength = 0.0f, fall = 0.0f, border = 0.0f;
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i) {
+    if (i >= p.parts) break;
+    strength += strengths[i];
+    fall += falls[i];
+    border += borders[i];
+  }
+  if (t >= valid) fall = 0.0f;
+  float sum = fall;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const float x = __shfl_up(sum, d);
+    if ((threadIdx.x & 63) >= (uint32_t)d) sum += x;
+  }
+  if (threadIdx.x == 63) upto = sum;
+  __syncthreads();
+  if (threadIdx.x >= 64) sum += upto;
+  if (t >= p.L) return;
+  float* const dg = const_cast<float*>(p.dlog_decay.d) + (int64_t)b * p.dlog_decay.batch + (int64_t)t * p.dlog_decay.token + (int64_t)h * p.dlog_decay.head;
+  float* const db = const_cast<float*>(p.dbeta.d) + (int64_t)b * p.dbeta.batch + (int64_t)t * p.dbeta.token + (int64_t)h * p.dbeta.head;
+  *dg = t < valid ? border - (sum - fall) : 0.0f;
+  *db = t < valid ? strength : 0.0f;
 }
 
 // Rows of heads that share one, added up in the heads' order: from [sequence and head][token][stride] in fp32.

@@ -270,8 +270,6 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   g.dvr = rows(dv, a.dtype, 1);
   g.log_decay = gates(a.log_decay);
   g.beta = gates(a.beta);
-  g.dlog_decay = gates(dlog_decay);
-  g.dbeta = gates(dbeta);
   g.lengths = a.lengths;
   g.L = a.L;
   g.H = a.H;
@@ -288,11 +286,11 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   g.dstates = b.dstates;
   g.y = run.y;
   g.dz = b.dz;
-  g.read = run.along;
-  g.along = b.along;
-  g.strength = b.strength;
-  g.border = b.border;
   e = launch_grads<T, DK>(g, bh, s);
+  if (e != hipSuccess) return e;
+  const DeltaGates sums{gates(dlog_decay), gates(dbeta), a.lengths, a.L, a.H, run.chunks, (a.dv + 31) / 32 * 2, run.along, b.along, b.strength, b.border};
+  k_delta_gates<<<bh * ((run.chunks + kBorder - 1) / kBorder), kBorder * kChunk, 0, s>>>(sums);
+  e = hipGetLastError();
   if (e == hipSuccess && !g.direct_q) e = fold<T>(a, g.fold_q, dq, a.Q, a.dk, a.dk, s);
   if (e == hipSuccess && !g.direct_k) e = fold<T>(a, g.fold_k, dk, a.K, a.dk, a.dk, s);
   if (e == hipSuccess && !g.direct_v) e = fold<T>(a, b.dz, dv, a.V, a.dv, (a.dv + 31) / 32 * 32, s);
