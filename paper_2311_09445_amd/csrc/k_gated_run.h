@@ -19,7 +19,8 @@ struct DeltaRun {
   int64_t in_batch, in_head, in_segment, to_batch, to_head;
   uint32_t L, H, dk, dv, chunks, slices, segments, segment, run;   // segment: chunks of one; run: segments that are taken
   float scale;
-  float* carried;                // [sequence, head][segment]: what a segment adds [dk][dv], what it makes of a state [dk][dk]
+  float* carried;                // [sequence, head][segment], `each` floats: what a segment adds [dk][dv], what it makes of a state [dk][dk], and
+  uint32_t each, turned;         // (turned) that transposed
   // kept for a gradient: the states before the chunks, Y, rows of out . dout
   bf16x8 *states, *lower;
   float *y, *along;
@@ -521,7 +522,10 @@ __global__ __launch_bounds__(256, DIRECT_ROWS ? 2 : 1) void k_delta_run(DeltaRun
     for (uint32_t t = chunks * kChunk + m; t < end; t += 16) store_four<T>(row_to<T>(p.out, b, t, h), p.out.wide, col0 + 4 * g, dv, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
   }
   float* to = seg + 1 == p.segments && p.to ? p.to + (int64_t)b * p.to_batch + (int64_t)h * p.to_head : nullptr;
-  if (MODE == CARRYING) to = p.carried + ((size_t)bh * p.segments + seg) * dk * (p.dv + dk) + (product ? dk * p.dv : 0);
+  if (MODE == CARRYING) to = p.carried + ((size_t)bh * p.segments + seg) * p.each + (product ? dk * p.dv : 0);
+  if (MODE == CARRYING && product && p.turned && on)
+#pragma unroll
+    for (int a = 0; a < TX; ++a) store_four<float>(to + dk * dk + col * dk, dk % 4 == 0, state_row(a, 4 * g), dk, s[a]);
   if (to && on)
 #pragma unroll
     for (int a = 0; a < TX; ++a)
@@ -538,7 +542,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS ? 2 : 1) void k_delta_run(DeltaRun
 // segment: it takes all of P apart by itself.)
 struct DeltaJoin {
   float* carried;            // [sequence, head][segment]: B or C, rows of dv
-  const float* products;     // P, rows of dk
+  const float* products;     // P (BACK: transposed), rows of dk
   const float* in;
   int64_t in_batch, in_head;
   size_t stride, product_stride;
@@ -564,6 +568,7 @@ __global__ __launch_bounds__(4 * DK) void k_delta_join(DeltaJoin p) {
       s[c][r] = p.in && on[c][r] ? p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + at[c][r]] : 0.0f;
     }
   f32x4 product[KX][2], add[4];
+  const bool fast = dk % 4 == 0;   // (rows of whole vectors: what a segment carries starts with dk dv or more floats before them)
   auto load = [&](uint32_t i) {
     const uint32_t seg = BACK ? p.segments - 1 - i : i;
     const float* const from = p.carried + ((size_t)bh * p.segments + seg) * p.stride;
@@ -573,12 +578,18 @@ __global__ __launch_bounds__(4 * DK) void k_delta_join(DeltaJoin p) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) add[c][r] = from[at[c][r]];
     if (i + 1 == p.segments) return;   // (the last one's product leads nowhere)
+    const float* const row_m = P + (of_m < dk ? of_m * dk : 0);
 #pragma unroll
     for (int k = 0; k < KX; ++k)
 #pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {
-        const uint32_t place = 32 * k + 8 * g + e, x = of_m < dk && place < dk ? (BACK ? place * dk + of_m : of_m * dk + place) : 0;
-        product[k][e / 4][e % 4] = P[x];
+      for (uint32_t e = 0; e < 8; e += 4) {
+        const uint32_t place = 32 * k + 8 * g + e;
+        if (fast) {
+          product[k][e / 4] = *reinterpret_cast<const f32x4*>(row_m + (place < dk ? place : 0));
+        } else {
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) product[k][e / 4][j] = row_m[place + j < dk ? place + j : 0];
+        }
       }
   };
   load(0);

@@ -5,7 +5,7 @@
 // Sequences are taken in chunks of 32 tokens (k_gated_pairs.h: what a chunk's tokens make of each other, all chunks at once; k_gated_run.h: the
 // states one chunk behind the other; k_gated_back.h: the gradient, against time and then all chunks at once), single tokens in k_gated_step.h.
 #include <atomic>
-#include <stdlib.h>
+#include <math.h>
 
 #include "dev_parts.h"
 
@@ -24,18 +24,51 @@ uint32_t chunks_of(uint32_t L) { return (L + kChunk - 1) / kChunk; }
 // (256 divides every chunk's part of a workspace, so that the parts stay aligned)
 uint32_t padded(uint32_t dk) { return dk <= 64 ? 64 : 128; }
 
-// How a sequence is cut: in segments of whole chunks, each from the state that those before it bring.
+// How a sequence is cut: in segments of whole chunks, each from the state that those before it bring.  A workgroup takes its chunks one behind
+// the other, so what cuts the time of few sequences is workgroups.  That costs another pass over all segments but the last, over dk
+// columns more (what a segment makes of a state is a product, k_delta_join), and two launches (a gradient: as much again but for the
+// product).  The fewest microseconds by these measured figures are taken, for widths up to 64 and above:
+//   a chunk's outputs 1.8, 2.45 (fp32 3.4, 5.5), what it carries 1.1, 1.65 (2.6, 4.0), its gradient's two passes 5.2, 7.2 (9, 15), what that carries 1.8,
+//   2.95 (4, 6); two workgroups on a compute unit take 1.75 times as long, more take turns; a gradient's, which move the states, take 1.4 times
+//   as long where every compute unit has one, 2.5 with two; to join 3.2, 4.5 a segment.
+// Measured, in 1, 4, 8, 16 segments, us: 65536 tokens of 16 heads of 128 x 128 5250, 2391, 1699, 1638; 2 x 8192 of them 666, 413, 407, 454, their gradient
+// 2356, 1447, 1403, 1501; 4 x 4096 of 8 of 64 x 64 245, 134, 106, 110 and 793, 453, 365, 374; 32 x 512 of them 60, 92 and 275, 350.
 struct Cut { uint32_t segments, segment; };
 Cut cut(const DeltaSizes& a, bool backward) {
-  const uint32_t chunks = chunks_of(a.L);
-  static const int force = getenv("PER_CUT") ? atoi(getenv("PER_CUT")) : 0;
-  uint32_t s = force ? force : 1;
-  if (s > chunks) s = chunks ? chunks : 1;
-  const uint32_t segment = chunks ? (chunks + s - 1) / s : 1;
-  return Cut{chunks ? (chunks + segment - 1) / segment : 1, segment};
+  const uint32_t chunks = chunks_of(a.L), wide = a.dk > 64, f32 = a.dtype == PER_SEQ_F32, slices = (a.dv + 63) / 64, more = slices + (a.dk + 63) / 64;
+  static const float forward_us[2][2] = {{1.8f, 2.45f}, {3.4f, 5.5f}}, carry_us[2][2] = {{1.1f, 1.65f}, {2.6f, 4.0f}};
+  static const float back_us[2][2] = {{5.2f, 7.2f}, {9.0f, 15.0f}}, carry_back_us[2][2] = {{1.8f, 2.95f}, {4.0f, 6.0f}};
+  const uint64_t rows = (uint64_t)a.B * a.H;
+  // (in fp32 above 64 the rows of one workgroup fill a compute unit's LDS)
+  auto crowd = [&](uint64_t workgroups) {
+    const float w = (float)workgroups / 256.0f;
+    return w <= 1.0f ? 1.0f : f32 && wide ? ceilf(w) : w <= 2.0f ? 1.75f : 0.15f + 0.8f * w;
+  };
+  auto crowd_back = [&](uint64_t workgroups) {
+    const float w = (float)workgroups / 256.0f;
+    return w <= 0.5f ? 1.0f : w <= 1.0f ? 1.4f : f32 && wide ? 1.4f * ceilf(w) : w <= 2.0f ? 2.5f : 1.25f * w;
+  };
+  const uint32_t most = chunks / 2 < 64 ? chunks / 2 : 64;
+  float best = 0.0f;
+  Cut c{1, chunks ? chunks : 1};
+  for (uint32_t s = 1; rows && chunks && (s == 1 || s <= most); ++s) {
+    const uint32_t segment = (chunks + s - 1) / s;
+    float us = (float)segment * (backward ? back_us[f32][wide] * crowd_back(rows * s * slices) : forward_us[f32][wide] * crowd(rows * s * slices));
+    if (s > 1) {
+      us += (float)segment * carry_us[f32][wide] * crowd(rows * (backward ? s : s - 1) * more) + 12.0f + (wide ? 4.5f : 3.2f) * (float)s * crowd(rows * slices);
+      if (backward) us += (float)segment * carry_back_us[f32][wide] * crowd(rows * (s - 1) * slices) + 12.0f + (wide ? 4.5f : 3.2f) * (float)s * crowd(rows * slices);
+    }
+    if (s == 1 || us < best) {
+      best = us;
+      c = Cut{(chunks + segment - 1) / segment, segment};
+    }
+  }
+  return c;
 }
-size_t carried_floats(const DeltaSizes& a) { return (size_t)a.dk * (a.dk + a.dv); }   // of a segment
-size_t carried_bytes(const DeltaSizes& a, const Cut& c) { return c.segments < 2 ? 0 : align256((size_t)a.B * a.H * c.segments * carried_floats(a) * sizeof(float)); }
+uint32_t carried_floats(const DeltaSizes& a, bool turned) { return a.dk * (a.dk * (turned ? 2 : 1) + a.dv); }   // of a segment
+size_t carried_bytes(const DeltaSizes& a, const Cut& c, bool turned) {
+  return c.segments < 2 ? 0 : align256((size_t)a.B * a.H * c.segments * carried_floats(a, turned) * sizeof(float));
+}
 
 size_t record_bytes(const DeltaSizes& a) { return (size_t)a.B * a.H * chunks_of(a.L) * sizeof(DeltaRecord); }
 
@@ -67,7 +100,7 @@ BackWork back_work(const DeltaSizes& a) {
   w.fold_q = take(a.Q == a.H ? 0 : tokens * a.dk * sizeof(float));
   w.fold_k = take(a.K == a.H ? 0 : tokens * a.dk * sizeof(float));
   const Cut c = cut(a, true);
-  w.carried = take(carried_bytes(a, c));
+  w.carried = take(carried_bytes(a, c, true));
   w.carried_back = take(c.segments < 2 ? 0 : bh * c.segments * a.dk * a.dv * sizeof(float));
   w.bytes = at;
   return w;
@@ -148,17 +181,20 @@ DeltaRun make_run(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows
   if (p.chunks) p.segment = p.chunks;
   return p;
 }
-// The states that segments start from: what each carries (all but the last; with `all`, the last's product too), then one behind the other.
+// The states that segments start from: what each carries (all but the last; with `all`, for a gradient, the last's too, and products
+// transposed), then one behind the other.
 template <typename T, int DK>
 hipError_t launch_carry(DeltaRun* p, const DeltaSizes& a, const Cut& c, const per_seq_states* state, float* carried, bool all, hipStream_t s) {
   p->segments = p->run = c.segments;
   p->segment = c.segment;
   if (c.segments < 2) return hipSuccess;
   p->carried = carried;
+  p->each = carried_floats(a, all);
+  p->turned = all;
   p->run = all ? c.segments : c.segments - 1;
   hipError_t e = launch_run<T, DK, CARRYING>(*p, a.B * a.H, s);
   if (e != hipSuccess) return e;
-  const size_t each = carried_floats(a);
+  const size_t each = p->each;
   DeltaJoin j{carried, carried + (size_t)a.dk * a.dv, nullptr, 0, 0, each, each, a.H, a.dk, a.dv, p->slices, c.segments};
   if (state) { j.in = state->d; j.in_batch = state->batch; j.in_head = state->head; }
   k_delta_join<DK, false><<<a.B * a.H * p->slices, 4 * DK, 0, s>>>(j);
@@ -247,7 +283,7 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
     e = launch_back<T, DK, true>(b, bh, s);
     if (e != hipSuccess) return e;
     const size_t each = (size_t)a.dk * a.dv;
-    const DeltaJoin j{b.carried, floats(w.carried) + each, b.in, b.in_batch, b.in_head, each, carried_floats(a), a.H, a.dk, a.dv, b.slices, c.segments};
+    const DeltaJoin j{b.carried, floats(w.carried) + (size_t)a.dk * (a.dv + a.dk), b.in, b.in_batch, b.in_head, each, carried_floats(a, true), a.H, a.dk, a.dv, b.slices, c.segments};
     k_delta_join<DK, true><<<bh * b.slices, 4 * DK, 0, s>>>(j);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -319,7 +355,7 @@ hipError_t step(DeltaStep p, uint32_t rows, hipStream_t s) {
 
 size_t delta_work_bytes(const DeltaSizes& a, bool backward) {
   if (!a.B || !a.H || !a.L) return 0;
-  return backward ? back_work(a).bytes : record_bytes(a) + carried_bytes(a, cut(a, false));
+  return backward ? back_work(a).bytes : record_bytes(a) + carried_bytes(a, cut(a, false), false);
 }
 
 hipError_t launch_delta(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state,
