@@ -40,32 +40,39 @@ struct DeltaPairs {
   float scale;
 };
 
-// Elements col .. col + 7 of a row, zeros behind `width` and where the row is not `on`.  FAST: rows are made of pieces of 16 bytes.
-template <typename T, bool FAST>
-__device__ __forceinline__ Operand<T> row_piece(const T* row, bool on, uint32_t col, uint32_t width) {
+// Elements col .. col + 7 of a row as it has them; the operand that they are, zeros behind `width` and where the row is not `on`.  FAST: rows are
+// made of pieces of 16 bytes.
+template <typename T>
+struct EightOf {
   typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T))));
-  T x[8];
-  if constexpr (FAST) {
-    const bool in = on && col < width;
-    const Vec* at = reinterpret_cast<const Vec*>(row + (col < width ? col : 0));
+  Vec v[sizeof(T) / 2];
+};
+template <typename T, bool FAST>
+__device__ __forceinline__ void ask_eight(const T* row, uint32_t col, uint32_t width, EightOf<T>* o) {
+  constexpr uint32_t W = 16 / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-      const bool there = sizeof(T) == 2 || (int)col + 4 * i < (int)width;
-      const Vec v = at[there ? i : 0];
+  for (uint32_t i = 0; i < 8 / W; ++i) {
+    if constexpr (FAST) {
+      o->v[i] = *reinterpret_cast<const typename EightOf<T>::Vec*>(row + (col + W * i < width ? col + W * i : 0));
+    } else {
 #pragma unroll
-      for (int e = 0; e < 16 / (int)sizeof(T); ++e) x[i * (16 / sizeof(T)) + e] = in && there ? v[e] : T(0.0f);
+      for (uint32_t e = 0; e < W; ++e) o->v[i][e] = row[col + W * i + e < width ? col + W * i + e : 0];
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = on && col + e < width ? row[col + e] : T(0.0f);
   }
+}
+template <typename T>
+__device__ __forceinline__ Operand<T> operand_of_eight(const EightOf<T>& x, bool on, uint32_t col, uint32_t width) {
+  constexpr uint32_t W = 16 / sizeof(T);
+  T y[8];
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) y[e] = on && col + e < width ? x.v[e / W][e % W] : T(0.0f);
   if constexpr (sizeof(T) == 2) {
     Operand<T> o;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o.v[0][e] = x[e];
+    for (int e = 0; e < 8; ++e) o.v[0][e] = y[e];
     return o;
   } else {
-    return Operand<T>::of(f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]});
+    return Operand<T>::of(f32x4{y[0], y[1], y[2], y[3]}, f32x4{y[4], y[5], y[6], y[7]});
   }
 }
 
@@ -85,37 +92,15 @@ __device__ __forceinline__ double decay_sums(const Gates& log_decay, uint32_t b,
 
 constexpr uint32_t kPairRow = 36;   // floats of a row of 32 in LDS
 
-template <typename T, int DK, bool BACK, bool FAST>
-__device__ __forceinline__ void pair_products(const DeltaPairs& p, uint32_t b, uint32_t h, uint32_t first, uint32_t valid, uint32_t m, uint32_t g,
-                                              f32x4 (&kk)[3], f32x4 (&qk)[3]) {
-  const T *qr[2], *kr[2];
-  bool on[2];
+// c + a b of 16 x 16 x 16 in fp32: four of the inner dimension's places 4 g .. to a lane.
+__device__ __forceinline__ f32x4 mma_f32(f32x4 a, f32x4 b, f32x4 c) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t t = first + 16 * i + m;
-    on[i] = t < valid;
-    const uint32_t at = on[i] ? t : valid - 1;
-    qr[i] = row_of<T>(p.q, b, at, h);
-    kr[i] = row_of<T>(p.k, b, at, h);
-  }
-#pragma unroll
-  for (int s = 0; s < DK / 32; ++s) {
-    Operand<T> q[2], k[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      q[i] = row_piece<T, FAST>(qr[i], on[i], 32 * s + 8 * g, p.dk);
-      k[i] = row_piece<T, FAST>(kr[i], on[i], 32 * s + 8 * g, p.dk);
-    }
-#pragma unroll
-    for (int x = 0; x < 3; ++x) {   // tiles (0, 0), (1, 0), (1, 1)
-      kk[x] = mma(k[x > 0].v, k[x > 1].v, kk[x]);
-      qk[x] = mma(q[x > 0].v, k[x > 1].v, qk[x]);
-    }
-  }
+  for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
+  return c;
 }
 
-template <typename T, int DK, bool BACK>
-__global__ __launch_bounds__(256) void k_delta_pairs(DeltaPairs p) {
+template <typename T, int DK, bool BACK, bool FAST>
+__global__ __launch_bounds__(256, 2) void k_delta_pairs(DeltaPairs p) {
   __shared__ __attribute__((aligned(16))) float lds_a[4][32 * kPairRow], lds_b[4][32 * kPairRow], lds_beta[4][32];
   __shared__ double lds_g[4][32];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
@@ -129,17 +114,44 @@ __global__ __launch_bounds__(256) void k_delta_pairs(DeltaPairs p) {
   float *const A = lds_a[wave], *const B = lds_b[wave], *const beta = lds_beta[wave];
   double* const G = lds_g[wave];
 
+  // all that comes from memory, before anything is waited for
+  EightOf<T> qx[DK / 32][2], kx[DK / 32][2];
+  bool on[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t t = first + 16 * i + m;
+    on[i] = t < valid;
+    const uint32_t at = on[i] ? t : valid - 1;
+    const T *const qr = row_of<T>(p.q, b, at, h), *const kr = row_of<T>(p.k, b, at, h);
+#pragma unroll
+    for (int s = 0; s < DK / 32; ++s) {
+      ask_eight<T, FAST>(kr, 32 * s + 8 * g, p.dk, &kx[s][i]);
+      ask_eight<T, FAST>(qr, 32 * s + 8 * g, p.dk, &qx[s][i]);
+    }
+  }
   const uint32_t column = lane & 31;
   const bool here = first + column < valid;
-  const double sum = decay_sums(p.log_decay, b, h, here ? first + column : first, here, lane);
   const float strength = here ? p.beta.at(b, first + column, h) : 0.0f;
+  const double sum = decay_sums(p.log_decay, b, h, here ? first + column : first, here, lane);
   if (lane < 32) {
     G[lane] = sum;
     beta[lane] = strength;
   }
   f32x4 kk[3] = {}, qk[3] = {};
-  if (p.q.wide && p.k.wide && p.dk % (16 / sizeof(T)) == 0) pair_products<T, DK, BACK, true>(p, b, h, first, valid, m, g, kk, qk);
-  else pair_products<T, DK, BACK, false>(p, b, h, first, valid, m, g, kk, qk);
+#pragma unroll
+  for (int s = 0; s < DK / 32; ++s) {
+    Operand<T> q[2], k[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      q[i] = operand_of_eight<T>(qx[s][i], on[i], 32 * s + 8 * g, p.dk);
+      k[i] = operand_of_eight<T>(kx[s][i], on[i], 32 * s + 8 * g, p.dk);
+    }
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {   // tiles (0, 0), (1, 0), (1, 1)
+      kk[x] = mma(k[x > 0].v, k[x > 1].v, kk[x]);
+      qk[x] = mma(q[x > 0].v, k[x > 1].v, qk[x]);
+    }
+  }
   wave_sync();
   const double total = G[31];
   if (lane < 32) {
@@ -186,14 +198,17 @@ __global__ __launch_bounds__(256) void k_delta_pairs(DeltaPairs p) {
     put(whole->pairs_t, 0, qk[0], qk[1]);
     put(whole->pairs_t, 1, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, qk[2]);
   }
-  const bool other = BACK && lane >= 32;   // (1 + diag(beta) N)^-1
-  float x[32], w[32];
+  // The inverse of  1 + N diag(beta)  (upper half: 1 + diag(beta) N) by halves: of the two blocks on the diagonal by substitution, a column to a lane,
+  // 16 lanes to a block; then the one below, -X11 A10 X00, by two products in fp32.
+  const bool other = BACK && lane >= 32;
+  const uint32_t corner = 16 * (g & 1);
+  float x[16], w[16];
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
+  for (int i = 0; i < 16; ++i) {
     float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
     for (int l = 0; l + 3 < i + 3; l += 4) {
-      const f32x4 n = *reinterpret_cast<const f32x4*>(A + i * kPairRow + l);
+      const f32x4 n = *reinterpret_cast<const f32x4*>(A + (corner + i) * kPairRow + corner + l);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (l + e < i) {
@@ -201,14 +216,33 @@ __global__ __launch_bounds__(256) void k_delta_pairs(DeltaPairs p) {
           else s0 = fmaf(n[e], w[l + e], s0);
         }
     }
-    const float all = s0 + s1, bi = beta[i];
-    x[i] = ((uint32_t)i == column ? 1.0f : 0.0f) - (other ? bi * all : all);
+    const float all = s0 + s1, bi = beta[corner + i];
+    x[i] = ((uint32_t)i == m ? 1.0f : 0.0f) - (other ? bi * all : all);
     w[i] = other ? x[i] : bi * x[i];
   }
+  // N10 as an operand, before its place is written over
+  const f32x4 below = *reinterpret_cast<const f32x4*>(A + (16 + m) * kPairRow + 4 * g);
+  const f32x4 beta0 = *reinterpret_cast<const f32x4*>(beta + 4 * g);
+  const float beta1 = beta[16 + m];
   wave_sync();
   float* const X = other ? B : A;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) X[i * kPairRow + column] = x[i];
+  for (int i = 0; i < 16; ++i) {
+    X[(corner + i) * kPairRow + corner + m] = x[i];
+    if (corner) X[i * kPairRow + 16 + m] = 0.0f;
+  }
+  wave_sync();
+#pragma unroll
+  for (int way = 0; way < (BACK ? 2 : 1); ++way) {
+    float* const Y = way ? B : A;
+    f32x4 upper, lower = *reinterpret_cast<const f32x4*>(Y + (16 + m) * kPairRow + 16 + 4 * g);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) upper[r] = Y[(4 * g + r) * kPairRow + m];
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    const f32x4 inner = mma_f32(way ? beta1 * below : below * beta0, upper, zero), under = mma_f32(lower, inner, zero);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) Y[(16 + 4 * g + r) * kPairRow + m] = -under[r];
+  }
   wave_sync();
   put_rows(record->solve, A);
   if constexpr (BACK) {

@@ -156,7 +156,8 @@ hipError_t launch_pairs(const DeltaSizes& a, const per_seq_rows& q, const per_se
   if (!items) return hipSuccess;
   const DeltaPairs p{rows(q, a.dtype, a.H / a.Q), rows(k, a.dtype, a.H / a.K), gates(a.log_decay), gates(a.beta), a.lengths, records,
                      a.L, a.H, a.dk, chunks_of(a.L), items, a.scale};
-  k_delta_pairs<T, DK, BACK><<<(items + 3) / 4, 256, 0, s>>>(p);
+  if (p.q.wide && p.k.wide && p.dk % (16 / sizeof(T)) == 0) k_delta_pairs<T, DK, BACK, true><<<(items + 3) / 4, 256, 0, s>>>(p);
+  else k_delta_pairs<T, DK, BACK, false><<<(items + 3) / 4, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
