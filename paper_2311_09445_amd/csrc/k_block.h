@@ -347,9 +347,13 @@ __global__ __launch_bounds__(256) void k_dropout(BlockArgs a, uint64_t n) {
     const Words r = philox(block, offset, a.seed);
     uint64_t row = first / a.dim;
     uint32_t col = (uint32_t)(first % a.dim);
-    for (uint32_t e = 0; e < count; ++e) {
-      const float o = kept_of(r, e) ? as_float(row_at<T>(a.x, row, a)[col]) * factor : 0.0f;
-      const_cast<T*>(row_at<T>(a.out, row, a))[col] = (T)(RESIDUAL ? as_float(row_at<T>(a.more, row, a)[col]) + o : o);
+    // (unrolled: words that are indexed by a number would lie in memory)
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+      if (e < count) {
+        const float o = kept_of(r, e) ? as_float(row_at<T>(a.x, row, a)[col]) * factor : 0.0f;
+        const_cast<T*>(row_at<T>(a.out, row, a))[col] = (T)(RESIDUAL ? as_float(row_at<T>(a.more, row, a)[col]) + o : o);
+      }
       if (++col == a.dim) {
         col = 0;
         ++row;
