@@ -428,10 +428,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_
       }
     }
     if (block + 1 < blocks) ask(block + 1);
-    if (tj <= ti) {
-      dm = mma<LESS>(ti ? d[1].v : d[0].v, tj ? u[1].v : u[0].v, dm);
-      dn = mma<LESS>(ti ? z[1].v : z[0].v, tj ? u[1].v : u[0].v, dn);
-    }
+    // (branches: operands that are chosen by a number would lie in memory)
+    auto pair = [&](int i, int j) {
+      dm = mma<LESS>(d[i].v, u[j].v, dm);
+      dn = mma<LESS>(z[i].v, u[j].v, dn);
+    };
+    if (wave == 0) pair(0, 0);
+    else if (wave == 2) pair(1, 0);
+    else if (wave == 3) pair(1, 1);
 #pragma unroll
     for (int a = 0; a < NC; ++a) {
       bf16x8 s[PS], r[PS];
