@@ -181,19 +181,20 @@ __global__ __launch_bounds__(256, 2) void k_delta_pairs(DeltaPairs p) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) B[(4 * g + r) * kPairRow + 16 + m] = 0.0f;
   wave_sync();
-  auto put = [&](bf16x8 (&to)[3][2][64], int tile, f32x4 a, f32x4 c) {
+  constexpr int PAIR_PARTS = sizeof(T) == 2 && !BACK ? 2 : 3;   // (as many as outputs in bfloat16 take)
+  auto put = [&](bf16x8 (&to)[3][2][64], int tile, f32x4 a, f32x4 c, int parts = 3) {
     const Parts<3> o = Parts<3>::of(a, c);
 #pragma unroll
-    for (int t = 0; t < 3; ++t) to[t][tile][lane] = o.v[t];
+    for (int t = 0; t < parts; ++t) to[t][tile][lane] = o.v[t];
   };
-  auto put_rows = [&](bf16x8 (&to)[3][2][64], const float* from) {
+  auto put_rows = [&](bf16x8 (&to)[3][2][64], const float* from, int parts = 3) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float* row = from + (16 * i + m) * kPairRow + 4 * g;
-      put(to, i, *reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + 16));
+      put(to, i, *reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + 16), parts);
     }
   };
-  put_rows(record->pairs, B);
+  put_rows(record->pairs, B, PAIR_PARTS);
   if constexpr (BACK) {
     put(whole->pairs_t, 0, qk[0], qk[1]);
     put(whole->pairs_t, 1, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, qk[2]);

@@ -385,6 +385,106 @@ def test_values_that_are_not_finite(dtype):
             assert i == 0 or (out[1, 100:, 1].isnan().all() and state[1, 1].isnan().all())
 
 
+@TYPES
+@pytest.mark.parametrize("B,L,H,Q,K,V,dk,dv", [(1, 300, 1, 1, 1, 1, 64, 64), (2, 777, 2, 1, 2, 1, 128, 72), (1, 1025, 3, 3, 1, 1, 40, 128), (3, 513, 2, 2, 2, 2, 61, 37)])
+def test_sequences_in_segments(B, L, H, Q, K, V, dk, dv, dtype):
+    """Few long sequences are cut; some end in the first segments, and the states they start from are made of those before."""
+    q, k, v, g, beta, S, _ = inputs(B, L, H, Q, K, V, dk, dv, dtype, fast=0.02)
+    dout, dS = normal(21, B, L, H, dv, dtype=dtype), 0.3 * normal(22, B, H, dk, dv)
+    for lengths in (None, torch.tensor([L - 1, 45, 0][:B], dtype=torch.int32).cuda()):
+        out, last = seq.gated_delta(q, k, v, g, beta, S, lengths)
+        want, state = oracle.delta_of(q, k, v, g, beta, S, lengths, dk ** -0.5)
+        check_out(out, want, L, dk, dtype)
+        near(last, state, u32(L, dk), "state")
+        got = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths)
+        check_grads(got, oracle.delta_backward(dout, q, k, v, g, beta, S, dS, lengths, dk ** -0.5), L, max(dk, dv), dtype)
+
+
+@TYPES
+def test_rows_far_apart(dtype):
+    """Tokens 2^24 elements apart, sequences more than 2^31: strides pass 32 bits."""
+    B, L, H, d = 2, 37, 1, 32
+    q, k, v, g, beta, S, _ = inputs(B, L, H, H, H, H, d, d, dtype)
+    dout = normal(21, B, L, H, d, dtype=dtype)
+    pool = torch.empty(3 * (1 << 24) * L + 4096, dtype=dtype, device="cuda")
+    places = [pool[64 * i:].as_strided((B, L, H, d), (2 * (1 << 24) * L + 8, 1 << 24, d, 1)) for i in range(1, 5)]
+    for place, t in zip(places, (q, k, v, dout)):
+        place.copy_(t)
+    want = [*seq.gated_delta(q, k, v, g, beta, S), *seq.gated_delta_backward(dout, q, k, v, g, beta, S)]
+    got = [*seq.gated_delta(*places[:3], g, beta, S), *seq.gated_delta_backward(places[3], *places[:3], g, beta, S)]
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    out = pool[64 * 6:].as_strided((B, L, H, d), (2 * (1 << 24) * L + 8, 1 << 24, d, 1))
+    seq.gated_delta(q, k, v, g, beta, S, out=out)
+    assert torch.equal(out, want[0])
+    rows = [pool[64 * i:].as_strided((B, L, H, d), (2 * (1 << 24) * L + 8, 1 << 24, d, 1)) for i in range(7, 10)]
+    seq.gated_delta_backward(dout, q, k, v, g, beta, S, dq=rows[0], dk=rows[1], dv=rows[2])
+    assert all(torch.equal(x, y) for x, y in zip(rows, want[2:5]))
+
+
+def test_rows_at_every_alignment():
+    B, L, H, dk, dv = 1, 70, 2, 24, 40
+    q, k, v, g, beta, S, _ = inputs(B, L, H, H, H, H, dk, dv, BF16)
+    want = seq.gated_delta(q, k, v, g, beta, S)
+    for shift in (1, 2, 3, 4, 7):
+        moved = []
+        for t in (q, k, v):
+            pool = torch.empty(t.numel() + 16, dtype=BF16, device="cuda")
+            moved.append(pool[shift:shift + t.numel()].view(t.shape).copy_(t))
+        out = torch.empty(want[0].numel() + 16, dtype=BF16, device="cuda")[shift:shift + want[0].numel()].view(want[0].shape)
+        got = seq.gated_delta(*moved, g, beta, S, out=out)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_block_of_all_three():
+    """x + dropout(memory(norm(x))) of a learner in fp32, its gradients through torch's graph, against the definitions in 64 bits; then the
+    same block by single tokens, as an actor runs it."""
+    B, L, H, d = 2, 60, 2, 32
+    D = H * d
+    x, w, b = normal(1, B, L, D), 1 + 0.1 * normal(2, D), 0.1 * normal(3, D)
+    gates = normal(4, B, L, 2 * H)
+    S = 0.3 * normal(5, B, H, d, d)
+    lengths = torch.tensor([L, 41], dtype=torch.int32).cuda()
+    keep = oracle.kept(B * L * D, 0.25, 9, 3).reshape(B, L, D)
+    dout = normal(6, B, L, D)
+
+    def block(x, w, b, gates, S, own):
+        if own:
+            y = seq.layer_norm(x, w, b)
+        else:
+            y = (x - x.mean(-1, keepdim=True)) / torch.sqrt(x.var(-1, unbiased=False, keepdim=True) + 1e-5) * w + b
+        rows = y.unflatten(-1, (H, d))
+        k = rows / rows.norm(dim=-1, keepdim=True)
+        g, beta = -torch.nn.functional.softplus(gates[..., :H]), torch.sigmoid(gates[..., H:])
+        if own:
+            o, last = seq.gated_delta(rows, k, rows, g, beta, S, lengths, scale=0.2)
+            return seq.dropout(o.flatten(-2), 0.25, 9, 3, residual=x), last
+        o, last = oracle.delta(rows, k, rows, g, beta, S, lengths.cpu(), 0.2)
+        return x + o.flatten(-2) * keep / 0.75, last
+
+    leaves = [t.clone().requires_grad_() for t in (x, w, b, gates, S)]
+    exact = [oracle.f64(t).requires_grad_() for t in (x, w, b, gates, S)]
+    got, want = block(*leaves, True), block(*exact, False)
+    near(got[0], want[0].detach(), 4 * u32(L, d), "out")
+    near(got[1], want[1].detach(), 4 * u32(L, d), "state")
+    dS = normal(7, B, H, d, d)
+    torch.autograd.backward(got, (dout, dS))
+    torch.autograd.backward(want, (oracle.f64(dout), oracle.f64(dS)))
+    for name, t, e in zip(("x", "w", "b", "gates", "state"), leaves, exact):
+        near(t.grad, e.grad, 16 * u32(L, d), name)
+    T, steps = S.clone(), []
+    with torch.no_grad():
+        for t in range(L):
+            at = x[:, t:t + 1]
+            rows = seq.layer_norm(at, w, b).unflatten(-1, (H, d))
+            k = rows / rows.norm(dim=-1, keepdim=True)
+            here = gates[:, t:t + 1]
+            o = seq.gated_delta_step(rows, k, rows, -torch.nn.functional.softplus(here[..., :H]), torch.sigmoid(here[..., H:]), T, active=(lengths > t).int(), scale=0.2)
+            steps.append(o.flatten(-2))
+    whole = seq.dropout(torch.cat(steps, 1), 0.25, 9, 3, residual=x)
+    near(whole, want[0].detach(), 4 * u32(L, d), "out by tokens")
+    near(T, want[1].detach(), 4 * u32(L, d), "state by tokens")
+
+
 # ------------------------------------------------------------------------------------------- streams, graphs, torch's graph
 def test_on_a_stream_of_its_own():
     q, k, v, g, beta, S, lengths = inputs(3, 500, 2, 2, 1, 2, 64, 64, BF16, ragged=True)
