@@ -49,13 +49,14 @@ __device__ __forceinline__ size_t state_at(uint32_t bh, uint32_t chunks, uint32_
 template <int N>
 struct RecordRows {
   bf16x8 solve[2][3], pairs[2][N];
+  template <bool PAIRS = true>
   __device__ __forceinline__ void load(const bf16x8* solves, const bf16x8* pairings, uint32_t lane) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
       for (int t = 0; t < 3; ++t) solve[i][t] = solves[(2 * t + i) * 64 + lane];
 #pragma unroll
-      for (int t = 0; t < N; ++t) pairs[i][t] = pairings[(2 * t + i) * 64 + lane];
+      for (int t = 0; t < (PAIRS ? N : 0); ++t) pairs[i][t] = pairings[(2 * t + i) * 64 + lane];
     }
   }
 };
@@ -288,18 +289,20 @@ struct TwoRows {
 
 // LDS of a chunk: rows of queries and keys, and where they come straight from memory those of 64 values and the record's products too (twice 32 KiB:
 // as far as such loads reach).
-template <typename T, int DK, int NP, bool DIRECT_ROWS>
+// (A pass that only carries has neither queries nor pairs there.)
+template <typename T, int DK, int NP, bool DIRECT_ROWS, bool ASKS = true>
 struct RunLds {
-  static constexpr uint32_t Q = 0, K = kParts<T> * Tile<DK>::SIZE, V = 2 * K, SOLVE = V + (DIRECT_ROWS ? Tile<64>::SIZE : 0),
-                            PAIRS = SOLVE + (DIRECT_ROWS ? 3 * 1024 : 0), SIZE = PAIRS + (DIRECT_ROWS ? NP * 1024 : 0), BYTES = 2 * SIZE * sizeof(bf16);
+  static constexpr uint32_t ROWS = kParts<T> * Tile<DK>::SIZE, Q = 0, K = ASKS || !DIRECT_ROWS ? ROWS : 0, V = K + ROWS,
+                            SOLVE = V + (DIRECT_ROWS ? Tile<64>::SIZE : 0), PAIRS = SOLVE + (DIRECT_ROWS ? 3 * 1024 : 0),
+                            SIZE = PAIRS + (DIRECT_ROWS && ASKS ? NP * 1024 : 0), BYTES = 2 * SIZE * sizeof(bf16);
 };
 template <typename T, DeltaMode MODE>
 constexpr int kPairParts = MODE == CARRYING ? 1 : sizeof(T) == 2 && MODE == FORWARD ? 2 : 3;
 
 template <typename T, int DK, DeltaMode MODE, bool DIRECT_ROWS>
-__global__ __launch_bounds__(256, DIRECT_ROWS ? 2 : 1) void k_delta_run(DeltaRun p) {
+__global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 64 ? 3 : 2) void k_delta_run(DeltaRun p) {
   constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = NP - 1;
-  typedef RunLds<T, DK, NP, DIRECT_ROWS> Lds;
+  typedef RunLds<T, DK, NP, DIRECT_ROWS, MODE != CARRYING> Lds;
   static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   bf16* const lds = reinterpret_cast<bf16*>(lds_raw);
@@ -346,7 +349,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS ? 2 : 1) void k_delta_run(DeltaRun
     } else {
       rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
       if (c + 1 < chunks) rows.load(p.q, p.k, q0, k0, (c + 1) * kChunk, valid, dk, pieces);
-      next.load(&record(c)->solve[0][0][0], &record(c)->pairs[0][0][0], lane);
+      next.template load<MODE != CARRYING>(&record(c)->solve[0][0][0], &record(c)->pairs[0][0][0], lane);
       next_v.ask(p.v, v0, c * kChunk, valid, takes, col, g);
     }
     if constexpr (MODE == KEEPING) {
@@ -368,7 +371,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS ? 2 : 1) void k_delta_run(DeltaRun
     direct_v.set(p.v, product ? 0 : dv - 64 * slice, wave, lane);
     if (dk < DK || dv - 64 * slice < 64 || product) {
       for (uint32_t i = 0; i < 2; ++i) {
-        DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::Q, 0, threadIdx.x);
+        if (MODE != CARRYING) DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::Q, 0, threadIdx.x);
         DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::K, 0, threadIdx.x);
         DirectRows<64>::clear(lds + i * Lds::SIZE + Lds::V, 0, threadIdx.x);
       }
@@ -415,7 +418,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS ? 2 : 1) void k_delta_run(DeltaRun
       if (MODE == KEEPING && works && c > chunk0 + 1) arrive<KX + 8>();
       else arrive<0>();
       if (valid - first < kChunk) {
-        DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
+        if (MODE != CARRYING) DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
         DirectRows<DK>::clear(K, valid - first, threadIdx.x);
         DirectRows<64>::clear(buffer + Lds::V, valid - first, threadIdx.x);
         __syncthreads();
@@ -465,7 +468,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS ? 2 : 1) void k_delta_run(DeltaRun
       }
       f32x4 v[2];
       if constexpr (DIRECT_ROWS) {
-        rec.load(reinterpret_cast<const bf16x8*>(buffer + Lds::SOLVE), reinterpret_cast<const bf16x8*>(buffer + Lds::PAIRS), lane);
+        rec.template load<MODE != CARRYING>(reinterpret_cast<const bf16x8*>(buffer + Lds::SOLVE), reinterpret_cast<const bf16x8*>(buffer + Lds::PAIRS), lane);
         Operand<bf16>::across<64>(buffer + Lds::V, [&](uint32_t i) { return 16 * wave + i; }, m, g).widen(&v[0], &v[1]);
       }
       else now_v.widen(first, valid, takes, g, v);

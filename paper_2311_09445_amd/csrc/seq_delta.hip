@@ -131,9 +131,9 @@ hipError_t launch_run(const DeltaRun& p, uint32_t bh, hipStream_t s) {
   const uint32_t grid = bh * p.run * (p.slices + (MODE == CARRYING ? (p.dk + 63) / 64 : 0));
   if constexpr (sizeof(T) == 2) {
     if (p.q.wide && p.k.wide && p.v.wide && p.dk % 8 == 0 && p.dv % 8 == 0)
-      return launch(k_delta_run<T, DK, MODE, true>, &granted[1], grid, RunLds<T, DK, NP, true>::BYTES, p, s);
+      return launch(k_delta_run<T, DK, MODE, true>, &granted[1], grid, RunLds<T, DK, NP, true, MODE != CARRYING>::BYTES, p, s);
   }
-  return launch(k_delta_run<T, DK, MODE, false>, &granted[0], grid, RunLds<T, DK, NP, false>::BYTES, p, s);
+  return launch(k_delta_run<T, DK, MODE, false>, &granted[0], grid, RunLds<T, DK, NP, false, MODE != CARRYING>::BYTES, p, s);
 }
 template <typename T, int DK, bool CARRY>
 hipError_t launch_back(const DeltaBack& p, uint32_t bh, hipStream_t s) {
