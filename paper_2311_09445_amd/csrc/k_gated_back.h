@@ -299,7 +299,7 @@ struct DeltaGrads {
 struct DeltaGates {
   Gates dlog_decay, dbeta;
   const int32_t* lengths;
-  uint32_t L, H, chunks, parts;   // parts: slices of 16 columns, which sums come in
+  uint32_t rows, L, H, chunks, parts;   // rows: sequences and heads; parts: slices of 16 columns, which sums come in
   const float *read, *along, *strength, *border;   // read, along: rows of out . dout, of dZ . V
 };
 // Eight neighbours of a row.
@@ -505,12 +505,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_
   }
 }
 
-// The gates' gradients: a thread takes a token, a workgroup the kBorder chunks behind a border.  The decays' falls from token to token by what is
-// read along dout less what is written along V.
-__global__ __launch_bounds__(kBorder * kChunk) void k_delta_gates(DeltaGates p) {
-  __shared__ float upto;
-  const uint32_t groups = (p.chunks + kBorder - 1) / kBorder, group = blockIdx.x % groups, bh = blockIdx.x / groups, h = bh % p.H, b = bh / p.H;
-  const uint32_t t = group * kBorder * kChunk + threadIdx.x, valid = valid_tokens(p.lengths, b, p.L), tokens = p.chunks * kChunk;
+// The gates' gradients: a thread takes a token, half a workgroup the kBorder chunks behind a border.  The decays' falls from token to token by
+// what is read along dout less what is written along V.
+__device__ __forceinline__ void gates_of(const DeltaGates& p, uint32_t block) {
+  static_assert(kBorder * kChunk == 128, "two waves");
+  __shared__ float upto[2];
+  const uint32_t half = threadIdx.x >> 7, at_half = threadIdx.x & 127, groups = (p.chunks + kBorder - 1) / kBorder, all = p.rows * groups;
+  const uint32_t item = 2 * block + half < all ? 2 * block + half : all - 1, group = item % groups, bh = item / groups, h = bh % p.H, b = bh / p.H;
+  const uint32_t t = group * kBorder * kChunk + at_half, valid = valid_tokens(p.lengths, b, p.L), tokens = p.chunks * kChunk;
   float strengths[8], falls[8], borders[8];
   const uint32_t from = t < valid ? t : 0;
 #pragma unroll
@@ -535,10 +537,10 @@ __global__ __launch_bounds__(kBorder * kChunk) void k_delta_gates(DeltaGates p) 
     const float x = __shfl_up(sum, d);
     if ((threadIdx.x & 63) >= (uint32_t)d) sum += x;
   }
-  if (threadIdx.x == 63) upto = sum;
+  if (at_half == 63) upto[half] = sum;
   __syncthreads();
-  if (threadIdx.x >= 64) sum += upto;
-  if (t >= p.L) return;
+  if (at_half >= 64) sum += upto[half];
+  if (t >= p.L || 2 * block + half >= all) return;
   float* const dg = const_cast<float*>(p.dlog_decay.d) + (int64_t)b * p.dlog_decay.batch + (int64_t)t * p.dlog_decay.token + (int64_t)h * p.dlog_decay.head;
   float* const db = const_cast<float*>(p.dbeta.d) + (int64_t)b * p.dbeta.batch + (int64_t)t * p.dbeta.token + (int64_t)h * p.dbeta.head;
   *dg = t < valid ? border - (sum - fall) : 0.0f;
@@ -549,22 +551,39 @@ __global__ __launch_bounds__(kBorder * kChunk) void k_delta_gates(DeltaGates p) 
 struct DeltaFold {
   const float* from;
   SeqRows to;
-  const int32_t* lengths;
-  uint64_t rows;   // B L n
-  uint32_t L, H, n, width, stride, tokens;
+  uint32_t n, width, stride, blocks;
 };
 template <typename T>
-__global__ __launch_bounds__(256) void k_delta_fold(DeltaFold f) {
-  const uint32_t lanes = (f.width + 3) / 4, per = 256 / lanes, at = threadIdx.x / lanes, col = threadIdx.x % lanes * 4, share = f.H / f.n;
+__device__ __forceinline__ void fold_of(const DeltaFold& f, const DeltaGates& p, uint32_t block) {
+  const uint32_t lanes = (f.width + 3) / 4, per = 256 / lanes, at = threadIdx.x / lanes, col = threadIdx.x % lanes * 4, share = p.H / f.n;
   if (at >= per) return;
-  for (uint64_t row = (uint64_t)blockIdx.x * per + at; row < f.rows; row += (uint64_t)gridDim.x * per) {
+  const uint64_t rows = (uint64_t)(p.rows / p.H) * p.L * f.n;
+  for (uint64_t row = (uint64_t)block * per + at; row < rows; row += (uint64_t)f.blocks * per) {
     const uint32_t i = (uint32_t)(row % f.n);
     const uint64_t tok = row / f.n;
-    const uint32_t b = (uint32_t)(tok / f.L), t = (uint32_t)(tok % f.L);
+    const uint32_t b = (uint32_t)(tok / p.L), t = (uint32_t)(tok % p.L);
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (t < valid_tokens(f.lengths, b, f.L))
+    if (t < valid_tokens(p.lengths, b, p.L))
       for (uint32_t s = 0; s < share; ++s)
-        sum += load_four<float>(f.from + (((size_t)b * f.H + i * share + s) * f.tokens + t) * f.stride, f.stride % 4 == 0, col, f.width);
+        sum += load_four<float>(f.from + (((size_t)b * p.H + i * share + s) * p.chunks * kChunk + t) * f.stride, f.stride % 4 == 0, col, f.width);
     store_four<T>(row_to<T>(f.to, b, t, i), f.to.wide, col, f.width, sum);
+  }
+}
+
+// What is left of a gradient when its rows are there, in one launch (each by itself took 6 us of 32 sequences of 512 tokens, 3 of them a launch's).
+struct DeltaFinish {
+  DeltaGates gates;
+  uint32_t gate_blocks;
+  DeltaFold fold[3];   // of queries, keys and values; blocks 0: there is nothing to add up
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_delta_finish(DeltaFinish p) {
+  uint32_t block = blockIdx.x;
+  if (block < p.gate_blocks) return gates_of(p.gates, block);
+  block -= p.gate_blocks;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    if (block < p.fold[i].blocks) return fold_of<T>(p.fold[i], p.gates, block);
+    block -= p.fold[i].blocks;
   }
 }

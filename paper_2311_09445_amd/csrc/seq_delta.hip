@@ -221,14 +221,13 @@ hipError_t forward(const DeltaSizes& a, const per_seq_rows& q, const per_seq_row
   return launch_run<T, DK, FORWARD>(p, a.B * a.H, s);
 }
 
-template <typename T>
-hipError_t fold(const DeltaSizes& a, const float* from, const per_seq_rows& to, uint32_t n, uint32_t width, uint32_t stride, hipStream_t s) {
-  const DeltaFold f{from, rows(to, a.dtype, 1), a.lengths, (uint64_t)a.B * a.L * n, a.L, a.H, n, width, stride, chunks_of(a.L) * kChunk};
-  if (!f.rows) return hipSuccess;
+DeltaFold fold(const DeltaSizes& a, const float* from, const per_seq_rows& to, uint32_t n, uint32_t width, uint32_t stride) {
+  DeltaFold f{from, rows(to, a.dtype, 1), n, width, stride, 0};
+  if (n == a.H) return f;
   const uint32_t per = 256 / ((width + 3) / 4);
-  const uint64_t blocks = (f.rows + per - 1) / per;
-  k_delta_fold<T><<<(uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), 256, 0, s>>>(f);
-  return hipGetLastError();
+  const uint64_t blocks = ((uint64_t)a.B * a.L * n + per - 1) / per;
+  f.blocks = (uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20);
+  return f;
 }
 
 template <typename T, int DK>
@@ -325,12 +324,14 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   g.dz = b.dz;
   e = launch_grads<T, DK>(g, bh, s);
   if (e != hipSuccess) return e;
-  const DeltaGates sums{gates(dlog_decay), gates(dbeta), a.lengths, a.L, a.H, run.chunks, (a.dv + 31) / 32 * 2, run.along, b.along, b.strength, b.border};
-  k_delta_gates<<<bh * ((run.chunks + kBorder - 1) / kBorder), kBorder * kChunk, 0, s>>>(sums);
+  DeltaFinish f{};
+  f.gates = DeltaGates{gates(dlog_decay), gates(dbeta), a.lengths, bh, a.L, a.H, run.chunks, (a.dv + 31) / 32 * 2, run.along, b.along, b.strength, b.border};
+  f.gate_blocks = (bh * ((run.chunks + kBorder - 1) / kBorder) + 1) / 2;
+  f.fold[0] = fold(a, g.fold_q, dq, a.Q, a.dk, a.dk);
+  f.fold[1] = fold(a, g.fold_k, dk, a.K, a.dk, a.dk);
+  f.fold[2] = fold(a, b.dz, dv, a.V, a.dv, (a.dv + 31) / 32 * 32);
+  k_delta_finish<T><<<f.gate_blocks + f.fold[0].blocks + f.fold[1].blocks + f.fold[2].blocks, 256, 0, s>>>(f);
   e = hipGetLastError();
-  if (e == hipSuccess && !g.direct_q) e = fold<T>(a, g.fold_q, dq, a.Q, a.dk, a.dk, s);
-  if (e == hipSuccess && !g.direct_k) e = fold<T>(a, g.fold_k, dk, a.K, a.dk, a.dk, s);
-  if (e == hipSuccess && !g.direct_v) e = fold<T>(a, b.dz, dv, a.V, a.dv, (a.dv + 31) / 32 * 32, s);
   return e;
 }
 
