@@ -19,9 +19,9 @@
  *    found on the host before anything is enqueued.  The library allocates nothing: the caller provides the workspace
  *    where one is needed (sized by the *_workspace function, 256-byte aligned; its contents need not be kept).  Calls hold
  *    no state between them and may be captured into a HIP graph and replayed.
- *  - Element type of rows: PER_SEQ_BF16 or PER_SEQ_F32.  Sums, norms, states and weights are fp32.  A result is rounded to
- *    its type once, at the end; only sequences of linear attention and their gradients in bfloat16 round inside as well,
- *    where it says so.
+ *  - Element type of rows: PER_SEQ_BF16 or PER_SEQ_F32.  Sums, norms, states, gates and weights are fp32.  A result is rounded to
+ *    its type once, at the end; only sequences of linear attention and of the gated delta rule and their gradients in bfloat16 round
+ *    inside as well, where it says so.
  *  - Outputs must not overlap inputs or each other, except where a call says so.
  *  - A batch, a length or a number of heads of 0 is valid: nothing is written but states (which are then copied), and zeros
  *    for gradients of keys and values that no head reads.
@@ -176,8 +176,8 @@ int per_gated_delta(const per_delta_config* c, const per_seq_rows* q, const per_
 
 /* Its gradient: from dout (of out) and dstate (of out_state; NULL: zeros) to dq, dk, dv, the gates' dlog_decay and dbeta, and dstate0 (of
  * state; NULL where not wanted).  Gradients of rows that several heads share are sums in a fixed order; behind a sequence's end all are
- * zeros.  In bfloat16 the products of rows round the states (once, to 2^-9) and what else they take (to 2^-17).  dstate0 may be dstate, and not
- * state. */
+ * zeros.  In bfloat16 the gradients of queries and keys take states and states' gradients rounded to it (2^-8), and of what else they
+ * take 16 bits.  dstate0 may be dstate, and not state. */
 int per_gated_delta_backward(const per_delta_config* c, const per_seq_rows* dout, const per_seq_rows* q, const per_seq_rows* k,
                              const per_seq_rows* v, const per_seq_gates* log_decay, const per_seq_gates* beta,
                              const int32_t* d_lengths, const per_seq_states* state, const per_seq_states* dstate,
