@@ -6,6 +6,11 @@
 // in columns that do not meet, as over time (k_delta_back).  What is left does not depend on the order of the chunks (k_delta_grads):
 //   dQ = scale e^G dO S^T + dM K,   dK = -e^G dZ S^T + left U R^T + dM^T Q + (dN + dN^T) K,
 //   dM = scale e_ij dO U^T (i >= j),   dN = -e_ij dZ U^T (i > j).
+//
+// What bounds them, in bfloat16: k_delta_back by itself takes 3.75 us for a chunk of 128 x 128, 3.1 of 64 x 64; with a workgroup on each compute unit
+// 4.6 (2 x 8192 tokens of 16 heads in segments 294 us, at 1.9 TB/s with what it leaves for k_delta_grads); that takes 334 us for 1.1 GB, waiting
+// for memory with two workgroups to a compute unit (three would spill: 710).
+//
 // The gradient of a decay's logarithm is that of the state before the token times the state itself.  At the first token of a chunk that is
 // <R, S>; from one token to the next it falls by out . dO - dZ . V, which is added up within a chunk only.
 

@@ -7,6 +7,10 @@
 // takes one chunk, the products on the matrix cores straight from memory, the inverse by substitution, a column to a lane (the upper
 // half of the wave forms (1 + diag(beta) N)^-1, which a gradient runs backwards through).
 //
+// What bounds it: 9 us for 768 chunks of 64 x 64 are loads' and LDS's latency and the substitution's chain (of 32 rows in one piece, with the
+// rows asked for behind the sums of decays, 11); 32768 chunks of 128 take 168 us for 350 MB written and 270 read.  Registers for
+// four waves to a SIMD would spill (300 us).
+//
 // What goes into the record of a chunk is laid out as the operands that the passes over the sequence take: places {4 g .. 4 g + 3, 16 + 4 g ..} of
 // the inner dimension in lane 16 g + m, in three parts.
 
