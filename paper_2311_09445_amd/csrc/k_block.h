@@ -13,13 +13,12 @@ struct Piece {
   typedef T Vec __attribute__((ext_vector_type(W)));
   typedef Vec Loose __attribute__((aligned(sizeof(T))));   // (memory is read at any address that its elements may have)
 };
-__device__ __forceinline__ const char* block_row(const SeqRows& r, uint64_t row, uint32_t L, uint32_t H, uint32_t e) {
-  const uint32_t h = (uint32_t)(row % H);
-  const uint64_t tok = row / H;
+__device__ __forceinline__ const char* block_row(const SeqRows& r, uint32_t row, uint32_t L, uint32_t H, uint32_t e) {
+  const uint32_t h = row % H, tok = row / H;
   return static_cast<const char*>(r.d) + ((int64_t)(tok / L) * r.batch + (int64_t)(tok % L) * r.token + (int64_t)h * r.head) * (int64_t)e;
 }
 template <typename T>
-__device__ __forceinline__ const T* row_at(const SeqRows& r, uint64_t row, const BlockArgs& a) {
+__device__ __forceinline__ const T* row_at(const SeqRows& r, uint32_t row, const BlockArgs& a) {
   return reinterpret_cast<const T*>(block_row(r, row, a.L, a.H, sizeof(T)));
 }
 
@@ -102,9 +101,14 @@ __device__ __forceinline__ float wave_sum(float x) {
   auto lane = [&](int i) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(y, i)); };
   return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
-// Sums of a row's lanes, two at once: of a wave, or of the workgroup's four in their order.
+// Sums of a row's lanes, two at once: of 16 lanes, of a wave, or of the workgroup's four in their order.
 template <int LANES>
 __device__ __forceinline__ void row_sums(float* a, float* b, float (*lds)[2]) {
+  if (LANES == 16) {
+    *a = sum16(*a);
+    *b = sum16(*b);
+    return;
+  }
   *a = wave_sum(*a);
   *b = wave_sum(*b);
   if (LANES == 64) return;
@@ -130,11 +134,13 @@ __device__ __forceinline__ void standardise(const HeldRow<T, LANES, N>& at, floa
   *r = 1.0f / sqrtf(square / (float)a.dim + a.eps);
 }
 
-// Which of a workgroup's rows a wave takes.
+// Which of a workgroup's rows a thread has part in.
 template <int LANES>
-__device__ __forceinline__ uint32_t row_of_block() { return LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0; }
+__device__ __forceinline__ uint32_t row_of_block() {
+  return LANES == 16 ? threadIdx.x >> 4 : LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+}
 
-// LANES 64: four rows to a workgroup.  Weights stay in registers from row to row.
+// LANES 16 or 64: 16 rows to a workgroup, or four.  Weights stay in registers from row to row.
 template <typename T, int LANES, int N>
 __global__ __launch_bounds__(256) void k_layer_norm(BlockArgs a) {
   constexpr int ALL = N * Piece<T>::W, ROWS = 256 / LANES;
@@ -143,8 +149,8 @@ __global__ __launch_bounds__(256) void k_layer_norm(BlockArgs a) {
   HeldRow<T, LANES, N> at(lane, a.dim);
   float w[ALL], b[ALL], x[ALL], r;
   typename HeldRow<T, LANES, N>::Raw next;
-  const uint64_t rows = (uint64_t)a.B * a.L * a.H, stride = (uint64_t)gridDim.x * ROWS;
-  uint64_t row = (uint64_t)blockIdx.x * ROWS + row_of_block<LANES>();
+  const uint32_t rows = a.B * a.L * a.H, stride = gridDim.x * ROWS;   // (up to 2^31)
+  uint32_t row = blockIdx.x * ROWS + row_of_block<LANES>();
   if (row < rows) at.load(row_at<T>(a.x, row, a), next);
   at.load_plain(a.weight, w, 1.0f);
   at.load_plain(a.bias, b, 0.0f);
@@ -169,8 +175,8 @@ __global__ __launch_bounds__(256, 2) void k_layer_norm_back(BlockArgs a) {
   HeldRow<T, LANES, N> at(lane, a.dim);
   float w[ALL], dw[ALL] = {}, db[ALL] = {}, x[ALL], d[ALL], r;
   typename HeldRow<T, LANES, N>::Raw next_x, next_d;
-  const uint64_t rows = (uint64_t)a.B * a.L * a.H, stride = (uint64_t)gridDim.x * ROWS;
-  uint64_t row = (uint64_t)blockIdx.x * ROWS + row_of_block<LANES>();
+  const uint32_t rows = a.B * a.L * a.H, stride = gridDim.x * ROWS;   // (up to 2^31)
+  uint32_t row = blockIdx.x * ROWS + row_of_block<LANES>();
   if (row < rows) {
     at.load(row_at<T>(a.x, row, a), next_x);
     at.load(row_at<T>(a.more, row, a), next_d);
@@ -203,10 +209,20 @@ __global__ __launch_bounds__(256, 2) void k_layer_norm_back(BlockArgs a) {
   }
   // The waves' sums one after the other, lane by lane: element e of piece i of lane l at (i W + e) LANES + l, as k_norm_sums takes them.
   extern __shared__ float sums[];
-  for (int turn = 0; turn < ROWS; ++turn) {
+  if (LANES == 16)
+#pragma unroll
+    for (int i = 0; i < ALL; ++i) {   // (the wave's four rows)
+      dw[i] += __shfl_xor(dw[i], 16);
+      dw[i] += __shfl_xor(dw[i], 32);
+      db[i] += __shfl_xor(db[i], 16);
+      db[i] += __shfl_xor(db[i], 32);
+    }
+  constexpr int TURNS = LANES == 256 ? 1 : 4;
+  const uint32_t wave = TURNS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int turn = 0; turn < TURNS; ++turn) {
     if (turn) __syncthreads();
-    if (row_of_block<LANES>() != (uint32_t)turn) continue;
-    float* const to = (turn + 1 < ROWS ? sums : a.partial + (size_t)blockIdx.x * 2 * ALL * LANES) + lane;
+    if (wave != (uint32_t)turn || (LANES == 16 && (threadIdx.x & 63) >= 16)) continue;
+    float* const to = (turn + 1 < TURNS ? sums : a.partial + (size_t)blockIdx.x * 2 * ALL * LANES) + lane;
 #pragma unroll
     for (int i = 0; i < ALL; ++i) {
       to[i * LANES] = turn ? sums[i * LANES + lane] + dw[i] : dw[i];
@@ -220,12 +236,12 @@ __global__ __launch_bounds__(256, 2) void k_layer_norm_back(BlockArgs a) {
 template <typename T, bool BACK>
 __global__ __launch_bounds__(256) void k_layer_norm_any(BlockArgs a) {
   __shared__ float lds[3][4][2];
-  const uint64_t rows = (uint64_t)a.B * a.L * a.H;
+  const uint32_t rows = a.B * a.L * a.H;
   float* const to = a.partial + (size_t)blockIdx.x * 2 * a.dim;
   if (BACK)
     for (uint32_t i = threadIdx.x; i < 2 * a.dim; i += 256) to[i] = 0.0f;
   __syncthreads();
-  for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+  for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
     const T* x = row_at<T>(a.x, row, a);
     T* out = const_cast<T*>(row_at<T>(a.out, row, a));
     float sum = 0.0f, along = 0.0f;
@@ -349,7 +365,7 @@ __global__ __launch_bounds__(256) void k_dropout(BlockArgs a, uint64_t n) {
       continue;
     }
     const Words r = philox(block, offset, a.seed);
-    uint64_t row = first / a.dim;
+    uint32_t row = (uint32_t)(first / a.dim);
     uint32_t col = (uint32_t)(first % a.dim);
     // (unrolled: words that are indexed by a number would lie in memory)
 #pragma unroll

@@ -11,8 +11,8 @@
 // 4.6 (2 x 8192 tokens of 16 heads in segments 294 us, at 1.9 TB/s with what it leaves for k_delta_grads); that takes 334 us for 1.1 GB, waiting
 // for memory with two workgroups to a compute unit (three would spill: 710).
 //
-// The gradient of a decay's logarithm is that of the state before the token times the state itself.  At the first token of a chunk that is
-// <R, S>; from one token to the next it falls by out . dO - dZ . V, which is added up within a chunk only.
+// The gradient of a decay's logarithm is that of the state before the token times the state itself.  At the first token of every kBorder-th chunk that is taken as
+// <R, S>; from one token to the next it falls by out . dO - dZ . V, which is added up over kBorder chunks at most.
 
 struct DeltaBack {
   SeqRows q, k, v, dout;
