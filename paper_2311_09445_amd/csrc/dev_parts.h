@@ -57,16 +57,20 @@ __device__ __forceinline__ void mma_turns(A a, B b, f32x4 (&c)[M]) {
 // LDS of a wave's own: written by some lanes, read by others behind this.
 __device__ __forceinline__ void wave_sync() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// The sum over the 16 lanes that share a lane's g.
-__device__ __forceinline__ float sum16(float x) {
+// The sum over four lanes in a row; over the 16 lanes that share a lane's g.
 #define PER_ADD_DPP(ctrl) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, 0xF, 0xF, false))
+__device__ __forceinline__ float sum4(float x) {
   PER_ADD_DPP(0xB1);    // lanes 1 apart
   PER_ADD_DPP(0x4E);    // 2 apart
-  PER_ADD_DPP(0x141);   // 4: the half row turned around
-  PER_ADD_DPP(0x140);   // 8: the row turned around
-#undef PER_ADD_DPP
   return x;
 }
+__device__ __forceinline__ float sum16(float x) {
+  x = sum4(x);
+  PER_ADD_DPP(0x141);   // 4: the half row turned around
+  PER_ADD_DPP(0x140);   // 8: the row turned around
+  return x;
+}
+#undef PER_ADD_DPP
 
 // Sums over the 16 lanes that share a lane's g, of 16 values at once: value m in lane m.  Halves of the values and of the lanes meet.
 __device__ __forceinline__ float sums16(float (&v)[16], uint32_t m) {

@@ -101,12 +101,12 @@ __device__ __forceinline__ float wave_sum(float x) {
   auto lane = [&](int i) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(y, i)); };
   return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
-// Sums of a row's lanes, two at once: of 16 lanes, of a wave, or of the workgroup's four in their order.
+// Sums of a row's lanes, two at once: of 4 or 16 lanes, of a wave, or of the workgroup's four in their order.
 template <int LANES>
 __device__ __forceinline__ void row_sums(float* a, float* b, float (*lds)[2]) {
-  if (LANES == 16) {
-    *a = sum16(*a);
-    *b = sum16(*b);
+  if (LANES <= 16) {
+    *a = LANES == 4 ? sum4(*a) : sum16(*a);
+    *b = LANES == 4 ? sum4(*b) : sum16(*b);
     return;
   }
   *a = wave_sum(*a);
@@ -137,10 +137,10 @@ __device__ __forceinline__ void standardise(const HeldRow<T, LANES, N>& at, floa
 // Which of a workgroup's rows a thread has part in.
 template <int LANES>
 __device__ __forceinline__ uint32_t row_of_block() {
-  return LANES == 16 ? threadIdx.x >> 4 : LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  return LANES <= 16 ? threadIdx.x / LANES : LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
 }
 
-// LANES 16 or 64: 16 rows to a workgroup, or four.  Weights stay in registers from row to row.
+// LANES 4, 16 or 64: 64, 16 or four rows to a workgroup.  Weights stay in registers from row to row.
 template <typename T, int LANES, int N>
 __global__ __launch_bounds__(256) void k_layer_norm(BlockArgs a) {
   constexpr int ALL = N * Piece<T>::W, ROWS = 256 / LANES;
@@ -209,19 +209,19 @@ __global__ __launch_bounds__(256, 2) void k_layer_norm_back(BlockArgs a) {
   }
   // The waves' sums one after the other, lane by lane: element e of piece i of lane l at (i W + e) LANES + l, as k_norm_sums takes them.
   extern __shared__ float sums[];
-  if (LANES == 16)
+  if (LANES < 64)
 #pragma unroll
-    for (int i = 0; i < ALL; ++i) {   // (the wave's four rows)
-      dw[i] += __shfl_xor(dw[i], 16);
-      dw[i] += __shfl_xor(dw[i], 32);
-      db[i] += __shfl_xor(db[i], 16);
-      db[i] += __shfl_xor(db[i], 32);
-    }
+    for (int i = 0; i < ALL; ++i)
+#pragma unroll
+      for (int d = LANES; d < 64; d *= 2) {   // (the wave's rows)
+        dw[i] += __shfl_xor(dw[i], d);
+        db[i] += __shfl_xor(db[i], d);
+      }
   constexpr int TURNS = LANES == 256 ? 1 : 4;
   const uint32_t wave = TURNS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int turn = 0; turn < TURNS; ++turn) {
     if (turn) __syncthreads();
-    if (wave != (uint32_t)turn || (LANES == 16 && (threadIdx.x & 63) >= 16)) continue;
+    if (wave != (uint32_t)turn || (LANES < 64 && (threadIdx.x & 63) >= LANES)) continue;
     float* const to = (turn + 1 < TURNS ? sums : a.partial + (size_t)blockIdx.x * 2 * ALL * LANES) + lane;
 #pragma unroll
     for (int i = 0; i < ALL; ++i) {

@@ -9,13 +9,13 @@ namespace {
 
 uint64_t count_of(const BlockArgs& a) { return (uint64_t)a.B * a.L * a.H; }
 
-// Lanes and pieces of a row (pieces 0: any width).  A lane holds up to 32 elements.  Narrow rows take 16 lanes: of 64, a row of 16 leaves 62 idle, and
-// sums over two million rows are a fourth as many, four times as long.
+// Lanes and pieces of a row (pieces 0: any width).  A lane holds up to 32 elements.  Narrow rows take 4 or 16 lanes: of 64, a row of 16 would
+// leave 62 idle (two million of them 904 us, of 16 lanes 202), and sums over many rows would be fewer and longer.
 struct Shape { uint32_t lanes, pieces; };
 Shape shape_of(uint32_t dtype, uint32_t dim) {
   const uint32_t W = dtype == PER_SEQ_BF16 ? 8 : 4, most = 32 / W;   // pieces of a lane
   if (dim < W || dim > 256 * most * W) return Shape{256, 0};
-  const uint32_t lanes = dim <= 16 * 2 * W ? 16 : dim <= 64 * most * W ? 64 : 256;
+  const uint32_t lanes = dim <= 4 * 2 * W ? 4 : dim <= 16 * 2 * W ? 16 : dim <= 64 * most * W ? 64 : 256;
   uint32_t n = 1;
   while (lanes * n * W < dim) n *= 2;
   return Shape{lanes, n};
@@ -53,6 +53,7 @@ hipError_t norm_pieces(const BlockArgs& a, uint32_t n, bool back, hipStream_t s)
 template <typename T>
 hipError_t norm(uint32_t dtype, const BlockArgs& a, bool back, hipStream_t s) {
   const Shape shape = shape_of(dtype, a.dim);
+  if (shape.lanes == 4) return shape.pieces == 1 ? norm_as<T, 4, 1>(a, back, s) : norm_as<T, 4, 2>(a, back, s);
   if (shape.lanes == 16) return shape.pieces == 1 ? norm_as<T, 16, 1>(a, back, s) : norm_as<T, 16, 2>(a, back, s);
   if (shape.pieces) return shape.lanes == 64 ? norm_pieces<T, 64>(a, shape.pieces, back, s) : norm_pieces<T, 256>(a, shape.pieces, back, s);
   if (back) {
