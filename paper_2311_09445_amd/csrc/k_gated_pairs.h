@@ -103,20 +103,21 @@ __device__ __forceinline__ f32x4 mma_f32(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
+// LDS of a wave that takes a chunk.
+struct PairLds {
+  float a[32 * kPairRow], b[32 * kPairRow], beta[32];
+  double g[32];
+};
 template <typename T, int DK, bool BACK, bool FAST>
-__global__ __launch_bounds__(256, 2) void k_delta_pairs(DeltaPairs p) {
-  __shared__ __attribute__((aligned(16))) float lds_a[4][32 * kPairRow], lds_b[4][32 * kPairRow], lds_beta[4][32];
-  __shared__ double lds_g[4][32];
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  const uint32_t item = blockIdx.x * 4 + wave;
-  if (item >= p.items) return;
+__device__ __forceinline__ void pairs_of(const DeltaPairs& p, uint32_t item, uint32_t lane, PairLds* lds) {
+  const uint32_t m = lane & 15, g = lane >> 4;
   const uint32_t chunk = item % p.chunks, bh = item / p.chunks, h = bh % p.H, b = bh / p.H;
   const uint32_t valid = valid_tokens(p.lengths, b, p.L), first = chunk * kChunk;
   if (first >= valid) return;
   typename RecordOf<BACK>::type* const whole = static_cast<typename RecordOf<BACK>::type*>(p.records) + item;
   DeltaRecord* const record = reinterpret_cast<DeltaRecord*>(whole);
-  float *const A = lds_a[wave], *const B = lds_b[wave], *const beta = lds_beta[wave];
-  double* const G = lds_g[wave];
+  float *const A = lds->a, *const B = lds->b, *const beta = lds->beta;
+  double* const G = lds->g;
 
   // all that comes from memory, before anything is waited for
   EightOf<T> qx[DK / 32][2], kx[DK / 32][2];
@@ -262,4 +263,10 @@ __global__ __launch_bounds__(256, 2) void k_delta_pairs(DeltaPairs p) {
       put(whole->solve_t, j, a, c);
     }
   }
+}
+template <typename T, int DK, bool BACK, bool FAST>
+__global__ __launch_bounds__(256, 2) void k_delta_pairs(DeltaPairs p) {
+  __shared__ __attribute__((aligned(16))) PairLds lds[4];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = blockIdx.x * 4 + wave;
+  if (item < p.items) pairs_of<T, DK, BACK, FAST>(p, item, threadIdx.x & 63, &lds[wave]);
 }

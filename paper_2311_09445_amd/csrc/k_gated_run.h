@@ -30,6 +30,7 @@ struct DeltaRun {
   // kept for a gradient: the states before the chunks, Y, rows of out . dout
   bf16x8 *states, *lower;
   float *y, *along;
+  DeltaPairs pairs;              // for a workgroup that makes its records itself
 };
 
 // CARRYING: no outputs; what a segment adds to a state, and (in slices of their own) what it makes of one: its product with the state before it.
@@ -305,7 +306,9 @@ struct RunLds {
 template <typename T, DeltaMode MODE>
 constexpr int kPairParts = MODE == CARRYING ? 1 : sizeof(T) == 2 && MODE == FORWARD ? 2 : 3;
 
-template <typename T, int DK, DeltaMode MODE, bool DIRECT_ROWS>
+// OWN: a workgroup forms its chunks' records itself, a wave a chunk: one launch less where sequences have no more than four (64 stretches of up to 80
+// tokens of 4 heads of 64 x 64: 20.0 us and 17.6).  It has all columns then, so that nobody else needs them.
+template <typename T, int DK, DeltaMode MODE, bool DIRECT_ROWS, bool OWN = false>
 __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 64 ? 3 : 2) void k_delta_run(DeltaRun p) {
   constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = NP - 1;
   typedef RunLds<T, DK, NP, DIRECT_ROWS, MODE != CARRYING> Lds;
@@ -324,6 +327,15 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
   const uint8_t* const records = static_cast<const uint8_t*>(p.records) + (size_t)bh * p.chunks * p.record_bytes;
   const bool pieces = p.q.near && p.k.near && dk >= 16 / sizeof(T);
   auto record = [&](uint32_t c) { return reinterpret_cast<const DeltaRecord*>(records + (size_t)c * p.record_bytes); };
+  if constexpr (OWN) {
+    const bool fast = DIRECT_ROWS || (p.q.wide && p.k.wide && dk % (16 / sizeof(T)) == 0);
+    PairLds* const own_lds = reinterpret_cast<PairLds*>(lds_raw) + wave;
+    for (uint32_t c = wave; c < chunks; c += 4) {
+      if (fast) pairs_of<T, DK, MODE == KEEPING, true>(p.pairs, bh * p.chunks + c, lane, own_lds);
+      else pairs_of<T, DK, MODE == KEEPING, false>(p.pairs, bh * p.chunks + c, lane, own_lds);
+    }
+    arrive<0>();   // (what the waves have stored is in L2, from where it is read)
+  }
 
   f32x4 s[TX];
 #pragma unroll

@@ -124,16 +124,17 @@ hipError_t launch(void (*kernel)(Args), std::atomic<uint64_t>* granted, uint32_t
   return hipGetLastError();
 }
 // In bfloat16 straight into LDS where rows are made up of pieces of 16 bytes.
-template <typename T, int DK, DeltaMode MODE>
+template <typename T, int DK, DeltaMode MODE, bool OWN = false>
 hipError_t launch_run(const DeltaRun& p, uint32_t bh, hipStream_t s) {
   static std::atomic<uint64_t> granted[2] = {};
   constexpr int NP = kPairParts<T, MODE>;
   const uint32_t grid = bh * p.run * (p.slices + (MODE == CARRYING ? (p.dk + 63) / 64 : 0));
+  auto lds = [](uint32_t bytes) { return OWN && bytes < 4 * sizeof(PairLds) ? (uint32_t)(4 * sizeof(PairLds)) : bytes; };
   if constexpr (sizeof(T) == 2) {
     if (p.q.wide && p.k.wide && p.v.wide && p.dk % 8 == 0 && p.dv % 8 == 0)
-      return launch(k_delta_run<T, DK, MODE, true>, &granted[1], grid, RunLds<T, DK, NP, true, MODE != CARRYING>::BYTES, p, s);
+      return launch(k_delta_run<T, DK, MODE, true, OWN>, &granted[1], grid, lds(RunLds<T, DK, NP, true, MODE != CARRYING>::BYTES), p, s);
   }
-  return launch(k_delta_run<T, DK, MODE, false>, &granted[0], grid, RunLds<T, DK, NP, false, MODE != CARRYING>::BYTES, p, s);
+  return launch(k_delta_run<T, DK, MODE, false, OWN>, &granted[0], grid, lds(RunLds<T, DK, NP, false, MODE != CARRYING>::BYTES), p, s);
 }
 template <typename T, int DK, bool CARRY>
 hipError_t launch_back(const DeltaBack& p, uint32_t bh, hipStream_t s) {
@@ -150,14 +151,16 @@ hipError_t launch_grads(const DeltaGrads& p, uint32_t bh, hipStream_t s) {
   static std::atomic<uint64_t> granted{0};
   return launch(k_delta_grads<T, DK>, &granted, bh * p.chunks, grads_lds<T, DK>(), p, s);
 }
+DeltaPairs make_pairs(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, void* records) {
+  return DeltaPairs{rows(q, a.dtype, a.H / a.Q), rows(k, a.dtype, a.H / a.K), gates(a.log_decay), gates(a.beta), a.lengths, records,
+                    a.L, a.H, a.dk, chunks_of(a.L), a.B * a.H * chunks_of(a.L), a.scale};
+}
 template <typename T, int DK, bool BACK>
 hipError_t launch_pairs(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, void* records, hipStream_t s) {
-  const uint32_t items = a.B * a.H * chunks_of(a.L);
-  if (!items) return hipSuccess;
-  const DeltaPairs p{rows(q, a.dtype, a.H / a.Q), rows(k, a.dtype, a.H / a.K), gates(a.log_decay), gates(a.beta), a.lengths, records,
-                     a.L, a.H, a.dk, chunks_of(a.L), items, a.scale};
-  if (p.q.wide && p.k.wide && p.dk % (16 / sizeof(T)) == 0) k_delta_pairs<T, DK, BACK, true><<<(items + 3) / 4, 256, 0, s>>>(p);
-  else k_delta_pairs<T, DK, BACK, false><<<(items + 3) / 4, 256, 0, s>>>(p);
+  const DeltaPairs p = make_pairs(a, q, k, records);
+  if (!p.items) return hipSuccess;
+  if (p.q.wide && p.k.wide && p.dk % (16 / sizeof(T)) == 0) k_delta_pairs<T, DK, BACK, true><<<(p.items + 3) / 4, 256, 0, s>>>(p);
+  else k_delta_pairs<T, DK, BACK, false><<<(p.items + 3) / 4, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -208,17 +211,27 @@ hipError_t launch_carry(DeltaRun* p, const DeltaSizes& a, const Cut& c, const pe
   return e;
 }
 
+// Whether the workgroups over the sequences form their chunks' records themselves (of a gradient, whose records are twice as much work, only where the
+// chip is not full: 500 x 100 tokens of 8 heads 747 us and 769).
+bool makes_own(const DeltaSizes& a, const Cut& c, bool backward) {
+  return a.L && chunks_of(a.L) <= 4 && c.segments == 1 && a.dv <= 64 && !(backward && (uint64_t)a.B * a.H > 1024);
+}
+
 template <typename T, int DK>
 hipError_t forward(const DeltaSizes& a, const per_seq_rows& q, const per_seq_rows& k, const per_seq_rows& v, const per_seq_states* state,
                    const per_seq_rows& out, const per_seq_states* out_state, void* work, hipStream_t s) {
-  hipError_t e = launch_pairs<T, DK, false>(a, q, k, work, s);
-  if (e != hipSuccess) return e;
   DeltaRun p = make_run(a, q, k, v, state, work, sizeof(DeltaRecord));
-  e = launch_carry<T, DK>(&p, a, cut(a, false), state, reinterpret_cast<float*>(static_cast<uint8_t*>(work) + record_bytes(a)), false, s);
+  const Cut c = cut(a, false);
+  const bool own = makes_own(a, c, false);
+  hipError_t e = own ? hipSuccess : launch_pairs<T, DK, false>(a, q, k, work, s);
+  if (e != hipSuccess) return e;
+  e = launch_carry<T, DK>(&p, a, c, state, reinterpret_cast<float*>(static_cast<uint8_t*>(work) + record_bytes(a)), false, s);
   if (e != hipSuccess) return e;
   p.out = rows(out, a.dtype, 1);
   if (out_state) { p.to = out_state->d; p.to_batch = out_state->batch; p.to_head = out_state->head; }
-  return launch_run<T, DK, FORWARD>(p, a.B * a.H, s);
+  if (!own) return launch_run<T, DK, FORWARD>(p, a.B * a.H, s);
+  p.pairs = make_pairs(a, q, k, work);
+  return launch_run<T, DK, FORWARD, true>(p, a.B * a.H, s);
 }
 
 DeltaFold fold(const DeltaSizes& a, const float* from, const per_seq_rows& to, uint32_t n, uint32_t width, uint32_t stride) {
@@ -239,7 +252,9 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   uint8_t* const at = static_cast<uint8_t*>(work);
   auto floats = [&](size_t o) { return reinterpret_cast<float*>(at + o); };
   const uint32_t bh = a.B * a.H;
-  hipError_t e = launch_pairs<T, DK, true>(a, q, k, at + w.records, s);
+  const Cut c = cut(a, true);
+  const bool own = makes_own(a, c, true);
+  hipError_t e = own ? hipSuccess : launch_pairs<T, DK, true>(a, q, k, at + w.records, s);
   if (e != hipSuccess) return e;
   DeltaRun run = make_run(a, q, k, v, state, at + w.records, sizeof(DeltaRecordBack));
   run.dout = rows(dout, a.dtype, 1);
@@ -247,9 +262,9 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   run.lower = reinterpret_cast<bf16x8*>(at + w.lower);
   run.y = floats(w.y);
   run.along = floats(w.read);
-  const Cut c = cut(a, true);
   e = launch_carry<T, DK>(&run, a, c, state, floats(w.carried), true, s);
-  if (e == hipSuccess && run.chunks) e = launch_run<T, DK, KEEPING>(run, bh, s);
+  if (own) run.pairs = make_pairs(a, q, k, at + w.records);
+  if (e == hipSuccess && run.chunks) e = own ? launch_run<T, DK, KEEPING, true>(run, bh, s) : launch_run<T, DK, KEEPING>(run, bh, s);
   if (e != hipSuccess) return e;
   DeltaBack b{};
   b.q = run.q;
