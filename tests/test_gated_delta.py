@@ -101,7 +101,7 @@ def check_grads(got, want, T, d, dtype, more=1.0):
 
 SHAPES = [(1, 1, 1, 1, 1, 1, 1, 1), (2, 31, 2, 2, 2, 2, 64, 64), (2, 32, 2, 1, 1, 2, 64, 64), (3, 33, 4, 4, 2, 2, 32, 16), (2, 65, 2, 2, 2, 1, 128, 128),
           (1, 100, 6, 6, 2, 2, 48, 80), (2, 97, 4, 2, 2, 4, 17, 5), (5, 64, 3, 3, 3, 3, 128, 40), (2, 130, 6, 2, 3, 1, 61, 127), (1, 257, 2, 2, 2, 2, 65, 33),
-          (4, 40, 2, 2, 2, 2, 3, 128)]
+          (4, 40, 2, 2, 2, 2, 3, 128), (600, 40, 2, 2, 1, 2, 16, 16)]
 
 
 @TYPES
@@ -498,6 +498,41 @@ def test_on_a_stream_of_its_own():
         got = call()
     s.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@TYPES
+def test_calls_at_once(dtype):
+    """Calls on two streams share nothing, and neither do graphs captured one after the other and replayed in turn."""
+    sets = [inputs(2, L, 2, 2, 1, 2, 128, 64, dtype, seed=10 * L, ragged=True) for L in (300, 70)]
+    douts = [normal(21 + i, *s[2].shape, dtype=dtype) for i, s in enumerate(sets)]
+
+    def call(i):
+        q, k, v, g, beta, S, lengths = sets[i]
+        return [*seq.gated_delta(q, k, v, g, beta, S, lengths), *seq.gated_delta_backward(douts[i], q, k, v, g, beta, S, S, lengths)]
+
+    want = [call(0), call(1)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = call(i)
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert all(torch.equal(p, q) for p, q in zip(x, y))
+    graphs, kept = [], []
+    for i in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            kept.append(call(i))
+        graphs.append(graph)
+    for _ in range(3):
+        for graph in graphs:
+            graph.replay()
+        call(0)
+        torch.cuda.synchronize()
+        for x, y in zip(kept, want):
+            assert all(torch.equal(p, q) for p, q in zip(x, y))
 
 
 def test_a_block_in_a_graph():
