@@ -7,15 +7,19 @@
 //   dQ = scale e^G dO S^T + dM K,   dK = -e^G dZ S^T + left U R^T + dM^T Q + (dN + dN^T) K,
 //   dM = scale e_ij dO U^T (i >= j),   dN = -e_ij dZ U^T (i > j).
 //
-// What bounds them, in bfloat16: k_delta_back by itself takes 3.75 us for a chunk of 128 x 128, 3.1 of 64 x 64; with a workgroup on each compute unit
-// 4.6 (2 x 8192 tokens of 16 heads in segments 294 us, at 1.9 TB/s with what it leaves for k_delta_grads); that takes 334 us for 1.1 GB, waiting
-// for memory with two workgroups to a compute unit (three would spill: 710).
+// What bounds them, in bfloat16: k_delta_back, which asks for everything a chunk ahead, takes 3.5 us for a chunk of 64 x 64 (32 sequences of 512 tokens of 8
+// heads 56 us) and, with a workgroup on each compute unit, 5.4 of 128 x 128 (2 x 8192 tokens of 16 heads in segments 348 us for 1.0 GB);
+// k_delta_grads takes 345 us for 1.1 GB of the latter, waiting for memory with two workgroups to a compute unit (three would spill: 710).
 //
-// The gradient of a decay's logarithm is that of the state before the token times the state itself.  At the first token of every kBorder-th chunk that is taken as
-// <R, S>; from one token to the next it falls by out . dO - dZ . V, which is added up over kBorder chunks at most.
+// The gradient of a decay's logarithm is the sum of all that goes past its token t, each term with the decays between as a factor.  Of a chunk that is
+//   sum (i >= t > j) dM_ij q_i.k_j + dN_ij k_i.k_j   (what tokens of the chunk read of each other's writes; k_delta_grads)
+//   + sum (i >= t) scale e^G_i dO_i . S^T q_i - dZ_i . e^G_i S^T k_i   (what they read of the state before the chunk; rows of both passes)
+//   + sum (j < t) left_j u_j . R^T k_j   (what they write to the state behind it)   + e^Gn <R, S>   (what stays).
+// So what a fast decay leaves is exact to 2^-24 of itself.  (As a border's <R, S> less a sum of out . dO - dZ . V over the tokens before t, it was what is
+// left of large numbers: noise of 2^-24 of theirs, also behind a decay that keeps nothing.)
 
 struct DeltaBack {
-  SeqRows q, k, v, dout;
+  SeqRows q, k, dout;
   const void* records;
   const int32_t* lengths;
   const float* in;
@@ -25,10 +29,10 @@ struct DeltaBack {
   uint32_t first_segment, run;   // the segments that are taken
   float scale;
   float* carried;                // [sequence, head][segment][dk][dv]: what a segment adds to the gradient of the state before it
-  const bf16x8 *states, *lower;
-  const float* y;
+  const bf16x8* states;
+  const float *y, *x;
   bf16x8* dstates;                 // the gradients of the states behind the chunks
-  float *dz, *along, *strength, *border;
+  float *dz, *along, *strength, *write, *stay;   // along: rows of dZ . what keys read; write: of left u . R^T k; stay: 32 terms of e^Gn <R, S>
 };
 
 template <typename T>
@@ -36,14 +40,16 @@ constexpr int kGradParts = sizeof(T) == 2 ? 1 : 3;   // of states in the product
 
 template <typename T, int DK, bool DIRECT_ROWS>
 struct BackLds {
-  static constexpr uint32_t Q = 0, K = kParts<T> * Tile<DK>::SIZE, V = 2 * K, D = V + (DIRECT_ROWS ? Tile<64>::SIZE : 0),
+  static constexpr uint32_t Q = 0, K = kParts<T> * Tile<DK>::SIZE, D = 2 * K,
                             SOLVE = D + (DIRECT_ROWS ? Tile<64>::SIZE : 0), SIZE = SOLVE + (DIRECT_ROWS ? 3 * 1024 : 0), BYTES = 2 * SIZE * sizeof(bf16);
 };
 
-// CARRY: only what a segment adds.
+// CARRY: only what a segment adds; two workgroups to a compute unit where rows go straight to LDS.  The whole pass has one: with two, registers for 64 x 64
+// spill (32 ragged sequences of 512 tokens of 8 heads, the whole gradient, 204 us and 254; 128 of them 951 and 1084).
 template <typename T, int DK, bool CARRY, bool DIRECT_ROWS>
-__global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) void k_delta_back(DeltaBack p) {
+__global__ __launch_bounds__(256, DIRECT_ROWS && CARRY ? 2 : 1) void k_delta_back(DeltaBack p) {
   constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, TURN = PT == 1 ? TX : 4;
+  constexpr bool AHEAD = DIRECT_ROWS && !CARRY;   // the state before a chunk is asked for a chunk ahead too
   typedef BackLds<T, DK, DIRECT_ROWS> Lds;
   static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
@@ -66,31 +72,41 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
       const uint32_t row = state_row(a, 4 * g + r);
       s[a][r] = !CARRY && p.in && on && row < dk ? p.in[(int64_t)b * p.in_batch + (int64_t)h * p.in_head + seg * p.in_segment + (size_t)row * dv + col] : 0.0f;
     }
-  const T *const q0 = row_of<T>(p.q, b, 0, h), *const k0 = row_of<T>(p.k, b, 0, h), *const v0 = row_of<T>(p.v, b, 0, h), *const d0 = row_of<T>(p.dout, b, 0, h);
+  const T *const q0 = row_of<T>(p.q, b, 0, h), *const k0 = row_of<T>(p.k, b, 0, h), *const d0 = row_of<T>(p.dout, b, 0, h);
   TwoRows<T, DK> rows;
   DirectRows<DK> direct_q, direct_k;
-  DirectRows<64> direct_v, direct_d;
-  Walk walk_q, walk_k, walk_v, walk_d;
+  DirectRows<64> direct_d;
+  Walk walk_q, walk_k, walk_d;
   struct Next {
     bf16x8 pairs[3][2], solve[3][2];
-    f32x4 y[2];
-    Column<T> v, d;
+    f32x4 y[2], x[2];
+    bf16x8 before[KX][kStateParts<T>];   // the state before the chunk
+    Column<T> d;
   } next, now;
   RecordNumbers num, next_num;
   const uint32_t lds0 = lds_address(lds);
+  auto ask_state = [&](uint32_t c, Next& to) {
+    if (CARRY || !works) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) to.x[i][r] = p.x[(row0 + c * kChunk + 16 * i + 4 * g + r) * width + col];
+#pragma unroll
+    for (int k = 0; k < KX; ++k)
+#pragma unroll
+      for (int t = 0; t < kStateParts<T>; ++t) to.before[k][t] = p.states[state_at<DK>(bh, p.chunks, c, blocks, kStateParts<T>, t, col0 / 16) + k * 64 + lane];
+  };
   auto fetch = [&](uint32_t c) {
     const DeltaRecordBack* const record = records + c;
     if constexpr (DIRECT_ROWS) {
       const uint32_t n = valid - c * kChunk, to = lds0 + (c & 1) * Lds::SIZE * 2;
       direct_q.ask(to + Lds::Q * 2, walk_q.next(), wave, n);
       direct_k.ask(to + Lds::K * 2, walk_k.next(), wave, n);
-      if (!CARRY) direct_v.ask(to + Lds::V * 2, walk_v.next(), wave, n);
       direct_d.ask(to + Lds::D * 2, walk_d.next(), wave, n);
       ask_rows<6>(to + Lds::SOLVE * 2, record->solve_t, wave, lane);
     } else {
       rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
       if (c > chunk0) rows.load(p.q, p.k, q0, k0, (c - 1) * kChunk, valid, dk, pieces);
-      if (!CARRY) next.v.ask(p.v, v0, c * kChunk, valid, on, col, g);
       next.d.ask(p.dout, d0, c * kChunk, valid, on, col, g);
 #pragma unroll
       for (int t = 0; t < 3; ++t)
@@ -100,29 +116,27 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
 #pragma unroll
     for (int t = 0; t < 3; ++t)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) next.pairs[t][i] = record->pairs_t[t][i][lane];
+      for (int i = 0; i < 2; ++i) next.pairs[t][i] = record->of.pairs[t][i][lane];
     if (!CARRY && works)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) next.y[i][r] = p.y[(row0 + c * kChunk + 16 * i + 4 * g + r) * width + col];
+    if (AHEAD) ask_state(c, next);
     next_num.load(&record->of, m, g);
   };
   if constexpr (DIRECT_ROWS) {
     const uint32_t last = chunks > chunk0 ? chunks - 1 : chunk0;
     walk_q.set(p.q, q0, last, true);
     walk_k.set(p.k, k0, last, true);
-    walk_v.set(p.v, v0 + 64 * slice, last, true);
     walk_d.set(p.dout, d0 + 64 * slice, last, true);
     direct_q.set(p.q, dk, wave, lane);
     direct_k.set(p.k, dk, wave, lane);
-    direct_v.set(p.v, dv - 64 * slice, wave, lane);
     direct_d.set(p.dout, dv - 64 * slice, wave, lane);
     if (dk < DK || dv - 64 * slice < 64) {
       for (uint32_t i = 0; i < 2; ++i) {
         DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::Q, 0, threadIdx.x);
         DirectRows<DK>::clear(lds + i * Lds::SIZE + Lds::K, 0, threadIdx.x);
-        DirectRows<64>::clear(lds + i * Lds::SIZE + Lds::V, 0, threadIdx.x);
         DirectRows<64>::clear(lds + i * Lds::SIZE + Lds::D, 0, threadIdx.x);
       }
       __syncthreads();
@@ -132,15 +146,16 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
   }
   if (chunk0 < chunks) fetch(chunks - 1);
   f32x4 dz[2] = {};
-  float sums = 0.0f, border = 0.0f;
+  float sums = 0.0f, more = 0.0f;
   auto flush = [&](uint32_t c) {   // (behind the next barrier, as over time)
     if (CARRY || !works) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) p.dz[(row0 + c * kChunk + 16 * i + 4 * g + r) * width + col] = dz[i][r];
-    (m & 8 ? p.strength : p.along)[part0 * kChunk + c * kChunk + 4 * (m & 4) + 4 * g + (m & 3)] = sums;
-    if (lane == 0) p.border[part0 + c] = border;
+    const size_t at = part0 * kChunk + c * kChunk + 4 * (m & 4) + 4 * g + (m & 3);
+    (m & 8 ? p.strength : p.along)[at] = sums;
+    (m & 8 ? p.stay : p.write)[at] = more;
   };
   for (uint32_t end = chunks; end > chunk0; --end) {
     const uint32_t c = end - 1, first = c * kChunk;
@@ -152,7 +167,6 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
       if (valid - first < kChunk) {
         DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
         DirectRows<DK>::clear(K, valid - first, threadIdx.x);
-        DirectRows<64>::clear(buffer + Lds::V, valid - first, threadIdx.x);
         DirectRows<64>::clear(buffer + Lds::D, valid - first, threadIdx.x);
         __syncthreads();
       }
@@ -163,23 +177,19 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       if (!CARRY) asm volatile("" : "+v"(next.y[i]));
+      if (AHEAD) asm volatile("" : "+v"(next.x[i]));
 #pragma unroll
       for (int t = 0; t < 3; ++t) asm volatile("" : "+v"(next.pairs[t][i]));
     }
     num = next_num;
-    now = next;
-    // (before a chunk at a border: the state's two halves, or its parts)
-    constexpr int HALVES = sizeof(T) == 2 ? 2 : 3;
-    const bool bordered = !CARRY && c % kBorder == 0;
-    bf16x8 before[KX][HALVES];
-    if (bordered && works) {
+    if constexpr (AHEAD) {
 #pragma unroll
       for (int k = 0; k < KX; ++k)
 #pragma unroll
-        for (int t = 0; t < HALVES; ++t)
-          before[k][t] = sizeof(T) == 2 && t == 1 ? p.lower[state_at<DK>(bh, (p.chunks + kBorder - 1) / kBorder, c / kBorder, blocks, 1, 0, col0 / 16) + k * 64 + lane]
-                                                  : p.states[state_at<DK>(bh, p.chunks, c, blocks, kStateParts<T>, t, col0 / 16) + k * 64 + lane];
+        for (int t = 0; t < kStateParts<T>; ++t) asm volatile("" : "+v"(next.before[k][t]));
     }
+    now = next;
+    if (!AHEAD) ask_state(c, now);
     if (c > chunk0) fetch(c - 1);
     if (end < chunks) flush(c + 1);
     if (!CARRY && works) {
@@ -200,7 +210,7 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
         const Parts<3> sp[2] = {Parts<3>::of(s[2 * k], s[2 * k + 1]), Parts<3>::of(s[2 * k + 2], s[2 * k + 3])};
         mma_turns<4, 2, PT, 3>([&](int j) -> const bf16x8 (&)[PT] { return rows_k[j].v; }, [&](int j) -> const bf16x8 (&)[3] { return sp[j / 2].v; }, w4);
       }
-      f32x4 v[2], d[2];
+      f32x4 d[2];
       bf16x8 solve[2][3], pairs[2][3];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -212,15 +222,40 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
       if constexpr (DIRECT_ROWS) {
         auto column = [&](uint32_t i) { return 16 * wave + i; };
         Operand<bf16>::across<64>(buffer + Lds::D, column, m, g).widen(&d[0], &d[1]);
-        if (!CARRY) Operand<bf16>::across<64>(buffer + Lds::V, column, m, g).widen(&v[0], &v[1]);
       } else {
         now.d.widen(first, valid, on, g, d);
-        if (!CARRY) now.v.widen(first, valid, on, g, v);
       }
       const Operand<T> dp = operand_of<T>(d);
       f32x4 w[2], du[2] = {};
 #pragma unroll
       for (int i = 0; i < 2; ++i) w[i] = num.left[i] * (w4[i] + w4[i + 2]);
+      if constexpr (!CARRY) {
+        float products[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          products[i] = w[i / 4][i % 4] * (num.beta[i / 4][i % 4] * now.y[i / 4][i % 4]);
+          products[i + 8] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < KX; ++k) {
+          f32x4 S[2] = {};
+          if constexpr (sizeof(T) == 2) {
+            of_halves(now.before[k], &S[0], &S[1]);
+          } else {
+#pragma unroll
+            for (int t = 2; t >= 0; --t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                S[0][e] += (float)now.before[k][t][e];
+                S[1][e] += (float)now.before[k][t][e + 4];
+              }
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) products[i + 8] = fmaf(S[i / 4][i % 4], s[2 * k + i / 4][i % 4], products[i + 8]);
+        }
+        more = sums16(products, m);
+        if (m & 8) more = fmaf(more, num.kept[0], more * num.kept[1]);
+      }
       mma_turns<2, 2, 3, PT>([&](int i) -> const bf16x8 (&)[3] { return pairs[i]; }, [&](int) -> const bf16x8 (&)[PT] { return dp.v; }, w);
       const Parts<3> wp = Parts<3>::of(w[0], w[1]);
       mma_turns<2, 2, 3, 3>([&](int i) -> const bf16x8 (&)[3] { return solve[i]; }, [&](int) -> const bf16x8 (&)[3] { return wp.v; }, du);
@@ -247,33 +282,10 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && (CARRY || DK == 64) ? 2 : 1) vo
         float products[16];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          products[i] = dz[i / 4][i % 4] * v[i / 4][i % 4];
+          products[i] = dz[i / 4][i % 4] * now.x[i / 4][i % 4];
           products[i + 8] = now.y[i / 4][i % 4] * du[i / 4][i % 4];
         }
         sums = sums16(products, m);
-        border = 0.0f;
-        if (bordered) {
-#pragma unroll
-          for (int k = 0; k < KX; ++k) {
-            f32x4 x[2] = {};
-            if constexpr (sizeof(T) == 2) {
-              of_halves(before[k], &x[0], &x[1]);
-            } else {
-#pragma unroll
-              for (int t = 2; t >= 0; --t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  x[0][e] += (float)before[k][t][e];
-                  x[1][e] += (float)before[k][t][e + 4];
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) border = fmaf(x[0][e], s[2 * k][e], fmaf(x[1][e], s[2 * k + 1][e], border));
-          }
-          border = sum16(border);
-          border += __shfl_xor(border, 16);
-          border += __shfl_xor(border, 32);
-        }
       }
     }
   }
@@ -300,12 +312,13 @@ struct DeltaGrads {
   float *fold_q, *fold_k;
   const bf16x8 *states, *dstates;
   const float *y, *dz;
+  float* past;   // [sequence and head][token]: what goes past it within its chunk
 };
 struct DeltaGates {
   Gates dlog_decay, dbeta;
   const int32_t* lengths;
   uint32_t rows, L, H, chunks, parts;   // rows: sequences and heads; parts: slices of 16 columns, which sums come in
-  const float *read, *along, *strength, *border;   // read, along: rows of out . dout, of dZ . V
+  const float *read, *along, *strength, *write, *stay, *past;
 };
 // Eight neighbours of a row.
 template <typename T>
@@ -326,7 +339,7 @@ __device__ __forceinline__ void store_eight(T* row, bool wide, uint32_t col, uin
 }
 
 template <typename T, int DK>
-constexpr uint32_t grads_lds() { return (2 * kParts<T> + 2 * kGradParts<T>) * Tile<DK>::SIZE * sizeof(bf16) + 2 * 32 * kPairRow * sizeof(float); }
+constexpr uint32_t grads_lds() { return (2 * kParts<T> + 2 * kGradParts<T>) * Tile<DK>::SIZE * sizeof(bf16) + 3 * 32 * kPairRow * sizeof(float); }
 
 // A workgroup takes a chunk; its waves share the chunk's columns of dk, and the four 16 x 16 tiles of its pairs.  Everything that comes from memory is
 // asked for before anything is waited for.  Columns of dv go to LDS mixed, column 8 g + 4 s + e of a block to row 16 s + 4 g + e, and so are rows of
@@ -341,6 +354,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_
   bf16* const R = S + PS * Tile<DK>::SIZE;
   float* const dM = reinterpret_cast<float*>(R + PS * Tile<DK>::SIZE);
   float* const dN = dM + 32 * kPairRow;
+  float* const pasts = dN + 32 * kPairRow;
   __shared__ double G[32];
   __shared__ __attribute__((aligned(16))) float gamma[32], left[32], beta[32];
   const uint32_t chunk = blockIdx.x % p.chunks, bh = blockIdx.x / p.chunks, h = bh % p.H, b = bh / p.H;
@@ -420,27 +434,27 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_
       }
     __syncthreads();
     Operand<T> d[2];
-    Parts<PU> z[2], u[2];
+    Parts<3> z[2], u[2];   // (whole for the pairs, which the gradients of decays are made of too; rows take PU of them)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t t = 16 * i + m;
       d[i] = Operand<T>::of(four_of<T>(next_d[i][0], t < n, 32 * block + 8 * g, dv), four_of<T>(next_d[i][1], t < n, 32 * block + 8 * g + 4, dv));
-      z[i] = Parts<PU>::of(next_z[i][0], next_z[i][1]);
-      u[i] = Parts<PU>::of(beta[t] * next_y[i][0], beta[t] * next_y[i][1]);
+      z[i] = Parts<3>::of(next_z[i][0], next_z[i][1]);
+      u[i] = Parts<3>::of(beta[t] * next_y[i][0], beta[t] * next_y[i][1]);
       if (p.direct_v && wave == (block & 3) && t < end) {
         T* const to = row_to<T>(p.dvr, b, first + t, h);
         store_eight<T>(to, p.dvr.wide, 32 * block + 8 * g, dv, t < n ? next_z[i][0] : zero, t < n ? next_z[i][1] : zero);
       }
     }
-    if (block + 1 < blocks) ask(block + 1);
     // (branches: operands that are chosen by a number would lie in memory)
     auto pair = [&](int i, int j) {
-      dm = mma<LESS>(d[i].v, u[j].v, dm);
-      dn = mma<LESS>(z[i].v, u[j].v, dn);
+      dm = mma(d[i].v, u[j].v, dm);
+      dn = mma(z[i].v, u[j].v, dn);
     };
     if (wave == 0) pair(0, 0);
     else if (wave == 2) pair(1, 0);
     else if (wave == 3) pair(1, 1);
+    if (block + 1 < blocks) ask(block + 1);
 #pragma unroll
     for (int a = 0; a < NC; ++a) {
       bf16x8 s[PS], r[PS];
@@ -457,14 +471,43 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_
       }
     }
   }
+  f32x4 qk = zero, kk = zero;
+#pragma unroll
+  for (int s = 0; s < DK / 32; ++s) {
+    const Operand<T> k = Operand<T>::template along<DK>(K, 16 * tj + m, s, g);
+    qk = mma(Operand<T>::template along<DK>(Q, 16 * ti + m, s, g).v, k.v, qk);
+    kk = mma(Operand<T>::template along<DK>(K, 16 * ti + m, s, g).v, k.v, kk);
+  }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const uint32_t i = 16 * ti + 4 * g + e, j = 16 * tj + m;
-    const float x = expf((float)(G[i] - G[j]));
-    dM[i * kPairRow + j] = i >= j ? p.scale * x * dm[e] : 0.0f;
-    dN[i * kPairRow + j] = i > j ? -x * dn[e] : 0.0f;
+    const float x = expf((float)(G[i] - G[j])), by_q = i >= j ? p.scale * x * dm[e] : 0.0f, by_k = i > j ? -x * dn[e] : 0.0f;
+    dM[i * kPairRow + j] = by_q;
+    dN[i * kPairRow + j] = by_k;
+    pasts[i * kPairRow + j] = i > j ? fmaf(by_q, qk[e], by_k * kk[e]) : 0.0f;
   }
   __syncthreads();
+  if (wave == 1) {   // (which has no pairs) the sums of rows i >= t, columns j < t: up each column, then along each row, 16 to a half of the wave
+    const uint32_t at = lane & 31, half = lane & 32 ? 0 : 16;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = pasts[(half + i) * kPairRow + at];
+#pragma unroll
+    for (int i = 14; i >= 0; --i) x[i] += x[i + 1];
+    const float upper = __shfl(x[0], at), below = half ? 0.0f : upper;   // (of rows 16 .. 31)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) pasts[(half + i) * kPairRow + at] = x[i] + below;
+    wave_sync();
+    float sum = 0.0f;
+#pragma unroll
+    for (uint32_t j = 0; j < 16; j += 4) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(pasts + at * kPairRow + half + j);
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) sum += half + j + e < at ? v[e] : 0.0f;
+    }
+    sum += __shfl_xor(sum, 32);
+    if (lane < 32) p.past[row0 + at] = sum;
+  }
   Operand<T> qs[NC], ks[NC];
 #pragma unroll
   for (int a = 0; a < NC; ++a) {
@@ -510,45 +553,44 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_
   }
 }
 
-// The gates' gradients: a thread takes a token, half a workgroup the kBorder chunks behind a border.  The decays' falls from token to token by
-// what is read along dout less what is written along V.
+// The gates' gradients: a thread takes a token, 32 of them a chunk.
 __device__ __forceinline__ void gates_of(const DeltaGates& p, uint32_t block) {
-  static_assert(kBorder * kChunk == 128, "two waves");
-  __shared__ float upto[2];
-  const uint32_t half = threadIdx.x >> 7, at_half = threadIdx.x & 127, groups = (p.chunks + kBorder - 1) / kBorder, all = p.rows * groups;
-  const uint32_t item = 2 * block + half < all ? 2 * block + half : all - 1, group = item % groups, bh = item / groups, h = bh % p.H, b = bh / p.H;
-  const uint32_t t = group * kBorder * kChunk + at_half, valid = valid_tokens(p.lengths, b, p.L), tokens = p.chunks * kChunk;
-  float strengths[8], falls[8], borders[8];
-  const uint32_t from = t < valid ? t : 0;
+  const uint32_t at = threadIdx.x & 31, all = p.rows * p.chunks, place = block * (256 / kChunk) + threadIdx.x / kChunk;
+  const uint32_t item = place < all ? place : all - 1, chunk = item % p.chunks, bh = item / p.chunks, h = bh % p.H, b = bh / p.H;
+  const uint32_t t = chunk * kChunk + at, valid = valid_tokens(p.lengths, b, p.L), tokens = p.chunks * kChunk;
+  float strengths[8], reads[8], writes[8], stays[8];
 #pragma unroll
   for (uint32_t i = 0; i < 8; ++i) {   // (all at once: a loop that adds as it loads takes a memory's latency for each)
-    const size_t at = (size_t)bh * p.parts + (i < p.parts ? i : p.parts - 1);
-    strengths[i] = p.strength[at * tokens + from];
-    falls[i] = p.read[at * tokens + from] - p.along[at * tokens + from];
-    borders[i] = p.border[at * p.chunks + group * kBorder];
+    const size_t part = (size_t)bh * p.parts + (i < p.parts ? i : p.parts - 1);
+    strengths[i] = p.strength[part * tokens + t];
+    reads[i] = p.read[part * tokens + t] - p.along[part * tokens + t];
+    writes[i] = p.write[part * tokens + t];
+    stays[i] = p.stay[part * tokens + t];
   }
-  float strength = 0.0f, fall = 0.0f, border = 0.0f;
+  const float past = p.past[(size_t)bh * tokens + t];
+  float strength = 0.0f, read = 0.0f, write = 0.0f, stay = 0.0f;
 #pragma unroll
   for (uint32_t i = 0; i < 8; ++i) {
     if (i >= p.parts) break;
     strength += strengths[i];
-    fall += falls[i];
-    border += borders[i];
+    read += reads[i];
+    write += writes[i];
+    stay += stays[i];
   }
-  if (t >= valid) fall = 0.0f;
-  float sum = fall;
+  // (a chunk is written whole or, behind the sequence's end, not at all)
+  float written = __shfl_up(write, 1, 32);   // of the tokens before
+  if (at == 0) written = 0.0f;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const float x = __shfl_up(sum, d);
-    if ((threadIdx.x & 63) >= (uint32_t)d) sum += x;
+  for (int d = 1; d < 32; d *= 2) {
+    const float later = __shfl_down(read, d, 32), before = __shfl_up(written, d, 32);
+    if (at + d < 32) read += later;
+    if (at >= (uint32_t)d) written += before;
+    stay += __shfl_xor(stay, d, 32);
   }
-  if (at_half == 63) upto[half] = sum;
-  __syncthreads();
-  if (at_half >= 64) sum += upto[half];
-  if (t >= p.L || 2 * block + half >= all) return;
+  if (t >= p.L || place >= all) return;
   float* const dg = const_cast<float*>(p.dlog_decay.d) + (int64_t)b * p.dlog_decay.batch + (int64_t)t * p.dlog_decay.token + (int64_t)h * p.dlog_decay.head;
   float* const db = const_cast<float*>(p.dbeta.d) + (int64_t)b * p.dbeta.batch + (int64_t)t * p.dbeta.token + (int64_t)h * p.dbeta.head;
-  *dg = t < valid ? border - (sum - fall) : 0.0f;
+  *dg = t < valid ? (past + read) + (written + stay) : 0.0f;
   *db = t < valid ? strength : 0.0f;
 }
 

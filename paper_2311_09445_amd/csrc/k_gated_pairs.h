@@ -21,14 +21,14 @@ struct Gates {
 };
 
 struct DeltaRecord {
-  bf16x8 solve[3][2][64], pairs[3][2][64];
+  bf16x8 solve[3][2][64], pairs[3][2][64];   // (of a gradient, which has no outputs: the pairs transposed)
   float gamma[32], left[32], beta[32];   // e^G, e^(G at the end - G), strengths
   float kept[2];                         // what is left of a state over the chunk, as a number and what rounding it left
   float pad[30];
 };
 struct DeltaRecordBack {
   DeltaRecord of;
-  bf16x8 solve_t[3][2][64], pairs_t[3][2][64];
+  bf16x8 solve_t[3][2][64];
 };
 template <bool BACK>
 struct RecordOf { typedef DeltaRecord type; };
@@ -186,7 +186,7 @@ __device__ __forceinline__ void pairs_of(const DeltaPairs& p, uint32_t item, uin
 #pragma unroll
   for (int r = 0; r < 4; ++r) B[(4 * g + r) * kPairRow + 16 + m] = 0.0f;
   wave_sync();
-  constexpr int PAIR_PARTS = sizeof(T) == 2 && !BACK ? 2 : 3;   // (as many as outputs in bfloat16 take)
+  constexpr int PAIR_PARTS = sizeof(T) == 2 ? 2 : 3;   // (as many as outputs in bfloat16 take)
   auto put = [&](bf16x8 (&to)[3][2][64], int tile, f32x4 a, f32x4 c, int parts = 3) {
     const Parts<3> o = Parts<3>::of(a, c);
 #pragma unroll
@@ -199,10 +199,11 @@ __device__ __forceinline__ void pairs_of(const DeltaPairs& p, uint32_t item, uin
       put(to, i, *reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + 16), parts);
     }
   };
-  put_rows(record->pairs, B, PAIR_PARTS);
   if constexpr (BACK) {
-    put(whole->pairs_t, 0, qk[0], qk[1]);
-    put(whole->pairs_t, 1, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, qk[2]);
+    put(record->pairs, 0, qk[0], qk[1]);
+    put(record->pairs, 1, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, qk[2]);
+  } else {
+    put_rows(record->pairs, B, PAIR_PARTS);
   }
   // The inverse of  1 + N diag(beta)  (upper half: 1 + diag(beta) N) by halves: of the two blocks on the diagonal by substitution, a column to a lane,
   // 16 lanes to a block; then the one below, -X11 A10 X00, by two products in fp32.

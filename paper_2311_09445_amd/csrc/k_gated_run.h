@@ -27,9 +27,9 @@ struct DeltaRun {
   float scale;
   float* carried;                // [sequence, head][segment], `each` floats: what a segment adds [dk][dv], what it makes of a state [dk][dk], and
   uint32_t each, turned;         // (turned) that transposed
-  // kept for a gradient: the states before the chunks, Y, rows of out . dout
-  bf16x8 *states, *lower;
-  float *y, *along;
+  // kept for a gradient: the states before the chunks, Y, what keys read of them (e^G K S), and rows of what queries read . dout
+  bf16x8* states;
+  float *y, *x, *read;
   DeltaPairs pairs;              // for a workgroup that makes its records itself
 };
 
@@ -37,12 +37,10 @@ struct DeltaRun {
 enum DeltaMode { FORWARD, KEEPING, CARRYING };
 
 // Planes of 16 bits that the states before the chunks are kept in for a gradient: where rows are bfloat16 the rounded state, which the products for
-// bfloat16 gradients take, else the three parts that an operand takes.  Before every kBorder-th chunk the gradient of a decay is the whole
-// state's product with its gradient; there the lower half of the sum that rounded it is kept too, so that both together are the 32 bits.
-// (From state to state the gradient is carried on by rows' products, which are off by 2^-24 of themselves; over four chunks that stays below 1e-6.)
+// bfloat16 gradients take, and the lower half of the sum that rounded it, so that both together are the 32 bits (the gradients of
+// decays take the state whole); else the three parts that an operand takes.
 template <typename T>
-constexpr int kStateParts = sizeof(T) == 2 ? 1 : 3;
-constexpr uint32_t kBorder = 4;
+constexpr int kStateParts = sizeof(T) == 2 ? 2 : 3;
 
 // Where plane `part` of the states kept for chunk c of a sequence and head lies: [part][16 columns of dv][32 places of dk][lane], eight places a lane
 // as registers hold them, so that a wave's instruction writes and reads 1 KiB in a row.  (As tiles of columns, pieces of 16 bytes in lines of
@@ -296,22 +294,22 @@ struct TwoRows {
 
 // LDS of a chunk: rows of queries and keys, and where they come straight from memory those of 64 values and the record's products too (twice 32 KiB:
 // as far as such loads reach).
-// (A pass that only carries has neither queries nor pairs there.)
-template <typename T, int DK, int NP, bool DIRECT_ROWS, bool ASKS = true>
+// (Only outputs take pairs; a pass that only carries has no queries either.)
+template <typename T, int DK, int NP, bool DIRECT_ROWS, DeltaMode MODE>
 struct RunLds {
-  static constexpr uint32_t ROWS = kParts<T> * Tile<DK>::SIZE, Q = 0, K = ASKS || !DIRECT_ROWS ? ROWS : 0, V = K + ROWS,
+  static constexpr uint32_t ROWS = kParts<T> * Tile<DK>::SIZE, Q = 0, K = MODE != CARRYING || !DIRECT_ROWS ? ROWS : 0, V = K + ROWS,
                             SOLVE = V + (DIRECT_ROWS ? Tile<64>::SIZE : 0), PAIRS = SOLVE + (DIRECT_ROWS ? 3 * 1024 : 0),
-                            SIZE = PAIRS + (DIRECT_ROWS && ASKS ? NP * 1024 : 0), BYTES = 2 * SIZE * sizeof(bf16);
+                            SIZE = PAIRS + (DIRECT_ROWS && MODE == FORWARD ? NP * 1024 : 0), BYTES = 2 * SIZE * sizeof(bf16);
 };
 template <typename T, DeltaMode MODE>
-constexpr int kPairParts = MODE == CARRYING ? 1 : sizeof(T) == 2 && MODE == FORWARD ? 2 : 3;
+constexpr int kPairParts = MODE != FORWARD ? 1 : sizeof(T) == 2 ? 2 : 3;
 
 // OWN: a workgroup forms its chunks' records itself, a wave a chunk: one launch less where sequences have no more than four (64 stretches of up to 80
 // tokens of 4 heads of 64 x 64: 20.0 us and 17.6).  It has all columns then, so that nobody else needs them.
 template <typename T, int DK, DeltaMode MODE, bool DIRECT_ROWS, bool OWN = false>
 __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 64 ? 3 : 2) void k_delta_run(DeltaRun p) {
-  constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = NP - 1;
-  typedef RunLds<T, DK, NP, DIRECT_ROWS, MODE != CARRYING> Lds;
+  constexpr int PT = kParts<T>, TX = DK / 16, KX = DK / 32, NP = kPairParts<T, MODE>, LESS = MODE == FORWARD ? NP - 1 : 2;
+  typedef RunLds<T, DK, NP, DIRECT_ROWS, MODE> Lds;
   static_assert(!DIRECT_ROWS || Lds::BYTES <= 65536, "loads to LDS have 16 bits of address");
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   bf16* const lds = reinterpret_cast<bf16*>(lds_raw);
@@ -363,11 +361,11 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
       direct_k.ask(to + Lds::K * 2, walk_k.next(), wave, n);
       if (!product) direct_v.ask(to + Lds::V * 2, walk_v.next(), wave, n);
       ask_rows<6>(to + Lds::SOLVE * 2, record(c)->solve, wave, lane);
-      if (MODE != CARRYING) ask_rows<2 * NP>(to + Lds::PAIRS * 2, record(c)->pairs, wave, lane);
+      if (MODE == FORWARD) ask_rows<2 * NP>(to + Lds::PAIRS * 2, record(c)->pairs, wave, lane);
     } else {
       rows.store(lds + (c & 1) * Lds::SIZE, valid - c * kChunk, dk, pieces);
       if (c + 1 < chunks) rows.load(p.q, p.k, q0, k0, (c + 1) * kChunk, valid, dk, pieces);
-      next.template load<MODE != CARRYING>(&record(c)->solve[0][0][0], &record(c)->pairs[0][0][0], lane);
+      next.template load<MODE == FORWARD>(&record(c)->solve[0][0][0], &record(c)->pairs[0][0][0], lane);
       next_v.ask(p.v, v0, c * kChunk, valid, takes, col, g);
     }
     if constexpr (MODE == KEEPING) {
@@ -408,11 +406,11 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
     if constexpr (MODE == KEEPING) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        float* to = p.y + ((size_t)bh * p.chunks * kChunk + first + 16 * i + 4 * g) * (blocks * 32) + col;
+        float* const to = p.y + ((size_t)bh * p.chunks * kChunk + first + 16 * i + 4 * g) * (blocks * 32) + col;
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[e * blocks * 32] = y[i][e];
         const uint32_t t = first + 16 * i + m;
-        if (g == 0) p.along[((size_t)bh * (blocks * 2) + col0 / 16) * p.chunks * kChunk + t] = o[i][0];
+        if (g == 0) p.read[((size_t)bh * (blocks * 2) + col0 / 16) * p.chunks * kChunk + t] = o[i][0];
       }
     } else if (DIRECT_ROWS && p.out.wide && valid - first >= kChunk) {
       uint8_t* const to = const_cast<uint8_t*>(walk_out.next());
@@ -432,8 +430,8 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
     const uint32_t first = c * kChunk;
     bf16 *const buffer = lds + (c & 1) * Lds::SIZE, *const Q = buffer + Lds::Q, *const K = buffer + Lds::K;
     if constexpr (DIRECT_ROWS) {
-      // (what a pass that keeps states stores behind the loads: the state's plane, and from the second chunk Y)
-      if (MODE == KEEPING && works && c > chunk0 + 1) arrive<KX + 8>();
+      // (what a pass that keeps states stores behind the loads: the state's planes, what keys read, and from the second chunk Y)
+      if (MODE == KEEPING && works && c > chunk0 + 1) arrive<2 * KX + 16>();
       else arrive<0>();
       if (valid - first < kChunk) {
         if (MODE != CARRYING) DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
@@ -459,16 +457,12 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
       if (works) {
 #pragma unroll
         for (int k = 0; k < KX; ++k) {
-          auto to = [&](int t) { return p.states + state_at<DK>(bh, p.chunks, c, blocks, kStateParts<T>, t, col0 / 16) + k * 64 + lane; };
-          if (sizeof(T) == 2 && c % kBorder == 0) {
-            const Halves both = halves_of(s[2 * k], s[2 * k + 1]);
-            *to(0) = both.v[0];
-            p.lower[state_at<DK>(bh, (p.chunks + kBorder - 1) / kBorder, c / kBorder, blocks, 1, 0, col0 / 16) + k * 64 + lane] = both.v[1];
-          } else {
-            const Parts<kStateParts<T>> parts = Parts<kStateParts<T>>::of(s[2 * k], s[2 * k + 1]);
+          auto put = [&](const auto& parts) {
 #pragma unroll
-            for (int t = 0; t < kStateParts<T>; ++t) *to(t) = parts.v[t];
-          }
+            for (int t = 0; t < kStateParts<T>; ++t) p.states[state_at<DK>(bh, p.chunks, c, blocks, kStateParts<T>, t, col0 / 16) + k * 64 + lane] = parts.v[t];
+          };
+          if constexpr (sizeof(T) == 2) put(halves_of(s[2 * k], s[2 * k + 1]));
+          else put(Parts<kStateParts<T>>::of(s[2 * k], s[2 * k + 1]));
         }
       }
     }
@@ -484,13 +478,22 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
         sp[k + 1] = Parts<3>::of(s[2 * k + 2], s[2 * k + 3]);
         mma_turns<4, 2, PT, 3>([&](int j) -> const bf16x8 (&)[PT] { return rows_k[j].v; }, [&](int j) -> const bf16x8 (&)[3] { return sp[k + j / 2].v; }, x4);
       }
-      f32x4 v[2];
+      f32x4 v[2], x[2];
       if constexpr (DIRECT_ROWS) {
-        rec.template load<MODE != CARRYING>(reinterpret_cast<const bf16x8*>(buffer + Lds::SOLVE), reinterpret_cast<const bf16x8*>(buffer + Lds::PAIRS), lane);
+        rec.template load<MODE == FORWARD>(reinterpret_cast<const bf16x8*>(buffer + Lds::SOLVE), reinterpret_cast<const bf16x8*>(buffer + Lds::PAIRS), lane);
         Operand<bf16>::across<64>(buffer + Lds::V, [&](uint32_t i) { return 16 * wave + i; }, m, g).widen(&v[0], &v[1]);
       }
       else now_v.widen(first, valid, takes, g, v);
-      const Parts<3> z = Parts<3>::of(v[0] - num.gamma[0] * (x4[0] + x4[2]), v[1] - num.gamma[1] * (x4[1] + x4[3]));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[i] = num.gamma[i] * (x4[i] + x4[i + 2]);
+        if constexpr (MODE == KEEPING) {
+          float* const to = p.x + ((size_t)bh * p.chunks * kChunk + first + 16 * i + 4 * g) * (blocks * 32) + col;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) to[e * blocks * 32] = x[i][e];
+        }
+      }
+      const Parts<3> z = Parts<3>::of(v[0] - x[0], v[1] - x[1]);
       f32x4 u[2];
       y[0] = y[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       mma_turns<2, 2, 3, 3>([&](int i) -> const bf16x8 (&)[3] { return rec.solve[i]; }, [&](int) -> const bf16x8 (&)[3] { return z.v; }, y);
@@ -508,7 +511,7 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
       const Parts<NP> up = Parts<NP>::of(u[0], u[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) o[i] = p.scale * num.gamma_m[i] * (o4[i] + o4[i + 2]);
-      if constexpr (MODE != CARRYING)
+      if constexpr (MODE == FORWARD)
         mma_turns<2, LESS, NP, NP>([&](int) -> const bf16x8 (&)[NP] { return up.v; }, [&](int i) -> const bf16x8 (&)[NP] { return rec.pairs[i]; }, o);
       constexpr int TURN = PT == 1 ? TX : 4;
 #pragma unroll

@@ -74,7 +74,7 @@ size_t record_bytes(const DeltaSizes& a) { return (size_t)a.B * a.H * chunks_of(
 
 // Where a gradient's intermediate results lie in the workspace.
 struct BackWork {
-  size_t records, states, lower, dstates, y, dz, read, along, strength, border, fold_q, fold_k, carried, carried_back, bytes;
+  size_t records, states, dstates, y, x, dz, read, along, strength, write, stay, past, fold_q, fold_k, carried, carried_back, bytes;
 };
 BackWork back_work(const DeltaSizes& a) {
   const uint64_t bh = (uint64_t)a.B * a.H, chunks = bh * chunks_of(a.L), tokens = chunks * kChunk;
@@ -88,15 +88,17 @@ BackWork back_work(const DeltaSizes& a) {
   };
   const uint64_t state = blocks * 32 * padded(a.dk) * sizeof(bf16);
   w.records = take(chunks * sizeof(DeltaRecordBack));
-  w.states = take(chunks * state * (e ? 1 : 3));
-  w.lower = take(e ? bh * ((chunks_of(a.L) + kBorder - 1) / kBorder) * state : 0);
+  w.states = take(chunks * state * (e ? 2 : 3));
   w.dstates = take(chunks * state * (e ? 1 : 3));
   w.y = take(tokens * blocks * 32 * sizeof(float));
+  w.x = take(tokens * blocks * 32 * sizeof(float));
   w.dz = take(tokens * blocks * 32 * sizeof(float));
   w.read = take(tokens * parts * sizeof(float));
   w.along = take(tokens * parts * sizeof(float));
   w.strength = take(tokens * parts * sizeof(float));
-  w.border = take(chunks * parts * sizeof(float));
+  w.write = take(tokens * parts * sizeof(float));
+  w.stay = take(tokens * parts * sizeof(float));
+  w.past = take(tokens * sizeof(float));
   w.fold_q = take(a.Q == a.H ? 0 : tokens * a.dk * sizeof(float));
   w.fold_k = take(a.K == a.H ? 0 : tokens * a.dk * sizeof(float));
   const Cut c = cut(a, true);
@@ -132,16 +134,16 @@ hipError_t launch_run(const DeltaRun& p, uint32_t bh, hipStream_t s) {
   auto lds = [](uint32_t bytes) { return OWN && bytes < 4 * sizeof(PairLds) ? (uint32_t)(4 * sizeof(PairLds)) : bytes; };
   if constexpr (sizeof(T) == 2) {
     if (p.q.wide && p.k.wide && p.v.wide && p.dk % 8 == 0 && p.dv % 8 == 0)
-      return launch(k_delta_run<T, DK, MODE, true, OWN>, &granted[1], grid, lds(RunLds<T, DK, NP, true, MODE != CARRYING>::BYTES), p, s);
+      return launch(k_delta_run<T, DK, MODE, true, OWN>, &granted[1], grid, lds(RunLds<T, DK, NP, true, MODE>::BYTES), p, s);
   }
-  return launch(k_delta_run<T, DK, MODE, false, OWN>, &granted[0], grid, lds(RunLds<T, DK, NP, false, MODE != CARRYING>::BYTES), p, s);
+  return launch(k_delta_run<T, DK, MODE, false, OWN>, &granted[0], grid, lds(RunLds<T, DK, NP, false, MODE>::BYTES), p, s);
 }
 template <typename T, int DK, bool CARRY>
 hipError_t launch_back(const DeltaBack& p, uint32_t bh, hipStream_t s) {
   static std::atomic<uint64_t> granted[2] = {};
   const uint32_t grid = bh * p.run * p.slices;
   if constexpr (sizeof(T) == 2) {
-    if (p.q.wide && p.k.wide && p.v.wide && p.dout.wide && p.dk % 8 == 0 && p.dv % 8 == 0)
+    if (p.q.wide && p.k.wide && p.dout.wide && p.dk % 8 == 0 && p.dv % 8 == 0)
       return launch(k_delta_back<T, DK, CARRY, true>, &granted[1], grid, BackLds<T, DK, true>::BYTES, p, s);
   }
   return launch(k_delta_back<T, DK, CARRY, false>, &granted[0], grid, BackLds<T, DK, false>::BYTES, p, s);
@@ -259,9 +261,9 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   DeltaRun run = make_run(a, q, k, v, state, at + w.records, sizeof(DeltaRecordBack));
   run.dout = rows(dout, a.dtype, 1);
   run.states = reinterpret_cast<bf16x8*>(at + w.states);
-  run.lower = reinterpret_cast<bf16x8*>(at + w.lower);
   run.y = floats(w.y);
-  run.along = floats(w.read);
+  run.x = floats(w.x);
+  run.read = floats(w.read);
   e = launch_carry<T, DK>(&run, a, c, state, floats(w.carried), true, s);
   if (own) run.pairs = make_pairs(a, q, k, at + w.records);
   if (e == hipSuccess && run.chunks) e = own ? launch_run<T, DK, KEEPING, true>(run, bh, s) : launch_run<T, DK, KEEPING>(run, bh, s);
@@ -269,7 +271,6 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   DeltaBack b{};
   b.q = run.q;
   b.k = run.k;
-  b.v = run.v;
   b.dout = run.dout;
   b.records = run.records;
   b.lengths = a.lengths;
@@ -284,13 +285,14 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   b.segment = c.segment;
   b.scale = a.scale;
   b.states = run.states;
-  b.lower = run.lower;
   b.y = run.y;
+  b.x = run.x;
   b.dstates = reinterpret_cast<bf16x8*>(at + w.dstates);
   b.dz = floats(w.dz);
   b.along = floats(w.along);
   b.strength = floats(w.strength);
-  b.border = floats(w.border);
+  b.write = floats(w.write);
+  b.stay = floats(w.stay);
   if (c.segments > 1) {   // what each segment but the first adds, then the gradients behind the segments
     b.carried = floats(w.carried_back);
     b.first_segment = 1;
@@ -337,11 +339,12 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
   g.dstates = b.dstates;
   g.y = run.y;
   g.dz = b.dz;
+  g.past = floats(w.past);
   e = launch_grads<T, DK>(g, bh, s);
   if (e != hipSuccess) return e;
   DeltaFinish f{};
-  f.gates = DeltaGates{gates(dlog_decay), gates(dbeta), a.lengths, bh, a.L, a.H, run.chunks, (a.dv + 31) / 32 * 2, run.along, b.along, b.strength, b.border};
-  f.gate_blocks = (bh * ((run.chunks + kBorder - 1) / kBorder) + 1) / 2;
+  f.gates = DeltaGates{gates(dlog_decay), gates(dbeta), a.lengths, bh, a.L, a.H, run.chunks, (a.dv + 31) / 32 * 2, run.read, b.along, b.strength, b.write, b.stay, g.past};
+  f.gate_blocks = (bh * run.chunks + 256 / kChunk - 1) / (256 / kChunk);
   f.fold[0] = fold(a, g.fold_q, dq, a.Q, a.dk, a.dk);
   f.fold[1] = fold(a, g.fold_k, dk, a.K, a.dk, a.dk);
   f.fold[2] = fold(a, b.dz, dv, a.V, a.dv, (a.dv + 31) / 32 * 32);

@@ -55,6 +55,28 @@ def delta_backward(dout, q, k, v, log_decay, beta, state=None, dstate=None, leng
     return [torch.zeros_like(x) if g is None else g for g, x in zip(grads, leaves)]
 
 
+def delta_decay_sizes(dout, q, k, v, log_decay, beta, state, dstate, lengths=None, scale=1.0):
+    """|D_t| |E_t| [B, L, H]: of the decayed state that a token sees and of its gradient, whose product the gradient of the decay's logarithm is."""
+    B, L, H = log_decay.shape
+    dout, q, k, v, log_decay, beta = (cleared(t, lengths) for t in (dout, q, k, v, log_decay, beta))
+    q, k, v = (t.repeat_interleave(H // t.shape[2], 2) for t in (q, k, v))
+    n = torch.full((B,), L) if lengths is None else lengths.cpu().long().clamp(0, L)
+    S, R, seen = f64(state), f64(dstate), []
+    for t in range(L):
+        D = S * torch.exp(log_decay[:, t])[..., None, None]
+        u = beta[:, t, :, None] * (v[:, t] - (k[:, t, :, None] @ D)[..., 0, :])
+        S = torch.where((t < n)[:, None, None, None], D + k[:, t, ..., None] * u[..., None, :], S)
+        seen.append(D.flatten(2).norm(dim=-1))
+    sizes = [None] * L
+    for t in range(L - 1, -1, -1):
+        here = (t < n)[:, None, None, None]
+        E = R + scale * q[:, t, ..., None] * dout[:, t, :, None]
+        E = E - k[:, t, ..., None] * (beta[:, t, :, None] * (k[:, t, :, None] @ E)[..., 0, :])[..., None, :]
+        sizes[t] = seen[t] * E.flatten(2).norm(dim=-1) * here[..., 0, 0]
+        R = torch.where(here, E * torch.exp(log_decay[:, t])[..., None, None], R)
+    return torch.stack(sizes, 1)
+
+
 def norm(x, weight, bias, eps):
     x = f64(x)
     y = (x - x.mean(-1, keepdim=True)) / torch.sqrt(x.var(-1, unbiased=False, keepdim=True) + eps)

@@ -248,6 +248,50 @@ def test_decays_at_their_ends(rate, dtype):
     check_grads(got, exact, L, d, dtype)
 
 
+def check_decays(got, want, sizes, T, d, what):
+    """The gradient of a decay's logarithm is <D, E>, of the decayed state that its token sees and of its gradient.  The first is off by u32 of itself in
+    2-norm, the second, a gradient, by four times that, so their product by no more than 5 u32 |D| |E|: where little of a state is left, or nothing, so
+    little may be off.  Below 2^-126, where fp32 has no normal numbers, decays lose their bits: 1e-30 for the terms of all that is multiplied."""
+    off = (oracle.f64(got) - want).abs()
+    worst = float((off / (5 * u32(T, d) * sizes + 1e-30)).max())
+    assert worst <= 1, f"{what}: off by {worst:.3g} of what is allowed"
+    assert float(off.norm()) <= 4 * u32(T, d) * float(want.norm()) + 1e-30, f"{what}: 2-norm off by {float(off.norm() / want.norm()):.3g}"
+
+
+@TYPES
+@pytest.mark.parametrize("rate", [0.5, 2.0, 8.0, 20.0])
+@pytest.mark.parametrize("B,L,H,Q,K,V,dk,dv", [(2, 130, 2, 2, 1, 2, 32, 48), (1, 300, 2, 2, 2, 2, 128, 128), (2, 100, 3, 1, 3, 1, 61, 33), (1, 1025, 1, 1, 1, 1, 64, 64)])
+def test_gradients_of_fast_decays(B, L, H, Q, K, V, dk, dv, rate, dtype):
+    q, k, v, g, beta, S, lengths = inputs(B, L, H, Q, K, V, dk, dv, dtype, ragged=B > 1, fast=rate)
+    dout, dS = normal(21, B, L, H, dv, dtype=dtype), normal(22, *S.shape)
+    got = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths, scale=0.7)
+    want = oracle.delta_backward(dout, q, k, v, g, beta, S, dS, lengths, 0.7)
+    check_decays(got[3], want[3], oracle.delta_decay_sizes(dout, q, k, v, g, beta, S, dS, lengths, 0.7), L, max(dk, dv), "dlog_decay")
+
+
+@TYPES
+@pytest.mark.parametrize("L", [130, 1025])
+@pytest.mark.parametrize("at", [0, 1, 31, 32, 50, 127, 128])
+def test_gradients_of_decays_around_a_reset(at, L, dtype):
+    """An episode ends at one token, and the next is 10000 times smaller: what its decays' gradients are off by is of its own size, and the
+    reset itself, which nothing goes past, has none."""
+    B, H, d = 1, 2, 32
+    q, k, v, g, beta, S, _ = inputs(B, L, H, 2, 2, 2, d, d, dtype, fast=0.05)
+    dout, dS = normal(21, B, L, H, d, dtype=dtype), normal(22, *S.shape)
+    g[:, at] = -math.inf
+    v[:, at:] *= 2.0 ** -13
+    dout[:, at:] *= 2.0 ** -13
+    dS *= 2.0 ** -13
+    got = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS)[3]
+    # (the definition's own gradient of a decay that keeps nothing is 0 times infinity)
+    given = (dout, q, k, v, g.clamp(min=-1e4), beta, S, dS, None, d ** -0.5)
+    want, sizes = oracle.delta_backward(*given)[3], oracle.delta_decay_sizes(*given)
+    assert not got[:, at].any()
+    for name, side in (("before", slice(0, at)), ("behind", slice(at + 1, L))):
+        if side.start < side.stop:
+            check_decays(got[:, side], want[:, side], sizes[:, side], L, d, name)
+
+
 @TYPES
 def test_strengths_of_zero_and_two(dtype):
     """A strength of 0 leaves the state alone, but has a gradient; one of 2 turns it around along the key."""
