@@ -562,7 +562,8 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
 
 // The states that segments start from, one behind the other: S <- P S + B, with what each segment carries; S takes the place of B.  BACK: of
 // the gradients behind the segments, R <- P^T R + C.  A workgroup takes 64 columns, a wave 16 rows of them; the rows' parts meet in LDS, where
-// they lie as operands, and the next segment's product is under way meanwhile.  (A wave for 16 columns and all rows took 45 us for a
+// they lie as operands, and the next segment's product is under way meanwhile.  Past segments without tokens a state goes as it is: of an
+// identity's zeros, one that is not finite would spoil its column.  (A wave for 16 columns and all rows took 45 us for a
 // segment: it takes all of P apart by itself.)
 struct DeltaJoin {
   float* carried;            // [sequence, head][segment]: B or C, rows of dv
@@ -570,7 +571,8 @@ struct DeltaJoin {
   const float* in;
   int64_t in_batch, in_head;
   size_t stride, product_stride;
-  uint32_t H, dk, dv, slices, segments;
+  const int32_t* lengths;
+  uint32_t L, H, dk, dv, slices, segments, segment;
 };
 template <int DK, bool BACK>
 __global__ __launch_bounds__(4 * DK) void k_delta_join(DeltaJoin p) {
@@ -579,6 +581,7 @@ __global__ __launch_bounds__(4 * DK) void k_delta_join(DeltaJoin p) {
   const uint32_t slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, h = bh % p.H, b = bh / p.H;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const uint32_t dk = p.dk, dv = p.dv, row = state_row(wave, 4 * g), of_m = state_row(wave, m);
+  const uint32_t valid = __builtin_amdgcn_readfirstlane(valid_tokens(p.lengths, b, p.L)), chunks = (valid + kChunk - 1) / kChunk;
   uint32_t at[4][4];   // of the wave's elements
   bool on[4][4];
   f32x4 s[4];
@@ -629,6 +632,10 @@ __global__ __launch_bounds__(4 * DK) void k_delta_join(DeltaJoin p) {
         if (on[c][r]) to[at[c][r]] = s[c][r];
       }
     if (i + 1 == p.segments) break;
+    if (seg * p.segment >= chunks) {
+      load(i + 1);
+      continue;
+    }
     Parts<3> P[KX];
 #pragma unroll
     for (int k = 0; k < KX; ++k) {

@@ -201,7 +201,7 @@ hipError_t launch_carry(DeltaRun* p, const DeltaSizes& a, const Cut& c, const pe
   hipError_t e = launch_run<T, DK, CARRYING>(*p, a.B * a.H, s);
   if (e != hipSuccess) return e;
   const size_t each = p->each;
-  DeltaJoin j{carried, carried + (size_t)a.dk * a.dv, nullptr, 0, 0, each, each, a.H, a.dk, a.dv, p->slices, c.segments};
+  DeltaJoin j{carried, carried + (size_t)a.dk * a.dv, nullptr, 0, 0, each, each, a.lengths, a.L, a.H, a.dk, a.dv, p->slices, c.segments, c.segment};
   if (state) { j.in = state->d; j.in_batch = state->batch; j.in_head = state->head; }
   k_delta_join<DK, false><<<a.B * a.H * p->slices, 4 * DK, 0, s>>>(j);
   e = hipGetLastError();
@@ -300,7 +300,8 @@ hipError_t backward(const DeltaSizes& a, const per_seq_rows& dout, const per_seq
     e = launch_back<T, DK, true>(b, bh, s);
     if (e != hipSuccess) return e;
     const size_t each = (size_t)a.dk * a.dv;
-    const DeltaJoin j{b.carried, floats(w.carried) + (size_t)a.dk * (a.dv + a.dk), b.in, b.in_batch, b.in_head, each, carried_floats(a, true), a.H, a.dk, a.dv, b.slices, c.segments};
+    const DeltaJoin j{b.carried, floats(w.carried) + (size_t)a.dk * (a.dv + a.dk), b.in, b.in_batch, b.in_head, each, carried_floats(a, true),
+                      a.lengths, a.L, a.H, a.dk, a.dv, b.slices, c.segments, c.segment};
     k_delta_join<DK, true><<<bh * b.slices, 4 * DK, 0, s>>>(j);
     e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -429,6 +429,31 @@ def test_values_that_are_not_finite(dtype):
             assert i == 0 or (out[1, 100:, 1].isnan().all() and state[1, 1].isnan().all())
 
 
+def equal(x, y):
+    """Bit for bit but for which NaN it is."""
+    return torch.equal(x.isnan(), y.isnan()) and torch.equal(x.nan_to_num(), y.nan_to_num())
+
+
+@TYPES
+@pytest.mark.parametrize("L", [40, 777])
+def test_states_of_sequences_without_tokens_are_copied_whatever_they_hold(L, dtype):
+    """Also where sequences are cut and states go from segment to segment; and none reaches another sequence."""
+    B, H, d = 3, 2, 64
+    q, k, v, g, beta, S, _ = inputs(B, L, H, 1, 2, 1, d, d, dtype)
+    dout, dS = normal(21, B, L, H, d, dtype=dtype), normal(22, *S.shape)
+    lengths = torch.tensor([L, 0, 33], dtype=torch.int32).cuda()
+    call = lambda S, dS: [*seq.gated_delta(q, k, v, g, beta, S, lengths), *seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths)]  # noqa: E731
+    want = call(S, dS)
+    for bad in (math.nan, math.inf, -math.inf, torch.finfo(torch.float32).max):
+        T, R = S.clone(), dS.clone()
+        T[1, 0, 3, 5] = T[1, 1, 63, 63] = R[1, 1, 7, 0] = R[1, 0, 0, 63] = bad
+        got = call(T, R)
+        assert equal(got[1][1], T[1]) and equal(got[7][1], R[1])
+        for i, (x, y) in enumerate(zip(got, want)):
+            rows = [0, 2] if i in (1, 7) else [0, 1, 2]
+            assert torch.equal(x[rows], y[rows]), i
+
+
 @TYPES
 @pytest.mark.parametrize("B,L,H,Q,K,V,dk,dv", [(1, 300, 1, 1, 1, 1, 64, 64), (2, 777, 2, 1, 2, 1, 128, 72), (1, 1025, 3, 3, 1, 1, 40, 128), (3, 513, 2, 2, 2, 2, 61, 37)])
 def test_sequences_in_segments(B, L, H, Q, K, V, dk, dv, dtype):
