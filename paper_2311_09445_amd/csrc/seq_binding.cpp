@@ -654,10 +654,20 @@ PyObject* do_dropout(Args a, Py_ssize_t n_args) {
   return answer(rc, {&out});
 }
 
+// No call forms derivatives along its inputs: a tangent would be lost without a word.
+void refuse_tangents(Args a, Py_ssize_t n) {
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (!THPVariable_Check(a[i]) || !THPVariable_Unpack(a[i])._fw_grad(0).defined()) continue;
+    PyErr_SetString(PyExc_RuntimeError, "a tensor carries a forward-mode derivative, which is not formed here: take its primal (torch.autograd.forward_ad.unpack_dual)");
+    throw Raised{};
+  }
+}
+
 // Every function: C++ and library errors become Python exceptions, nothing is thrown past the interpreter.
 template <PyObject* (*F)(Args, Py_ssize_t)>
 PyObject* function(PyObject*, Args a, Py_ssize_t n) {
   try {
+    refuse_tangents(a, n);
     return F(a, n);
   } catch (const Raised&) {
   } catch (const std::exception& e) {

@@ -147,6 +147,25 @@ def test_block_checks_before_any_work():
     assert back(block(), fake(0x8000), fake(), None, fake(0x9000), w, w, WORK, size, None) == per.EINVAL      # both at one place
 
 
+def test_forward_mode_is_refused():
+    """A tangent that a call does not know of would be lost without a word; every tensor of every call is asked, before anything else."""
+    from torch.autograd import forward_ad
+    t = torch.zeros(2, 4, 2, 8)
+    s, g, w = torch.zeros(2, 2, 8, 8), torch.zeros(2, 4, 2), torch.zeros(8)
+    calls = [(lambda x, f: seq.rotate(x, None, f), (t, w[:4])), (lambda q, k, a, b, f: seq.norm_rotate(q, k, a, b, None, f), (t, t, w, w, w[:4])),
+             (lambda x, y, q, k, a, b, f: seq.norm_rotate_backward(x, y, q, k, a, b, None, f), (t, t, t, t, w, w, w[:4])), (seq.linear_attention, (t, t, t, w[:2], s)),
+             (seq.linear_attention_backward, (t, t, t, t, w[:2], s)), (seq.linear_attention_step, (t, t, t, w[:2], s)), (seq.gated_delta, (t, t, t, g, g, s)),
+             (seq.gated_delta_backward, (t, t, t, t, g, g, s, s)), (seq.gated_delta_step, (t, t, t, g, g, s)), (seq.layer_norm, (t, w, w)),
+             (seq.layer_norm_backward, (t, t, w)), (lambda x, r: seq.dropout(x, 0.1, 0, residual=r), (t, t))]
+    with forward_ad.dual_level():
+        for call, args in calls:
+            for i, a in enumerate(args):
+                given = list(args)
+                given[i] = forward_ad.make_dual(a, torch.ones_like(a))
+                with pytest.raises(RuntimeError, match="forward"):
+                    call(*given)
+
+
 def test_random_words():
     """Known answers of Philox4x32-10, as its authors publish them."""
     assert oracle.philox((0, 0, 0, 0), (0, 0)) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
