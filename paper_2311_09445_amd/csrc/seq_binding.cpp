@@ -654,12 +654,17 @@ PyObject* do_dropout(Args a, Py_ssize_t n_args) {
   return answer(rc, {&out});
 }
 
-// No call forms derivatives along its inputs: a tangent would be lost without a word.
-void refuse_tangents(Args a, Py_ssize_t n) {
+// What a tensor has besides its memory.  No call forms derivatives along its inputs: a tangent would be lost without a word.  A view that
+// torch negates when it reads it (the imaginary part of a conjugate) would be read with the other sign.
+void refuse_unseen(Args a, Py_ssize_t n) {
   for (Py_ssize_t i = 0; i < n; ++i) {
-    if (!THPVariable_Check(a[i]) || !THPVariable_Unpack(a[i])._fw_grad(0).defined()) continue;
-    PyErr_SetString(PyExc_RuntimeError, "a tensor carries a forward-mode derivative, which is not formed here: take its primal (torch.autograd.forward_ad.unpack_dual)");
-    throw Raised{};
+    if (!THPVariable_Check(a[i])) continue;
+    const at::Tensor& t = THPVariable_Unpack(a[i]);
+    if (t._fw_grad(0).defined()) {
+      PyErr_SetString(PyExc_RuntimeError, "a tensor carries a forward-mode derivative, which is not formed here: take its primal (torch.autograd.forward_ad.unpack_dual)");
+      throw Raised{};
+    }
+    if (t.is_neg()) raise_value("a tensor is a view that stands for its negative: call resolve_neg() on it first");
   }
 }
 
@@ -667,7 +672,7 @@ void refuse_tangents(Args a, Py_ssize_t n) {
 template <PyObject* (*F)(Args, Py_ssize_t)>
 PyObject* function(PyObject*, Args a, Py_ssize_t n) {
   try {
-    refuse_tangents(a, n);
+    refuse_unseen(a, n);
     return F(a, n);
   } catch (const Raised&) {
   } catch (const std::exception& e) {

@@ -166,6 +166,17 @@ def test_forward_mode_is_refused():
                     call(*given)
 
 
+def test_views_that_stand_for_their_negative_are_refused():
+    """torch keeps the imaginary part of a conjugate as a view of the memory that holds the opposite."""
+    t, s, g = torch.zeros(2, 4, 2, 8), torch.zeros(2, 2, 8, 8), torch.zeros(2, 4, 2)
+    lazy = torch.complex(g, g).conj().imag
+    assert lazy.is_neg()
+    for call in (lambda: seq.gated_delta(t, t, t, lazy, g), lambda: seq.gated_delta(t, t, t, g, lazy), lambda: seq.layer_norm(t._neg_view()),
+                 lambda: seq.gated_delta_step(t[:, :1], t[:, :1], t[:, :1], g[:, :1], lazy[:, :1], s), lambda: seq.dropout(t, 0.1, 0, residual=t._neg_view())):
+        with pytest.raises(ValueError, match="negative"):
+            call()
+
+
 def test_random_words():
     """Known answers of Philox4x32-10, as its authors publish them."""
     assert oracle.philox((0, 0, 0, 0), (0, 0)) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
