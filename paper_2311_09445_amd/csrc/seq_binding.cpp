@@ -8,6 +8,8 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
 #include <initializer_list>
 #include <stdexcept>
 #include <string>
@@ -632,8 +634,9 @@ PyObject* do_dropout(Args a, Py_ssize_t n_args) {
   const at::Tensor& x = tensor(a[0], "x");
   Block p(x);
   const c10::DeviceGuard guard(p.n.device);
-  p.c.p = (float)real(a[1]);
-  if (!(p.c.p >= 0.0f && p.c.p < 1.0f)) raise_value("p: expected 0 <= p < 1");
+  const double share = real(a[1]);
+  if (!(share >= 0.0 && share < 1.0)) raise_value("p: expected 0 <= p < 1");
+  p.c.p = (float)(std::min(65535.0, std::floor(share * 65536.0 + 0.5)) / 65536.0);   // (a whole number of 1/65536, which a float has)
   p.c.seed = whole(a[2], "seed");
   const int64_t* at_offset = nullptr;
   if (THPVariable_Check(a[3])) {

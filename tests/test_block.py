@@ -196,6 +196,16 @@ def test_dropped_places_may_hold_anything():
     assert torch.equal(seq.dropout(x, 0.5, 1, 2).cpu(), 2.0 * keep.float())
 
 
+def test_shares_next_to_one_and_next_to_half_a_step():
+    """The share is taken to the nearest 1/65536 as it is given, in 64 bits: in fp32 one next to 1 would be 1, and one next to a tie the tie."""
+    x = torch.ones(1 << 16, device="cuda")
+    assert torch.equal(seq.dropout(x, 1 - 1e-12, 3), seq.dropout(x, 65535 / 65536, 3))
+    tie = 100.5 / 65536
+    assert torch.equal(seq.dropout(x, tie * (1 - 1e-12), 3), seq.dropout(x, 100 / 65536, 3))
+    assert torch.equal(seq.dropout(x, tie, 3), seq.dropout(x, 101 / 65536, 3))
+    assert not torch.equal(seq.dropout(x, 100 / 65536, 3), seq.dropout(x, 101 / 65536, 3))
+
+
 def test_dropout_drops_its_share():
     """Of 2^20 elements; the count's standard deviation is sqrt(n p (1 - p)), and six of them are allowed."""
     n = 1 << 20
