@@ -82,6 +82,21 @@ def test_layer_norm_of_many_rows(shape, dtype):
 
 
 @TYPES
+@pytest.mark.parametrize("shape", [(70000, 16), (70000, 48), (20000, 40), (20000, 65), (20000, 100), (40000, 128), (20001, 200), (20000, 256), (5000, 129), (5000, 300),
+                                   (5000, 600), (1100, 5000)])
+def test_layer_norm_of_many_rows_of_every_shape(shape, dtype):
+    """Rows for two turns of a loop over them, forward and against, in each number of lanes and pieces that widths are given."""
+    test_layer_norm_of_many_rows(shape, dtype)
+
+
+@TYPES
+@pytest.mark.parametrize("D", [65, 100, 127, 128, 129, 200])
+@pytest.mark.parametrize("weights", [True, False])
+def test_layer_norm_of_rows_of_sixteen_lanes(D, weights, dtype):
+    test_layer_norm(D, weights, dtype)
+
+
+@TYPES
 @pytest.mark.parametrize("D", [5, 40, 513, 2500, 9001])
 def test_layer_norm_strides_and_in_place(D, dtype):
     pool = normal(1, 4, 3, 6, D + 3, dtype=dtype)
