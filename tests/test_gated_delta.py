@@ -455,6 +455,31 @@ def test_states_of_sequences_without_tokens_are_copied_whatever_they_hold(L, dty
 
 
 @TYPES
+@pytest.mark.parametrize("B,L,H,Q,K,V", [(2, 60, 4, 4, 4, 4), (2, 200, 4, 2, 4, 2), (2, 777, 4, 2, 1, 4)])
+def test_gradients_of_values_that_are_not_finite(B, L, H, Q, K, V, dtype):
+    """They reach their own sequence and head, and of others' gradients only the rows that those share with it."""
+    d = 32
+    clean = inputs(B, L, H, Q, K, V, d, d, dtype)[:6]
+    dout, dS = normal(21, B, L, H, d, dtype=dtype), normal(22, B, H, d, d)
+    want = seq.gated_delta_backward(dout, *clean, dS)
+    for i in range(8):
+        spoilt = [t.clone() for t in (*clean, dout, dS)]
+        # one sequence and head (of rows that several heads read: those heads)
+        heads = spoilt[i].shape[1 if spoilt[i].shape[1:] == (H, d, d) else 2]
+        at = (1, heads - 1) if i in (5, 7) else (1, 20, heads - 1)
+        spoilt[i][at] = math.nan
+        reached = torch.zeros(B, H, dtype=torch.bool)
+        reached[1, H - H // heads:] = True
+        got = seq.gated_delta_backward(spoilt[6], *spoilt[:6], spoilt[7])
+        for j, (x, y) in enumerate(zip(got, want)):
+            rows = x.shape[1] if j == 5 else x.shape[2]
+            clear = ~reached.reshape(B, rows, H // rows).any(-1)
+            x, y = (t if j == 5 else t.transpose(1, 2) for t in (x, y))
+            assert torch.equal(x[clear.cuda()], y[clear.cuda()]), (i, j)
+            assert clear.any()
+
+
+@TYPES
 @pytest.mark.parametrize("B,L,H,Q,K,V,dk,dv", [(1, 300, 1, 1, 1, 1, 64, 64), (2, 777, 2, 1, 2, 1, 128, 72), (1, 1025, 3, 3, 1, 1, 40, 128), (3, 513, 2, 2, 2, 2, 61, 37)])
 def test_sequences_in_segments(B, L, H, Q, K, V, dk, dv, dtype):
     """Few long sequences are cut; some end in the first segments, and the states they start from are made of those before."""
