@@ -41,21 +41,21 @@ hipError_t norm_as(const BlockArgs& a, bool back, hipStream_t s) {
   }
   return hipGetLastError();
 }
-template <typename T, int LANES>
+// FEWEST, MOST: the pieces that widths of these lanes come to (256 lanes are for rows that 64 do not hold).
+template <typename T, int LANES, int FEWEST, int MOST>
 hipError_t norm_pieces(const BlockArgs& a, uint32_t n, bool back, hipStream_t s) {
-  if (n == 1) return norm_as<T, LANES, 1>(a, back, s);
-  if (n == 2) return norm_as<T, LANES, 2>(a, back, s);
-  if (n == 4) return norm_as<T, LANES, 4>(a, back, s);
-  if constexpr (sizeof(T) == 4)
-    if (n == 8) return norm_as<T, LANES, 8>(a, back, s);
-  return hipErrorInvalidValue;
+  if constexpr (FEWEST < MOST)
+    if (n > (uint32_t)FEWEST) return norm_pieces<T, LANES, 2 * FEWEST, MOST>(a, n, back, s);
+  return n == (uint32_t)FEWEST ? norm_as<T, LANES, FEWEST>(a, back, s) : hipErrorInvalidValue;
 }
 template <typename T>
 hipError_t norm(uint32_t dtype, const BlockArgs& a, bool back, hipStream_t s) {
   const Shape shape = shape_of(dtype, a.dim);
-  if (shape.lanes == 4) return shape.pieces == 1 ? norm_as<T, 4, 1>(a, back, s) : norm_as<T, 4, 2>(a, back, s);
-  if (shape.lanes == 16) return shape.pieces == 1 ? norm_as<T, 16, 1>(a, back, s) : norm_as<T, 16, 2>(a, back, s);
-  if (shape.pieces) return shape.lanes == 64 ? norm_pieces<T, 64>(a, shape.pieces, back, s) : norm_pieces<T, 256>(a, shape.pieces, back, s);
+  constexpr int MOST = 32 / Piece<T>::W;
+  if (shape.lanes == 4) return norm_pieces<T, 4, 1, 2>(a, shape.pieces, back, s);
+  if (shape.lanes == 16) return norm_pieces<T, 16, 1, 2>(a, shape.pieces, back, s);
+  if (shape.lanes == 64) return norm_pieces<T, 64, 1, MOST>(a, shape.pieces, back, s);
+  if (shape.pieces) return norm_pieces<T, 256, MOST / 2, MOST>(a, shape.pieces, back, s);
   if (back) {
     k_layer_norm_any<T, true><<<back_blocks(a, 1), 256, 0, s>>>(a);
   } else {
