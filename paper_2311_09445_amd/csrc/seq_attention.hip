@@ -8,8 +8,7 @@
 //     gradient of v:           k, q, dout;  S the state's gradient; against time, lag 1
 //     gradient of k:           v, dout, q;  the same, transposed;   against time, lag 1
 #include "dev_tiles.h"
-
-#include <atomic>
+#include "seq_launch.h"
 
 namespace per {
 
@@ -207,18 +206,9 @@ template <typename T, int DX, int NT, int WAVES, bool OUT, Way WAY, int TEAMS = 
 hipError_t launch_as(const AttentionPasses& p, hipStream_t s) {
   constexpr uint32_t lds = lds_bytes<T, DX, NT, WAVES, OUT, WAY, TEAMS>();
   auto* kernel = k_attend<T, DX, NT, WAVES, OUT, WAY, TEAMS>;
-  if constexpr (lds > 64 * 1024) {   // granted once per kernel and device
-    static std::atomic<uint64_t> granted{0};
-    int device = 0;
-    hipError_t e = hipGetDevice(&device);
-    if (e != hipSuccess) return e;
-    const uint64_t bit = device < 64 ? 1ull << device : 0;
-    if (!(granted.load(std::memory_order_relaxed) & bit)) {
-      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-      if (e != hipSuccess) return e;
-      granted.fetch_or(bit, std::memory_order_relaxed);
-    }
-  }
+  static std::atomic<uint64_t> granted{0};
+  const hipError_t e = grant_lds(reinterpret_cast<const void*>(kernel), &granted, lds);
+  if (e != hipSuccess) return e;
   kernel<<<(p.items + 7) / 8 * 8 * p.count, dim3(64 * WAVES, TEAMS), lds, s>>>(p);
   return hipGetLastError();
 }

@@ -4,10 +4,10 @@
 //
 // Sequences are taken in chunks of 32 tokens (k_gated_pairs.h: what a chunk's tokens make of each other, all chunks at once; k_gated_run.h: the
 // states one chunk behind the other; k_gated_back.h: the gradient, against time and then all chunks at once), single tokens in k_gated_step.h.
-#include <atomic>
 #include <math.h>
 
 #include "dev_parts.h"
+#include "seq_launch.h"
 
 namespace per {
 
@@ -108,20 +108,10 @@ BackWork back_work(const DeltaSizes& a) {
   return w;
 }
 
-// A launch with more than 64 KB of LDS: granted once per kernel and device.
 template <typename Args>
 hipError_t launch(void (*kernel)(Args), std::atomic<uint64_t>* granted, uint32_t grid, uint32_t lds, const Args& args, hipStream_t s) {
-  if (lds > 64 * 1024) {
-    int device = 0;
-    hipError_t e = hipGetDevice(&device);
-    if (e != hipSuccess) return e;
-    const uint64_t bit = device < 64 ? 1ull << device : 0;
-    if (!(granted->load(std::memory_order_relaxed) & bit)) {
-      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-      if (e != hipSuccess) return e;
-      granted->fetch_or(bit, std::memory_order_relaxed);
-    }
-  }
+  const hipError_t e = grant_lds(reinterpret_cast<const void*>(kernel), granted, lds);
+  if (e != hipSuccess) return e;
   kernel<<<grid, 256, lds, s>>>(args);
   return hipGetLastError();
 }
