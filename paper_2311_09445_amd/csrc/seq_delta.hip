@@ -28,16 +28,16 @@ uint32_t padded(uint32_t dk) { return dk <= 64 ? 64 : 128; }
 // the other, so what cuts the time of few sequences is workgroups.  That costs another pass over all segments but the last, over dk
 // columns more (what a segment makes of a state is a product, k_delta_join), and two launches (a gradient: as much again but for the
 // product).  The fewest microseconds by these measured figures are taken, for widths up to 64 and above:
-//   a chunk's outputs 1.8, 2.45 (fp32 3.4, 5.5), what it carries 1.1, 1.65 (2.6, 4.0), its gradient's two passes 5.2, 7.2 (9, 15), what that carries 1.8,
+//   a chunk's outputs 1.8, 2.45 (fp32 3.4, 5.5), what it carries 1.1, 1.65 (2.6, 4.0), its gradient's two passes 5.2, 8.3 (9, 15), what that carries 1.8,
 //   2.95 (4, 6); two workgroups on a compute unit take 1.75 times as long, more take turns; a gradient's, which move the states, take 1.4 times
 //   as long where every compute unit has one, 2.5 with two; to join 3.2, 4.5 a segment.
 // Measured, in 1, 4, 8, 16 segments, us: 65536 tokens of 16 heads of 128 x 128 5250, 2391, 1699, 1638; 2 x 8192 of them 666, 413, 407, 454, their gradient
-// 2356, 1447, 1403, 1501; 4 x 4096 of 8 of 64 x 64 245, 134, 106, 110 and 793, 453, 365, 374; 32 x 512 of them 60, 92 and 275, 350.
+// 2538, 1446, 1368, 1475; 4 x 4096 of 8 of 64 x 64 245, 134, 106, 110 and 800, 442, 348, 365; 32 x 512 of them, in 1 and 4, 60, 92 and 247, 349.
 struct Cut { uint32_t segments, segment; };
 Cut cut(const DeltaSizes& a, bool backward) {
   const uint32_t chunks = chunks_of(a.L), wide = a.dk > 64, f32 = a.dtype == PER_SEQ_F32, slices = (a.dv + 63) / 64, more = slices + (a.dk + 63) / 64;
   static const float forward_us[2][2] = {{1.8f, 2.45f}, {3.4f, 5.5f}}, carry_us[2][2] = {{1.1f, 1.65f}, {2.6f, 4.0f}};
-  static const float back_us[2][2] = {{5.2f, 7.2f}, {9.0f, 15.0f}}, carry_back_us[2][2] = {{1.8f, 2.95f}, {4.0f, 6.0f}};
+  static const float back_us[2][2] = {{5.2f, 8.3f}, {9.0f, 15.0f}}, carry_back_us[2][2] = {{1.8f, 2.95f}, {4.0f, 6.0f}};
   const uint64_t rows = (uint64_t)a.B * a.H;
   // (in fp32 above 64 the rows of one workgroup fill a compute unit's LDS)
   auto crowd = [&](uint64_t workgroups) {
@@ -203,10 +203,17 @@ hipError_t launch_carry(DeltaRun* p, const DeltaSizes& a, const Cut& c, const pe
   return e;
 }
 
-// Whether the workgroups over the sequences form their chunks' records themselves (of a gradient, whose records are twice as much work, only where the
-// chip is not full: 500 x 100 tokens of 8 heads 747 us and 769).
+// Whether the workgroups over the sequences form their chunks' records themselves: a launch less, but a wave for a chunk, so that waves stand idle where
+// there are fewer than four chunks, and no other workgroup's passes beside them where the chip is full.  64 x 64, 4 heads, us, as a launch of
+// their own and by the workgroups: 64 x 32 tokens 15.6, 13.4; 128 x 64 24.2, 19.3; 256 x 64 36.2, 35.2; 512 x 64 60.8, 63.4; 4096 x 32 322, 413;
+// of three or four chunks 64 x 80 21.2, 17.7; 512 x 128 98.8, 96.3; 1024 x 128 208, 196; 4096 x 80 601, 607.  In fp32, where a workgroup has a compute unit,
+// 64 x 64 23.1, 19.9; 128 x 64 34.5, 37.4.  A gradient, whose records are twice as much work: 128 x 32 54.9, 53.3; 256 x 32 91.6, 93.2.
 bool makes_own(const DeltaSizes& a, const Cut& c, bool backward) {
-  return a.L && chunks_of(a.L) <= 4 && c.segments == 1 && a.dv <= 64 && !(backward && (uint64_t)a.B * a.H > 1024);
+  const uint32_t chunks = chunks_of(a.L);
+  if (!a.L || chunks > 4 || c.segments > 1 || a.dv > 64) return false;
+  const uint64_t rows = (uint64_t)a.B * a.H;
+  if (a.dtype == PER_SEQ_F32) return rows <= 256;
+  return rows <= (backward ? 512 : chunks > 2 ? ~0ull : 1024);
 }
 
 template <typename T, int DK>

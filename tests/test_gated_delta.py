@@ -405,6 +405,17 @@ def test_results_do_not_change_from_call_to_call():
 
 
 @TYPES
+@pytest.mark.parametrize("B,L", [(600, 40), (600, 20), (300, 100)])
+def test_few_sequences_are_computed_as_among_many(B, L, dtype):
+    """What makes a chunk's record, a launch of its own or the workgroup that takes it, goes by how many there are; results do not."""
+    q, k, v, g, beta, S, _ = inputs(B, L, 2, 2, 1, 2, 64, 48, dtype)
+    dout = normal(21, B, L, 2, 48, dtype=dtype)
+    call = lambda n: [*seq.gated_delta(*(t[:n] for t in (q, k, v, g, beta, S))), *seq.gated_delta_backward(*(t[:n] for t in (dout, q, k, v, g, beta, S, S)))]  # noqa: E731
+    for x, y in zip(call(40), call(B)):
+        assert torch.equal(x, y[:40])
+
+
+@TYPES
 def test_values_that_are_not_finite(dtype):
     """They reach what depends on them, tokens of their own chunk of 32 at most before them, and no other sequence or head."""
     B, L, H, d = 2, 200, 2, 32
