@@ -166,9 +166,8 @@ typedef struct per_delta_config {
  *   d_lengths : as for linear attention.  Tokens behind a sequence's are not read; their outputs are zeros.
  *   out_state : S behind the last valid token, or NULL.  It may be state.
  * Rows, states and gates in fp32 are computed to fp32's accuracy whatever the rows' type; results in bfloat16 carry their own rounding and
- * up to 2^-16 inside.  A value among the valid tokens, or of the state, that is not finite makes all that depends on it not
- * finite, and may do so to outputs of the up to 31 tokens before it that it shares a chunk of 32 with; sequences and heads do not
- * reach each other. */
+ * up to 2^-16 inside.  A value among the valid tokens, or of the state, that is not finite makes all that depends on it not finite, and
+ * nothing else: no token before it, no other column of the values, sequence or head. */
 int per_gated_delta_workspace(const per_delta_config* c, int backward, size_t* bytes);
 int per_gated_delta(const per_delta_config* c, const per_seq_rows* q, const per_seq_rows* k, const per_seq_rows* v,
                     const per_seq_gates* log_decay, const per_seq_gates* beta, const int32_t* d_lengths, const per_seq_states* state,

@@ -246,7 +246,12 @@ __device__ __forceinline__ void pairs_of(const DeltaPairs& p, uint32_t item, uin
 #pragma unroll
     for (int r = 0; r < 4; ++r) upper[r] = Y[(4 * g + r) * kPairRow + m];
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    const f32x4 inner = mma_f32(way ? beta1 * below : below * beta0, upper, zero), under = mma_f32(lower, inner, zero);
+    f32x4 inner = mma_f32(way ? beta1 * below : below * beta0, upper, zero);
+    // (outputs: a row that is not finite would reach the rows before it, of which it is taken 0 times)
+    if constexpr (!BACK)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) inner[r] = inner[r] * 0.0f == 0.0f ? inner[r] : 0.0f;
+    const f32x4 under = mma_f32(lower, inner, zero);
 #pragma unroll
     for (int r = 0; r < 4; ++r) Y[(16 + 4 * g + r) * kPairRow + m] = -under[r];
   }

@@ -292,6 +292,30 @@ struct TwoRows {
   }
 };
 
+// Values that are not finite and the tokens before them.  Products over a chunk take every token with every other, those behind it 0 times, and 0 times such
+// a value is one too.  So where a column (rows 16 i + 4 g + r of it in a lane) has one, it is cleared from there, and what depends on it is made NaN behind
+// the product.
+__device__ __forceinline__ bool all_finite(const f32x4 (&x)[2]) {   // of the wave
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum = fmaf(x[i / 4][i % 4], 0.0f, sum);
+  return __ballot(!(sum == 0.0f)) == 0;
+}
+__device__ __forceinline__ uint32_t clear_from_first(f32x4 (&x)[2], uint32_t g) {   // the column's first such row, or 32
+  uint32_t first = kChunk;
+#pragma unroll
+  for (int i = 7; i >= 0; --i)
+    if (!(x[i / 4][i % 4] * 0.0f == 0.0f)) first = 16 * (i / 4) + 4 * g + i % 4;
+  for (int d = 16; d < 64; d *= 2) {
+    const uint32_t other = __shfl_xor(first, d);
+    first = other < first ? other : first;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (16 * (i / 4) + 4 * g + i % 4 >= first) x[i / 4][i % 4] = 0.0f;
+  return first;
+}
+
 // LDS of a chunk: rows of queries and keys, and where they come straight from memory those of 64 values and the record's products too (twice 32 KiB:
 // as far as such loads reach).
 // (Only outputs take pairs; a pass that only carries has no queries either.)
@@ -493,8 +517,11 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
           for (int e = 0; e < 4; ++e) to[e * blocks * 32] = x[i][e];
         }
       }
-      const Parts<3> z = Parts<3>::of(v[0] - x[0], v[1] - x[1]);
-      f32x4 u[2];
+      f32x4 zs[2] = {v[0] - x[0], v[1] - x[1]}, u[2];
+      const bool spoilt = MODE == FORWARD && !all_finite(zs);
+      uint32_t from = kChunk;
+      if (spoilt) from = clear_from_first(zs, g);
+      const Parts<3> z = Parts<3>::of(zs[0], zs[1]);
       y[0] = y[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       mma_turns<2, 2, 3, 3>([&](int i) -> const bf16x8 (&)[3] { return rec.solve[i]; }, [&](int) -> const bf16x8 (&)[3] { return z.v; }, y);
       if constexpr (MODE != CARRYING)
@@ -505,14 +532,28 @@ __global__ __launch_bounds__(256, !DIRECT_ROWS ? 1 : MODE == CARRYING && DK == 6
         for (int j = 0; j < 4; ++j) rows_q[j] = Operand<T>::template along<DK>(Q, 16 * (j & 1) + m, k + j / 2, g);
         mma_turns<4, LESS, 3, PT>([&](int j) -> const bf16x8 (&)[3] { return sp[k + j / 2].v; }, [&](int j) -> const bf16x8 (&)[PT] { return rows_q[j].v; }, o4);
       }
+      if (spoilt)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (16 * (i / 4) + 4 * g + i % 4 >= from) y[i / 4][i % 4] = __builtin_nanf("");
 #pragma unroll
       for (int i = 0; i < 2; ++i) u[i] = num.beta[i] * y[i];
       const Parts<3> w = Parts<3>::of(num.left[0] * u[0], num.left[1] * u[1]);
+      const bool spoils = MODE == FORWARD && !all_finite(u);
+      if (spoils) from = clear_from_first(u, g);
       const Parts<NP> up = Parts<NP>::of(u[0], u[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) o[i] = p.scale * num.gamma_m[i] * (o4[i] + o4[i + 2]);
       if constexpr (MODE == FORWARD)
         mma_turns<2, LESS, NP, NP>([&](int) -> const bf16x8 (&)[NP] { return up.v; }, [&](int i) -> const bf16x8 (&)[NP] { return rec.pairs[i]; }, o);
+      if (spoils)
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+          const uint32_t first = __shfl(from, 4 * g + e);   // of the column that the element is of
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (16 * i + m >= first) o[i][e] = __builtin_nanf("");
+        }
       constexpr int TURN = PT == 1 ? TX : 4;
 #pragma unroll
       for (int a0 = 0; a0 < TX; a0 += TURN) {

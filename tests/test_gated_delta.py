@@ -440,6 +440,56 @@ def test_values_that_are_not_finite(dtype):
             assert i == 0 or (out[1, 100:, 1].isnan().all() and state[1, 1].isnan().all())
 
 
+@TYPES
+@pytest.mark.parametrize("L,at", [(200, 100), (200, 116), (200, 96), (200, 127), (200, 199), (70, 1), (70, 20), (1100, 500)])
+@pytest.mark.parametrize("dk,dv", [(32, 32), (128, 72)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_tokens_before_a_value_that_is_not_finite(bad, dk, dv, L, at, dtype):
+    """They are as without it, bit for bit, and so are other columns where it is in the values alone."""
+    B, H = 2, 2
+    clean = inputs(B, L, H, H, H, H, dk, dv, dtype)[:5]
+    want, last = seq.gated_delta(*clean)
+    for i, name in enumerate("q k v decay beta".split()):
+        if name == "decay" and bad != math.nan:
+            continue      # (at most 0; one that keeps nothing is a number)
+        spoilt = [t.clone() for t in clean]
+        place = (1, at, 1) + ((5,) if i < 3 else ())
+        spoilt[i][place] = bad
+        out, state = seq.gated_delta(*spoilt)
+        assert torch.equal(out[0], want[0]) and torch.equal(out[:, :, 0], want[:, :, 0]), name
+        assert torch.equal(out[1, :at], want[1, :at]), name
+        hit = out[1, at:, 1]
+        if name == "q":
+            assert not hit[0].isfinite().any() and torch.equal(hit[1:], want[1, at + 1:, 1]) and torch.equal(state, last)
+        elif name == "v":
+            others = [c for c in range(dv) if c != 5]
+            assert not hit[:, 5].isfinite().any() and torch.equal(hit[:, others], want[1, at:, 1][:, others])
+            assert not state[1, 1, :, 5].isfinite().any() and torch.equal(state[1, 1][:, others], last[1, 1][:, others])
+        else:
+            assert not hit.isfinite().any() and not state[1, 1].isfinite().any(), name
+
+
+@TYPES
+@pytest.mark.parametrize("L", [1, 50, 777])
+def test_columns_of_a_state_do_not_reach_each_other(L, dtype):
+    B, H, d = 1, 2, 64
+    q, k, v, g, beta, S, _ = inputs(B, L, H, H, H, H, d, d, dtype)
+    T = S.clone()
+    T[0, 1, 7, 20] = math.nan
+    others = [c for c in range(d) if c != 20]
+    calls = [lambda S: seq.gated_delta(q, k, v, g, beta, S)]
+    if L == 1:
+        def one(S):
+            S = S.clone()
+            return seq.gated_delta_step(q, k, v, g, beta, S), S
+        calls.append(one)
+    for call in calls:
+        (want, last), (out, state) = call(S), call(T)
+        assert torch.equal(out[:, :, 0], want[:, :, 0]) and torch.equal(state[:, 0], last[:, 0])
+        assert torch.equal(out[0, :, 1][:, others], want[0, :, 1][:, others]) and torch.equal(state[0, 1][:, others], last[0, 1][:, others])
+        assert out[0, :, 1, 20].isnan().all() and state[0, 1, :, 20].isnan().all()
+
+
 def equal(x, y):
     """Bit for bit but for which NaN it is."""
     return torch.equal(x.isnan(), y.isnan()) and torch.equal(x.nan_to_num(), y.nan_to_num())
