@@ -176,8 +176,8 @@ int per_gated_delta(const per_delta_config* c, const per_seq_rows* q, const per_
 /* Its gradient: from dout (of out) and dstate (of out_state; NULL: zeros) to dq, dk, dv, the gates' dlog_decay and dbeta, and dstate0 (of
  * state; NULL where not wanted).  Gradients of rows that several heads share are sums in a fixed order; behind a sequence's end all are
  * zeros.  That of log_decay[t] is a sum over what goes past token t, each term as small as the decays make it: nothing of what a fast decay
- * drops is in it, and where log_decay[t] is -infinity it is 0.  In bfloat16 the gradients of queries and keys take states and states'
- * gradients rounded to it (2^-8), and of what else they take 16 bits.  A value that is not finite may make all gradients of its sequence and head not finite, and those of rows that the head shares.
+ * drops is in it, and where log_decay[t] is -infinity it is 0.  Results in bfloat16 carry their own rounding and up
+ * to 2^-16 inside, as outputs do.  A value that is not finite may make all gradients of its sequence and head not finite, and those of rows that the head shares.
  * dstate0 may be dstate, and not state. */
 int per_gated_delta_backward(const per_delta_config* c, const per_seq_rows* dout, const per_seq_rows* q, const per_seq_rows* k,
                              const per_seq_rows* v, const per_seq_gates* log_decay, const per_seq_gates* beta,

@@ -35,8 +35,11 @@ struct DeltaBack {
   float *dz, *along, *strength, *write, *stay;   // along: rows of dZ . what keys read; write: of left u . R^T k; stay: 32 terms of e^Gn <R, S>
 };
 
+// Parts of states and their gradients in the products for rows.  (In bfloat16 with one, rounded, gradients of keys were off by 1.9 to 2.6e-3 in 2-norm, of
+// queries by up to 2.1e-3, where their own rounding, all that is left with two, is 1.7e-3.  It took 204 us for 217 of 32 ragged sequences of 512 tokens of 8 heads of
+// 64 x 64, 951 for 995 of 128 of them, 1367 for 1480 of 2 x 8192 of 16 heads of 128 x 128.)
 template <typename T>
-constexpr int kGradParts = sizeof(T) == 2 ? 1 : 3;   // of states in the products for rows
+constexpr int kGradParts = sizeof(T) == 2 ? 2 : 3;
 
 template <typename T, int DK, bool DIRECT_ROWS>
 struct BackLds {
@@ -161,8 +164,8 @@ __global__ __launch_bounds__(256, DIRECT_ROWS && CARRY ? 2 : 1) void k_delta_bac
     const uint32_t c = end - 1, first = c * kChunk;
     bf16 *const buffer = lds + (c & 1) * Lds::SIZE, *const Q = buffer + Lds::Q, *const K = buffer + Lds::K;
     if constexpr (DIRECT_ROWS) {
-      // (what is stored behind the loads: the gradient's plane, and from the second chunk dZ)
-      if (!CARRY && works && end + 1 < chunks) arrive<KX + 8>();
+      // (what is stored behind the loads: the gradient's planes, and from the second chunk dZ)
+      if (!CARRY && works && end + 1 < chunks) arrive<kGradParts<T> * KX + 8>();
       else arrive<0>();
       if (valid - first < kChunk) {
         DirectRows<DK>::clear(Q, valid - first, threadIdx.x);
@@ -346,7 +349,8 @@ constexpr uint32_t grads_lds() { return (2 * kParts<T> + 2 * kGradParts<T>) * Ti
 // results, so that what a lane reads and writes of a token are eight elements in a row.
 template <typename T, int DK>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_delta_grads(DeltaGrads p) {
-  constexpr int NC = DK / 64, PT = kParts<T>, PS = kGradParts<T>, PU = sizeof(T) == 2 ? 2 : 3, LESS = PU - 1;
+  constexpr int NC = DK / 64, PT = kParts<T>, PS = kGradParts<T>, PU = PS, LESS = PU - 1;
+  static_assert(kStateParts<T> == PS, "planes are read as parts, or halves of as many");
   extern __shared__ __attribute__((aligned(256))) uint8_t lds_raw[];
   bf16* const Q = reinterpret_cast<bf16*>(lds_raw);
   bf16* const K = Q + PT * Tile<DK>::SIZE;
@@ -424,14 +428,25 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : DK == 64 ? 3 : 2) void k_
   for (uint32_t block = 0; block < blocks; ++block) {
     if (block) __syncthreads();
 #pragma unroll
-    for (int t = 0; t < PS; ++t)
+    for (uint32_t i = 0; i < HELD; ++i) {   // lane 16 g + m of tile and k: column 16 tile + m, places 32 k + 8 g ..
+      const uint32_t at = threadIdx.x + 256 * i, c = 16 * (at / (64 * (DK / 32))) + (at & 15);
+      const uint32_t place = Tile<DK>::at(16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3), 4 * (at / 64 % (DK / 32)) + (at >> 4 & 3));
+      Parts<PS> s;
+      if constexpr (sizeof(T) == 2) {
+        const bf16x8 both[2] = {next_s[0][i], next_s[1][i]};
+        f32x4 a, b;
+        of_halves(both, &a, &b);
+        s = Parts<PS>::of(a, b);
+      } else {
 #pragma unroll
-      for (uint32_t i = 0; i < HELD; ++i) {   // lane 16 g + m of tile and k: column 16 tile + m, places 32 k + 8 g ..
-        const uint32_t at = threadIdx.x + 256 * i, c = 16 * (at / (64 * (DK / 32))) + (at & 15);
-        const uint32_t place = Tile<DK>::at(16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3), 4 * (at / 64 % (DK / 32)) + (at >> 4 & 3));
-        *reinterpret_cast<bf16x8*>(S + t * Tile<DK>::SIZE + place) = next_s[t][i];
+        for (int t = 0; t < PS; ++t) s.v[t] = next_s[t][i];
+      }
+#pragma unroll
+      for (int t = 0; t < PS; ++t) {
+        *reinterpret_cast<bf16x8*>(S + t * Tile<DK>::SIZE + place) = s.v[t];
         *reinterpret_cast<bf16x8*>(R + t * Tile<DK>::SIZE + place) = next_r[t][i];
       }
+    }
     __syncthreads();
     Operand<T> d[2];
     Parts<3> z[2], u[2];   // (whole for the pairs, which the gradients of decays are made of too; rows take PU of them)

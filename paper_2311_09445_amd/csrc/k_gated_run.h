@@ -36,9 +36,8 @@ struct DeltaRun {
 // CARRYING: no outputs; what a segment adds to a state, and (in slices of their own) what it makes of one: its product with the state before it.
 enum DeltaMode { FORWARD, KEEPING, CARRYING };
 
-// Planes of 16 bits that the states before the chunks are kept in for a gradient: where rows are bfloat16 the rounded state, which the products for
-// bfloat16 gradients take, and the lower half of the sum that rounded it, so that both together are the 32 bits (the gradients of
-// decays take the state whole); else the three parts that an operand takes.
+// Planes of 16 bits that the states before the chunks are kept in for a gradient: where rows are bfloat16 the two halves of the 32 bits (the
+// gradients of decays take the state whole), else the three parts that an operand takes.
 template <typename T>
 constexpr int kStateParts = sizeof(T) == 2 ? 2 : 3;
 

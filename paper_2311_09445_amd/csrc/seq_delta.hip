@@ -78,7 +78,8 @@ struct BackWork {
 };
 BackWork back_work(const DeltaSizes& a) {
   const uint64_t bh = (uint64_t)a.B * a.H, chunks = bh * chunks_of(a.L), tokens = chunks * kChunk;
-  const uint64_t blocks = (a.dv + 31) / 32, parts = blocks * 2, e = a.dtype == PER_SEQ_BF16;
+  const uint64_t blocks = (a.dv + 31) / 32, parts = blocks * 2;
+  const bool f32 = a.dtype == PER_SEQ_F32;
   BackWork w{};
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -88,8 +89,8 @@ BackWork back_work(const DeltaSizes& a) {
   };
   const uint64_t state = blocks * 32 * padded(a.dk) * sizeof(bf16);
   w.records = take(chunks * sizeof(DeltaRecordBack));
-  w.states = take(chunks * state * (e ? 2 : 3));
-  w.dstates = take(chunks * state * (e ? 1 : 3));
+  w.states = take(chunks * state * (f32 ? kStateParts<float> : kStateParts<bf16>));
+  w.dstates = take(chunks * state * (f32 ? kGradParts<float> : kGradParts<bf16>));
   w.y = take(tokens * blocks * 32 * sizeof(float));
   w.x = take(tokens * blocks * 32 * sizeof(float));
   w.dz = take(tokens * blocks * 32 * sizeof(float));

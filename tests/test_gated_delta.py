@@ -5,8 +5,8 @@ tokens: sums over dk and 32 terms in fp32 (roundings of either sign: about the r
 apart into 24 bits; with keys of length 1 and strengths up to 1 what one round is off is not enlarged by the next.  So states, and all that is
 fp32, are held to  u(T, d) = 2^-24 (6 + sqrt(d)) (1 + sqrt(T / 32))  of themselves by the 2-norm, and gradients, which take states and
 the states' gradients, to four times that.  A single element may be off by 16 times the root mean square of that.
-Results in bfloat16 are rounded once, 2^-8 of an element at most; inside, outputs and gradients of values keep 2^-16.  Gradients
-of queries and keys take states rounded to bfloat16: each product is then off by up to 2^-8 of its terms, of either sign, that is by
+Results in bfloat16 are rounded once, 2^-8 of an element at most; inside, outputs and gradients keep 2^-16 (test_gradients_in_bfloat16_are_rounded_once).
+Elsewhere gradients of queries and keys are held to what states rounded to bfloat16 would leave: each product is then off by up to 2^-8 of its terms, of either sign, that is by
 2^-8 of the root mean square in 2-norm and a few times that in an element.  The terms of an element are those of its token: with R the state's
 gradient, of which an element is off by up to 2^-8 of itself, dk = R u is off by sqrt(sum over j of (2^-8 R_ij u_j)^2) in the mean, as large as 2^-8 of
 the root mean square of R u over the token's row, and rows differ by more than ten times (tokens next to the end see a dstate of
@@ -125,6 +125,19 @@ def test_gradients(B, L, H, Q, K, V, dk, dv, ragged, dtype):
     got = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths, scale=0.7)
     want = oracle.delta_backward(dout, q, k, v, g, beta, S, dS, lengths, 0.7)
     check_grads(got, want, L, max(dk, dv), dtype, cancelled(k, v, g, beta, S, L, dk, dv))
+
+
+@pytest.mark.parametrize("fast", [0.02, 0.5, 8.0])
+@pytest.mark.parametrize("B,L,H,Q,K,V,dk,dv", SHAPES[1:])
+def test_gradients_in_bfloat16_are_rounded_once(B, L, H, Q, K, V, dk, dv, fast):
+    """States, their gradients, U and dZ come into the products for rows in two parts, each off by 2^-17 of itself at most, and what is left out is 2^-16 of
+    a product; four such factors and terms, 2^-14, as gradients of values are held to, and one rounding to bfloat16."""
+    q, k, v, g, beta, S, lengths = inputs(B, L, H, Q, K, V, dk, dv, BF16, ragged=True, fast=fast)
+    dout, dS = normal(21, B, L, H, dv, dtype=BF16), 0.3 * normal(22, B, H, dk, dv)
+    got = seq.gated_delta_backward(dout, q, k, v, g, beta, S, dS, lengths, scale=0.7)
+    want = oracle.delta_backward(dout, q, k, v, g, beta, S, dS, lengths, 0.7)
+    for name, x, y in zip(("dq", "dk", "dv"), got, want):
+        near(x, y, 2 ** -14, name, element=oracle.U_BF16)
 
 
 @TYPES
