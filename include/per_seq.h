@@ -168,6 +168,9 @@ typedef struct per_delta_config {
  * Rows, states and gates in fp32 are computed to fp32's accuracy whatever the rows' type; results in bfloat16 carry their own rounding and
  * up to 2^-16 inside.  A value among the valid tokens, or of the state, that is not finite makes all that depends on it not finite, and
  * nothing else: no token before it, no other column of the values, sequence or head. */
+/* 12.5 KiB for each 32 tokens and head; backward 18.5 KiB and, with dk rounded up to 64 or 128 and dv to 32, 8 dk dv + 424 dv bytes of bfloat16
+ * rows, 12 dk dv + 424 dv of fp32 (1.7 GB for 2^18 tokens and heads of 128 x 128 in bfloat16).  Sequences that are cut, and heads that share
+ * queries or keys, take some more. */
 int per_gated_delta_workspace(const per_delta_config* c, int backward, size_t* bytes);
 int per_gated_delta(const per_delta_config* c, const per_seq_rows* q, const per_seq_rows* k, const per_seq_rows* v,
                     const per_seq_gates* log_decay, const per_seq_gates* beta, const int32_t* d_lengths, const per_seq_states* state,

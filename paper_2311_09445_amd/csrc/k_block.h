@@ -3,8 +3,8 @@
 // Rows are read in pieces of 16 bytes at any alignment; the last piece of a row whose width is no multiple of one ends with the row, and
 // what it holds twice counts once.
 //
-// What bounds them: memory.  The norm of 32768 x 2048 in bfloat16 takes 52 us (5.2 TB/s; with weights element by element and a wave's row not
-// ahead 78), dropout of as much with a residual 70 (5.7 TB/s).  The gradient of 8184 x 1537 takes 27: one round of workgroups, four rows to a wave
+// What bounds them: memory.  The norm of 32768 x 2048 in bfloat16 takes 52 us (5.2 TB/s; 44 where the last cache holds part of the rows from the call
+// before; with weights element by element and a wave's row not ahead 78), dropout of as much with a residual 70 (5.7 TB/s).  The gradient of 8184 x 1537 takes 27: one round of workgroups, four rows to a wave
 // (24, at 3.1 TB/s), and the sums' launch (a row to a workgroup of 256 lanes instead 35); of 32768 x 2048 88.
 
 template <typename T>

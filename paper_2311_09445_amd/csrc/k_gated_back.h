@@ -7,9 +7,9 @@
 //   dQ = scale e^G dO S^T + dM K,   dK = -e^G dZ S^T + left U R^T + dM^T Q + (dN + dN^T) K,
 //   dM = scale e_ij dO U^T (i >= j),   dN = -e_ij dZ U^T (i > j).
 //
-// What bounds them, in bfloat16: k_delta_back, which asks for everything a chunk ahead, takes 3.5 us for a chunk of 64 x 64 (32 sequences of 512 tokens of 8
-// heads 56 us) and, with a workgroup on each compute unit, 5.4 of 128 x 128 (2 x 8192 tokens of 16 heads in segments 348 us for 1.0 GB);
-// k_delta_grads takes 345 us for 1.1 GB of the latter, waiting for memory with two workgroups to a compute unit (three would spill: 710).
+// What bounds them, in bfloat16: k_delta_back, which asks for everything a chunk ahead, takes 3.9 us for a chunk of 64 x 64 (32 sequences of 512 tokens of 8
+// heads 62 us); of 2 x 8192 tokens of 16 heads of 128 x 128 it moves 2.1 GB in 369 us, memory's rate.  k_delta_grads takes 426 us for 1.8 GB of
+// the latter, waiting for memory with two workgroups to a compute unit (three spilled: 710 where two took 447).
 //
 // The gradient of a decay's logarithm is the sum of all that goes past its token t, each term with the decays between as a factor.  Of a chunk that is
 //   sum (i >= t > j) dM_ij q_i.k_j + dN_ij k_i.k_j   (what tokens of the chunk read of each other's writes; k_delta_grads)

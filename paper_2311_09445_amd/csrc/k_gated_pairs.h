@@ -8,7 +8,7 @@
 // half of the wave forms (1 + diag(beta) N)^-1, which a gradient runs backwards through).
 //
 // What bounds it: 9 us for 768 chunks of 64 x 64 are loads' and LDS's latency and the substitution's chain (of 32 rows in one piece, with the
-// rows asked for behind the sums of decays, 11); 32768 chunks of 128 take 168 us for 350 MB written and 270 read.  Registers for
+// rows asked for behind the sums of decays, 11); 32768 chunks of 128 take 167 us for 350 MB written and 670 read (rows that two heads share by both).  Registers for
 // four waves to a SIMD would spill (300 us).
 //
 // What goes into the record of a chunk is laid out as the operands that the passes over the sequence take: places {4 g .. 4 g + 3, 16 + 4 g ..} of

@@ -7,9 +7,9 @@
 // tokens, which the next product runs over.  The outputs are formed transposed, so that a lane has four neighbours of a token.
 //
 // What bounds it, in bfloat16 at 128 x 128: a workgroup by itself takes 2.45 us for a chunk (1.8 of its products alone, 1.5 of its loads alone; at
-// 64 x 64 1.8 in all); with the chip full a SIMD's two waves take 3500 cycles each, of which 552 vector instructions are 2200 and 82 matrix
-// instructions 1300: 65536 tokens of 16 heads 484 us, and what their segments carry, over twice the columns, 666.  A third of the vector
-// instructions take the state apart.  Rows are asked for a chunk ahead, straight to LDS where they are whole pieces (by way of registers a
+// 64 x 64 1.8 in all); with the chip full a SIMD's two waves take 3600 cycles each, of which 500 vector instructions are 2000 and 82 matrix
+// instructions 1300: 65536 tokens of 16 heads 504 us, and what their segments carry, over twice the columns, 666.  A third of the vector
+// instructions take the state apart.  Keeping states for a gradient is bound by memory: 1.4 GB in 260 us of 2 x 8192 tokens of 16 heads.  Rows are asked for a chunk ahead, straight to LDS where they are whole pieces (by way of registers a
 // chunk took 6.6 us), and results are stored behind the next barrier, so that nothing waits for a store.
 //
 // Whatever is computed is taken apart into three parts in bfloat16 where it becomes an operand, since the state is fp32 and what is

@@ -3,8 +3,8 @@
 // With a = e^g: r = S^T k, w = S^T q, u = beta (v - a r), S <- a S + k u^T, out = scale (a w + (q.k) u).  Nothing but the state's bytes
 // counts, so it is read once and held: a workgroup takes the state of one head, VEC columns to a thread, `groups` threads of rows side by
 // side, R rows of each.  Both products with the state are formed while it comes in and added up over the groups in their order; what is
-// written follows one barrier.  512 MiB of states (512 sequences of 16 heads of 128 x 128) take 219 us, 4.9 TB/s, as fast as a copy; 64 sequences
-// of 4 heads of 64 x 64 5.2, a launch.  How states pass the last cache: see k_attend_step.h.
+// written follows one barrier.  512 MiB of states (512 sequences of 16 heads of 128 x 128) take 219 us, 4.9 TB/s, as fast as a copy (171 where
+// the last cache holds part of them from the call before); 64 sequences of 4 heads of 64 x 64 5.2, a launch.  How states pass the last cache: see k_attend_step.h.
 struct DeltaStep {
   SeqRows q, k, v, out;
   Gates log_decay, beta;

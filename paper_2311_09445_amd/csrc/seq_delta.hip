@@ -31,8 +31,8 @@ uint32_t padded(uint32_t dk) { return dk <= 64 ? 64 : 128; }
 //   a chunk's outputs 1.8, 2.45 (fp32 3.4, 5.5), what it carries 1.1, 1.65 (2.6, 4.0), its gradient's two passes 5.2, 8.3 (9, 15), what that carries 1.8,
 //   2.95 (4, 6); two workgroups on a compute unit take 1.75 times as long, more take turns; a gradient's, which move the states, take 1.4 times
 //   as long where every compute unit has one, 2.5 with two; to join 3.2, 4.5 a segment.
-// Measured, in 1, 4, 8, 16 segments, us: 65536 tokens of 16 heads of 128 x 128 5250, 2391, 1699, 1638; 2 x 8192 of them 666, 413, 407, 454, their gradient
-// 2538, 1446, 1368, 1475; 4 x 4096 of 8 of 64 x 64 245, 134, 106, 110 and 800, 442, 348, 365; 32 x 512 of them, in 1 and 4, 60, 92 and 247, 349.
+// Measured, in 1, 4, 8, 16 segments, us: 65536 tokens of 16 heads of 128 x 128 5453, 2363, 1513, 1351; 2 x 8192 of them 690, 411, 380, 433, their gradient
+// 2673, 1577, 1502, 1611; 4 x 4096 of 8 of 64 x 64 256, 136, 102, 110 and 836, 466, 370, 388; 32 x 512 of them, in 1 and 4, 58, 90 and 267, 368.
 struct Cut { uint32_t segments, segment; };
 Cut cut(const DeltaSizes& a, bool backward) {
   const uint32_t chunks = chunks_of(a.L), wide = a.dk > 64, f32 = a.dtype == PER_SEQ_F32, slices = (a.dv + 63) / 64, more = slices + (a.dk + 63) / 64;
