@@ -8,7 +8,8 @@ results allocated, in ``_seq_binding.so`` (``csrc/seq_binding.cpp``: the checks 
 Inputs that ask for a gradient get one: the calls of sequences are then nodes of torch's graph (with no tensors given for their
 results, which could not be).  Gradients of gradients are refused but for the rotation's and dropout's, and so are gradients of linear
 attention's decays and of frequencies; the calls that form gradients, and single tokens, are no nodes.  Tensors with forward-mode
-derivatives are refused.
+derivatives are refused.  Nodes may be captured into a HIP graph with their backward pass, as torch's own: on leaves that no graph from
+outside the capture holds.
 
 The rows of a block (``layer_norm``, ``dropout``) are tensors of one to four dimensions, the last one contiguous.
 

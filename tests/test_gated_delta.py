@@ -748,6 +748,39 @@ def test_a_block_in_a_graph():
     assert not torch.equal(kept[0], kept[1])      # (what is dropped moves on)
 
 
+def test_nodes_of_torchs_graph_in_a_captured_one():
+    """Forward and gradient of a block through torch's graph, captured as a whole and replayed on new data, eager calls in between."""
+    B, L, H, d = 2, 70, 2, 32
+    D = H * d
+    dtype = BF16
+    x, w, b = normal(1, B, L, D, dtype=dtype), 1 + 0.1 * normal(2, D), 0.1 * normal(3, D)
+    g, beta, dout = -normal(5, B, L, H).abs(), torch.sigmoid(normal(6, B, L, H)), normal(4, B, L, D, dtype=dtype)
+
+    def work():
+        leaves = [t.detach().requires_grad_() for t in (x, w, b, g, beta)]
+        rows = seq.layer_norm(*leaves[:3]).unflatten(-1, (H, d))
+        o, _ = seq.gated_delta(rows, rows, rows, *leaves[3:], scale=0.1)
+        out = seq.dropout(o.flatten(-2), 0.2, 3, 4, residual=leaves[0])
+        return [out.detach(), *torch.autograd.grad(out, leaves, dout)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = work()
+    for i in range(4):
+        x.copy_(normal(20 + i, *x.shape, dtype=dtype))
+        g.copy_(-normal(30 + i, *g.shape).abs())
+        graph.replay()
+        want = work()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), f"replay {i}"
+
+
 def test_autograd():
     B, L, H, d = 2, 50, 4, 32
     q, k, v, g, beta, S, lengths = inputs(B, L, H, 2, 1, 4, d, d, F32, ragged=True)
